@@ -494,6 +494,50 @@ fg_status channel_slice_copy(const uint16_t *src, int32_t src_ld, const uint16_t
                              int32_t gate_ld, uint16_t *dst, int32_t dst_ld, int64_t npix,
                              int32_t nch, int32_t accumulate, hipStream_t stream);
 
+/* ---- classification head: dropout and softmax cross entropy ---------------
+ * Element type of the tensors that a call calls `dtype`. */
+enum { FG_F16 = 0, FG_BF16 = 1, FG_F32 = 2 };
+
+/* Dropout (Section 6.2, Neural Network Architecture: dropout after each dense
+ * block's ReLU) over rows x cols elements in row-major buffers with row strides of
+ * their own (elements; 0: dense). Element i = row * cols + col is kept where a
+ * 16-bit number is below t = round((1 - p) * 65536), halves up, and kept elements are
+ * multiplied by the fp32 value 65536 / t, so the mean is kept exactly for the p
+ * that t stands for; p within 2^-17 of 0 keeps and of 1 drops everything. The
+ * number is half i % 2 (0: low) of word (i % 8) / 2 of the Philox 4x32 block
+ * (7 rounds) with the counter (i / 8, 0, step + *step_count, site) and the key
+ * (low, high word of seed): a function of seed, step, site and index alone, so
+ * nothing is stored for the backward pass, and the strides, the type and the
+ * launch do not matter. `step_count` (device int32, e.g. the optimizer's; may be
+ * null: 0) is read by the kernel, so a captured graph draws a new mask each replay. */
+typedef struct {
+    int64_t rows, cols;
+    int64_t x_ld, y_ld, z_ld;  /* of the input, the output, the residual or gate */
+    uint64_t seed;
+    double p;                  /* probability of dropping, 0 .. 1 */
+    uint32_t site, step;       /* which dropout of the network; which step */
+    int32_t dtype;             /* FG_F16, FG_BF16 or FG_F32: every tensor */
+} fg_dropout_desc;
+
+/* y = residual + (kept ? x * 65536 / t : +0), fp32 arithmetic, one rounding;
+ * residual may be null (0). A dropped element counts as +0 whatever x holds there.
+ * y may be x or the residual itself (same stride), or a channel slice interleaved
+ * with theirs at one stride, but overlap neither otherwise.
+ * rows = 0 is a call with nothing to do (pointers may be null). FG_EINVAL for a
+ * null x or y, rows < 0, cols < 1, a stride below cols, p outside [0, 1] or NaN, an
+ * unknown dtype, a pointer not aligned to its elements, or a forbidden overlap
+ * (step_count with y among them); FG_EUNSUPPORTED for 2^35 elements or more, cols
+ * of 2^31 or more, or a buffer that spans 2^60 bytes or more. */
+fg_status dropout_fwd(const fg_dropout_desc *d, const void *x, const void *residual, void *y,
+                      const int32_t *step_count, hipStream_t stream);
+
+/* Its gradient: dx = kept && gate > 0 ? dy * 65536 / t : +0; gate (z_ld; may be
+ * null: open everywhere) is the output of a ReLU before the dropout, or the
+ * dropout's own output. Strides, aliasing and errors as dropout_fwd, dy and dx in
+ * the places of x and y and the gate in that of the residual. */
+fg_status dropout_bwd(const fg_dropout_desc *d, const void *dy, const void *gate, void *dx,
+                      const int32_t *step_count, hipStream_t stream);
+
 /* Output spatial size: transpose = 0 gives the forward P, Q; 1 gives the
  * transposed convolution's output size. FG_EINVAL if it is not positive. */
 fg_status fg_conv_out_dims(const fg_conv_desc *d, int transpose, int32_t *p,

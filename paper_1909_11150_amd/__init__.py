@@ -18,6 +18,7 @@ EPI_NONE, EPI_RELU, EPI_GATE, EPI_ACC = 0, 1, 2, 3
 OP_FWD, OP_BWD_DATA, OP_BWD_WEIGHT, OP_CONVT = 0, 1, 2, 3
 MAX_SEGMENTS = 64
 GRAD_F32, GRAD_F16_SCALED = 0, 1
+F16, BF16, F32 = 0, 1, 2
 
 ENTRY_POINTS = (
     "conv2d_fwd", "conv2d_bwd_data", "conv2d_bwd_weight",
@@ -30,6 +31,7 @@ ENTRY_POINTS = (
     "huber_head_grad", "avg_pool2d_fwd", "avg_pool2d_bwd", "channel_slice_copy",
     "grad_flags_clear", "fg_loss_scale_update", "fg_lr_at", "fg_profile_next_launch",
     "conv2d_bwd_weight_noalloc", "fg_mfma_loop",
+    "dropout_fwd", "dropout_bwd",
 )
 MFMA_LOOP_MAX_WORK = 1 << 28  # blocks * iters accepted by fg_mfma_loop
 MFMA_LOOP_FLOPS_PER_BLOCK_ITER = 1 << 20
@@ -62,6 +64,19 @@ class LRScheduleParams(ctypes.Structure):
     _fields_ = [("base", ctypes.c_double), ("peak", ctypes.c_double),
                 ("warmup", ctypes.c_int64), ("every", ctypes.c_int64),
                 ("rate", ctypes.c_double)]
+
+
+class DropoutDesc(ctypes.Structure):
+    """fg_dropout_desc. Strides 0: dense."""
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("x_ld", ctypes.c_int64), ("y_ld", ctypes.c_int64),
+                ("z_ld", ctypes.c_int64), ("seed", ctypes.c_uint64),
+                ("p", ctypes.c_double), ("site", ctypes.c_uint32),
+                ("step", ctypes.c_uint32), ("dtype", ctypes.c_int32)]
+
+    @classmethod
+    def make(cls, rows, cols, p, seed, site=0, step=0, dtype=F16, x_ld=0, y_ld=0, z_ld=0):
+        return cls(rows, cols, x_ld, y_ld, z_ld, seed, p, site, step, dtype)
 
 
 class LibraryNotBuilt(RuntimeError):
@@ -127,6 +142,8 @@ def lib():
         "fg_profile_next_launch": [vp, vp],
         "fg_mfma_loop": [vp, i32, i32, i32, vp],
         "huber_head_grad": [vp, vp, u64, ctypes.c_double, ctypes.c_double, vp, vp],
+        "dropout_fwd": [ctypes.POINTER(DropoutDesc), vp, vp, vp, vp, vp],
+        "dropout_bwd": [ctypes.POINTER(DropoutDesc), vp, vp, vp, vp, vp],
         "avg_pool2d_fwd": [vp, i32, i32, i32, i32, vp, vp],
         "avg_pool2d_bwd": [vp, vp, i32, i32, i32, i32, vp, vp],
         "channel_slice_copy": [vp, i32, vp, i32, vp, i32, ctypes.c_int64, i32, i32, vp],
@@ -373,6 +390,63 @@ def channel_slice_copy(src, src_ld, dst, dst_ld, npix, nch, gate=None, gate_ld=0
     _check("channel_slice_copy", lib().channel_slice_copy(
         a(src), src_ld, a(gate), gate_ld, a(dst), dst_ld, npix, nch, int(accumulate),
         _s(stream)))
+
+
+# ---- classification head ----------------------------------------------------
+def dtype_of(t):
+    """Element type code (F16, BF16, F32) of a tensor."""
+    import torch
+    try:
+        return {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}[t.dtype]
+    except KeyError:
+        raise ValueError(f"element type {t.dtype} is not supported") from None
+
+
+def _matrix(name, t, rows, cols, ld, dtype):
+    """Address of a rows x cols matrix in t: the tensor has those sizes in some
+    shape (its last axis unit-strided, the others one stride) and row stride ld."""
+    if t is None:
+        return None
+    if dtype_of(t) != dtype:
+        raise ValueError(f"{name}: element type {t.dtype} where the descriptor says another")
+    if t.numel() != rows * cols or (t.numel() and (t.dim() < 1 or t.shape[-1] != cols)):
+        raise ValueError(f"{name}: shape {tuple(t.shape)} where {rows} x {cols} is needed")
+    if t.numel():
+        want = 1 if cols > 1 else None   # stride expected of the axis, None: any
+        for i, (n, s) in enumerate(zip(reversed(t.shape), reversed(t.stride()))):
+            if n > 1 and want is not None and s != want:
+                raise ValueError(f"{name}: strides {t.stride()} where rows {ld or cols} "
+                                 "elements apart are needed")
+            want = (ld or cols) if i == 0 else want * n
+    return t.data_ptr()
+
+
+def _counter(name, t):
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.numel() < 1 or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor")
+    return t.data_ptr()
+
+
+def _dropout(fn, desc, x, y, z, z_name, step_count, stream):
+    m = lambda n, t, ld: _matrix(n, t, desc.rows, desc.cols, ld, desc.dtype)
+    _check(fn, getattr(lib(), fn)(
+        ctypes.byref(desc), m("x", x, desc.x_ld), m(z_name, z, desc.z_ld),
+        m("y", y, desc.y_ld), _counter("step_count", step_count), _s(stream)))
+
+
+def dropout_fwd(desc, x, y, residual=None, step_count=None, stream=None):
+    """y = residual + dropout(x) (see include/fcngrad.h); tensors of desc's element
+    type and strides, e.g. channel slices of wider buffers. step_count: device int32
+    added to desc.step by the kernel."""
+    _dropout("dropout_fwd", desc, x, y, residual, "residual", step_count, stream)
+
+
+def dropout_bwd(desc, dy, dx, gate=None, step_count=None, stream=None):
+    """Gradient of dropout_fwd's x from dy into dx, zero where gate <= 0."""
+    _dropout("dropout_bwd", desc, dy, dx, gate, "gate", step_count, stream)
 
 
 def grad_flags_clear(flags, stream=None):

@@ -961,6 +961,49 @@ fg_status channel_slice_copy(const uint16_t *src, int32_t src_ld, const uint16_t
                                                  npix, nch, accumulate != 0, stream));
 }
 
+// Shared checks of the two dropout calls; z is the residual or the gate.
+static fg_status dropout_call(const fg_dropout_desc *d, const void *x, const void *z, bool gate,
+                              void *y, const int32_t *step_count, hipStream_t stream) {
+  if (!d || d->rows < 0 || d->cols < 1 || !(d->p >= 0.0 && d->p <= 1.0) ||
+      d->dtype < FG_F16 || d->dtype > FG_F32)
+    return FG_EINVAL;
+  const int64_t xl = d->x_ld ? d->x_ld : d->cols, yl = d->y_ld ? d->y_ld : d->cols,
+                zl = d->z_ld ? d->z_ld : d->cols;
+  if (xl < d->cols || yl < d->cols || zl < d->cols) return FG_EINVAL;
+  if (d->cols >= kMaxElems || d->rows >= ((int64_t)1 << 35) / d->cols + 1 ||
+      d->rows * d->cols >= (int64_t)1 << 35)
+    return FG_EUNSUPPORTED;
+  if (d->rows == 0) return FG_OK;
+  if (!x || !y) return FG_EINVAL;
+  const int64_t esz = d->dtype == FG_F32 ? 4 : 2, lim = ((int64_t)1 << 60) / esz;
+  if (d->rows > 1 && std::max(std::max(xl, yl), zl) >= lim / d->rows) return FG_EUNSUPPORTED;
+  if (((uintptr_t)x | (uintptr_t)y | (uintptr_t)z) % esz || (uintptr_t)step_count % 4)
+    return FG_EINVAL;
+  const auto span = [&](int64_t ld) { return (size_t)((d->rows - 1) * ld + d->cols) * esz; };
+  // y may be an input (an element's inputs are read by the lane that then writes
+  // it) or interleave with one, as channel slices of one buffer do
+  const auto clash = [&](const void *in, int64_t ld) {
+    if (in == y && (ld == yl || d->rows == 1)) return false;
+    const int64_t db = (int64_t)((uintptr_t)y - (uintptr_t)in);
+    const int64_t r = ((db / esz) % ld + ld) % ld;
+    if (ld == yl && d->cols <= r && r + d->cols <= ld) return false;
+    return overlap(y, span(yl), in, span(ld));
+  };
+  if (clash(x, xl) || (z && clash(z, zl))) return FG_EINVAL;
+  if (step_count && overlap(y, span(yl), step_count, 4)) return FG_EINVAL;
+  return launch_status(launch_dropout(*d, x, z, gate, y, step_count, stream));
+}
+
+fg_status dropout_fwd(const fg_dropout_desc *d, const void *x, const void *residual, void *y,
+                      const int32_t *step_count, hipStream_t stream) {
+  return dropout_call(d, x, residual, false, y, step_count, stream);
+}
+
+fg_status dropout_bwd(const fg_dropout_desc *d, const void *dy, const void *gate, void *dx,
+                      const int32_t *step_count, hipStream_t stream) {
+  return dropout_call(d, dy, gate, true, dx, step_count, stream);
+}
+
 fg_status relu_backward(const uint16_t *dy, const uint16_t *act,
                         uint64_t numel, uint16_t *out, hipStream_t stream) {
   if (!dy || !act || !out || numel == 0) return FG_EINVAL;

@@ -180,6 +180,11 @@ hipError_t launch_head_wgrad(const uint16_t *x, const uint16_t *dy,
                              uint16_t *dw, int64_t npix, int32_t c,
                              float *ws, int32_t *flag, hipStream_t st);
 
+// 16-bit numbers below it keep an element (p in [0, 1]).
+inline uint32_t dropout_threshold(double p) { return (uint32_t)((1.0 - p) * 65536.0 + 0.5); }
+hipError_t launch_dropout(const fg_dropout_desc &d, const void *x, const void *z, bool gate,
+                          void *y, const int32_t *step_count, hipStream_t st);
+
 // One-shot profiling events (fg_profile_next_launch): prof_begin records the
 // armed start event on the stream, prof_end the stop event, then disarms.
 // Both do nothing when no events are armed.

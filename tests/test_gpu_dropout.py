@@ -1,0 +1,174 @@
+"""dropout_fwd and dropout_bwd bit for bit against the definition, evaluated with NumPy
+in 64 bits and rounded once: every type, residuals and gates, channel slices and dense
+rows of any width and alignment, in place, values that a mask must not let through
+(infinities, NaN), all or nothing dropped, and the step counted on the device.
+
+The result is exact: x * (65536 / t) is one fp32 rounding of the product of two fp32
+values, the sum with the residual a second one, and the store a third, each of which
+NumPy's fp32 arithmetic does alike (no tolerance).
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_1909_11150_amd as fg
+from oracle import dropout as D
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+SEED = 0xDEADBEEF12345678
+
+
+def buffer(rows, cols, ld, dt, rng, lead=0, positive=False):
+    """(view of rows x cols, whole buffer): row stride ld, lead elements before it."""
+    a = rng.standard_normal(rows * ld + lead).astype(np.float32)
+    if positive:
+        a = np.maximum(a, 0)
+    t = torch.from_numpy(a).to(dt).cuda()
+    return t[lead:].view(rows, ld)[:, :cols], t
+
+
+def expect(x, keep, scale, z=None, gate=None):
+    """The definition's value in x's type (x, z, gate: CPU tensors)."""
+    if gate is not None:
+        keep = keep & (gate.float().numpy() > 0)
+    with np.errstate(over="ignore", invalid="ignore"):
+        v = np.where(keep, x.float().numpy() * np.float32(scale), np.float32(0))
+        if z is not None:
+            v = z.float().numpy() + v
+    return torch.from_numpy(v.astype(np.float32)).to(x.dtype)
+
+
+def same(got, want):
+    it = torch.int32 if got.dtype == torch.float32 else torch.int16
+    g, w = got.contiguous(), want.contiguous()
+    nan = torch.isnan(w)
+    assert torch.equal(torch.isnan(g), nan)
+    assert torch.equal(g.view(it)[~nan], w.view(it)[~nan])
+
+
+def scale_of(p):
+    t = D.threshold(p)
+    return np.float32(65536) / np.float32(t) if t else np.float32(0)
+
+
+# rows, cols, x_ld, y_ld, z_ld, elements before the first one
+SHAPES = [(1, 1, 1, 1, 1, 0), (1, 7, 7, 7, 7, 0), (3, 8, 8, 8, 8, 0), (5, 1, 3, 2, 1, 0),
+          (64, 256, 1024, 256, 512, 0), (17, 40, 48, 64, 40, 8), (33, 129, 129, 129, 129, 0),
+          (33, 129, 140, 131, 129, 1), (257, 64, 64, 64, 64, 3), (9, 511, 511, 520, 512, 0),
+          (2, 4099, 4099, 4099, 4099, 0), (1000, 3, 3, 3, 3, 0), (1031, 1000, 1000, 1000, 1000, 0)]
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("kind", ["plain", "residual", "gate"])
+def test_matches_the_definition(dt, shape, kind):
+    rows, cols, xl, yl, zl, lead = shape
+    rng = np.random.default_rng(rows * 31 + cols)
+    x, _ = buffer(rows, cols, xl, TYPES[dt], rng, lead)
+    z, _ = buffer(rows, cols, zl, TYPES[dt], rng, lead)
+    y, whole = buffer(rows, cols, yl, TYPES[dt], rng, lead)
+    before = whole.cpu()
+    p, site, step = 0.3, 5, 0xFFFFFFF0
+    keep = D.keep(rows * cols, SEED, step, site, p).reshape(rows, cols)
+    d = fg.DropoutDesc.make(rows, cols, p, SEED, site=site, step=step, dtype=fg.dtype_of(x),
+                            x_ld=xl, y_ld=yl, z_ld=zl if kind != "plain" else 0)
+    if kind == "gate":
+        fg.dropout_bwd(d, x, y, gate=z)
+    else:
+        fg.dropout_fwd(d, x, y, residual=z if kind == "residual" else None)
+    want = expect(x.cpu(), keep, scale_of(p), z.cpu() if kind == "residual" else None,
+                  z.cpu() if kind == "gate" else None)
+    same(y.cpu(), want)
+    # nothing around the rows is touched
+    after = whole.cpu()
+    after[lead:].view(rows, yl)[:, :cols] = before[lead:].view(rows, yl)[:, :cols]
+    assert torch.equal(after, before)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("p", [0.0, 1e-7, 0.1, 0.5, 0.999, 1.0])
+def test_all_or_nothing_and_masked_values(dt, p):
+    """Dropped infinities and NaN become +0; kept ones pass."""
+    rng = np.random.default_rng(3)
+    x, _ = buffer(40, 72, 72, TYPES[dt], rng)
+    x[::3, ::5] = float("inf")
+    x[1::3, ::7] = float("nan")
+    x[2::3, ::4] = -0.0
+    y = torch.empty_like(x)
+    d = fg.DropoutDesc.make(40, 72, p, 7, dtype=fg.dtype_of(x))
+    fg.dropout_fwd(d, x, y)
+    keep = D.keep(40 * 72, 7, 0, 0, p).reshape(40, 72)
+    assert keep.all() if p < 1e-6 else not keep.any() if p == 1 else 0 < keep.sum() < keep.size
+    same(y.cpu(), expect(x.cpu(), keep, scale_of(p)))
+
+
+def test_in_place_and_beside_itself():
+    """y = x; y = the residual; y a slice beside x's in one buffer."""
+    rng = np.random.default_rng(4)
+    rows, cols, ld, p = 129, 64, 192, 0.5
+    keep = D.keep(rows * cols, SEED, 9, 2, p).reshape(rows, cols)
+    d = fg.DropoutDesc.make(rows, cols, p, SEED, site=2, step=9, x_ld=ld, y_ld=ld, z_ld=ld)
+    x, _ = buffer(rows, cols, ld, torch.float16, rng)
+    x0 = x.cpu()
+    fg.dropout_fwd(d, x, x)
+    same(x.cpu(), expect(x0, keep, 2))
+    _, whole = buffer(rows, ld, ld, torch.float16, rng)
+    whole = whole.view(rows, ld)
+    w0 = whole.cpu()
+    a, b = whole[:, :64], whole[:, 64:128]
+    fg.dropout_fwd(d, a, b, residual=b)
+    same(b.cpu(), expect(w0[:, :64], keep, 2, z=w0[:, 64:128]))
+    assert torch.equal(whole.cpu()[:, :64], w0[:, :64])
+    assert torch.equal(whole.cpu()[:, 128:], w0[:, 128:])
+
+
+def test_forward_and_gradient_draw_one_mask():
+    """Whatever the strides and types of each, and gated by the dropout's own output."""
+    rng = np.random.default_rng(5)
+    rows, cols = 200, 96
+    x, _ = buffer(rows, cols, 96, torch.float32, rng, positive=True)
+    dy, _ = buffer(rows, cols, 104, torch.bfloat16, rng)
+    y, dx = torch.empty_like(x), torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    fg.dropout_fwd(fg.DropoutDesc.make(rows, cols, 0.4, 11, dtype=fg.F32), x, y)
+    gate = y.to(torch.bfloat16)
+    d = fg.DropoutDesc.make(rows, cols, 0.4, 11, dtype=fg.BF16, x_ld=104)
+    fg.dropout_bwd(d, dy, dx, gate=gate)
+    kept = (y > 0).cpu()
+    assert torch.equal(dx.cpu() != 0, kept & (dy.cpu() != 0))
+    fg.dropout_bwd(d, dy, dx)
+    keep = torch.from_numpy(D.keep(rows * cols, 11, 0, 0, 0.4).reshape(rows, cols))
+    assert torch.equal(dx.cpu() != 0, keep & (dy.cpu() != 0))
+
+
+def test_step_is_counted_on_the_device():
+    """The mask follows the step count, also in a captured graph."""
+    rows, cols = 64, 512
+    x = torch.ones(rows, cols, dtype=torch.float16, device="cuda")
+    y = torch.empty_like(x)
+    step = torch.zeros(1, dtype=torch.int32, device="cuda")
+    d = fg.DropoutDesc.make(rows, cols, 0.5, 77, site=1, step=100)
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            fg.dropout_fwd(d, x, y, step_count=step)
+            step += 1
+    torch.cuda.synchronize()
+    step.zero_()
+    for k in range(3):
+        g.replay()
+        torch.cuda.synchronize()
+        keep = D.keep(rows * cols, 77, 100 + k, 1, 0.5).reshape(rows, cols)
+        assert np.array_equal(y.cpu().numpy() != 0, keep)
+
+
+def test_many_elements_beyond_the_grid():
+    """More elements than one turn of the launch takes, dense and with odd rows."""
+    for rows, cols in ((1, (1 << 24) + (1 << 22) + 13), (20_001, 1049)):
+        x = torch.randn(rows, cols, device="cuda").half()
+        y = torch.empty_like(x)
+        fg.dropout_fwd(fg.DropoutDesc.make(rows, cols, 0.5, SEED, step=3), x, y)
+        keep = D.keep(rows * cols, SEED, 3, 0, 0.5).reshape(rows, cols)
+        same(y.cpu(), expect(x.cpu(), keep, 2))
