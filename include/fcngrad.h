@@ -538,6 +538,54 @@ fg_status dropout_fwd(const fg_dropout_desc *d, const void *x, const void *resid
 fg_status dropout_bwd(const fg_dropout_desc *d, const void *dy, const void *gate, void *dx,
                       const int32_t *step_count, hipStream_t stream);
 
+/* Softmax cross entropy of a linear head (an FC-DenseNet's per-pixel classes, or a
+ * vocabulary): logits l = h w^T of `rows` feature vectors h against `vocab` classes'
+ * weights w (a 1x1 convolution's, K = vocab), which are never stored; per row
+ *   lse = log sum_v exp(l_v), loss = weight * (lse - l_target).
+ * fp16 or bf16 operands; products, exponentials and sums in fp32. */
+typedef struct {
+    int64_t rows;
+    int64_t h_ld, w_ld, dh_ld, dw_ld;  /* row strides, elements; 0: dense (hidden) */
+    double scale;      /* the gradients are those of scale * L (loss scale, shares) */
+    int32_t hidden, vocab;
+    int32_t dtype;     /* of h, w, dh and dw: FG_F16 or FG_BF16 */
+    int32_t mean;      /* L: 0: the sum of the losses; 1: that over the weights' sum */
+} fg_xent_desc;
+
+/* Device workspace in bytes that linear_xent_grad (grad != 0) or linear_xent_fwd needs;
+ * 0 for an invalid or unsupported descriptor. For gradients it holds 16-bit softmax
+ * numerators of a piece of the rows: at most 1 GiB or 256 rows' of them. */
+size_t fg_linear_xent_workspace_bytes(const fg_xent_desc *d, int grad);
+
+/* Losses. h: rows x hidden, w: vocab x hidden. target: int32 per row; a row whose
+ * target is outside [0, vocab), or whose weight is 0, is masked: its loss and lse are
+ * 0 and nothing else depends on it, whatever h holds there. weight: fp32 per row, or
+ * null (1). loss: fp32 per row. lse (fp32 per row) and totals (two fp32: the sum of the
+ * losses, and of the live rows' weights) may be null. rows = 0 is allowed (pointers of
+ * per-row arrays may then be null): the totals are 0. Not-a-number logits give NaN
+ * losses; logits of -inf are fine while a row has a finite one. ws: 16-byte aligned,
+ * scratch. FG_EINVAL for a null pointer, rows < 0, hidden or vocab < 1, a stride below
+ * hidden, a non-finite scale, an unknown dtype or mean, a pointer not aligned to its
+ * elements, or an output overlapping another tensor; FG_EUNSUPPORTED for rows of 2^28,
+ * hidden above 2^16, vocab of 2^22 - 64 or strides of 2^20 or more, FG_F32, or w not
+ * 16-byte aligned while hidden and w_ld are multiples of 8; FG_EWORKSPACE. */
+fg_status linear_xent_fwd(const fg_xent_desc *d, const void *h, const void *w,
+                          const int32_t *target, const float *weight, float *loss, float *lse,
+                          float *totals, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Losses, as above, and the gradients of scale * L, each rounded once to dtype:
+ * dh (rows x hidden; 0 in masked rows) and dw (vocab x hidden; e.g. a member's place in
+ * its gradient group); either may be null. G = weight * (softmax - onehot) is rounded to
+ * dtype for the products dh = G w and dw = G^T h, its largest magnitude being scaled to
+ * 2^15; their sums are fp32. found_nonfinite (device int32, may be null) is set to 1 if
+ * an element of dw is infinite or NaN, never cleared. With mean and weights that sum to
+ * 0 (or no live row) the gradients are 0, as dw is without rows. Deterministic: every
+ * sum has a fixed order. Errors as above, and FG_EINVAL if both dh and dw are null. */
+fg_status linear_xent_grad(const fg_xent_desc *d, const void *h, const void *w,
+                           const int32_t *target, const float *weight, float *loss, float *lse,
+                           float *totals, void *dh, void *dw, int32_t *found_nonfinite,
+                           void *ws, size_t ws_bytes, hipStream_t stream);
+
 /* Output spatial size: transpose = 0 gives the forward P, Q; 1 gives the
  * transposed convolution's output size. FG_EINVAL if it is not positive. */
 fg_status fg_conv_out_dims(const fg_conv_desc *d, int transpose, int32_t *p,

@@ -32,6 +32,7 @@ ENTRY_POINTS = (
     "grad_flags_clear", "fg_loss_scale_update", "fg_lr_at", "fg_profile_next_launch",
     "conv2d_bwd_weight_noalloc", "fg_mfma_loop",
     "dropout_fwd", "dropout_bwd",
+    "linear_xent_fwd", "linear_xent_grad", "fg_linear_xent_workspace_bytes",
 )
 MFMA_LOOP_MAX_WORK = 1 << 28  # blocks * iters accepted by fg_mfma_loop
 MFMA_LOOP_FLOPS_PER_BLOCK_ITER = 1 << 20
@@ -77,6 +78,20 @@ class DropoutDesc(ctypes.Structure):
     @classmethod
     def make(cls, rows, cols, p, seed, site=0, step=0, dtype=F16, x_ld=0, y_ld=0, z_ld=0):
         return cls(rows, cols, x_ld, y_ld, z_ld, seed, p, site, step, dtype)
+
+
+class XentDesc(ctypes.Structure):
+    """fg_xent_desc. Strides 0: dense."""
+    _fields_ = [("rows", ctypes.c_int64), ("h_ld", ctypes.c_int64),
+                ("w_ld", ctypes.c_int64), ("dh_ld", ctypes.c_int64),
+                ("dw_ld", ctypes.c_int64), ("scale", ctypes.c_double),
+                ("hidden", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("mean", ctypes.c_int32)]
+
+    @classmethod
+    def make(cls, rows, hidden, vocab, dtype=F16, mean=True, scale=1.0, h_ld=0, w_ld=0,
+             dh_ld=0, dw_ld=0):
+        return cls(rows, h_ld, w_ld, dh_ld, dw_ld, scale, hidden, vocab, dtype, int(mean))
 
 
 class LibraryNotBuilt(RuntimeError):
@@ -144,6 +159,8 @@ def lib():
         "huber_head_grad": [vp, vp, u64, ctypes.c_double, ctypes.c_double, vp, vp],
         "dropout_fwd": [ctypes.POINTER(DropoutDesc), vp, vp, vp, vp, vp],
         "dropout_bwd": [ctypes.POINTER(DropoutDesc), vp, vp, vp, vp, vp],
+        "linear_xent_fwd": [ctypes.POINTER(XentDesc)] + [vp] * 8 + [sz, vp],
+        "linear_xent_grad": [ctypes.POINTER(XentDesc)] + [vp] * 11 + [sz, vp],
         "avg_pool2d_fwd": [vp, i32, i32, i32, i32, vp, vp],
         "avg_pool2d_bwd": [vp, vp, i32, i32, i32, i32, vp, vp],
         "channel_slice_copy": [vp, i32, vp, i32, vp, i32, ctypes.c_int64, i32, i32, vp],
@@ -171,6 +188,8 @@ def lib():
     L.lars_adam_apply.restype = ctypes.c_int
     L.fg_lars_adam_workspace_bytes.argtypes = [ctypes.POINTER(OptTensor), i32]
     L.fg_lars_adam_workspace_bytes.restype = ctypes.c_size_t
+    L.fg_linear_xent_workspace_bytes.argtypes = [ctypes.POINTER(XentDesc), ctypes.c_int]
+    L.fg_linear_xent_workspace_bytes.restype = ctypes.c_size_t
     L.fg_conv_workspace_bytes.argtypes = [pdesc, ctypes.c_int]
     L.fg_conv_workspace_bytes.restype = ctypes.c_size_t
     L.fg_conv_kernel_name.argtypes = [pdesc, ctypes.c_int]
@@ -447,6 +466,51 @@ def dropout_fwd(desc, x, y, residual=None, step_count=None, stream=None):
 def dropout_bwd(desc, dy, dx, gate=None, step_count=None, stream=None):
     """Gradient of dropout_fwd's x from dy into dx, zero where gate <= 0."""
     _dropout("dropout_bwd", desc, dy, dx, gate, "gate", step_count, stream)
+
+
+def linear_xent_workspace_bytes(desc, grad):
+    return lib().fg_linear_xent_workspace_bytes(ctypes.byref(desc), int(grad))
+
+
+def _vector(name, t, n, dtype):
+    import torch
+    if t is None:
+        return None
+    if t.dtype != getattr(torch, dtype) or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements")
+    return t.data_ptr()
+
+
+def _xent_args(desc, h, w, target, loss, lse, totals, weight):
+    n = desc.rows
+    return (ctypes.byref(desc), _matrix("h", h, n, desc.hidden, desc.h_ld, desc.dtype),
+            _matrix("w", w, desc.vocab, desc.hidden, desc.w_ld, desc.dtype),
+            _vector("target", target, n, "int32"), _vector("weight", weight, n, "float32"),
+            _vector("loss", loss, n, "float32"), _vector("lse", lse, n, "float32"),
+            _vector("totals", totals, 2, "float32"))
+
+
+def linear_xent_fwd(desc, h, w, target, loss, lse=None, totals=None, weight=None, ws=None,
+                    stream=None):
+    """Softmax cross entropy of the logits h w^T (see include/fcngrad.h): fp32 losses per
+    row, their log-sum-exp, and the sums of losses and weights. ws: uint8 tensor of
+    linear_xent_workspace_bytes(desc, False)."""
+    wp, wb = _ws(ws)
+    _check("linear_xent_fwd", lib().linear_xent_fwd(
+        *_xent_args(desc, h, w, target, loss, lse, totals, weight), wp, wb, _s(stream)))
+
+
+def linear_xent_grad(desc, h, w, target, loss, dh, dw, lse=None, totals=None, weight=None,
+                     found_nonfinite=None, ws=None, stream=None):
+    """linear_xent_fwd with the gradients of desc.scale times the losses' sum (or weighted
+    mean, desc.mean) into dh and dw (either may be None). found_nonfinite: device int32
+    raised if dw holds an infinity or NaN. ws: linear_xent_workspace_bytes(desc, True)."""
+    wp, wb = _ws(ws)
+    _check("linear_xent_grad", lib().linear_xent_grad(
+        *_xent_args(desc, h, w, target, loss, lse, totals, weight),
+        _matrix("dh", dh, desc.rows, desc.hidden, desc.dh_ld, desc.dtype),
+        _matrix("dw", dw, desc.vocab, desc.hidden, desc.dw_ld, desc.dtype),
+        _counter("found_nonfinite", found_nonfinite), wp, wb, _s(stream)))
 
 
 def grad_flags_clear(flags, stream=None):

@@ -1004,6 +1004,77 @@ fg_status dropout_bwd(const fg_dropout_desc *d, const void *dy, const void *gate
   return dropout_call(d, dy, gate, true, dx, step_count, stream);
 }
 
+static fg_status xent_desc_ok(const fg_xent_desc *d) {
+  if (!d || d->rows < 0 || d->hidden < 1 || d->vocab < 1 || !std::isfinite(d->scale) ||
+      d->dtype < FG_F16 || d->dtype > FG_F32 || (d->mean != 0 && d->mean != 1))
+    return FG_EINVAL;
+  for (int64_t ld : {d->h_ld, d->w_ld, d->dh_ld, d->dw_ld})
+    if (ld != 0 && ld < d->hidden) return FG_EINVAL;
+  for (int64_t ld : {d->h_ld, d->w_ld, d->dh_ld, d->dw_ld})
+    if (ld >= (int64_t)1 << 20) return FG_EUNSUPPORTED;
+  if (d->dtype == FG_F32 || d->rows >= (int64_t)1 << 28 || d->hidden > 1 << 16 ||
+      d->vocab >= (1 << 22) - 64)
+    return FG_EUNSUPPORTED;
+  return FG_OK;
+}
+
+size_t fg_linear_xent_workspace_bytes(const fg_xent_desc *d, int grad) {
+  return xent_desc_ok(d) == FG_OK ? linear_xent_ws_bytes(*d, grad != 0) : 0;
+}
+
+static fg_status xent_call(const fg_xent_desc *d, const void *h, const void *w,
+                           const int32_t *target, const float *weight, float *loss, float *lse,
+                           float *totals, void *dh, void *dw, int32_t *flag, bool grad, void *ws,
+                           size_t ws_bytes, hipStream_t stream) {
+  const fg_status ok = xent_desc_ok(d);
+  if (ok != FG_OK) return ok;
+  if (!w || !ws || (d->rows && (!h || !target || !loss))) return FG_EINVAL;
+  if (grad && !dh && !dw) return FG_EINVAL;
+  if (((uintptr_t)h | (uintptr_t)w | (uintptr_t)dh | (uintptr_t)dw) % 2 ||
+      ((uintptr_t)target | (uintptr_t)weight | (uintptr_t)loss | (uintptr_t)lse |
+       (uintptr_t)totals | (uintptr_t)flag) % 4)
+    return FG_EINVAL;
+  const auto ld = [&](int64_t v) { return v ? v : (int64_t)d->hidden; };
+  if (d->hidden % 8 == 0 && ld(d->w_ld) % 8 == 0 && ((uintptr_t)w & 15)) return FG_EUNSUPPORTED;
+  const size_t need = linear_xent_ws_bytes(*d, grad);
+  if (ws_bytes < need || ((uintptr_t)ws & 15)) return FG_EWORKSPACE;
+  const auto span = [&](int64_t n, int64_t l) {
+    return n ? (size_t)((n - 1) * ld(l) + d->hidden) * 2 : (size_t)0;
+  };
+  const size_t rows4 = (size_t)d->rows * 4;
+  const struct {
+    const void *p;
+    size_t n;
+    bool out;
+  } t[] = {{loss, rows4, true},       {lse, rows4, true},
+           {totals, 8, true},         {dh, span(d->rows, d->dh_ld), true},
+           {dw, span(d->vocab, d->dw_ld), true}, {flag, 4, true},
+           {ws, need, true},          {h, span(d->rows, d->h_ld), false},
+           {w, span(d->vocab, d->w_ld), false},  {target, rows4, false},
+           {weight, rows4, false}};
+  for (const auto &a : t)
+    for (const auto &b : t)
+      if (a.out && &a != &b && a.p && b.p && a.n && b.n && overlap(a.p, a.n, b.p, b.n))
+        return FG_EINVAL;
+  return launch_status(launch_linear_xent(*d, h, w, target, weight, loss, lse, totals, dh, dw,
+                                          flag, grad, ws, stream));
+}
+
+fg_status linear_xent_fwd(const fg_xent_desc *d, const void *h, const void *w,
+                          const int32_t *target, const float *weight, float *loss, float *lse,
+                          float *totals, void *ws, size_t ws_bytes, hipStream_t stream) {
+  return xent_call(d, h, w, target, weight, loss, lse, totals, nullptr, nullptr, nullptr, false,
+                   ws, ws_bytes, stream);
+}
+
+fg_status linear_xent_grad(const fg_xent_desc *d, const void *h, const void *w,
+                           const int32_t *target, const float *weight, float *loss, float *lse,
+                           float *totals, void *dh, void *dw, int32_t *found_nonfinite,
+                           void *ws, size_t ws_bytes, hipStream_t stream) {
+  return xent_call(d, h, w, target, weight, loss, lse, totals, dh, dw, found_nonfinite, true, ws,
+                   ws_bytes, stream);
+}
+
 fg_status relu_backward(const uint16_t *dy, const uint16_t *act,
                         uint64_t numel, uint16_t *out, hipStream_t stream) {
   if (!dy || !act || !out || numel == 0) return FG_EINVAL;

@@ -16,6 +16,7 @@ constexpr unsigned kOOB = 0x80000000u;   // beyond any tensor: loads zero
 // the LDS ring, WGM x WGN waves each owning (TM/WGM) x (TN/WGN).
 template <int BK_, int NS_, int WGM_, int WGN_, int TM_, int TN_>
 struct Pipe {
+  static constexpr bool BF = false;                  // operands: fp16, or bf16
   static constexpr int BK = BK_, NS = NS_, WGM = WGM_, WGN = WGN_, TM = TM_, TN = TN_;
   static constexpr int NW = WGM * WGN, NT = 64 * NW;
   static constexpr int WM = TM / WGM, WN = TN / WGN;
@@ -30,6 +31,10 @@ struct Pipe {
   static constexpr int WPE = 160 * 1024 / (NS * (A_BYTES + B_BYTES)) * NW / 4;
   static_assert(A_BYTES == 1024 * NW * PA && B_BYTES == 1024 * NW * PB,
                 "DMA instructions must divide among waves");
+};
+template <class P>
+struct Bf16 : P {
+  static constexpr bool BF = true;
 };
 // Square tiles of the large kernels.
 template <int BK_, int NS_, int WGM_, int WGN_, int T_ = 256>
@@ -187,7 +192,9 @@ __device__ __forceinline__ void mma(f32x16 (&acc)[C::FM][C::FN],
 #pragma unroll
   for (int i = 0; i < C::FM; ++i)
 #pragma unroll
-    for (int j = 0; j < C::FN; ++j) acc[i][j] = mfma32(f.a[i], f.b[j], acc[i][j]);
+    for (int j = 0; j < C::FN; ++j)
+      acc[i][j] = C::BF ? mfma32_bf16(f.a[i], f.b[j], acc[i][j])
+                        : mfma32(f.a[i], f.b[j], acc[i][j]);
 }
 
 // s_waitcnt with only lgkmcnt (LDS) constrained to 0.

@@ -185,6 +185,12 @@ inline uint32_t dropout_threshold(double p) { return (uint32_t)((1.0 - p) * 6553
 hipError_t launch_dropout(const fg_dropout_desc &d, const void *x, const void *z, bool gate,
                           void *y, const int32_t *step_count, hipStream_t st);
 
+size_t linear_xent_ws_bytes(const fg_xent_desc &d, bool grad);
+hipError_t launch_linear_xent(const fg_xent_desc &d, const void *h, const void *w,
+                              const int32_t *target, const float *weight, float *loss,
+                              float *lse, float *totals, void *dh, void *dw, int32_t *flag,
+                              bool grad, void *ws, hipStream_t st);
+
 // One-shot profiling events (fg_profile_next_launch): prof_begin records the
 // armed start event on the stream, prof_end the stop event, then disarms.
 // Both do nothing when no events are armed.

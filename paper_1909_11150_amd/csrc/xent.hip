@@ -1,0 +1,1043 @@
+// Softmax cross entropy of a linear head, with its gradients, over any number of
+// classes; the logits are never stored.
+//
+//   l = h W^T,  lse = log sum_v exp(l_v),  loss = w (lse - l_target)
+//   G = w (exp(l - lse) - onehot),  dh = c G W,  dW = c G^T h
+//
+// Rows whose target is no class (or whose weight is 0) are masked. The live rows
+// are first copied one after another into the workspace (features padded with
+// zeros to a multiple of 64), so masked rows cost no matrix work, whatever they
+// hold, infinities and NaN too, reaches nothing, and every operand of the matrix
+// products is aligned.
+//
+// Products run on MFMA tiles fed by LDS DMA (dma_pipe.h), in pieces of the live
+// rows and tiles of the classes:
+//   logits   one tile of l in the accumulators, classes x rows, so a row's classes
+//            lie in one lane's registers (and its neighbour's half): the tile's
+//            maximum m and sum of exp(l - m) per row are stored; for gradients also
+//            2^15 exp(l - m) in fp16, the only trace of a logit in memory, for the
+//            rows of one piece;
+//   softmax  joins a row's tiles into lse, and turns the numerators into 2^15 G in
+//            the features' type, in place;
+//   product  dh = G W and dW = G^T h, whose strided operands are read with
+//            transposing LDS reads; the sum over the classes (rows) is split where
+//            there are few tiles, and joined in a fixed order.
+// The gradients thus take three products of rows x hidden x classes; without the
+// numerators they would take four.
+#include <algorithm>
+
+#include "dma_pipe.h"
+
+namespace fg {
+namespace xent {
+
+using namespace dma;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// Numerators and G are held times 2^15: the largest is then 2^15, within fp16, and
+// values down to 2^-29 of it keep all their bits (2^-14 otherwise).
+constexpr float kUp = 32768.f;
+constexpr int kSlot = 16;       // rows of a workgroup of the copy and softmax kernels
+constexpr int kCount = 1024;    // rows of a workgroup of the counting kernel
+
+using P256 = Pipe<32, 5, 2, 4, 256, 256>;  // 8 waves of 128 x 64
+using P128 = Pipe<64, 2, 2, 2, 128, 128>;  // 4 waves of 64 x 64
+using P64 = Pipe<64, 3, 2, 2, 64, 64>;     // 4 waves of 32 x 32
+
+// What the first kernels find out, read by the others.
+struct Found {
+  int32_t live;     // rows
+  float wmax_inv;   // 1 / largest |weight|
+  float mult;       // G W and G^T h times this are the gradients
+  float wsum;
+};
+
+// ---- live rows -----------------------------------------------------------------
+struct RowArgs {
+  const uint16_t *h;
+  int64_t h_ld;
+  const int32_t *target;
+  const float *weight;
+  int32_t T, H, Hp, V;
+  int32_t nb;            // workgroups of the counting kernel
+  double scale;
+  int32_t mean, hvec, dhvec;
+  int32_t *count;        // live rows per counted block, then before it
+  double *wsum;
+  float *wmax;
+  Found *found;
+  int32_t *idx, *ctarget;
+  float *cweight;
+  uint16_t *hc;
+  float *loss, *lse;
+  uint16_t *dh;          // null: no gradients of the features
+  int64_t dh_ld;
+};
+
+__device__ __forceinline__ bool live_row(const RowArgs &a, int r, float &w) {
+  w = 1.f;
+  if (r >= a.T || (uint32_t)a.target[r] >= (uint32_t)a.V) return false;
+  if (a.weight) w = a.weight[r];
+  return w != 0.f;
+}
+
+template <class T>
+__device__ __forceinline__ T wave_sum(T v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+
+// Live rows, their weights' sum and largest magnitude, per block of 1024 rows.
+__global__ __launch_bounds__(256) void xent_count_kernel(RowArgs a) {
+  __shared__ double ws[4];
+  __shared__ float wm[4];
+  __shared__ int cn[4];
+  int n = 0;
+  double sum = 0;
+  float mx = 0.f;
+#pragma unroll
+  for (int k = 0; k < kCount / 256; ++k) {
+    float w;
+    if (live_row(a, blockIdx.x * kCount + k * 256 + threadIdx.x, w)) {
+      ++n;
+      sum += w;
+      mx = fmaxf(mx, fabsf(w));
+    }
+  }
+  n = wave_sum(n);
+  sum = wave_sum(sum);
+  mx = wave_max(mx);
+  if ((threadIdx.x & 63) == 0) {
+    const int k = threadIdx.x >> 6;
+    cn[k] = n, ws[k] = sum, wm[k] = mx;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a.count[blockIdx.x] = cn[0] + cn[1] + cn[2] + cn[3];
+    a.wsum[blockIdx.x] = (ws[0] + ws[1]) + (ws[2] + ws[3]);
+    a.wmax[blockIdx.x] = fmaxf(fmaxf(wm[0], wm[1]), fmaxf(wm[2], wm[3]));
+  }
+}
+
+// One workgroup: counts become the live rows before each block; the totals.
+__global__ __launch_bounds__(1024) void xent_scan_kernel(RowArgs a) {
+  __shared__ double ws[16];
+  __shared__ float wm[16];
+  __shared__ int cn[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int base = 0;
+  double sum = 0;
+  float mx = 0.f;
+  for (int b0 = 0; b0 < a.nb; b0 += 1024) {
+    const int b = b0 + threadIdx.x;
+    const int c = b < a.nb ? a.count[b] : 0;
+    if (b < a.nb) {
+      sum += a.wsum[b];
+      mx = fmaxf(mx, a.wmax[b]);
+    }
+    int incl = c;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(incl, o);
+      if (lane >= o) incl += v;
+    }
+    __syncthreads();
+    if (lane == 63) cn[wave] = incl;
+    __syncthreads();
+    int before = base;
+    for (int k = 0; k < wave; ++k) before += cn[k];
+    if (b < a.nb) a.count[b] = before + incl - c;
+    for (int k = 0; k < 16; ++k) base += cn[k];
+  }
+  sum = wave_sum(sum);
+  mx = wave_max(mx);
+  if (lane == 0) ws[wave] = sum, wm[wave] = mx;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int k = 1; k < 16; ++k) {
+      sum += ws[k];
+      mx = fmaxf(mx, wm[k]);
+    }
+    // no live row, or weights that cancel: a mean of nothing has no gradient
+    const double den = a.mean ? sum : 1.0;
+    a.found->live = base;
+    a.found->wsum = (float)sum;
+    a.found->wmax_inv = mx > 0.f ? 1.f / mx : 1.f;
+    a.found->mult = den != 0.0 ? (float)(a.scale / den * (mx > 0.f ? mx : 1.f) / kUp) : 0.f;
+  }
+}
+
+// 8 elements of a row from column c on, zeros past its end.
+__device__ __forceinline__ u32x4 row8(const uint16_t *row, int c, int n, bool vec) {
+  if (vec && c + 8 <= n) return *reinterpret_cast<const u32x4 *>(row + c);
+  u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (c + e < n) v[e >> 1] |= (uint32_t)row[c + e] << (16 * (e & 1));
+  return v;
+}
+__device__ __forceinline__ void put8(uint16_t *row, int c, int n, bool vec, const u32x4 &v) {
+  if (vec && c + 8 <= n) {
+    *reinterpret_cast<u32x4 *>(row + c) = v;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (c + e < n) row[c + e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+}
+
+// Copies live rows to their places, in order; results of masked rows are written
+// here. (What stands after the last live row is never read into a result.)
+__global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
+  __shared__ int cn[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int r0 = blockIdx.x * kSlot, blk = r0 / kCount;
+  // live rows of this counted block before r0
+  int n = 0;
+  for (int r = blk * kCount + threadIdx.x; r < r0; r += 256) {
+    float w;
+    n += live_row(a, r, w);
+  }
+  n = wave_sum(n);
+  if (lane == 0) cn[wave] = n;
+  __syncthreads();
+  const int before = a.count[blk] + cn[0] + cn[1] + cn[2] + cn[3];
+  float w = 0.f;
+  const bool mine = lane < kSlot && live_row(a, r0 + lane, w);
+  const uint64_t mask = __ballot(mine);
+  const int place = before + __popcll(mask & ((1ull << lane) - 1));
+  if (wave == 0 && lane < kSlot) {
+    const int r = r0 + lane;
+    if (mine) {
+      a.idx[place] = r;
+      a.ctarget[place] = a.target[r];
+      a.cweight[place] = w;
+    } else if (r < a.T) {
+      a.loss[r] = 0.f;
+      if (a.lse) a.lse[r] = 0.f;
+    }
+  }
+  for (int k = wave; k < kSlot; k += 4) {
+    const int r = r0 + k, to = __shfl(place, k);
+    const bool on = mask >> k & 1;
+    const uint16_t *src = a.h + (int64_t)r * a.h_ld;
+    for (int c = 8 * lane; on && c < a.Hp; c += 512)
+      *reinterpret_cast<u32x4 *>(a.hc + (size_t)to * a.Hp + c) = row8(src, c, a.H, a.hvec);
+    if (!on && a.dh && r < a.T)
+      for (int c = 8 * lane; c < a.H; c += 512)
+        put8(a.dh + (int64_t)r * a.dh_ld, c, a.H, a.dhvec, u32x4{0, 0, 0, 0});
+  }
+}
+
+// The head's weights with rows padded to a multiple of 64, where theirs are not
+// aligned as the DMA needs them.
+__global__ __launch_bounds__(256) void xent_pad_kernel(const uint16_t *w, int64_t ld, int32_t H,
+                                                       uint16_t *wc, int32_t Hp, int64_t chunks) {
+  const int64_t stride = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < chunks; i += stride) {
+    const int64_t r = i / (Hp / 8);
+    const int c = (int)(i - r * (Hp / 8)) * 8;
+    *reinterpret_cast<u32x4 *>(wc + r * Hp + c) = row8(w + r * ld, c, H, false);
+  }
+}
+
+// ---- tiles -----------------------------------------------------------------------
+// This wave's part of the ring, 64 WM bytes, once every wave is done reading it.
+template <class P>
+__device__ __forceinline__ uint8_t *wave_buf(const Ring &R, int wave) {
+  constexpr int S = 64 * P::WM, PER = P::A_BYTES / S;
+  static_assert(PER > 0 && (P::NW + PER - 1) / PER <= P::NS, "the ring stages a store");
+  uint8_t *buf = R.a[0];
+#pragma unroll
+  for (int k = 1; k < (P::NW + PER - 1) / PER; ++k)
+    if (wave / PER == k) buf = R.a[k];
+  return buf + (wave % PER) * S;
+}
+
+// 16-bit store of a wave's block: pack(i, j, g) gives 4 consecutive columns of lane
+// row 32 j + lane % 32, put(row, column, 8 values) writes them, both counted in the
+// block. 32 rows at a time go through this wave's buffer, 16-byte chunks permuted
+// by the row, so that neighbouring lanes write one row's consecutive bytes.
+template <class P, class Pack, class Put>
+__device__ __forceinline__ void store16(uint8_t *buf, int lane, Pack &&pack, Put &&put) {
+  constexpr int CPW = P::WM / 8, RB = P::WM * 2, SH = CPW == 16 ? 0 : CPW == 8 ? 1 : 2;
+#pragma unroll
+  for (int j = 0; j < P::FN; ++j) {
+    const int p = lane & 31;
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<u32x2 *>(buf + p * RB +
+                                   (((4 * i + g) ^ ((p >> SH) & (CPW - 1))) << 4) +
+                                   8 * (lane >> 5)) = pack(i, j, g);
+    wait_lds();
+    __builtin_amdgcn_wave_barrier();
+    constexpr int RPI = 64 / CPW;
+    const int q = lane % CPW;
+    u32x4 d[32 / RPI];
+#pragma unroll
+    for (int k = 0; k < 32 / RPI; ++k) {
+      const int r = k * RPI + lane / CPW;
+      d[k] = *reinterpret_cast<const u32x4 *>(buf + r * RB + ((q ^ ((r >> SH) & (CPW - 1))) << 4));
+    }
+#pragma unroll
+    for (int k = 0; k < 32 / RPI; ++k) put(32 * j + k * RPI + lane / CPW, 8 * q, d[k]);
+    wait_lds();
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b, bool bf) {
+  if (bf) {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, b2{(__bf16)a, (__bf16)b});
+  }
+  return (uint32_t)f32_to_h(a) | ((uint32_t)f32_to_h(b) << 16);
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void *p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, kRsrcFlags);
+}
+
+// ---- logits ------------------------------------------------------------------------
+struct LogitArgs {
+  const uint16_t *w;
+  int64_t w_ld;
+  int32_t wh;             // elements of a row of w that are there (a multiple of 8)
+  int32_t V;
+  const uint16_t *hc;     // the piece's first row
+  int32_t Hp;
+  const Found *found;
+  int32_t row0, Tc;       // first live row of the piece, rows it may have
+  const int32_t *ctarget;
+  uint16_t *e;            // [Tc][Vp] numerators, fp16 (STORE)
+  int32_t Vp;
+  float2 *stats;          // [tile of classes][Tc]: numerators times 2^x are exp(l); sum
+  float *tlogit;          // [Tc]
+};
+
+// exp(l) 2^scale_of(m) is the numerator of l in a tile whose largest logit is m (all
+// -inf, where no class of a tile is possible: any finite scale gives zeros).
+__device__ __forceinline__ float scale_of(float m) {
+  return m == -INFINITY ? 15.f : 15.f - m * kLog2e;
+}
+
+__device__ __forceinline__ int piece_rows(const Found *f, int row0, int Tc) {
+  return min(max(f->live - row0, 0), Tc);
+}
+
+template <class P, bool STORE>
+__global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a, TileMap tm) {
+  FG_DMA_RING(P, R);
+  constexpr int PA = P::PA, PB = P::PB, BK = P::BK;
+  int tx, ty, tz;  // rows, classes
+  if (!tm.decode(blockIdx.x, tx, ty, tz)) return;
+  const int n0 = tx * P::TN, m0 = ty * P::TM;
+  const int rows = piece_rows(a.found, a.row0, a.Tc);
+  if (n0 >= rows) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / P::WGN, wm0 = wm * P::WM, wn0 = (wave % P::WGN) * P::WN;
+
+  const int wrows = min(P::TM, a.V - m0);
+  const __amdgpu_buffer_rsrc_t rs_w =
+      rsrc(a.w + m0 * a.w_ld, (uint32_t)((wrows - 1) * a.w_ld + a.wh) * 2u);
+  const __amdgpu_buffer_rsrc_t rs_h = rsrc(a.hc + (size_t)n0 * a.Hp, (uint32_t)P::TN * a.Hp * 2u);
+  const KmSlot<PA> as = km_slots<BK, PA>(wave, lane);
+  const KmSlot<PB> bs = km_slots<BK, PB>(wave, lane);
+  unsigned oa[PA], ob[PB];
+#pragma unroll
+  for (int jj = 0; jj < PA; ++jj) oa[jj] = (unsigned)(as.row[jj] * (int)a.w_ld + as.coff[jj]) * 2u;
+#pragma unroll
+  for (int jj = 0; jj < PB; ++jj) ob[jj] = (unsigned)(bs.row[jj] * a.Hp + bs.coff[jj]) * 2u;
+  auto issue = [&](int st, int slot) __attribute__((always_inline)) {
+    uint8_t *ta = R.a[slot], *tb = R.b[slot];
+    const int k0 = st * BK;
+#pragma unroll
+    for (int jj = 0; jj < PB; ++jj) dma16(rs_h, tb + dma_dst<PB>(wave, jj), ob[jj] + 2u * k0);
+#pragma unroll
+    for (int jj = 0; jj < PA; ++jj)
+      dma16(rs_w, ta + dma_dst<PA>(wave, jj), as.coff[jj] < a.wh - k0 ? oa[jj] + 2u * k0 : kOOB);
+  };
+  f32x16 acc[P::FM][P::FN];
+  zero<P>(acc);
+  pipeline<P, true, true>(acc, R, (a.wh + BK - 1) / BK, wm0, wn0, lane, issue);
+
+  // classes past the last one: logit -inf
+  if (m0 + P::TM > a.V) {
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if (m0 + wm0 + 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3) >= a.V)
+#pragma unroll
+          for (int j = 0; j < P::FN; ++j) acc[i][j][v] = -INFINITY;
+  }
+  __syncthreads();  // every wave is done reading the ring
+  float *xm = reinterpret_cast<float *>(R.b[0]), *xs = xm + P::WGM * P::TN;
+  static_assert(2 * P::WGM * P::TN * 4 <= P::B_BYTES, "exchange fits a stage");
+#pragma unroll
+  for (int j = 0; j < P::FN; ++j) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) m = fmaxf(m, acc[i][j][v]);
+    m = fmaxf(m, __shfl_xor(m, 32));
+    if (lane < 32) xm[wm * P::TN + wn0 + 32 * j + lane] = m;
+    // the target's logit, where it is one of this wave's classes
+    const int n = n0 + wn0 + 32 * j + (lane & 31);
+    const int t = n < rows ? a.ctarget[n] - (m0 + wm0) : -1;
+    if (__any(t >= 0 && t < P::WM)) {
+#pragma unroll
+      for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (t == 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) a.tlogit[n] = acc[i][j][v];
+    }
+  }
+  __syncthreads();
+  float up[P::FN], s[P::FN];
+#pragma unroll
+  for (int j = 0; j < P::FN; ++j) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < P::WGM; ++k) m = fmaxf(m, xm[k * P::TN + wn0 + 32 * j + (lane & 31)]);
+    up[j] = scale_of(m);
+    s[j] = 0.f;
+  }
+  // 2^15 exp(l - m), with one rounding of the power's exponent
+  auto num = [&](int i, int j, int v) __attribute__((always_inline)) {
+    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][v], kLog2e, up[j]));
+    s[j] += x;
+    return x;
+  };
+  if constexpr (STORE) {
+    store16<P>(
+        wave_buf<P>(R, wave), lane,
+        [&](int i, int j, int g) __attribute__((always_inline)) {
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = num(i, j, 4 * g + e);
+          return u32x2{pack2(x[0], x[1], false), pack2(x[2], x[3], false)};
+        },
+        [&](int r, int c, const u32x4 &d) __attribute__((always_inline)) {
+          const int n = n0 + wn0 + r, v = m0 + wm0 + c;
+          if (n < rows && v < a.Vp)
+            *reinterpret_cast<u32x4 *>(a.e + (size_t)n * a.Vp + v) = d;
+        });
+  } else {
+#pragma unroll
+    for (int j = 0; j < P::FN; ++j)
+#pragma unroll
+      for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) num(i, j, v);
+  }
+#pragma unroll
+  for (int j = 0; j < P::FN; ++j) {
+    s[j] += __shfl_xor(s[j], 32);
+    if (lane < 32) xs[wm * P::TN + wn0 + 32 * j + lane] = s[j];
+  }
+  __syncthreads();
+  for (int p = tid; p < P::TN; p += P::NT) {
+    float m = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < P::WGM; ++k) {
+      m = fmaxf(m, xm[k * P::TN + p]);
+      sum += xs[k * P::TN + p];
+    }
+    if (n0 + p < rows) a.stats[(size_t)ty * a.Tc + n0 + p] = float2{-scale_of(m), sum};
+  }
+}
+
+// ---- softmax ------------------------------------------------------------------------
+struct SoftmaxArgs {
+  const Found *found;
+  int32_t row0, Tc, V, Vp, tlog, ntile;  // 2^tlog: classes of a logits tile
+  int32_t vper;                          // classes of a workgroup, a multiple of 512
+  int32_t bf;                            // G in bf16, not fp16
+  const int32_t *idx, *ctarget;
+  const float *cweight;
+  const float2 *stats;
+  const float *tlogit;
+  uint16_t *e;                           // null: losses only
+  float *loss, *lse;
+  double *lsum;                          // per 16 rows
+};
+
+// 16 rows' lse and losses from their tiles, then (gradients) a range of their
+// classes: numerators to 2^15 G.
+__global__ __launch_bounds__(256) void xent_softmax_kernel(SoftmaxArgs a) {
+  __shared__ float sm[16][kSlot], ss[16][kSlot], lse2[kSlot], wt[kSlot], pt[kSlot];
+  __shared__ int tg[kSlot];
+  const int rows = piece_rows(a.found, a.row0, a.Tc);
+  const int r0 = blockIdx.x * kSlot, tid = threadIdx.x;
+  const bool first = blockIdx.y == 0;
+  if (r0 < rows) {
+    // 16 lanes of each row take its tiles in turn
+    const int r = tid & 15, g = tid >> 4, n = r0 + r;
+    float m = -INFINITY, s = 0.f;
+    if (n < rows)
+      for (int p = g; p < a.ntile; p += 16) {
+        const float2 x = a.stats[(size_t)p * a.Tc + n];
+        if (x.y == 0.f) continue;  // all -inf
+        const float t = fmaxf(m, x.x);
+        s = s * __builtin_amdgcn_exp2f(m - t) + x.y * __builtin_amdgcn_exp2f(x.x - t);
+        m = t;
+      }
+    sm[g][r] = m, ss[g][r] = s;
+    __syncthreads();
+    if (tid < kSlot) {
+      for (int k = 0; k < 16; ++k) m = fmaxf(m, sm[k][r]);
+      s = 0.f;
+      for (int k = 0; k < 16; ++k)
+        if (ss[k][r] != 0.f) s += ss[k][r] * __builtin_amdgcn_exp2f(sm[k][r] - m);
+      const float l2 = m + __log2f(s);  // of a row with every logit -inf: NaN
+      double part = 0;
+      lse2[r] = l2;
+      if (n < rows) {
+        const float w = a.cweight[n], d = l2 * kLn2 - a.tlogit[n];
+        tg[r] = a.ctarget[n];
+        wt[r] = kUp * w * a.found->wmax_inv;
+        pt[r] = wt[r] * expm1f(-d);  // 2^15 w (p - 1)
+        if (first) {
+          a.loss[a.idx[n]] = w * d;
+          if (a.lse) a.lse[a.idx[n]] = l2 * kLn2;
+          part = w * d;
+        }
+      }
+      if (first) {
+#pragma unroll
+        for (int o = 8; o; o >>= 1) part += __shfl_xor(part, o);
+        if (tid == 0) a.lsum[blockIdx.x] = part;
+      }
+    }
+    __syncthreads();
+  } else if (first && tid == 0) {
+    a.lsum[blockIdx.x] = 0;
+  }
+  if (!a.e || r0 >= rows) return;
+  const int lane = tid & 63, wave = tid >> 6;
+  const int v0 = blockIdx.y * a.vper, v1 = min(a.Vp, v0 + a.vper);
+  for (int k = wave; k < kSlot; k += 4) {
+    const int n = r0 + k;
+    if (n >= rows) break;
+    uint16_t *row = a.e + (size_t)n * a.Vp;
+    const float l2 = lse2[k], w = wt[k], p1 = pt[k];
+    const int t = tg[k];
+    for (int v = v0 + 8 * lane; v < v1; v += 512) {
+      const u32x4 x = *reinterpret_cast<const u32x4 *>(row + v);
+      const float f =
+          w * __builtin_amdgcn_exp2f(a.stats[(size_t)(v >> a.tlog) * a.Tc + n].x - l2);
+      u32x4 o;
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        y[e] = h_to_f32((uint16_t)(x[e >> 1] >> (16 * (e & 1)))) * f;
+        if (v + e == t) y[e] = p1;
+        if (v + e >= a.V) y[e] = 0.f;  // NaN rows keep the classes past the last at 0
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = pack2(y[2 * e], y[2 * e + 1], a.bf);
+      *reinterpret_cast<u32x4 *>(row + v) = o;
+    }
+  }
+}
+
+// One workgroup: the sums of the losses and of the weights.
+__global__ __launch_bounds__(1024) void xent_totals_kernel(const double *lsum, int32_t n,
+                                                           const Found *found, float *totals) {
+  __shared__ double ws[16];
+  double s = 0;
+  for (int i = threadIdx.x; i < n; i += 1024) s += lsum[i];
+  s = wave_sum(s);
+  if ((threadIdx.x & 63) == 0) ws[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int k = 1; k < 16; ++k) s += ws[k];
+    totals[0] = (float)s;
+    totals[1] = found->wsum;
+  }
+}
+
+// ---- products -------------------------------------------------------------------------
+// out[n][m] = mult * sum_k A[k][m] B(n, k), m < M (hidden), with A (the weights, or
+// the features) read row by row; B = G, rows n (dh, k: classes) or columns n (dW, k:
+// rows).
+struct ProdArgs {
+  const uint16_t *a;
+  int64_t a_ld;
+  int32_t a_rows, a_cols;    // rows there are; columns (a multiple of 8)
+  const uint16_t *b;         // [Tc][Vp]
+  int64_t b_ld;
+  int32_t N;                 // columns n of B that are there (dW: Vp)
+  int32_t K, kper;           // the sum's length; of a part (a multiple of 64)
+  int32_t M, row0, Tc;
+  const Found *found;
+  const int32_t *idx;        // dh: row of the output
+  int32_t V;                 // dW: rows of the output
+  uint16_t *out;             // null: fp32 sums to part
+  int64_t out_ld;
+  int32_t ovec;
+  float *part;               // [parts][rows][Mq]
+  int64_t pstride;           // elements of a part
+  int32_t Mq, add;           // add: the sum is added to part's
+  int32_t *flag;
+};
+
+template <class P, bool DH>
+__global__ __launch_bounds__(P::NT, P::WPE) void xent_product_kernel(ProdArgs a, TileMap tm) {
+  FG_DMA_RING(P, R);
+  constexpr int PA = P::PA, PB = P::PB, BK = P::BK;
+  int tx, ty, split;  // hidden, rows (classes), part
+  if (!tm.decode(blockIdx.x, tx, ty, split)) return;
+  const int m0 = tx * P::TM, n0 = ty * P::TN;
+  const int rows = piece_rows(a.found, a.row0, a.Tc);
+  if (DH && n0 >= rows) return;
+  const int kbeg = split * a.kper, kend = min(min(a.K, DH ? a.K : rows), kbeg + a.kper);
+  const int nst = kend > kbeg ? (kend - kbeg + BK - 1) / BK : 0;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm0 = (wave / P::WGN) * P::WM, wn0 = (wave % P::WGN) * P::WN;
+
+  const MnSlot<PA> as = mn_slots<P::RBA, PA>(wave, lane);
+  unsigned oa[PA], ob[PB];
+#pragma unroll
+  for (int jj = 0; jj < PA; ++jj)
+    oa[jj] = m0 + as.ncol[jj] < a.a_cols
+                 ? (unsigned)(as.krow[jj] * (int)a.a_ld + m0 + as.ncol[jj]) * 2u
+                 : kOOB;
+#pragma unroll
+  for (int jj = 0; jj < PB; ++jj) {
+    if constexpr (DH) {
+      const KmSlot<PB> bs = km_slots<BK, PB>(wave, lane);
+      ob[jj] = (unsigned)(bs.row[jj] * (int)a.b_ld + bs.coff[jj]) * 2u;
+    } else {
+      const MnSlot<PB> bs = mn_slots<P::RBB, PB>(wave, lane);
+      ob[jj] = n0 + bs.ncol[jj] < a.N ? (unsigned)(bs.krow[jj] * (int)a.b_ld + bs.ncol[jj]) * 2u
+                                      : kOOB;
+    }
+  }
+  // the buffers begin at the stage's first row and end with the last one there is
+  // (kept in 64 bits: operands may pass 2^32 bytes)
+  const uint16_t *pa = a.a + kbeg * a.a_ld;
+  const uint16_t *pb = DH ? a.b + n0 * a.b_ld + kbeg : a.b + kbeg * a.b_ld + n0;
+  int left = max(min(a.a_rows, kend) - kbeg, 0), bleft = kend - kbeg;
+  auto issue = [&](int, int slot) __attribute__((always_inline)) {
+    uint8_t *ta = R.a[slot], *tb = R.b[slot];
+    const int ra = min(left, BK), rb = min(bleft, BK);
+    const __amdgpu_buffer_rsrc_t rs_a =
+        rsrc(pa, ra > 0 ? (uint32_t)((ra - 1) * (int)a.a_ld + a.a_cols) * 2u : 0u);
+    const __amdgpu_buffer_rsrc_t rs_b =
+        DH ? rsrc(pb, (uint32_t)((P::TN - 1) * (int)a.b_ld + BK) * 2u)
+           : rsrc(pb, rb > 0 ? (uint32_t)(rb * (int)a.b_ld - n0) * 2u : 0u);
+#pragma unroll
+    for (int jj = 0; jj < PB; ++jj) dma16(rs_b, tb + dma_dst<PB>(wave, jj), ob[jj]);
+#pragma unroll
+    for (int jj = 0; jj < PA; ++jj) dma16(rs_a, ta + dma_dst<PA>(wave, jj), oa[jj]);
+    pa += BK * a.a_ld;
+    pb += DH ? BK : BK * a.b_ld;
+    left -= BK;
+    bleft -= BK;
+  };
+  f32x16 acc[P::FM][P::FN];
+  zero<P>(acc);
+  pipeline<P, false, !DH ? false : true>(acc, R, nst, wm0, wn0, lane, issue);
+
+  const int nrow = DH ? rows : a.V;
+  if (a.part) {
+    float *part = a.part + split * a.pstride;
+#pragma unroll
+    for (int j = 0; j < P::FN; ++j) {
+      const int n = n0 + wn0 + 32 * j + (lane & 31);
+      if (n >= nrow) continue;
+#pragma unroll
+      for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int m = m0 + wm0 + 32 * i + 8 * g + 4 * (lane >> 5);
+          if (m >= a.M) continue;
+          f32x4 *p = reinterpret_cast<f32x4 *>(part + (size_t)n * a.Mq + m);
+          f32x4 v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
+                     acc[i][j][4 * g + 3]};
+          if (a.add) v += *p;
+          if (!a.out) {
+            *p = v;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] = v[e];
+          }
+        }
+    }
+    if (!a.out) return;
+  }
+  __syncthreads();  // every wave is done reading the ring
+  const float mult = a.found->mult;
+  bool bad = false;
+  store16<P>(
+      wave_buf<P>(R, wave), lane,
+      [&](int i, int j, int g) __attribute__((always_inline)) {
+        const f32x16 &c = acc[i][j];
+        return u32x2{pack2(c[4 * g] * mult, c[4 * g + 1] * mult, P::BF),
+                     pack2(c[4 * g + 2] * mult, c[4 * g + 3] * mult, P::BF)};
+      },
+      [&](int r, int c, const u32x4 &d) __attribute__((always_inline)) {
+        const int n = n0 + wn0 + r, m = m0 + wm0 + c;
+        if (n >= nrow || m >= a.M) return;
+        constexpr uint32_t EX = P::BF ? 0x7F80u : 0x7C00u;
+        if (!DH) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            bad |= m + e < a.M && (d[e >> 1] >> (16 * (e & 1)) & EX) == EX;
+        }
+        put8(a.out + (int64_t)(DH ? a.idx[n] : n) * a.out_ld, m, a.M, a.ovec, d);
+      });
+  if (!DH && a.flag) flag_nonfinite(a.flag, bad);
+}
+
+// Joins the parts of a split sum, in their order: 8 columns of a row per lane.
+struct JoinArgs {
+  const float *part;
+  int64_t pstride;
+  int32_t nsplit, rows, M, Mq;  // rows: -1: the piece's live ones
+  int32_t row0, Tc;
+  const Found *found;
+  const int32_t *idx;
+  uint16_t *out;
+  int64_t out_ld;
+  int32_t ovec, bf;
+  int32_t *flag;
+};
+__global__ __launch_bounds__(256) void xent_join_kernel(JoinArgs a) {
+  const int rows = a.rows < 0 ? piece_rows(a.found, a.row0, a.Tc) : a.rows;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int c8 = a.Mq / 8;
+  const int64_t n = i / c8;
+  const int m = (int)(i - n * c8) * 8;
+  bool bad = false;
+  if (n < rows) {
+    float v[8] = {};
+    const float *p = a.part + n * a.Mq + m;
+    for (int s = 0; s < a.nsplit; ++s, p += a.pstride)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(p + 4 * h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * h + e] += x[e];
+      }
+    const float mult = a.found->mult;
+    u32x4 d;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) d[e] = pack2(v[2 * e] * mult, v[2 * e + 1] * mult, a.bf);
+    const uint32_t ex = a.bf ? 0x7F80u : 0x7C00u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bad |= m + e < a.M && (d[e >> 1] >> (16 * (e & 1)) & ex) == ex;
+    put8(a.out + (a.idx ? a.idx[n] : n) * a.out_ld, m, a.M, a.ovec, d);
+  }
+  if (a.flag) flag_nonfinite(a.flag, bad);
+}
+
+// ---- host ------------------------------------------------------------------------------
+// The numerators of a piece of rows take at most this much of the workspace. Fewer,
+// longer pieces add the fp32 sums of dW (8 bytes an element of the weights) less
+// often; a gibibyte holds 4096 rows of 131072 classes.
+constexpr int64_t kPieceBytes = (int64_t)1 << 30;
+
+constexpr int kTileOf[3] = {64, 128, 256};
+
+// Tile and number of parts for a product of M x N sums of length K. Estimated time of
+// the tiles in rounds of the workgroups that the chip holds, from the rates that a
+// CU reached with 1 .. 3 of them, and of writing and joining the parts.
+struct Shape {
+  int tile, ns, kper;  // tile: index into kTileOf
+};
+Shape pick(int64_t M, int64_t N, int64_t K, bool split) {
+  // TFLOP/s of a CU with 1, 2, 3 workgroups of a tile
+  static const double rate[3][3] = {{1.0, 1.6, 2.0}, {2.6, 3.6, 3.6}, {4.7, 4.7, 4.7}};
+  static const int occ[3] = {3, 2, 1};
+  Shape best{0, 1, 0};
+  double tbest = 1e300;
+  for (int t = 0; t < 3; ++t) {
+    const int64_t ts = kTileOf[t];
+    const int64_t tiles = ((M + ts - 1) / ts) * ((N + ts - 1) / ts);
+    for (int ns = 1; ns <= (split ? 512 : 1); ns *= 2) {
+      const int64_t kper = std::max<int64_t>(64, ((K + ns - 1) / ns + 63) / 64 * 64);
+      if (ns > 1 && kper < 256) break;
+      const int64_t parts = std::max<int64_t>(1, (K + kper - 1) / kper);
+      const int64_t n = tiles * parts, slots = 256 * occ[t];
+      const int64_t full = n / slots, rest = n - full * slots;
+      const double work = 2e-6 * ts * ts * kper;  // us at 1 TFLOP/s
+      auto round = [&](int j) { return j * work / rate[t][j - 1] + 2.0; };
+      double us = full * round(occ[t]);
+      if (rest) us += round((int)((rest + 255) / 256));
+      if (parts > 1) us += 3.0 + (double)parts * M * N * 8 / 4e6;
+      if (us < tbest) tbest = us, best = {t, (int)parts, (int)kper};
+    }
+  }
+  return best;
+}
+
+struct Plan {
+  int64_t T, H, V, Tp, Hp, Vp, Hq, Tc, pieces, nb, wh, w_ld;
+  bool pad_w;
+  Shape s1, s2, s3;
+  int64_t ntile;
+  // workspace, bytes
+  size_t count, wsum, wmax, found, idx, ctarget, cweight, hc, wc, stats, tlogit, e, pdh, pdw,
+      lsum, total;
+};
+
+int64_t up(int64_t n, int64_t unit) { return (n + unit - 1) / unit * unit; }
+
+Plan make_plan(const fg_xent_desc &d, bool grad) {
+  Plan p{};
+  p.T = d.rows, p.H = d.hidden, p.V = d.vocab;
+  p.Tp = up(p.T, 256), p.Hp = up(p.H, 64), p.Vp = up(p.V, 64), p.Hq = up(p.H, 8);
+  p.w_ld = d.w_ld ? d.w_ld : p.H;
+  p.pad_w = p.H % 8 != 0 || p.w_ld % 8 != 0;
+  p.wh = p.pad_w ? p.Hp : p.H;
+  if (p.pad_w) p.w_ld = p.Hp;
+  p.nb = (p.T + kCount - 1) / kCount;
+  const int64_t per_row = grad ? p.Vp * 2 : (p.V + 63) / 64 * 8;
+  const int64_t most = std::max<int64_t>(256, kPieceBytes / per_row / 256 * 256);
+  p.pieces = std::max<int64_t>(1, (p.Tp + most - 1) / most);
+  p.Tc = std::max<int64_t>(256, up((p.T + p.pieces - 1) / p.pieces, 256));
+  p.pieces = std::max<int64_t>(1, (p.T + p.Tc - 1) / p.Tc);
+  const int64_t rows = std::min(p.T, p.Tc);
+  p.s1 = pick(p.V, rows, p.H, false);
+  p.ntile = (p.V + kTileOf[p.s1.tile] - 1) / kTileOf[p.s1.tile];
+  p.s2 = pick(p.H, rows, p.Vp, true);
+  p.s3 = pick(p.H, p.V, rows, true);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t was = at;
+    at += (bytes + 255) / 256 * 256;
+    return was;
+  };
+  p.found = take(sizeof(Found));
+  p.count = take(p.nb * 4);
+  p.wsum = take(p.nb * 8);
+  p.wmax = take(p.nb * 4);
+  p.idx = take(p.Tp * 4);
+  p.ctarget = take(p.Tp * 4);
+  p.cweight = take(p.Tp * 4);
+  p.lsum = take(p.pieces * (p.Tc / kSlot) * 8);
+  // the products read whole tiles of rows: a tile past the last piece's rows too
+  p.hc = take((size_t)p.pieces * p.Tc * p.Hp * 2);
+  p.stats = take((size_t)p.ntile * p.Tc * 8);
+  p.tlogit = take(p.Tc * 4);
+  if (grad) {
+    p.e = take((size_t)p.Tc * p.Vp * 2);
+    p.pdh = take(p.s2.ns > 1 ? (size_t)p.s2.ns * p.Tc * p.Hq * 4 : 0);
+    p.pdw = take(p.s3.ns > 1 || p.pieces > 1 ? (size_t)p.s3.ns * p.V * p.Hq * 4 : 0);
+  }
+  p.wc = take(p.pad_w ? (size_t)p.V * p.Hp * 2 : 0);
+  p.total = at;
+  return p;
+}
+
+TileMap tile_map(int64_t n0, int64_t n1, int64_t n2) {
+  return {(int32_t)n0, (int32_t)n1, (int32_t)n2, (int32_t)((n0 * n1 * n2 + 7) / 8), kOutputMajor};
+}
+
+template <class P>
+hipError_t launch_logits(const LogitArgs &a, int64_t rows, hipStream_t st) {
+  const TileMap tm = tile_map((rows + P::TN - 1) / P::TN, (a.V + P::TM - 1) / P::TM, 1);
+  if (a.e)
+    hipLaunchKernelGGL((xent_logits_kernel<P, true>), dim3(8 * tm.per), dim3(P::NT), 0, st, a, tm);
+  else
+    hipLaunchKernelGGL((xent_logits_kernel<P, false>), dim3(8 * tm.per), dim3(P::NT), 0, st, a,
+                       tm);
+  return hipGetLastError();
+}
+
+template <class P>
+hipError_t launch_product(const ProdArgs &a, bool dh, int64_t rows, int ns, hipStream_t st) {
+  const TileMap tm = tile_map((a.M + P::TM - 1) / P::TM,
+                              ((dh ? rows : a.V) + P::TN - 1) / P::TN, ns);
+  if (dh)
+    hipLaunchKernelGGL((xent_product_kernel<P, true>), dim3(8 * tm.per), dim3(P::NT), 0, st, a,
+                       tm);
+  else
+    hipLaunchKernelGGL((xent_product_kernel<P, false>), dim3(8 * tm.per), dim3(P::NT), 0, st, a,
+                       tm);
+  return hipGetLastError();
+}
+
+#define FG_XENT_TILE(FN, tile, bf, ...)                                              \
+  ((tile) == 2   ? ((bf) ? FN<Bf16<P256>>(__VA_ARGS__) : FN<P256>(__VA_ARGS__))       \
+   : (tile) == 1 ? ((bf) ? FN<Bf16<P128>>(__VA_ARGS__) : FN<P128>(__VA_ARGS__))       \
+                 : ((bf) ? FN<Bf16<P64>>(__VA_ARGS__) : FN<P64>(__VA_ARGS__)))
+
+struct Call {
+  const void *h, *w;
+  const int32_t *target;
+  const float *weight;
+  float *loss, *lse, *totals;
+  void *dh, *dw;
+  int32_t *flag;
+  bool grad;
+};
+
+bool aligned16(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+
+hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
+  const int64_t w_ld = d.w_ld ? d.w_ld : d.hidden;
+  const Plan p = make_plan(d, c.grad);
+  uint8_t *base = static_cast<uint8_t *>(ws);
+  auto at = [&](size_t off) { return base + off; };
+  const int bf = d.dtype == FG_BF16;
+#define FG_TRY(x)                      \
+  do {                                 \
+    const hipError_t e_ = (x);         \
+    if (e_ != hipSuccess) return e_;   \
+  } while (0)
+
+  RowArgs r{};
+  r.h = (const uint16_t *)c.h;
+  r.h_ld = d.h_ld ? d.h_ld : d.hidden;
+  r.target = c.target, r.weight = c.weight;
+  r.T = (int32_t)p.T, r.H = (int32_t)p.H, r.Hp = (int32_t)p.Hp, r.V = (int32_t)p.V;
+  r.nb = (int32_t)p.nb;
+  r.scale = d.scale, r.mean = d.mean;
+  r.hvec = aligned16(c.h, r.h_ld);
+  r.dh = (uint16_t *)c.dh;
+  r.dh_ld = d.dh_ld ? d.dh_ld : d.hidden;
+  r.dhvec = aligned16(c.dh, r.dh_ld);
+  r.count = (int32_t *)at(p.count), r.wsum = (double *)at(p.wsum), r.wmax = (float *)at(p.wmax);
+  r.found = (Found *)at(p.found);
+  r.idx = (int32_t *)at(p.idx), r.ctarget = (int32_t *)at(p.ctarget);
+  r.cweight = (float *)at(p.cweight);
+  r.hc = (uint16_t *)at(p.hc);
+  r.loss = c.loss, r.lse = c.lse;
+  if (p.T) {
+    hipLaunchKernelGGL(xent_count_kernel, dim3((uint32_t)p.nb), dim3(256), 0, st, r);
+    FG_TRY(hipGetLastError());
+  }
+  hipLaunchKernelGGL(xent_scan_kernel, dim3(1), dim3(1024), 0, st, r);
+  FG_TRY(hipGetLastError());
+  if (p.T) {
+    hipLaunchKernelGGL(xent_rows_kernel, dim3((uint32_t)((p.T + kSlot - 1) / kSlot)), dim3(256), 0,
+                       st, r);
+    FG_TRY(hipGetLastError());
+  }
+  const uint16_t *w = (const uint16_t *)c.w;
+  if (p.pad_w && p.T) {
+    const int64_t chunks = p.V * (p.Hp / 8);
+    hipLaunchKernelGGL(xent_pad_kernel, dim3((uint32_t)std::min<int64_t>((chunks + 255) / 256, 8192)),
+                       dim3(256), 0, st, w, w_ld, (int32_t)p.H, (uint16_t *)at(p.wc), (int32_t)p.Hp,
+                       chunks);
+    FG_TRY(hipGetLastError());
+    w = (const uint16_t *)at(p.wc);
+  }
+  for (int64_t i = 0; i < p.pieces; ++i) {
+    const int64_t row0 = i * p.Tc, rows = std::min(p.Tc, p.T - row0);
+    const uint16_t *hc = r.hc + (size_t)row0 * p.Hp;
+    double *lsum = (double *)at(p.lsum) + i * (p.Tc / kSlot);
+    if (rows > 0) {
+      LogitArgs l{};
+      l.w = w, l.w_ld = p.w_ld, l.wh = (int32_t)p.wh, l.V = (int32_t)p.V;
+      l.hc = hc, l.Hp = (int32_t)p.Hp;
+      l.found = r.found, l.row0 = (int32_t)row0, l.Tc = (int32_t)p.Tc;
+      l.ctarget = r.ctarget + row0;
+      l.e = c.grad ? (uint16_t *)at(p.e) : nullptr, l.Vp = (int32_t)p.Vp;
+      l.stats = (float2 *)at(p.stats), l.tlogit = (float *)at(p.tlogit);
+      FG_TRY(FG_XENT_TILE(launch_logits, p.s1.tile, bf, l, rows, st));
+      SoftmaxArgs s{};
+      s.found = r.found, s.row0 = (int32_t)row0, s.Tc = (int32_t)p.Tc;
+      s.V = (int32_t)p.V, s.Vp = (int32_t)p.Vp;
+      s.tlog = 6 + p.s1.tile, s.ntile = (int32_t)p.ntile;
+      s.bf = bf;
+      s.idx = r.idx + row0, s.ctarget = l.ctarget, s.cweight = r.cweight + row0;
+      s.stats = l.stats, s.tlogit = l.tlogit, s.e = l.e;
+      s.loss = c.loss, s.lse = c.lse, s.lsum = lsum;
+      // workgroups: at least 2048, where the classes give as many ranges of 2048
+      const int64_t blocks = (rows + kSlot - 1) / kSlot;
+      int64_t ny = c.grad ? std::min<int64_t>((p.Vp + 2047) / 2048,
+                                              std::max<int64_t>(1, 2048 / blocks)) : 1;
+      s.vper = (int32_t)up((p.Vp + ny - 1) / ny, 512);
+      ny = (p.Vp + s.vper - 1) / s.vper;
+      hipLaunchKernelGGL(xent_softmax_kernel, dim3((uint32_t)blocks, c.grad ? (uint32_t)ny : 1),
+                         dim3(256), 0, st, s);
+      FG_TRY(hipGetLastError());
+    }
+    if (!c.grad) continue;
+    ProdArgs g{};
+    g.b = (const uint16_t *)at(p.e), g.b_ld = p.Vp;
+    g.M = (int32_t)p.H, g.Mq = (int32_t)p.Hq;
+    g.row0 = (int32_t)row0, g.Tc = (int32_t)p.Tc, g.found = r.found;
+    g.V = (int32_t)p.V;
+    JoinArgs j{};
+    j.M = g.M, j.Mq = g.Mq, j.row0 = g.row0, j.Tc = g.Tc, j.found = r.found, j.bf = bf;
+    if (c.dh && rows > 0) {
+      ProdArgs a = g;
+      a.a = w, a.a_ld = p.w_ld, a.a_rows = (int32_t)p.V, a.a_cols = (int32_t)p.wh;
+      a.K = (int32_t)p.Vp, a.kper = p.s2.kper;
+      a.idx = r.idx + row0;
+      const bool split = p.s2.ns > 1;
+      a.out = split ? nullptr : (uint16_t *)c.dh, a.out_ld = r.dh_ld, a.ovec = r.dhvec;
+      a.part = split ? (float *)at(p.pdh) : nullptr, a.pstride = p.Tc * p.Hq;
+      FG_TRY(FG_XENT_TILE(launch_product, p.s2.tile, bf, a, true, rows, p.s2.ns, st));
+      if (split) {
+        JoinArgs q = j;
+        q.part = a.part, q.pstride = a.pstride, q.nsplit = p.s2.ns, q.rows = -1;
+        q.idx = a.idx, q.out = (uint16_t *)c.dh, q.out_ld = r.dh_ld, q.ovec = r.dhvec;
+        hipLaunchKernelGGL(xent_join_kernel, dim3((uint32_t)((rows * (p.Hq / 8) + 255) / 256)),
+                           dim3(256), 0, st, q);
+        FG_TRY(hipGetLastError());
+      }
+    }
+    if (c.dw) {
+      ProdArgs a = g;
+      a.a = hc, a.a_ld = p.Hp, a.a_rows = (int32_t)p.Tc, a.a_cols = (int32_t)p.Hp;
+      a.N = (int32_t)p.Vp;
+      a.K = (int32_t)p.Tc, a.kper = p.s3.kper;
+      const bool last = i + 1 == p.pieces, split = p.s3.ns > 1;
+      const int64_t dw_ld = d.dw_ld ? d.dw_ld : d.hidden;
+      const int dwvec = aligned16(c.dw, dw_ld);
+      a.out = split || !last ? nullptr : (uint16_t *)c.dw, a.out_ld = dw_ld, a.ovec = dwvec;
+      a.part = split || p.pieces > 1 ? (float *)at(p.pdw) : nullptr, a.pstride = p.V * p.Hq;
+      a.add = i > 0;
+      a.flag = c.flag;
+      FG_TRY(FG_XENT_TILE(launch_product, p.s3.tile, bf, a, false, rows, p.s3.ns, st));
+      if (split && last) {
+        JoinArgs q = j;
+        q.part = a.part, q.pstride = a.pstride, q.nsplit = p.s3.ns, q.rows = (int32_t)p.V;
+        q.out = (uint16_t *)c.dw, q.out_ld = dw_ld, q.ovec = dwvec, q.flag = c.flag;
+        hipLaunchKernelGGL(xent_join_kernel, dim3((uint32_t)((p.V * (p.Hq / 8) + 255) / 256)),
+                           dim3(256), 0, st, q);
+        FG_TRY(hipGetLastError());
+      }
+    }
+  }
+  if (c.totals) {
+    const int32_t n = (int32_t)((p.T + kSlot - 1) / kSlot);
+    hipLaunchKernelGGL(xent_totals_kernel, dim3(1), dim3(1024), 0, st, (double *)at(p.lsum), n,
+                       r.found, c.totals);
+    FG_TRY(hipGetLastError());
+  }
+  return hipSuccess;
+}
+
+}  // namespace xent
+
+size_t linear_xent_ws_bytes(const fg_xent_desc &d, bool grad) {
+  return xent::make_plan(d, grad).total;
+}
+
+hipError_t launch_linear_xent(const fg_xent_desc &d, const void *h, const void *w,
+                              const int32_t *target, const float *weight, float *loss,
+                              float *lse, float *totals, void *dh, void *dw, int32_t *flag,
+                              bool grad, void *ws, hipStream_t st) {
+  return xent::run(d, {h, w, target, weight, loss, lse, totals, dh, dw, flag, grad}, ws, st);
+}
+
+}  // namespace fg

@@ -67,3 +67,84 @@ def test_dropout_binding_checks_tensors():
         fg.dropout_fwd(d(), x, y, step_count=torch.zeros(1), stream=0)
     with pytest.raises(fg.FgError):
         fg.dropout_fwd(fg.DropoutDesc.make(24, 8, 2.0, 1), x, y, stream=0)
+
+
+def _xent(**kw):
+    base = dict(rows=64, hidden=32, vocab=100)
+    base.update(kw)
+    return fg.XentDesc.make(**base)
+
+
+# addresses 16 MiB apart
+H, W, TG, WT, LOSS, LSE, TOT, DH, DW, FLAG, WS = (0x1000000 * i for i in range(1, 12))
+
+
+def test_xent_refusals(L):
+    big = 1 << 30
+
+    def fwd(d, h=H, w=W, t=TG, wt=None, loss=LOSS, lse=None, tot=None, ws=WS, n=big):
+        return L.linear_xent_fwd(ctypes.byref(d) if d else None, h, w, t, wt, loss, lse, tot, ws,
+                                 n, None)
+
+    def grad(d, h=H, w=W, t=TG, wt=None, loss=LOSS, lse=None, tot=None, dh=DH, dw=DW, flag=None,
+             ws=WS, n=big):
+        return L.linear_xent_grad(ctypes.byref(d) if d else None, h, w, t, wt, loss, lse, tot, dh,
+                                  dw, flag, ws, n, None)
+
+    for call in (fwd, grad):
+        assert call(None) == fg.FG_EINVAL
+        for k in ("h", "w", "t", "loss", "ws"):
+            assert call(_xent(), **{k: None}) == fg.FG_EINVAL, k
+        for bad in (dict(rows=-1), dict(hidden=0), dict(vocab=0), dict(dtype=5), dict(dtype=-1),
+                    dict(mean=2), dict(scale=float("inf")), dict(scale=float("nan")),
+                    dict(h_ld=31), dict(w_ld=31), dict(dh_ld=31), dict(dw_ld=-1)):
+            assert call(_xent(**bad)) == fg.FG_EINVAL, bad
+            assert L.fg_linear_xent_workspace_bytes(ctypes.byref(_xent(**bad)), 1) == 0
+        for bad in (dict(dtype=fg.F32), dict(rows=1 << 28), dict(hidden=(1 << 16) + 1),
+                    dict(vocab=(1 << 22) - 64), dict(h_ld=1 << 20), dict(w_ld=1 << 20)):
+            assert call(_xent(**bad)) == fg.FG_EUNSUPPORTED, bad
+            assert L.fg_linear_xent_workspace_bytes(ctypes.byref(_xent(**bad)), 0) == 0
+        assert call(_xent(), w=W + 8) == fg.FG_EUNSUPPORTED
+        assert call(_xent(), h=H + 1) == fg.FG_EINVAL
+        assert call(_xent(), t=TG + 2) == fg.FG_EINVAL
+        assert call(_xent(), n=100) == fg.FG_EWORKSPACE
+        assert call(_xent(), ws=WS + 8) == fg.FG_EWORKSPACE
+        # outputs over inputs, over each other and over the workspace
+        assert call(_xent(), loss=H + 8) == fg.FG_EINVAL
+        assert call(_xent(), lse=LOSS + 4) == fg.FG_EINVAL
+        assert call(_xent(), tot=LOSS + 252) == fg.FG_EINVAL
+        assert call(_xent(), h=WS + 256) == fg.FG_EINVAL
+    assert grad(_xent(), dh=None, dw=None) == fg.FG_EINVAL
+    assert grad(_xent(), dh=H) == fg.FG_EINVAL
+    assert grad(_xent(), dw=DH + 64) == fg.FG_EINVAL
+    assert grad(_xent(), flag=DW + 4) == fg.FG_EINVAL
+
+
+def test_xent_workspace(L):
+    """Numerators of at most a gibibyte (or 256 rows), whatever the number of rows."""
+    need = lambda **kw: L.fg_linear_xent_workspace_bytes(ctypes.byref(_xent(**kw)), 1)
+    base = dict(hidden=64, vocab=131072, dtype=fg.BF16)
+    few = need(rows=100_000, **base)
+    # features' copy 12.8 MB, fp32 sums of dw 33.6 MB, small change
+    assert (1 << 30) <= few <= (1 << 30) + (100 << 20)
+    assert need(rows=200_000, **base) - few <= 40 << 20
+    assert need(rows=16, hidden=64, vocab=4_000_000) <= 3 << 30
+    assert L.fg_linear_xent_workspace_bytes(ctypes.byref(_xent()), 0) <= need()
+    assert 0 < need(rows=0) <= need()
+
+
+def test_xent_binding_checks_tensors():
+    z = lambda *s, dt=torch.float16: torch.zeros(*s, dtype=dt)
+    d = _xent()
+    ok = dict(h=z(64, 32), w=z(100, 32), target=z(64, dt=torch.int32), loss=z(64, dt=torch.float32))
+    for bad in (dict(h=z(64, 31)), dict(h=z(64, 32, dt=torch.bfloat16)), dict(w=z(99, 32)),
+                dict(target=z(64, dt=torch.int64)), dict(loss=z(63, dt=torch.float32)),
+                dict(h=z(64, 64)[:, :32])):
+        a = dict(ok, **bad)
+        with pytest.raises(ValueError):
+            fg.linear_xent_fwd(d, a["h"], a["w"], a["target"], a["loss"], stream=0)
+    with pytest.raises(fg.FgError):      # no workspace
+        fg.linear_xent_fwd(d, ok["h"], ok["w"], ok["target"], ok["loss"], stream=0)
+    with pytest.raises(ValueError):
+        fg.linear_xent_grad(d, ok["h"], ok["w"], ok["target"], ok["loss"], z(64, 32), z(32, 100),
+                            stream=0)
