@@ -37,12 +37,30 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // Numerators and G are held times 2^15: the largest is then 2^15, within fp16, and
 // values down to 2^-29 of it keep all their bits (2^-14 otherwise).
 constexpr float kUp = 32768.f;
-constexpr int kSlot = 16;       // rows of a workgroup of the copy and softmax kernels
+constexpr int kSlot = 16;       // rows of a workgroup of the softmax kernel
 constexpr int kCount = 1024;    // rows of a workgroup of the counting kernel
+constexpr int kDirect = 8192;   // rows up to which there is none
 
-using P256 = Pipe<32, 5, 2, 4, 256, 256>;  // 8 waves of 128 x 64
+#ifndef FG_P1
+#define FG_P1 64, 2, 2, 4
+#endif
+#ifndef FG_P2
+#define FG_P2 32, 5, 2, 4
+#endif
+#ifndef FG_P3
+#define FG_P3 32, 5, 2, 4
+#endif
 using P128 = Pipe<64, 2, 2, 2, 128, 128>;  // 4 waves of 64 x 64
 using P64 = Pipe<64, 3, 2, 2, 64, 64>;     // 4 waves of 32 x 32
+struct LogitTiles {
+  using T256 = Pipe<FG_P1, 256, 256>;
+};
+struct DhTiles {
+  using T256 = Pipe<FG_P2, 256, 256>;
+};
+struct DwTiles {
+  using T256 = Pipe<FG_P3, 256, 256>;
+};
 
 // What the first kernels find out, read by the others.
 struct Found {
@@ -59,7 +77,7 @@ struct RowArgs {
   const int32_t *target;
   const float *weight;
   int32_t T, H, Hp, V;
-  int32_t nb;            // workgroups of the counting kernel
+  int32_t nb;            // workgroups of the counting kernel; 0: the copies count
   double scale;
   int32_t mean, hvec, dhvec;
   int32_t *count;        // live rows per counted block, then before it
@@ -125,6 +143,17 @@ __global__ __launch_bounds__(256) void xent_count_kernel(RowArgs a) {
   }
 }
 
+// The totals, by one thread.
+__device__ __forceinline__ void put_found(const RowArgs &a, int live, double sum, float mx) {
+  // no live row, or weights that cancel: a mean of nothing has no gradient
+  const double den = a.mean ? sum : 1.0;
+  const float top = mx > 0.f ? mx : 1.f;
+  a.found->live = live;
+  a.found->wsum = (float)sum;
+  a.found->wmax_inv = 1.f / top;
+  a.found->mult = den != 0.0 ? (float)(a.scale / den * top / kUp) : 0.f;
+}
+
 // One workgroup: counts become the live rows before each block; the totals.
 __global__ __launch_bounds__(1024) void xent_scan_kernel(RowArgs a) {
   __shared__ double ws[16];
@@ -164,12 +193,7 @@ __global__ __launch_bounds__(1024) void xent_scan_kernel(RowArgs a) {
       sum += ws[k];
       mx = fmaxf(mx, wm[k]);
     }
-    // no live row, or weights that cancel: a mean of nothing has no gradient
-    const double den = a.mean ? sum : 1.0;
-    a.found->live = base;
-    a.found->wsum = (float)sum;
-    a.found->wmax_inv = mx > 0.f ? 1.f / mx : 1.f;
-    a.found->mult = den != 0.0 ? (float)(a.scale / den * (mx > 0.f ? mx : 1.f) / kUp) : 0.f;
+    put_found(a, base, sum, mx);
   }
 }
 
@@ -193,26 +217,51 @@ __device__ __forceinline__ void put8(uint16_t *row, int c, int n, bool vec, cons
 }
 
 // Copies live rows to their places, in order; results of masked rows are written
-// here. (What stands after the last live row is never read into a result.)
+// here. (What stands after the last live row is never read into a result.) 4 R rows
+// per workgroup. Up to kDirect rows every workgroup counts the live ones before its
+// own by itself, and one more finds the totals: two launches fewer.
+template <int R>
 __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
   __shared__ int cn[4];
+  __shared__ double ws[4];
+  __shared__ float wm[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int r0 = blockIdx.x * kSlot, blk = r0 / kCount;
-  // live rows of this counted block before r0
+  const int r0 = blockIdx.x * 4 * R, blk = a.nb ? r0 / kCount : 0;
+  const bool totals = r0 >= a.T;
+  // live rows before r0, of this counted block where blocks are counted
   int n = 0;
-  for (int r = blk * kCount + threadIdx.x; r < r0; r += 256) {
+  double sum = 0;
+  float mx = 0.f;
+#pragma unroll 8
+  for (int r = blk * kCount + threadIdx.x; r < min(r0, a.T); r += 256) {
     float w;
-    n += live_row(a, r, w);
+    if (live_row(a, r, w)) {
+      ++n;
+      if (totals) {
+        sum += w;
+        mx = fmaxf(mx, fabsf(w));
+      }
+    }
   }
   n = wave_sum(n);
   if (lane == 0) cn[wave] = n;
+  if (totals) {
+    sum = wave_sum(sum);
+    mx = wave_max(mx);
+    if (lane == 0) ws[wave] = sum, wm[wave] = mx;
+    __syncthreads();
+    if (threadIdx.x == 0)
+      put_found(a, cn[0] + cn[1] + cn[2] + cn[3], (ws[0] + ws[1]) + (ws[2] + ws[3]),
+                fmaxf(fmaxf(wm[0], wm[1]), fmaxf(wm[2], wm[3])));
+    return;
+  }
   __syncthreads();
-  const int before = a.count[blk] + cn[0] + cn[1] + cn[2] + cn[3];
+  const int before = (a.nb ? a.count[blk] : 0) + cn[0] + cn[1] + cn[2] + cn[3];
   float w = 0.f;
-  const bool mine = lane < kSlot && live_row(a, r0 + lane, w);
+  const bool mine = lane < 4 * R && live_row(a, r0 + lane, w);
   const uint64_t mask = __ballot(mine);
   const int place = before + __popcll(mask & ((1ull << lane) - 1));
-  if (wave == 0 && lane < kSlot) {
+  if (wave == 0 && lane < 4 * R) {
     const int r = r0 + lane;
     if (mine) {
       a.idx[place] = r;
@@ -223,8 +272,9 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
       if (a.lse) a.lse[r] = 0.f;
     }
   }
-  for (int k = wave; k < kSlot; k += 4) {
-    const int r = r0 + k, to = __shfl(place, k);
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const int k = 4 * j + wave, r = r0 + k, to = __shfl(place, k);
     const bool on = mask >> k & 1;
     const uint16_t *src = a.h + (int64_t)r * a.h_ld;
     for (int c = 8 * lane; on && c < a.Hp; c += 512)
@@ -459,6 +509,7 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
 }
 
 // ---- softmax ------------------------------------------------------------------------
+constexpr int kAhead = 8;  // loads in flight: a row's tiles are joined by 16 lanes
 struct SoftmaxArgs {
   const Found *found;
   int32_t row0, Tc, V, Vp, tlog, ntile;  // 2^tlog: classes of a logits tile
@@ -486,12 +537,18 @@ __global__ __launch_bounds__(256) void xent_softmax_kernel(SoftmaxArgs a) {
     const int r = tid & 15, g = tid >> 4, n = r0 + r;
     float m = -INFINITY, s = 0.f;
     if (n < rows)
-      for (int p = g; p < a.ntile; p += 16) {
-        const float2 x = a.stats[(size_t)p * a.Tc + n];
-        if (x.y == 0.f) continue;  // all -inf
-        const float t = fmaxf(m, x.x);
-        s = s * __builtin_amdgcn_exp2f(m - t) + x.y * __builtin_amdgcn_exp2f(x.x - t);
-        m = t;
+      for (int p0 = g; p0 < a.ntile; p0 += 16 * kAhead) {
+        float2 x[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+          x[k] = a.stats[(size_t)min(p0 + 16 * k, a.ntile - 1) * a.Tc + n];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          if (p0 + 16 * k >= a.ntile || x[k].y == 0.f) continue;  // none, or all -inf
+          const float t = fmaxf(m, x[k].x);
+          s = s * __builtin_amdgcn_exp2f(m - t) + x[k].y * __builtin_amdgcn_exp2f(x[k].x - t);
+          m = t;
+        }
       }
     sm[g][r] = m, ss[g][r] = s;
     __syncthreads();
@@ -716,23 +773,43 @@ struct JoinArgs {
   int32_t ovec, bf;
   int32_t *flag;
 };
-__global__ __launch_bounds__(256) void xent_join_kernel(JoinArgs a) {
+// SW waves share a sum, a run of the parts each (12 x 512 sums of 256 parts took 42 us
+// by single lanes).
+template <int SW>
+__global__ __launch_bounds__(512) void xent_join_kernel(JoinArgs a) {
+  __shared__ float sh[SW][SW > 1 ? 64 : 1][8];
   const int rows = a.rows < 0 ? piece_rows(a.found, a.row0, a.Tc) : a.rows;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t i = (int64_t)blockIdx.x * (512 / SW) + (SW > 1 ? lane : (int)threadIdx.x);
   const int c8 = a.Mq / 8;
   const int64_t n = i / c8;
   const int m = (int)(i - n * c8) * 8;
+  const int per = (a.nsplit + SW - 1) / SW;
+  const int s0 = SW > 1 ? wave * per : 0, s1 = min(a.nsplit, s0 + per);
   bool bad = false;
+  float v[8] = {};
   if (n < rows) {
-    float v[8] = {};
-    const float *p = a.part + n * a.Mq + m;
-    for (int s = 0; s < a.nsplit; ++s, p += a.pstride)
+    const float *p = a.part + s0 * a.pstride + n * a.Mq + m;
+#pragma unroll 4
+    for (int s = s0; s < s1; ++s, p += a.pstride)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const f32x4 x = *reinterpret_cast<const f32x4 *>(p + 4 * h);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[4 * h + e] += x[e];
       }
+  }
+  if constexpr (SW > 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sh[wave][lane][e] = v[e];
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int k = 1; k < SW; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += sh[k][lane][e];
+  }
+  if (n < rows) {
     const float mult = a.found->mult;
     u32x4 d;
 #pragma unroll
@@ -860,20 +937,30 @@ hipError_t launch_logits(const LogitArgs &a, int64_t rows, hipStream_t st) {
 }
 
 template <class P>
-hipError_t launch_product(const ProdArgs &a, bool dh, int64_t rows, int ns, hipStream_t st) {
-  const TileMap tm = tile_map((a.M + P::TM - 1) / P::TM,
-                              ((dh ? rows : a.V) + P::TN - 1) / P::TN, ns);
-  if (dh)
-    hipLaunchKernelGGL((xent_product_kernel<P, true>), dim3(8 * tm.per), dim3(P::NT), 0, st, a,
-                       tm);
-  else
-    hipLaunchKernelGGL((xent_product_kernel<P, false>), dim3(8 * tm.per), dim3(P::NT), 0, st, a,
-                       tm);
+hipError_t launch_dh(const ProdArgs &a, int64_t rows, int ns, hipStream_t st) {
+  const TileMap tm = tile_map((a.M + P::TM - 1) / P::TM, (rows + P::TN - 1) / P::TN, ns);
+  hipLaunchKernelGGL((xent_product_kernel<P, true>), dim3(8 * tm.per), dim3(P::NT), 0, st, a, tm);
+  return hipGetLastError();
+}
+template <class P>
+hipError_t launch_dw(const ProdArgs &a, int ns, hipStream_t st) {
+  const TileMap tm = tile_map((a.M + P::TM - 1) / P::TM, (a.V + P::TN - 1) / P::TN, ns);
+  hipLaunchKernelGGL((xent_product_kernel<P, false>), dim3(8 * tm.per), dim3(P::NT), 0, st, a,
+                     tm);
   return hipGetLastError();
 }
 
-#define FG_XENT_TILE(FN, tile, bf, ...)                                              \
-  ((tile) == 2   ? ((bf) ? FN<Bf16<P256>>(__VA_ARGS__) : FN<P256>(__VA_ARGS__))       \
+hipError_t launch_join(const JoinArgs &a, int64_t rows, hipStream_t st) {
+  const int64_t n = rows * (a.Mq / 8);
+  if (a.nsplit >= 16)
+    hipLaunchKernelGGL(xent_join_kernel<8>, dim3((uint32_t)((n + 63) / 64)), dim3(512), 0, st, a);
+  else
+    hipLaunchKernelGGL(xent_join_kernel<1>, dim3((uint32_t)((n + 511) / 512)), dim3(512), 0, st, a);
+  return hipGetLastError();
+}
+
+#define FG_XENT_TILE(FN, TS, tile, bf, ...)                                          \
+  ((tile) == 2   ? ((bf) ? FN<Bf16<TS::T256>>(__VA_ARGS__) : FN<TS::T256>(__VA_ARGS__)) \
    : (tile) == 1 ? ((bf) ? FN<Bf16<P128>>(__VA_ARGS__) : FN<P128>(__VA_ARGS__))       \
                  : ((bf) ? FN<Bf16<P64>>(__VA_ARGS__) : FN<P64>(__VA_ARGS__)))
 
@@ -918,15 +1005,17 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
   r.cweight = (float *)at(p.cweight);
   r.hc = (uint16_t *)at(p.hc);
   r.loss = c.loss, r.lse = c.lse;
-  if (p.T) {
+  if (p.T <= kDirect) {
+    r.nb = 0;  // a row per wave: a few rows are bound by one row's latency
+    hipLaunchKernelGGL(xent_rows_kernel<1>, dim3((uint32_t)((p.T + 3) / 4 + 1)), dim3(256), 0, st,
+                       r);
+    FG_TRY(hipGetLastError());
+  } else {
     hipLaunchKernelGGL(xent_count_kernel, dim3((uint32_t)p.nb), dim3(256), 0, st, r);
     FG_TRY(hipGetLastError());
-  }
-  hipLaunchKernelGGL(xent_scan_kernel, dim3(1), dim3(1024), 0, st, r);
-  FG_TRY(hipGetLastError());
-  if (p.T) {
-    hipLaunchKernelGGL(xent_rows_kernel, dim3((uint32_t)((p.T + kSlot - 1) / kSlot)), dim3(256), 0,
-                       st, r);
+    hipLaunchKernelGGL(xent_scan_kernel, dim3(1), dim3(1024), 0, st, r);
+    FG_TRY(hipGetLastError());
+    hipLaunchKernelGGL(xent_rows_kernel<4>, dim3((uint32_t)((p.T + 15) / 16)), dim3(256), 0, st, r);
     FG_TRY(hipGetLastError());
   }
   const uint16_t *w = (const uint16_t *)c.w;
@@ -950,7 +1039,7 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       l.ctarget = r.ctarget + row0;
       l.e = c.grad ? (uint16_t *)at(p.e) : nullptr, l.Vp = (int32_t)p.Vp;
       l.stats = (float2 *)at(p.stats), l.tlogit = (float *)at(p.tlogit);
-      FG_TRY(FG_XENT_TILE(launch_logits, p.s1.tile, bf, l, rows, st));
+      FG_TRY(FG_XENT_TILE(launch_logits, LogitTiles, p.s1.tile, bf, l, rows, st));
       SoftmaxArgs s{};
       s.found = r.found, s.row0 = (int32_t)row0, s.Tc = (int32_t)p.Tc;
       s.V = (int32_t)p.V, s.Vp = (int32_t)p.Vp;
@@ -985,14 +1074,12 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       const bool split = p.s2.ns > 1;
       a.out = split ? nullptr : (uint16_t *)c.dh, a.out_ld = r.dh_ld, a.ovec = r.dhvec;
       a.part = split ? (float *)at(p.pdh) : nullptr, a.pstride = p.Tc * p.Hq;
-      FG_TRY(FG_XENT_TILE(launch_product, p.s2.tile, bf, a, true, rows, p.s2.ns, st));
+      FG_TRY(FG_XENT_TILE(launch_dh, DhTiles, p.s2.tile, bf, a, rows, p.s2.ns, st));
       if (split) {
         JoinArgs q = j;
         q.part = a.part, q.pstride = a.pstride, q.nsplit = p.s2.ns, q.rows = -1;
         q.idx = a.idx, q.out = (uint16_t *)c.dh, q.out_ld = r.dh_ld, q.ovec = r.dhvec;
-        hipLaunchKernelGGL(xent_join_kernel, dim3((uint32_t)((rows * (p.Hq / 8) + 255) / 256)),
-                           dim3(256), 0, st, q);
-        FG_TRY(hipGetLastError());
+        FG_TRY(launch_join(q, rows, st));
       }
     }
     if (c.dw) {
@@ -1007,14 +1094,12 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       a.part = split || p.pieces > 1 ? (float *)at(p.pdw) : nullptr, a.pstride = p.V * p.Hq;
       a.add = i > 0;
       a.flag = c.flag;
-      FG_TRY(FG_XENT_TILE(launch_product, p.s3.tile, bf, a, false, rows, p.s3.ns, st));
+      FG_TRY(FG_XENT_TILE(launch_dw, DwTiles, p.s3.tile, bf, a, p.s3.ns, st));
       if (split && last) {
         JoinArgs q = j;
         q.part = a.part, q.pstride = a.pstride, q.nsplit = p.s3.ns, q.rows = (int32_t)p.V;
         q.out = (uint16_t *)c.dw, q.out_ld = dw_ld, q.ovec = dwvec, q.flag = c.flag;
-        hipLaunchKernelGGL(xent_join_kernel, dim3((uint32_t)((p.V * (p.Hq / 8) + 255) / 256)),
-                           dim3(256), 0, st, q);
-        FG_TRY(hipGetLastError());
+        FG_TRY(launch_join(q, p.V, st));
       }
     }
   }
