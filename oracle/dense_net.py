@@ -48,8 +48,9 @@ def _gate(d, act):
     return np.where(np.asarray(act, np.float64) > 0, np.asarray(d, np.float64), 0.0)
 
 
-def forward(layers, x16, weights, store_fp16=True):
-    """Returns a dict: every layer's (post-ReLU) output under its name, the
+def forward(layers, x16, weights, store_fp16=True, drop=None):
+    """drop: {dense layer: (mask of kept elements, factor)} for the dropout after its
+    ReLU. Returns a dict: every layer's (post-ReLU) output under its name, the
     pooled maps 'P1'.., the skips 'skip1'.., every block's concatenations
     ('Z:<block>:<l>', l = 0 the block input) and 'y' (the head output)."""
     by, levels, per = _net(layers)
@@ -70,6 +71,9 @@ def forward(layers, x16, weights, store_fp16=True):
         out[f"Z:{blk}:0"] = z
         for l in range(1, per + 1):
             y = conv(f"{blk}.{l}", z)
+            if drop is not None:
+                keep, factor = drop[f"{blk}.{l}"]
+                y = S(np.where(keep, np.asarray(y, np.float64) * factor, 0.0))
             out[f"{blk}.{l}"] = y
             z = np.concatenate([z, y], axis=-1)
             out[f"Z:{blk}:{l}"] = z
@@ -102,9 +106,11 @@ def forward(layers, x16, weights, store_fp16=True):
     return out
 
 
-def backward(layers, fwd, x16, weights, g_out, store_fp16=True):
+def backward(layers, fwd, x16, weights, g_out, store_fp16=True, factor=1.0, dnf=None):
     """fp16 (or fp64) kernel gradients by layer name and the gradient of the
-    network input, from the gradient g_out of the head output."""
+    network input, from the gradient g_out of the head output, or from that of
+    the head's input, dnf. factor: the dense layers' dropout factor (their
+    outputs in fwd are dropped out: the gate closes where one was dropped)."""
     by, levels, per = _net(layers)
     W = {L.name: w for L, w in zip(layers, weights)}
     S = _Store(store_fp16)
@@ -127,7 +133,7 @@ def backward(layers, fwd, x16, weights, g_out, store_fp16=True):
         for l in range(per, 0, -1):
             name = f"{blk}.{l}"
             lo = c0 + (l - 1) * k
-            dy = S(_gate(G[..., lo:lo + k], fwd[name]))
+            dy = S(_gate(G[..., lo:lo + k], fwd[name]) * factor)
             dz = back(name, fwd[f"Z:{blk}:{l - 1}"], dy)
             G[..., :lo] = S(G[..., :lo].astype(np.float64) + np.asarray(dz, np.float64))
         return G
@@ -138,7 +144,8 @@ def backward(layers, fwd, x16, weights, g_out, store_fp16=True):
         G[..., zl.shape[-1] - dnew.shape[-1]:] = dnew
         return G
 
-    dnf = back("F1x1", fwd["in:F1x1"], g_out)
+    if dnf is None:
+        dnf = back("F1x1", fwd["in:F1x1"], g_out)
     up = {}
     for d in range(1, levels + 1):
         G = block_back(f"U{d}", fresh(f"U{d}", dnf))

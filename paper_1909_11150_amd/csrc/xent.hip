@@ -42,24 +42,24 @@ constexpr int kCount = 1024;    // rows of a workgroup of the counting kernel
 constexpr int kDirect = 8192;   // rows up to which there is none
 
 #ifndef FG_P1
-#define FG_P1 64, 2, 2, 4
+#define FG_P1 64, 2, 2, 4, 256, 256
 #endif
 #ifndef FG_P2
-#define FG_P2 32, 5, 2, 4
+#define FG_P2 32, 5, 2, 4, 256, 256
 #endif
 #ifndef FG_P3
-#define FG_P3 32, 5, 2, 4
+#define FG_P3 32, 5, 2, 4, 256, 256
 #endif
 using P128 = Pipe<64, 2, 2, 2, 128, 128>;  // 4 waves of 64 x 64
 using P64 = Pipe<64, 3, 2, 2, 64, 64>;     // 4 waves of 32 x 32
 struct LogitTiles {
-  using T256 = Pipe<FG_P1, 256, 256>;
+  using T256 = Pipe<FG_P1>;
 };
 struct DhTiles {
-  using T256 = Pipe<FG_P2, 256, 256>;
+  using T256 = Pipe<FG_P2>;
 };
 struct DwTiles {
-  using T256 = Pipe<FG_P3, 256, 256>;
+  using T256 = Pipe<FG_P3>;
 };
 
 // What the first kernels find out, read by the others.

@@ -29,6 +29,17 @@ buffer and write, or add, into a channel slice of one (pixel strides):
     skip's slice of its up block's G (a strided view), so the skip gradient
     is in place when the transition conv adds its input gradient to it.
 fp16 storage throughout; every addition is one rounding.
+
+Options, both off by default:
+  * ``dropout``: every dense layer's output passes a dropout after its ReLU (Section
+    6.2), in place in its slice; its gradient is masked and gated by that output on the
+    way out of G, in the pass that gates it by the ReLU otherwise. A layer's mask is a
+    function of the seed, the layer's place and ``step_count`` (device int32: the
+    optimizer's, where there is one), drawn again in the backward pass.
+  * ``loss="xent"``: the 1x1 head has a channel per class (``synth.densenet_layers``'s
+    classes), the target is an int32 class per pixel (any other number: unlabelled), and
+    head, softmax cross entropy and the head's two gradients are one library call, which
+    stores no logits. The loss is the mean over the labelled pixels.
 """
 import ctypes
 from collections import namedtuple
@@ -36,8 +47,9 @@ from collections import namedtuple
 import torch
 
 from . import (EPI_ACC, EPI_NONE, EPI_RELU, OP_BWD_DATA, OP_BWD_WEIGHT, OP_CONVT,
-               OP_FWD, ConvDesc, FgError, Segment, grad_group_plan, kernel_name, lib,
-               profile_next_launch, workspace_bytes)
+               OP_FWD, ConvDesc, DropoutDesc, FgError, Segment, XentDesc, grad_group_plan,
+               kernel_name, lib, linear_xent_workspace_bytes, profile_next_launch,
+               workspace_bytes)
 from .fcn import (Call, chain_workspace_bytes, kernel_gradient_workspace_bytes)
 
 F16 = torch.float16
@@ -75,7 +87,11 @@ def _desc(L, op, x_ld=0, y_ld=0):
 
 class DenseNet:
     def __init__(self, layers, weights, x, loss_scale=2.0 ** 15, delta=10.0,
-                 device="cuda", stream=None, group_cap_bytes=None, group_align_bytes=256):
+                 device="cuda", stream=None, group_cap_bytes=None, group_align_bytes=256,
+                 loss="huber", dropout=0.0, seed=0, step_count=None):
+        if loss not in ("huber", "xent"):
+            raise ValueError(f"loss {loss!r}: huber or xent")
+        self.loss = loss
         self.layers = list(layers)
         self.L = {L.name: L for L in self.layers}
         self.levels, self.per = _structure(self.layers)
@@ -116,12 +132,24 @@ class DenseNet:
         self.Z["B"] = e((n_, h, w, c0b + (per - 1) * k))
         self._block_tail("B", self.Z["B"], c0b)
         self.out["C0"] = self.inp["D1.1"]._replace(ch=self.L["C0"].y_shape[3])
-        self.out["F1x1"] = _dense(e(self.L["F1x1"].y_shape))
+        if loss == "huber":   # the other head keeps neither its output nor its gradient
+            self.out["F1x1"] = _dense(e(self.L["F1x1"].y_shape))
+            self.g_out = e(self.L["F1x1"].y_shape)
         # post-ReLU outputs as (possibly strided) tensor views
         self.act = {name: self._view(s) for name, s in self.out.items()}
+        self.dropout, self.seed = float(dropout), int(seed)
+        self.step_count = step_count if step_count is not None or not self.dropout else \
+            torch.zeros(1, dtype=torch.int32, device=self.dev)
+        if loss == "xent":   # per-pixel losses; their sum and the labelled pixels' number
+            n_, h, w, c = self.L["F1x1"].x_shape
+            self.xent = XentDesc.make(n_ * h * w, c, self.L["F1x1"].y_shape[3],
+                                      scale=self.loss_scale)
+            f = lambda m: torch.empty(m, dtype=torch.float32, device=self.dev)
+            self.pixel_loss, self.totals = f(n_ * h * w), f(2)
+            self.xent_ws = torch.empty(linear_xent_workspace_bytes(self.xent, True),
+                                       dtype=torch.uint8, device=self.dev)
         # gradients: one output-gradient buffer per layer (its kernel
         # gradient may still read it on the side stream)
-        self.g_out = e(self.L["F1x1"].y_shape)
         self.dX = e(self.x.shape)
         self.dY = {f"{b}.{l}": e(self.L[f"{b}.{l}"].y_shape)
                    for b in self._blocks() for l in range(1, self.per + 1)}
@@ -349,7 +377,7 @@ class _DenseProgram:
         if n.groups is not None and name in n._group_done_at:
             self._group_calls(n._group_done_at[name])
 
-    def _group_calls(self, gi):
+    def _group_calls(self, gi, deps=()):
         """Pack, unscale with the non-finite check, unpack (Sections 4.2 and
         6.2) of a group once its last kernel gradient is written: on the
         kernel-gradient stream, after every member's kernel gradient."""
@@ -365,7 +393,7 @@ class _DenseProgram:
         g16, g32 = n.gbuf16[gi], n.gbuf32[gi]
         sid = self._dw_sid
         self._add(f"G{gi}.pack", "copy_pieces_kernel<2>", 4 * num, self._L.grad_group_pack,
-                  (src, len(g["members"]), g16.data_ptr(), num), sid=sid)
+                  (src, len(g["members"]), g16.data_ptr(), num), sid=sid, deps=deps)
         self._add(f"G{gi}.unscale", "unscale_vec_kernel", 6 * num,
                   self._L.grad_unscale_check,
                   (g16.data_ptr(), num, self._inv_scale, g32.data_ptr(), flag.data_ptr()),
@@ -391,6 +419,54 @@ class _DenseProgram:
                           self._ptr(dst), dst.ld, npix, nch, int(acc)),
                          sid=sid, deps=deps)
 
+    def _dropout(self, name, label, fn, kernel, reads, x, out, z=None):
+        """Dropout of a dense layer's output, or (z: its gate) of its gradient; `reads`
+        tensors are read."""
+        n = self.net
+        npix = out.t.numel() // out.ld
+        for s in (x, out) + ((z,) if z is not None else ()):
+            assert s.ch == out.ch
+            self._span_ok(s, npix)
+        d = DropoutDesc.make(npix, out.ch, n.dropout, n.seed,
+                             site=[L.name for L in n.layers].index(name), x_ld=x.ld,
+                             y_ld=out.ld, z_ld=0 if z is None else z.ld)
+        self._keep.append(n.step_count)
+        return self._add(label, kernel, 2 * npix * out.ch * (reads + 1), fn,
+                         (self._keep_desc(d), self._ptr(x),
+                          None if z is None else self._ptr(z), self._ptr(out),
+                          n.step_count.data_ptr()))
+
+    def _xent_head(self, target, nf, deps):
+        """Head, loss and both gradients of the head."""
+        n = self.net
+        L = n.L["F1x1"]
+        npix = n.xent.rows
+        if target.dtype != torch.int32 or target.numel() != npix or not target.is_contiguous():
+            raise ValueError(f"the target must be {npix} contiguous int32 classes")
+        self._shape_ok(nf, L.x_shape)
+        dnf = n.dNF["U1"]
+        self._shape_ok(dnf, L.x_shape)
+        self._add("F1x1.xent", "xent_logits_kernel", 3 * L.flops, self._L.linear_xent_grad,
+                  (ctypes.byref(n.xent), nf.data_ptr(), n.w["F1x1"].data_ptr(),
+                   target.data_ptr(), None, n.pixel_loss.data_ptr(), None,
+                   n.totals.data_ptr(), dnf.data_ptr(), n.dw["F1x1"].data_ptr(), None,
+                   n.xent_ws.data_ptr(), n.xent_ws.numel()), single=False, deps=deps)
+        self._dw_seen.append("F1x1")
+        if n.groups is not None and "F1x1" in n._group_done_at:
+            self._group_calls(n._group_done_at["F1x1"], deps=(len(self.calls) - 1,))
+
+    def _huber_head(self, target, nf, deps):
+        """Head, the loss-scaled mean Huber loss and the head's backward passes."""
+        n = self.net
+        y = n.act["F1x1"]
+        self.conv_fwd("F1x1", _dense(nf), n.out["F1x1"], False, deps=deps)
+        self._head_args = [y.data_ptr(), target.data_ptr(), y.numel(),
+                           ctypes.c_double(n.loss_scale / y.numel()),
+                           ctypes.c_double(n.delta), n.g_out.data_ptr()]
+        self._add("head_grad", "huber_head_grad_kernel", 10 * y.numel(),
+                  self._L.huber_head_grad, tuple(self._head_args))
+        self.conv_bwd("F1x1", _dense(nf), n.g_out, _dense(n.dNF["U1"]), acc=False)
+
     # -- the step --
     def _block_fwd(self, blk, ready):
         """Dense layers of a block whose input slice is complete once the
@@ -403,6 +479,9 @@ class _DenseProgram:
         for l in range(1, n.per + 1):
             name = f"{blk}.{l}"
             conv = self.conv_fwd(name, n.inp[name], n.out[name], True, deps=ready)
+            if n.dropout:
+                conv = self._dropout(name, f"{name}.drop", self._L.dropout_fwd,
+                                     "dropout_kernel", 1, n.out[name], n.out[name])
             ready = (conv,)
             if blk.startswith("D"):
                 continue
@@ -429,7 +508,11 @@ class _DenseProgram:
             dY = n.dY[name]
             src = Slice(dnf, (l - 1) * n.k, nk, n.k) if fresh and l == n.per else \
                 Slice(G.t, G.off + lo, G.ld, n.k)
-            self.copy(f"{name}.dy", src, _dense(dY), gate=n.out[name])
+            if n.dropout:
+                self._dropout(name, f"{name}.dy", self._L.dropout_bwd, "dropout_kernel", 2,
+                              src, _dense(dY), n.out[name])
+            else:
+                self.copy(f"{name}.dy", src, _dense(dY), gate=n.out[name])
             first = fresh and l == n.per          # nothing in G to add to yet
             self.conv_bwd(name, n.inp[name], dY, Slice(G.t, G.off, G.ld, lo),
                           acc=not first)
@@ -469,16 +552,11 @@ class _DenseProgram:
             tconv = self.conv_fwd(tu, _dense(nf), n.out[tu], True, deps=nf_ready)
             nf_ready = self._block_fwd(f"U{d}", (tconv,) + tuple(skip_ready[d]))
             nf = n.NF[f"U{d}"]
-        y = n.act["F1x1"]
-        self.conv_fwd("F1x1", _dense(nf), n.out["F1x1"], False, deps=nf_ready)
-        # ---- head: loss-scaled mean Huber loss
-        self._head_args = [y.data_ptr(), target.data_ptr(), y.numel(),
-                           ctypes.c_double(n.loss_scale / y.numel()),
-                           ctypes.c_double(n.delta), n.g_out.data_ptr()]
-        self._add("head_grad", "huber_head_grad_kernel", 10 * y.numel(),
-                  Lb.huber_head_grad, tuple(self._head_args))
-        # ---- backward: head, up blocks (level 1 first), bottleneck, down path
-        self.conv_bwd("F1x1", _dense(nf), n.g_out, _dense(n.dNF["U1"]), acc=False)
+        if n.loss == "xent":
+            self._xent_head(target, nf, nf_ready)
+        else:
+            self._huber_head(target, nf, nf_ready)
+        # ---- backward: up blocks (level 1 first), bottleneck, down path
         for d in range(1, n.levels + 1):
             blk, tu = f"U{d}", f"TU{d}"
             G = _dense(n.G[blk])
@@ -513,7 +591,10 @@ class _DenseProgram:
 
     def set_loss_scale(self, s):
         self.net.loss_scale = float(s)
-        self._head_args[3].value = s / self.net.act["F1x1"].numel()
+        if self.net.loss == "xent":
+            self.net.xent.scale = float(s)
+        else:
+            self._head_args[3].value = s / self.net.act["F1x1"].numel()
         self._inv_scale.value = 1.0 / s
 
     def run(self, events=None, kernel_events=None):

@@ -89,7 +89,8 @@ def fcn_layers(n=4, h=256, c_in=256, widths=(512, 1024, 1024, 1024),
     return L
 
 
-def densenet_layers(n=4, h=128, c_in=256, c0=256, growth=256, levels=2, per_block=2):
+def densenet_layers(n=4, h=128, c_in=256, c0=256, growth=256, levels=2, per_block=2,
+                    classes=1):
     """Conv layers of the FC-DenseNet variant (Section 6.2: dense blocks
     with growth rate 256, average pooling), forward order. The paper gives
     no layer counts; this Tiramisu-shaped reading has:
@@ -105,7 +106,8 @@ def densenet_layers(n=4, h=128, c_in=256, c0=256, growth=256, levels=2, per_bloc
       U{d}.{l} dense layers of up level d, whose block input is the
                concatenation of TU{d}'s output and the skip (the full
                concatenation of down level d);
-      F1x1     1x1 head over the last block's new features -> 1 channel.
+      F1x1     1x1 head over the last block's new features -> 1 channel (or one
+               per class).
     A ReLU follows every layer except the head. Defaults: 4 x 128 x 128 x
     256 input, 38,928,896 weights."""
     L = [_conv("C0", n, h, c_in, c0, 3, 1, 1, True)]
@@ -129,7 +131,7 @@ def densenet_layers(n=4, h=128, c_in=256, c0=256, growth=256, levels=2, per_bloc
         for l in range(1, per_block + 1):
             L.append(_conv(f"U{d}.{l}", n, hh, c, growth, 3, 1, 1, True))
             c += growth
-    L.append(_conv("F1x1", n, hh, new, 1, 1, 1, 0, False))
+    L.append(_conv("F1x1", n, hh, new, classes, 1, 1, 0, False))
     return L
 
 
