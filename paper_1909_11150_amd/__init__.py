@@ -412,13 +412,27 @@ def channel_slice_copy(src, src_ld, dst, dst_ld, npix, nch, gate=None, gate_ld=0
 
 
 # ---- classification head ----------------------------------------------------
+# A small call's time is the host's: checks look at each tensor once.
+_codes = {}      # torch element type -> code, filled on first use (torch may be absent)
+
+
+def _code(t):
+    if not _codes:
+        import torch
+        _codes.update({torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32,
+                       torch.int32: _I32})
+    return _codes.get(t.dtype)
+
+
+_I32 = 100       # not a code of the library's
+
+
 def dtype_of(t):
     """Element type code (F16, BF16, F32) of a tensor."""
-    import torch
-    try:
-        return {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}[t.dtype]
-    except KeyError:
-        raise ValueError(f"element type {t.dtype} is not supported") from None
+    c = _code(t)
+    if c is None or c == _I32:
+        raise ValueError(f"element type {t.dtype} is not supported")
+    return c
 
 
 def _matrix(name, t, rows, cols, ld, dtype):
@@ -426,68 +440,75 @@ def _matrix(name, t, rows, cols, ld, dtype):
     shape (its last axis unit-strided, the others one stride) and row stride ld."""
     if t is None:
         return None
-    if dtype_of(t) != dtype:
+    if _code(t) != dtype:
         raise ValueError(f"{name}: element type {t.dtype} where the descriptor says another")
-    if t.numel() != rows * cols or (t.numel() and (t.dim() < 1 or t.shape[-1] != cols)):
-        raise ValueError(f"{name}: shape {tuple(t.shape)} where {rows} x {cols} is needed")
-    if t.numel():
-        want = 1 if cols > 1 else None   # stride expected of the axis, None: any
-        for i, (n, s) in enumerate(zip(reversed(t.shape), reversed(t.stride()))):
-            if n > 1 and want is not None and s != want:
-                raise ValueError(f"{name}: strides {t.stride()} where rows {ld or cols} "
-                                 "elements apart are needed")
-            want = (ld or cols) if i == 0 else want * n
+    shape, stride, ld = t.shape, t.stride(), ld or cols
+    if len(shape) == 2 and shape[0] == rows and shape[1] == cols:
+        if (cols > 1 and stride[1] != 1) or (rows > 1 and stride[0] != ld):
+            raise ValueError(f"{name}: strides {stride} where rows {ld} elements apart "
+                             "are needed")
+        return t.data_ptr()
+    if t.numel() != rows * cols or (rows and (not shape or shape[-1] != cols)):
+        raise ValueError(f"{name}: shape {tuple(shape)} where {rows} x {cols} is needed")
+    want = 1
+    for i in range(len(shape) - 1, -1, -1):
+        if rows and shape[i] > 1 and stride[i] != want:
+            raise ValueError(f"{name}: strides {stride} where rows {ld} elements apart "
+                             "are needed")
+        want = ld if i == len(shape) - 1 else want * shape[i]
+    return t.data_ptr()
+
+
+def _vector(name, t, n, dtype):
+    if t is None:
+        return None
+    if _code(t) != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous "
+                         f"{'int32' if dtype == _I32 else 'float32'} tensor of {n} elements")
     return t.data_ptr()
 
 
 def _counter(name, t):
-    import torch
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.numel() < 1 or not t.is_contiguous():
+    if _code(t) != _I32 or t.numel() < 1 or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor")
     return t.data_ptr()
 
 
-def _dropout(fn, desc, x, y, z, z_name, step_count, stream):
-    m = lambda n, t, ld: _matrix(n, t, desc.rows, desc.cols, ld, desc.dtype)
-    _check(fn, getattr(lib(), fn)(
-        ctypes.byref(desc), m("x", x, desc.x_ld), m(z_name, z, desc.z_ld),
-        m("y", y, desc.y_ld), _counter("step_count", step_count), _s(stream)))
+def _dropout(fn, name, desc, x, y, z, z_name, step_count, stream):
+    rows, cols, dtype = desc.rows, desc.cols, desc.dtype
+    _check(name, fn(
+        ctypes.byref(desc), _matrix("x", x, rows, cols, desc.x_ld, dtype),
+        _matrix(z_name, z, rows, cols, desc.z_ld, dtype),
+        _matrix("y", y, rows, cols, desc.y_ld, dtype), _counter("step_count", step_count),
+        _s(stream)))
 
 
 def dropout_fwd(desc, x, y, residual=None, step_count=None, stream=None):
     """y = residual + dropout(x) (see include/fcngrad.h); tensors of desc's element
     type and strides, e.g. channel slices of wider buffers. step_count: device int32
     added to desc.step by the kernel."""
-    _dropout("dropout_fwd", desc, x, y, residual, "residual", step_count, stream)
+    _dropout(lib().dropout_fwd, "dropout_fwd", desc, x, y, residual, "residual", step_count,
+             stream)
 
 
 def dropout_bwd(desc, dy, dx, gate=None, step_count=None, stream=None):
     """Gradient of dropout_fwd's x from dy into dx, zero where gate <= 0."""
-    _dropout("dropout_bwd", desc, dy, dx, gate, "gate", step_count, stream)
+    _dropout(lib().dropout_bwd, "dropout_bwd", desc, dy, dx, gate, "gate", step_count, stream)
 
 
 def linear_xent_workspace_bytes(desc, grad):
     return lib().fg_linear_xent_workspace_bytes(ctypes.byref(desc), int(grad))
 
 
-def _vector(name, t, n, dtype):
-    import torch
-    if t is None:
-        return None
-    if t.dtype != getattr(torch, dtype) or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements")
-    return t.data_ptr()
-
-
 def _xent_args(desc, h, w, target, loss, lse, totals, weight):
-    n = desc.rows
-    return (ctypes.byref(desc), _matrix("h", h, n, desc.hidden, desc.h_ld, desc.dtype),
-            _matrix("w", w, desc.vocab, desc.hidden, desc.w_ld, desc.dtype),
-            _vector("target", target, n, "int32"), _vector("weight", weight, n, "float32"),
-            _vector("loss", loss, n, "float32"), _vector("lse", lse, n, "float32"),
-            _vector("totals", totals, 2, "float32"))
+    n, hidden, dtype = desc.rows, desc.hidden, desc.dtype
+    return (ctypes.byref(desc), _matrix("h", h, n, hidden, desc.h_ld, dtype),
+            _matrix("w", w, desc.vocab, hidden, desc.w_ld, dtype),
+            _vector("target", target, n, _I32), _vector("weight", weight, n, F32),
+            _vector("loss", loss, n, F32), _vector("lse", lse, n, F32),
+            _vector("totals", totals, 2, F32))
 
 
 def linear_xent_fwd(desc, h, w, target, loss, lse=None, totals=None, weight=None, ws=None,

@@ -47,19 +47,13 @@ constexpr int kDirect = 8192;   // rows up to which there is none
 #ifndef FG_P2
 #define FG_P2 32, 5, 2, 4, 256, 256
 #endif
-#ifndef FG_P3
-#define FG_P3 32, 5, 2, 4, 256, 256
-#endif
 using P128 = Pipe<64, 2, 2, 2, 128, 128>;  // 4 waves of 64 x 64
 using P64 = Pipe<64, 3, 2, 2, 64, 64>;     // 4 waves of 32 x 32
 struct LogitTiles {
   using T256 = Pipe<FG_P1>;
 };
-struct DhTiles {
+struct ProdTiles {
   using T256 = Pipe<FG_P2>;
-};
-struct DwTiles {
-  using T256 = Pipe<FG_P3>;
 };
 
 // What the first kernels find out, read by the others.
@@ -79,7 +73,7 @@ struct RowArgs {
   int32_t T, H, Hp, V;
   int32_t nb;            // workgroups of the counting kernel; 0: the copies count
   double scale;
-  int32_t mean, hvec, dhvec;
+  int32_t mean;
   int32_t *count;        // live rows per counted block, then before it
   double *wsum;
   float *wmax;
@@ -197,18 +191,24 @@ __global__ __launch_bounds__(1024) void xent_scan_kernel(RowArgs a) {
   }
 }
 
+// 16 bytes at any address: global memory is accessed in one instruction whatever the
+// alignment (the compiler's default for this target), only slower across lines.
+struct __attribute__((packed, aligned(2))) Any16 {
+  u32x4 v;
+};
+
 // 8 elements of a row from column c on, zeros past its end.
-__device__ __forceinline__ u32x4 row8(const uint16_t *row, int c, int n, bool vec) {
-  if (vec && c + 8 <= n) return *reinterpret_cast<const u32x4 *>(row + c);
+__device__ __forceinline__ u32x4 row8(const uint16_t *row, int c, int n) {
+  if (c + 8 <= n) return reinterpret_cast<const Any16 *>(row + c)->v;
   u32x4 v = {0, 0, 0, 0};
 #pragma unroll
   for (int e = 0; e < 8; ++e)
     if (c + e < n) v[e >> 1] |= (uint32_t)row[c + e] << (16 * (e & 1));
   return v;
 }
-__device__ __forceinline__ void put8(uint16_t *row, int c, int n, bool vec, const u32x4 &v) {
-  if (vec && c + 8 <= n) {
-    *reinterpret_cast<u32x4 *>(row + c) = v;
+__device__ __forceinline__ void put8(uint16_t *row, int c, int n, const u32x4 &v) {
+  if (c + 8 <= n) {
+    reinterpret_cast<Any16 *>(row + c)->v = v;
     return;
   }
 #pragma unroll
@@ -278,10 +278,10 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
     const bool on = mask >> k & 1;
     const uint16_t *src = a.h + (int64_t)r * a.h_ld;
     for (int c = 8 * lane; on && c < a.Hp; c += 512)
-      *reinterpret_cast<u32x4 *>(a.hc + (size_t)to * a.Hp + c) = row8(src, c, a.H, a.hvec);
+      *reinterpret_cast<u32x4 *>(a.hc + (size_t)to * a.Hp + c) = row8(src, c, a.H);
     if (!on && a.dh && r < a.T)
       for (int c = 8 * lane; c < a.H; c += 512)
-        put8(a.dh + (int64_t)r * a.dh_ld, c, a.H, a.dhvec, u32x4{0, 0, 0, 0});
+        put8(a.dh + (int64_t)r * a.dh_ld, c, a.H, u32x4{0, 0, 0, 0});
   }
 }
 
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(256) void xent_pad_kernel(const uint16_t *w, int64_
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < chunks; i += stride) {
     const int64_t r = i / (Hp / 8);
     const int c = (int)(i - r * (Hp / 8)) * 8;
-    *reinterpret_cast<u32x4 *>(wc + r * Hp + c) = row8(w + r * ld, c, H, false);
+    *reinterpret_cast<u32x4 *>(wc + r * Hp + c) = row8(w + r * ld, c, H);
   }
 }
 
@@ -643,7 +643,6 @@ struct ProdArgs {
   int32_t V;                 // dW: rows of the output
   uint16_t *out;             // null: fp32 sums to part
   int64_t out_ld;
-  int32_t ovec;
   float *part;               // [parts][rows][Mq]
   int64_t pstride;           // elements of a part
   int32_t Mq, add;           // add: the sum is added to part's
@@ -651,11 +650,11 @@ struct ProdArgs {
 };
 
 template <class P, bool DH>
-__global__ __launch_bounds__(P::NT, P::WPE) void xent_product_kernel(ProdArgs a, TileMap tm) {
-  FG_DMA_RING(P, R);
+__device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &tm, int block,
+                                             const Ring &R) {
   constexpr int PA = P::PA, PB = P::PB, BK = P::BK;
   int tx, ty, split;  // hidden, rows (classes), part
-  if (!tm.decode(blockIdx.x, tx, ty, split)) return;
+  if (!tm.decode(block, tx, ty, split)) return;
   const int m0 = tx * P::TM, n0 = ty * P::TN;
   const int rows = piece_rows(a.found, a.row0, a.Tc);
   if (DH && n0 >= rows) return;
@@ -755,9 +754,41 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_product_kernel(ProdArgs a,
           for (int e = 0; e < 8; ++e)
             bad |= m + e < a.M && (d[e >> 1] >> (16 * (e & 1)) & EX) == EX;
         }
-        put8(a.out + (int64_t)(DH ? a.idx[n] : n) * a.out_ld, m, a.M, a.ovec, d);
+        put8(a.out + (int64_t)(DH ? a.idx[n] : n) * a.out_ld, m, a.M, d);
       });
   if (!DH && a.flag) flag_nonfinite(a.flag, bad);
+}
+
+// Both gradients in one launch, dh's tiles in the first nh workgroups: neither waits
+// for the other's last tiles. The first wave also sums up the losses where they are
+// few, which saves a launch.
+constexpr int kSumHere = 1024;  // partial sums of 16 rows
+struct SumArgs {
+  const double *lsum;
+  int32_t n;         // partial sums; 0: not here
+  const Found *found;
+  float *totals;
+};
+template <class P>
+__global__ __launch_bounds__(P::NT, P::WPE) void xent_products_kernel(ProdArgs dh, TileMap th,
+                                                                      ProdArgs dw, TileMap tw,
+                                                                      int nh, SumArgs sum) {
+  FG_DMA_RING(P, R);
+  const int block = blockIdx.x;
+  if (sum.n && block == 0 && threadIdx.x < 64) {
+    double s = 0;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < sum.n; i += 64) s += sum.lsum[i];
+    s = wave_sum(s);
+    if (threadIdx.x == 0) {
+      sum.totals[0] = (float)s;
+      sum.totals[1] = sum.found->wsum;
+    }
+  }
+  if (block < nh)
+    product_tile<P, true>(dh, th, block, R);
+  else
+    product_tile<P, false>(dw, tw, block - nh, R);
 }
 
 // Joins the parts of a split sum, in their order: 8 columns of a row per lane.
@@ -765,27 +796,32 @@ struct JoinArgs {
   const float *part;
   int64_t pstride;
   int32_t nsplit, rows, M, Mq;  // rows: -1: the piece's live ones
+  int32_t shared;               // by a workgroup's waves
   int32_t row0, Tc;
   const Found *found;
   const int32_t *idx;
   uint16_t *out;
   int64_t out_ld;
-  int32_t ovec, bf;
+  int32_t bf;
   int32_t *flag;
 };
-// SW waves share a sum, a run of the parts each (12 x 512 sums of 256 parts took 42 us
-// by single lanes).
-template <int SW>
-__global__ __launch_bounds__(512) void xent_join_kernel(JoinArgs a) {
-  __shared__ float sh[SW][SW > 1 ? 64 : 1][8];
+// Where there are many, the workgroup's 8 waves share a sum, a run of the parts each
+// (12 x 512 sums of 256 parts took 42 us by single lanes). Both gradients' in one
+// launch, dh's in the first nh workgroups.
+__global__ __launch_bounds__(512) void xent_join_kernel(JoinArgs dh, JoinArgs dw, int nh) {
+  __shared__ float sh[8][64][8];
+  const bool first = (int)blockIdx.x < nh;
+  const JoinArgs &a = first ? dh : dw;
+  const int block = first ? blockIdx.x : blockIdx.x - nh;
   const int rows = a.rows < 0 ? piece_rows(a.found, a.row0, a.Tc) : a.rows;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t i = (int64_t)blockIdx.x * (512 / SW) + (SW > 1 ? lane : (int)threadIdx.x);
+  const bool shared = a.shared;
+  const int64_t i = shared ? (int64_t)block * 64 + lane : (int64_t)block * 512 + threadIdx.x;
   const int c8 = a.Mq / 8;
   const int64_t n = i / c8;
   const int m = (int)(i - n * c8) * 8;
-  const int per = (a.nsplit + SW - 1) / SW;
-  const int s0 = SW > 1 ? wave * per : 0, s1 = min(a.nsplit, s0 + per);
+  const int per = shared ? (a.nsplit + 7) / 8 : a.nsplit;
+  const int s0 = shared ? wave * per : 0, s1 = min(a.nsplit, s0 + per);
   bool bad = false;
   float v[8] = {};
   if (n < rows) {
@@ -799,13 +835,13 @@ __global__ __launch_bounds__(512) void xent_join_kernel(JoinArgs a) {
         for (int e = 0; e < 4; ++e) v[4 * h + e] += x[e];
       }
   }
-  if constexpr (SW > 1) {
+  if (shared) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) sh[wave][lane][e] = v[e];
     __syncthreads();
     if (wave) return;
 #pragma unroll
-    for (int k = 1; k < SW; ++k)
+    for (int k = 1; k < 8; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += sh[k][lane][e];
   }
@@ -817,7 +853,7 @@ __global__ __launch_bounds__(512) void xent_join_kernel(JoinArgs a) {
     const uint32_t ex = a.bf ? 0x7F80u : 0x7C00u;
 #pragma unroll
     for (int e = 0; e < 8; ++e) bad |= m + e < a.M && (d[e >> 1] >> (16 * (e & 1)) & ex) == ex;
-    put8(a.out + (a.idx ? a.idx[n] : n) * a.out_ld, m, a.M, a.ovec, d);
+    put8(a.out + (a.idx ? a.idx[n] : n) * a.out_ld, m, a.M, d);
   }
   if (a.flag) flag_nonfinite(a.flag, bad);
 }
@@ -836,28 +872,27 @@ constexpr int kTileOf[3] = {64, 128, 256};
 struct Shape {
   int tile, ns, kper;  // tile: index into kTileOf
 };
-Shape pick(int64_t M, int64_t N, int64_t K, bool split) {
+// The best number of parts for one tile, and its time.
+Shape pick_tile(int t, int64_t M, int64_t N, int64_t K, bool split, double &us_best) {
   // TFLOP/s of a CU with 1, 2, 3 workgroups of a tile
   static const double rate[3][3] = {{1.0, 1.6, 2.0}, {2.6, 3.6, 3.6}, {4.7, 4.7, 4.7}};
   static const int occ[3] = {3, 2, 1};
-  Shape best{0, 1, 0};
-  double tbest = 1e300;
-  for (int t = 0; t < 3; ++t) {
-    const int64_t ts = kTileOf[t];
-    const int64_t tiles = ((M + ts - 1) / ts) * ((N + ts - 1) / ts);
-    for (int ns = 1; ns <= (split ? 512 : 1); ns *= 2) {
-      const int64_t kper = std::max<int64_t>(64, ((K + ns - 1) / ns + 63) / 64 * 64);
-      if (ns > 1 && kper < 256) break;
-      const int64_t parts = std::max<int64_t>(1, (K + kper - 1) / kper);
-      const int64_t n = tiles * parts, slots = 256 * occ[t];
-      const int64_t full = n / slots, rest = n - full * slots;
-      const double work = 2e-6 * ts * ts * kper;  // us at 1 TFLOP/s
-      auto round = [&](int j) { return j * work / rate[t][j - 1] + 2.0; };
-      double us = full * round(occ[t]);
-      if (rest) us += round((int)((rest + 255) / 256));
-      if (parts > 1) us += 3.0 + (double)parts * M * N * 8 / 4e6;
-      if (us < tbest) tbest = us, best = {t, (int)parts, (int)kper};
-    }
+  Shape best{t, 1, 0};
+  us_best = 1e300;
+  const int64_t ts = kTileOf[t];
+  const int64_t tiles = ((M + ts - 1) / ts) * ((N + ts - 1) / ts);
+  for (int ns = 1; ns <= (split ? 512 : 1); ns *= 2) {
+    const int64_t kper = std::max<int64_t>(64, ((K + ns - 1) / ns + 63) / 64 * 64);
+    if (ns > 1 && kper < 256) break;
+    const int64_t parts = std::max<int64_t>(1, (K + kper - 1) / kper);
+    const int64_t n = tiles * parts, slots = 256 * occ[t];
+    const int64_t full = n / slots, rest = n - full * slots;
+    const double work = 2e-6 * ts * ts * kper;  // us at 1 TFLOP/s
+    auto round = [&](int j) { return j * work / rate[t][j - 1] + 2.0; };
+    double us = full * round(occ[t]);
+    if (rest) us += round((int)((rest + 255) / 256));
+    if (parts > 1) us += 3.0 + (double)parts * M * N * 8 / 4e6;
+    if (us < us_best) us_best = us, best = {t, (int)parts, (int)kper};
   }
   return best;
 }
@@ -889,10 +924,18 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   p.Tc = std::max<int64_t>(256, up((p.T + p.pieces - 1) / p.pieces, 256));
   p.pieces = std::max<int64_t>(1, (p.T + p.Tc - 1) / p.Tc);
   const int64_t rows = std::min(p.T, p.Tc);
-  p.s1 = pick(p.V, rows, p.H, false);
+  double best = 1e300, us, us2;
+  for (int t = 0; t < 3; ++t) {
+    const Shape a = pick_tile(t, p.V, rows, p.H, false, us);
+    if (us < best) best = us, p.s1 = a;
+  }
   p.ntile = (p.V + kTileOf[p.s1.tile] - 1) / kTileOf[p.s1.tile];
-  p.s2 = pick(p.H, rows, p.Vp, true);
-  p.s3 = pick(p.H, p.V, rows, true);
+  best = 1e300;  // one launch, one tile for both products
+  for (int t = 0; t < 3; ++t) {
+    const Shape a = pick_tile(t, p.H, rows, p.Vp, true, us);
+    const Shape b = pick_tile(t, p.H, p.V, rows, true, us2);
+    if (us + us2 < best) best = us + us2, p.s2 = a, p.s3 = b;
+  }
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t was = at;
@@ -936,26 +979,33 @@ hipError_t launch_logits(const LogitArgs &a, int64_t rows, hipStream_t st) {
   return hipGetLastError();
 }
 
+struct Products {
+  ProdArgs dh, dw;
+  JoinArgs jdh, jdw;
+  int nsdh, nsdw;     // parts; 0: that gradient is not wanted
+  int64_t rows;
+  SumArgs sum;
+};
+
 template <class P>
-hipError_t launch_dh(const ProdArgs &a, int64_t rows, int ns, hipStream_t st) {
-  const TileMap tm = tile_map((a.M + P::TM - 1) / P::TM, (rows + P::TN - 1) / P::TN, ns);
-  hipLaunchKernelGGL((xent_product_kernel<P, true>), dim3(8 * tm.per), dim3(P::NT), 0, st, a, tm);
-  return hipGetLastError();
-}
-template <class P>
-hipError_t launch_dw(const ProdArgs &a, int ns, hipStream_t st) {
-  const TileMap tm = tile_map((a.M + P::TM - 1) / P::TM, (a.V + P::TN - 1) / P::TN, ns);
-  hipLaunchKernelGGL((xent_product_kernel<P, false>), dim3(8 * tm.per), dim3(P::NT), 0, st, a,
-                     tm);
+hipError_t launch_products(const Products &a, hipStream_t st) {
+  const TileMap th = tile_map((a.dh.M + P::TM - 1) / P::TM, (a.rows + P::TN - 1) / P::TN, a.nsdh);
+  const TileMap tw = tile_map((a.dw.M + P::TM - 1) / P::TM, (a.dw.V + P::TN - 1) / P::TN, a.nsdw);
+  hipLaunchKernelGGL((xent_products_kernel<P>), dim3(8 * (th.per + tw.per)), dim3(P::NT), 0, st,
+                     a.dh, th, a.dw, tw, 8 * th.per, a.sum);
   return hipGetLastError();
 }
 
-hipError_t launch_join(const JoinArgs &a, int64_t rows, hipStream_t st) {
-  const int64_t n = rows * (a.Mq / 8);
-  if (a.nsplit >= 16)
-    hipLaunchKernelGGL(xent_join_kernel<8>, dim3((uint32_t)((n + 63) / 64)), dim3(512), 0, st, a);
-  else
-    hipLaunchKernelGGL(xent_join_kernel<1>, dim3((uint32_t)((n + 511) / 512)), dim3(512), 0, st, a);
+hipError_t launch_join(Products &a, bool dh, bool dw, hipStream_t st) {
+  if (!dh && !dw) return hipSuccess;
+  const auto blocks = [](JoinArgs &j, int64_t rows) {
+    const int64_t n = rows * (j.Mq / 8);
+    j.shared = j.nsplit >= 16;
+    return (int)((n + (j.shared ? 63 : 511)) / (j.shared ? 64 : 512));
+  };
+  const int nh = dh ? blocks(a.jdh, a.rows) : 0, nw = dw ? blocks(a.jdw, a.dw.V) : 0;
+  hipLaunchKernelGGL(xent_join_kernel, dim3((uint32_t)(nh + nw)), dim3(512), 0, st, a.jdh, a.jdw,
+                     nh);
   return hipGetLastError();
 }
 
@@ -973,8 +1023,6 @@ struct Call {
   int32_t *flag;
   bool grad;
 };
-
-bool aligned16(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
 
 hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
   const int64_t w_ld = d.w_ld ? d.w_ld : d.hidden;
@@ -995,10 +1043,8 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
   r.T = (int32_t)p.T, r.H = (int32_t)p.H, r.Hp = (int32_t)p.Hp, r.V = (int32_t)p.V;
   r.nb = (int32_t)p.nb;
   r.scale = d.scale, r.mean = d.mean;
-  r.hvec = aligned16(c.h, r.h_ld);
   r.dh = (uint16_t *)c.dh;
   r.dh_ld = d.dh_ld ? d.dh_ld : d.hidden;
-  r.dhvec = aligned16(c.dh, r.dh_ld);
   r.count = (int32_t *)at(p.count), r.wsum = (double *)at(p.wsum), r.wmax = (float *)at(p.wmax);
   r.found = (Found *)at(p.found);
   r.idx = (int32_t *)at(p.idx), r.ctarget = (int32_t *)at(p.ctarget);
@@ -1027,6 +1073,8 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
     FG_TRY(hipGetLastError());
     w = (const uint16_t *)at(p.wc);
   }
+  const int32_t nsum = (int32_t)((p.T + kSlot - 1) / kSlot);
+  bool summed = false;
   for (int64_t i = 0; i < p.pieces; ++i) {
     const int64_t row0 = i * p.Tc, rows = std::min(p.Tc, p.T - row0);
     const uint16_t *hc = r.hc + (size_t)row0 * p.Hp;
@@ -1059,53 +1107,57 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       FG_TRY(hipGetLastError());
     }
     if (!c.grad) continue;
-    ProdArgs g{};
-    g.b = (const uint16_t *)at(p.e), g.b_ld = p.Vp;
-    g.M = (int32_t)p.H, g.Mq = (int32_t)p.Hq;
-    g.row0 = (int32_t)row0, g.Tc = (int32_t)p.Tc, g.found = r.found;
-    g.V = (int32_t)p.V;
-    JoinArgs j{};
-    j.M = g.M, j.Mq = g.Mq, j.row0 = g.row0, j.Tc = g.Tc, j.found = r.found, j.bf = bf;
+    const bool last = i + 1 == p.pieces;
+    Products g{};
+    g.rows = rows;
+    ProdArgs &a = g.dh;
+    a.b = (const uint16_t *)at(p.e), a.b_ld = p.Vp;
+    a.M = (int32_t)p.H, a.Mq = (int32_t)p.Hq;
+    a.row0 = (int32_t)row0, a.Tc = (int32_t)p.Tc, a.found = r.found;
+    a.V = (int32_t)p.V;
+    JoinArgs &j = g.jdh;
+    j.M = a.M, j.Mq = a.Mq, j.row0 = a.row0, j.Tc = a.Tc, j.found = r.found, j.bf = bf;
+    g.dw = a, g.jdw = j;
+    bool join_dh = false, join_dw = false;
     if (c.dh && rows > 0) {
-      ProdArgs a = g;
+      const bool split = p.s2.ns > 1;
+      g.nsdh = p.s2.ns;
       a.a = w, a.a_ld = p.w_ld, a.a_rows = (int32_t)p.V, a.a_cols = (int32_t)p.wh;
       a.K = (int32_t)p.Vp, a.kper = p.s2.kper;
       a.idx = r.idx + row0;
-      const bool split = p.s2.ns > 1;
-      a.out = split ? nullptr : (uint16_t *)c.dh, a.out_ld = r.dh_ld, a.ovec = r.dhvec;
+      a.out = split ? nullptr : (uint16_t *)c.dh, a.out_ld = r.dh_ld;
       a.part = split ? (float *)at(p.pdh) : nullptr, a.pstride = p.Tc * p.Hq;
-      FG_TRY(FG_XENT_TILE(launch_dh, DhTiles, p.s2.tile, bf, a, rows, p.s2.ns, st));
-      if (split) {
-        JoinArgs q = j;
-        q.part = a.part, q.pstride = a.pstride, q.nsplit = p.s2.ns, q.rows = -1;
-        q.idx = a.idx, q.out = (uint16_t *)c.dh, q.out_ld = r.dh_ld, q.ovec = r.dhvec;
-        FG_TRY(launch_join(q, rows, st));
-      }
+      j.part = a.part, j.pstride = a.pstride, j.nsplit = p.s2.ns, j.rows = -1;
+      j.idx = a.idx, j.out = (uint16_t *)c.dh, j.out_ld = a.out_ld;
+      join_dh = split;
     }
     if (c.dw) {
-      ProdArgs a = g;
-      a.a = hc, a.a_ld = p.Hp, a.a_rows = (int32_t)p.Tc, a.a_cols = (int32_t)p.Hp;
-      a.N = (int32_t)p.Vp;
-      a.K = (int32_t)p.Tc, a.kper = p.s3.kper;
-      const bool last = i + 1 == p.pieces, split = p.s3.ns > 1;
-      const int64_t dw_ld = d.dw_ld ? d.dw_ld : d.hidden;
-      const int dwvec = aligned16(c.dw, dw_ld);
-      a.out = split || !last ? nullptr : (uint16_t *)c.dw, a.out_ld = dw_ld, a.ovec = dwvec;
-      a.part = split || p.pieces > 1 ? (float *)at(p.pdw) : nullptr, a.pstride = p.V * p.Hq;
-      a.add = i > 0;
-      a.flag = c.flag;
-      FG_TRY(FG_XENT_TILE(launch_dw, DwTiles, p.s3.tile, bf, a, p.s3.ns, st));
-      if (split && last) {
-        JoinArgs q = j;
-        q.part = a.part, q.pstride = a.pstride, q.nsplit = p.s3.ns, q.rows = (int32_t)p.V;
-        q.out = (uint16_t *)c.dw, q.out_ld = dw_ld, q.ovec = dwvec, q.flag = c.flag;
-        FG_TRY(launch_join(q, p.V, st));
-      }
+      ProdArgs &b = g.dw;
+      JoinArgs &q = g.jdw;
+      const bool split = p.s3.ns > 1;
+      g.nsdw = p.s3.ns;
+      b.a = hc, b.a_ld = p.Hp, b.a_rows = (int32_t)p.Tc, b.a_cols = (int32_t)p.Hp;
+      b.N = (int32_t)p.Vp;
+      b.K = (int32_t)p.Tc, b.kper = p.s3.kper;
+      b.out = split || !last ? nullptr : (uint16_t *)c.dw;
+      b.out_ld = d.dw_ld ? d.dw_ld : d.hidden;
+      b.part = split || p.pieces > 1 ? (float *)at(p.pdw) : nullptr, b.pstride = p.V * p.Hq;
+      b.add = i > 0;
+      b.flag = c.flag;
+      q.part = b.part, q.pstride = b.pstride, q.nsplit = p.s3.ns, q.rows = (int32_t)p.V;
+      q.out = (uint16_t *)c.dw, q.out_ld = b.out_ld, q.flag = c.flag;
+      join_dw = split && last;
     }
+    if (!g.nsdh && !g.nsdw) continue;
+    if (c.totals && last && nsum <= kSumHere) {
+      g.sum = {(const double *)at(p.lsum), nsum, r.found, c.totals};
+      summed = nsum > 0;
+    }
+    FG_TRY(FG_XENT_TILE(launch_products, ProdTiles, p.s2.tile, bf, g, st));
+    FG_TRY(launch_join(g, join_dh, join_dw, st));
   }
-  if (c.totals) {
-    const int32_t n = (int32_t)((p.T + kSlot - 1) / kSlot);
-    hipLaunchKernelGGL(xent_totals_kernel, dim3(1), dim3(1024), 0, st, (double *)at(p.lsum), n,
+  if (c.totals && !summed) {
+    hipLaunchKernelGGL(xent_totals_kernel, dim3(1), dim3(1024), 0, st, (double *)at(p.lsum), nsum,
                        r.found, c.totals);
     FG_TRY(hipGetLastError());
   }
