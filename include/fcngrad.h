@@ -567,8 +567,8 @@ size_t fg_linear_xent_workspace_bytes(const fg_xent_desc *d, int grad);
  * scratch. FG_EINVAL for a null pointer, rows < 0, hidden or vocab < 1, a stride below
  * hidden, a non-finite scale, an unknown dtype or mean, a pointer not aligned to its
  * elements, or an output overlapping another tensor; FG_EUNSUPPORTED for rows of 2^28,
- * hidden above 2^16, vocab of 2^22 - 64 or strides of 2^20 or more, FG_F32, or w not
- * 16-byte aligned while hidden and w_ld are multiples of 8; FG_EWORKSPACE. */
+ * hidden above 2^16, vocab of 2^22 - 64 or strides of 2^20 or more, or FG_F32;
+ * FG_EWORKSPACE. */
 fg_status linear_xent_fwd(const fg_xent_desc *d, const void *h, const void *w,
                           const int32_t *target, const float *weight, float *loss, float *lse,
                           float *totals, void *ws, size_t ws_bytes, hipStream_t stream);

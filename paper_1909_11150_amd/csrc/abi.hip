@@ -1035,7 +1035,6 @@ static fg_status xent_call(const fg_xent_desc *d, const void *h, const void *w,
        (uintptr_t)totals | (uintptr_t)flag) % 4)
     return FG_EINVAL;
   const auto ld = [&](int64_t v) { return v ? v : (int64_t)d->hidden; };
-  if (d->hidden % 8 == 0 && ld(d->w_ld) % 8 == 0 && ((uintptr_t)w & 15)) return FG_EUNSUPPORTED;
   const size_t need = linear_xent_ws_bytes(*d, grad);
   if (ws_bytes < need || ((uintptr_t)ws & 15)) return FG_EWORKSPACE;
   const auto span = [&](int64_t n, int64_t l) {

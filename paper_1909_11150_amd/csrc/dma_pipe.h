@@ -365,11 +365,18 @@ __device__ __forceinline__ void sched_mfma_reads_dma() {
 struct NoFold {
   __device__ __forceinline__ void operator()() const {}
 };
-template <class C, bool AK, bool BKM, int U, class Issue, class Fold>
+// `fix` may change the fragments of stage it, step ks, before their MFMAs; it is
+// called in the last stages only (the last one among them; no-op by default).
+struct NoFix {
+  template <class F>
+  __device__ __forceinline__ void operator()(F &, int, int) const {}
+};
+template <class C, bool AK, bool BKM, int U, class Issue, class Fold, class Fix>
 __device__ __forceinline__ void stage(f32x16 (&acc)[C::FM][C::FN],
                                       Frags<C> (&f)[2], const Ring &R, int it,
                                       int nst, bool next, bool full, int wm0,
-                                      int wn0, int lane, Issue &issue, Fold &fold) {
+                                      int wn0, int lane, Issue &issue, Fold &fold,
+                                      Fix &fix) {
   constexpr int NS = C::NS, KS = C::KS;
   constexpr int NMF = C::FM * C::FN;
   constexpr int NRD = C::FM * (AK ? 1 : 2) + C::FN * (BKM ? 1 : 2);
@@ -378,6 +385,7 @@ __device__ __forceinline__ void stage(f32x16 (&acc)[C::FM][C::FN],
     if (ks + 1 < KS)
       load_frags<C, AK, BKM>(f[(ks + 1) & 1], R.a[U], R.b[U], ks + 1, wm0, wn0,
                              lane);
+    if (!full) fix(f[ks & 1], it, ks);
     mma<C>(acc, f[ks & 1]);
     if (ks + 1 < KS) sched_mfma_reads<NMF, NRD>();
     __builtin_amdgcn_s_setprio(0);
@@ -404,21 +412,21 @@ __device__ __forceinline__ void stage(f32x16 (&acc)[C::FM][C::FN],
   fold();
 }
 
-template <class C, bool AK, bool BKM, int U, class Issue, class Fold>
+template <class C, bool AK, bool BKM, int U, class Issue, class Fold, class Fix>
 __device__ __forceinline__ void group(f32x16 (&acc)[C::FM][C::FN],
                                       Frags<C> (&f)[2], const Ring &R, int it0,
                                       int nst, bool tail, int wm0, int wn0,
-                                      int lane, Issue &issue, Fold &fold) {
+                                      int lane, Issue &issue, Fold &fold, Fix &fix) {
   if constexpr (U < C::NS) {
     const int it = it0 + U;
     if (!tail) {
       stage<C, AK, BKM, U>(acc, f, R, it, nst, true, true, wm0, wn0, lane, issue,
-                           fold);
+                           fold, fix);
     } else if (it < nst) {
       stage<C, AK, BKM, U>(acc, f, R, it, nst, it + 1 < nst, false, wm0, wn0,
-                           lane, issue, fold);
+                           lane, issue, fold, fix);
     }
-    group<C, AK, BKM, U + 1>(acc, f, R, it0, nst, tail, wm0, wn0, lane, issue, fold);
+    group<C, AK, BKM, U + 1>(acc, f, R, it0, nst, tail, wm0, wn0, lane, issue, fold, fix);
   }
 }
 
@@ -428,11 +436,11 @@ __device__ __forceinline__ void group(f32x16 (&acc)[C::FM][C::FN],
 // data-dependent control flow around the MFMAs (so the compiler's own LDS
 // waits stay exact and its scheduling regions span whole steps); the last
 // groups run with per-stage checks.
-template <class C, bool AK, bool BKM, class Issue, class Fold = NoFold>
+template <class C, bool AK, bool BKM, class Issue, class Fold = NoFold, class Fix = NoFix>
 __device__ __forceinline__ void pipeline(f32x16 (&acc)[C::FM][C::FN],
                                          const Ring &R, int nst, int wm0,
                                          int wn0, int lane, Issue &&issue,
-                                         Fold &&fold = Fold{}) {
+                                         Fold &&fold = Fold{}, Fix &&fix = Fix{}) {
   constexpr int NS = C::NS, KS = C::KS;
   static_assert(NS >= 2 && NS <= 5 && KS >= 2 && KS % 2 == 0, "pipeline shape");
   if (nst <= 0) return;
@@ -449,9 +457,9 @@ __device__ __forceinline__ void pipeline(f32x16 (&acc)[C::FM][C::FN],
   // checks: it0 + 2 NS - 1 < nst.
   int it0 = 0;
   for (; it0 + 2 * NS - 1 < nst; it0 += NS)
-    group<C, AK, BKM, 0>(acc, f, R, it0, nst, false, wm0, wn0, lane, issue, fold);
+    group<C, AK, BKM, 0>(acc, f, R, it0, nst, false, wm0, wn0, lane, issue, fold, fix);
   for (; it0 < nst; it0 += NS)
-    group<C, AK, BKM, 0>(acc, f, R, it0, nst, true, wm0, wn0, lane, issue, fold);
+    group<C, AK, BKM, 0>(acc, f, R, it0, nst, true, wm0, wn0, lane, issue, fold, fix);
 }
 
 template <class C>

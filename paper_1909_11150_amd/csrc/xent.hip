@@ -37,7 +37,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // Numerators and G are held times 2^15: the largest is then 2^15, within fp16, and
 // values down to 2^-29 of it keep all their bits (2^-14 otherwise).
 constexpr float kUp = 32768.f;
-constexpr int kSlot = 16;       // rows of a workgroup of the softmax kernel
+constexpr int kTickets = 64;    // softmax workgroups up to which the last one sums up
+constexpr int kFew = 1024;      // rows up to which the softmax kernel takes 4 per workgroup
 constexpr int kCount = 1024;    // rows of a workgroup of the counting kernel
 constexpr int kDirect = 8192;   // rows up to which there is none
 
@@ -62,6 +63,7 @@ struct Found {
   float wmax_inv;   // 1 / largest |weight|
   float mult;       // G W and G^T h times this are the gradients
   float wsum;
+  uint32_t ticket;  // workgroups done (losses only)
 };
 
 // ---- live rows -----------------------------------------------------------------
@@ -144,6 +146,7 @@ __device__ __forceinline__ void put_found(const RowArgs &a, int live, double sum
   const float top = mx > 0.f ? mx : 1.f;
   a.found->live = live;
   a.found->wsum = (float)sum;
+  a.found->ticket = 0;
   a.found->wmax_inv = 1.f / top;
   a.found->mult = den != 0.0 ? (float)(a.scale / den * top / kUp) : 0.f;
 }
@@ -196,6 +199,12 @@ __global__ __launch_bounds__(1024) void xent_scan_kernel(RowArgs a) {
 struct __attribute__((packed, aligned(2))) Any16 {
   u32x4 v;
 };
+
+// Rows are taken in chunks of 8 elements. A width that is no multiple of 8 has a last
+// chunk that begins before its place, at width - 8, so that nothing outside the row is
+// read or written; what it repeats is left out of sums over the width (logits), and
+// written twice, alike, where the width is an output's (dh, dW).
+__device__ __forceinline__ int chunk_at(int c, int width) { return min(c, width - 8); }
 
 // 8 elements of a row from column c on, zeros past its end.
 __device__ __forceinline__ u32x4 row8(const uint16_t *row, int c, int n) {
@@ -285,16 +294,11 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
   }
 }
 
-// The head's weights with rows padded to a multiple of 64, where theirs are not
-// aligned as the DMA needs them.
+// Rows of fewer than 8 elements, padded with zeros to 8.
 __global__ __launch_bounds__(256) void xent_pad_kernel(const uint16_t *w, int64_t ld, int32_t H,
-                                                       uint16_t *wc, int32_t Hp, int64_t chunks) {
-  const int64_t stride = (int64_t)gridDim.x * 256;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < chunks; i += stride) {
-    const int64_t r = i / (Hp / 8);
-    const int c = (int)(i - r * (Hp / 8)) * 8;
-    *reinterpret_cast<u32x4 *>(wc + r * Hp + c) = row8(w + r * ld, c, H);
-  }
+                                                       uint16_t *wc, int32_t V) {
+  const int r = blockIdx.x * 256 + threadIdx.x;
+  if (r < V) *reinterpret_cast<u32x4 *>(wc + (size_t)r * 8) = row8(w + r * ld, 0, H);
 }
 
 // ---- tiles -----------------------------------------------------------------------
@@ -308,6 +312,11 @@ __device__ __forceinline__ uint8_t *wave_buf(const Ring &R, int wave) {
   for (int k = 1; k < (P::NW + PER - 1) / PER; ++k)
     if (wave / PER == k) buf = R.a[k];
   return buf + (wave % PER) * S;
+}
+
+// Writes 8 columns of a row of `width` elements that were computed as chunk c.
+__device__ __forceinline__ void put_chunk(uint16_t *row, int c, int width, const u32x4 &v) {
+  put8(row, width >= 8 ? chunk_at(c, width) : c, width, v);
 }
 
 // 16-bit store of a wave's block: pack(i, j, g) gives 4 consecutive columns of lane
@@ -360,7 +369,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void *p, uint32_t b
 struct LogitArgs {
   const uint16_t *w;
   int64_t w_ld;
-  int32_t wh;             // elements of a row of w that are there (a multiple of 8)
+  int32_t wh;             // elements of a row (of w and of hc), at least 8
   int32_t V;
   const uint16_t *hc;     // the piece's first row
   int32_t Hp;
@@ -407,18 +416,44 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
   for (int jj = 0; jj < PA; ++jj) oa[jj] = (unsigned)(as.row[jj] * (int)a.w_ld + as.coff[jj]) * 2u;
 #pragma unroll
   for (int jj = 0; jj < PB; ++jj) ob[jj] = (unsigned)(bs.row[jj] * a.Hp + bs.coff[jj]) * 2u;
+  const int nst = (a.wh + BK - 1) / BK;
   auto issue = [&](int st, int slot) __attribute__((always_inline)) {
     uint8_t *ta = R.a[slot], *tb = R.b[slot];
     const int k0 = st * BK;
+    if (k0 + BK <= a.wh) {
 #pragma unroll
-    for (int jj = 0; jj < PB; ++jj) dma16(rs_h, tb + dma_dst<PB>(wave, jj), ob[jj] + 2u * k0);
+      for (int jj = 0; jj < PB; ++jj) dma16(rs_h, tb + dma_dst<PB>(wave, jj), ob[jj] + 2u * k0);
 #pragma unroll
-    for (int jj = 0; jj < PA; ++jj)
-      dma16(rs_w, ta + dma_dst<PA>(wave, jj), as.coff[jj] < a.wh - k0 ? oa[jj] + 2u * k0 : kOOB);
+      for (int jj = 0; jj < PA; ++jj) dma16(rs_w, ta + dma_dst<PA>(wave, jj), oa[jj] + 2u * k0);
+    } else {  // chunks past the end: zeros
+      auto tail = [&](unsigned o, int coff) __attribute__((always_inline)) {
+        return k0 + coff < a.wh ? o + 2u * (chunk_at(k0 + coff, a.wh) - coff) : kOOB;
+      };
+#pragma unroll
+      for (int jj = 0; jj < PB; ++jj)
+        dma16(rs_h, tb + dma_dst<PB>(wave, jj), tail(ob[jj], bs.coff[jj]));
+#pragma unroll
+      for (int jj = 0; jj < PA; ++jj)
+        dma16(rs_w, ta + dma_dst<PA>(wave, jj), tail(oa[jj], as.coff[jj]));
+    }
+  };
+  // the last chunk's repeated elements: zeros in both operands, whatever they are
+  auto fix = [&](Frags<P> &f, int it, int ks) __attribute__((always_inline)) {
+    if (it + 1 < nst || a.wh % 8 == 0) return;
+    const int over = it * BK + 16 * ks + 8 * (lane >> 5) + 8 - a.wh;  // 1 .. 7: that chunk
+    const int cut = over < 8 ? over : 0;
+    u32x4 m;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+      m[d] = (2 * d < cut ? 0u : 0xFFFFu) | (2 * d + 1 < cut ? 0u : 0xFFFF0000u);
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i) f.a[i] &= m;
+#pragma unroll
+    for (int j = 0; j < P::FN; ++j) f.b[j] &= m;
   };
   f32x16 acc[P::FM][P::FN];
   zero<P>(acc);
-  pipeline<P, true, true>(acc, R, (a.wh + BK - 1) / BK, wm0, wn0, lane, issue);
+  pipeline<P, true, true>(acc, R, nst, wm0, wn0, lane, issue, NoFold{}, fix);
 
   // classes past the last one: logit -inf
   if (m0 + P::TM > a.V) {
@@ -509,9 +544,8 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
 }
 
 // ---- softmax ------------------------------------------------------------------------
-constexpr int kAhead = 8;  // loads in flight: a row's tiles are joined by 16 lanes
 struct SoftmaxArgs {
-  const Found *found;
+  Found *found;
   int32_t row0, Tc, V, Vp, tlog, ntile;  // 2^tlog: classes of a logits tile
   int32_t vper;                          // classes of a workgroup, a multiple of 512
   int32_t bf;                            // G in bf16, not fp16
@@ -521,44 +555,51 @@ struct SoftmaxArgs {
   const float *tlogit;
   uint16_t *e;                           // null: losses only
   float *loss, *lse;
-  double *lsum;                          // per 16 rows
+  double *lsum;                          // per RS rows
+  float *totals;                         // null, or written by the last workgroup
+  int32_t nsum;
 };
 
-// 16 rows' lse and losses from their tiles, then (gradients) a range of their
-// classes: numerators to 2^15 G.
+// RS rows' lse and losses from their tiles, then (gradients) a range of their
+// classes: numerators to 2^15 G. 256 / RS lanes join a row's tiles, 8 loads of each
+// in flight; few rows take few per workgroup, for more lanes each.
+template <int RS>
 __global__ __launch_bounds__(256) void xent_softmax_kernel(SoftmaxArgs a) {
-  __shared__ float sm[16][kSlot], ss[16][kSlot], lse2[kSlot], wt[kSlot], pt[kSlot];
-  __shared__ int tg[kSlot];
+  constexpr int G = 256 / RS, kAhead = 8;
+  __shared__ float lse2[RS], wt[RS], pt[RS];
+  __shared__ int tg[RS];
+  __shared__ double part[RS], ws[4];
+  __shared__ bool last;
   const int rows = piece_rows(a.found, a.row0, a.Tc);
-  const int r0 = blockIdx.x * kSlot, tid = threadIdx.x;
+  const int r0 = blockIdx.x * RS, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool first = blockIdx.y == 0;
   if (r0 < rows) {
-    // 16 lanes of each row take its tiles in turn
-    const int r = tid & 15, g = tid >> 4, n = r0 + r;
+    const int r = tid / G, g = tid % G, n = r0 + r;
     float m = -INFINITY, s = 0.f;
     if (n < rows)
-      for (int p0 = g; p0 < a.ntile; p0 += 16 * kAhead) {
+      for (int p0 = g; p0 < a.ntile; p0 += G * kAhead) {
         float2 x[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-          x[k] = a.stats[(size_t)min(p0 + 16 * k, a.ntile - 1) * a.Tc + n];
+          x[k] = a.stats[(size_t)min(p0 + G * k, a.ntile - 1) * a.Tc + n];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-          if (p0 + 16 * k >= a.ntile || x[k].y == 0.f) continue;  // none, or all -inf
+          if (p0 + G * k >= a.ntile || x[k].y == 0.f) continue;  // none, or all -inf
           const float t = fmaxf(m, x[k].x);
           s = s * __builtin_amdgcn_exp2f(m - t) + x[k].y * __builtin_amdgcn_exp2f(x[k].x - t);
           m = t;
         }
       }
-    sm[g][r] = m, ss[g][r] = s;
-    __syncthreads();
-    if (tid < kSlot) {
-      for (int k = 0; k < 16; ++k) m = fmaxf(m, sm[k][r]);
-      s = 0.f;
-      for (int k = 0; k < 16; ++k)
-        if (ss[k][r] != 0.f) s += ss[k][r] * __builtin_amdgcn_exp2f(sm[k][r] - m);
-      const float l2 = m + __log2f(s);  // of a row with every logit -inf: NaN
-      double part = 0;
+#pragma unroll
+    for (int o = G / 2; o; o >>= 1) {
+      const float m1 = __shfl_xor(m, o), s1 = __shfl_xor(s, o), t = fmaxf(m, m1);
+      s = (s != 0.f ? s * __builtin_amdgcn_exp2f(m - t) : 0.f) +
+          (s1 != 0.f ? s1 * __builtin_amdgcn_exp2f(m1 - t) : 0.f);
+      m = t;
+    }
+    if (g == 0) {
+      const float l2 = m + __log2f(s);  // of a row with every logit -inf: -inf
+      double d64 = 0;
       lse2[r] = l2;
       if (n < rows) {
         const float w = a.cweight[n], d = l2 * kLn2 - a.tlogit[n];
@@ -568,23 +609,43 @@ __global__ __launch_bounds__(256) void xent_softmax_kernel(SoftmaxArgs a) {
         if (first) {
           a.loss[a.idx[n]] = w * d;
           if (a.lse) a.lse[a.idx[n]] = l2 * kLn2;
-          part = w * d;
+          d64 = w * d;
         }
       }
-      if (first) {
-#pragma unroll
-        for (int o = 8; o; o >>= 1) part += __shfl_xor(part, o);
-        if (tid == 0) a.lsum[blockIdx.x] = part;
-      }
+      part[r] = d64;
     }
     __syncthreads();
+    if (first && tid == 0) {
+      double sum = 0;
+      for (int k = 0; k < RS; ++k) sum += part[k];
+      a.lsum[blockIdx.x] = sum;
+    }
   } else if (first && tid == 0) {
     a.lsum[blockIdx.x] = 0;
   }
+  if (a.totals) {  // losses only: the workgroup that comes last sums them up
+    if (tid == 0) {
+      __threadfence();
+      last = atomicAdd(&a.found->ticket, 1u) + 1u == gridDim.x;
+    }
+    __syncthreads();
+    if (last) {
+      __threadfence();
+      double sum = 0;
+      for (int i = tid; i < a.nsum; i += 256) sum += __hip_atomic_load(
+          a.lsum + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      sum = wave_sum(sum);
+      if (lane == 0) ws[wave] = sum;
+      __syncthreads();
+      if (tid == 0) {
+        a.totals[0] = (float)((ws[0] + ws[1]) + (ws[2] + ws[3]));
+        a.totals[1] = a.found->wsum;
+      }
+    }
+  }
   if (!a.e || r0 >= rows) return;
-  const int lane = tid & 63, wave = tid >> 6;
   const int v0 = blockIdx.y * a.vper, v1 = min(a.Vp, v0 + a.vper);
-  for (int k = wave; k < kSlot; k += 4) {
+  for (int k = wave; k < RS; k += 4) {
     const int n = r0 + k;
     if (n >= rows) break;
     uint16_t *row = a.e + (size_t)n * a.Vp;
@@ -632,7 +693,7 @@ __global__ __launch_bounds__(1024) void xent_totals_kernel(const double *lsum, i
 struct ProdArgs {
   const uint16_t *a;
   int64_t a_ld;
-  int32_t a_rows, a_cols;    // rows there are; columns (a multiple of 8)
+  int32_t a_rows, a_cols;    // rows there are; columns (at least 8)
   const uint16_t *b;         // [Tc][Vp]
   int64_t b_ld;
   int32_t N;                 // columns n of B that are there (dW: Vp)
@@ -669,7 +730,7 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
 #pragma unroll
   for (int jj = 0; jj < PA; ++jj)
     oa[jj] = m0 + as.ncol[jj] < a.a_cols
-                 ? (unsigned)(as.krow[jj] * (int)a.a_ld + m0 + as.ncol[jj]) * 2u
+                 ? (unsigned)(as.krow[jj] * (int)a.a_ld + chunk_at(m0 + as.ncol[jj], a.a_cols)) * 2u
                  : kOOB;
 #pragma unroll
   for (int jj = 0; jj < PB; ++jj) {
@@ -720,7 +781,7 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const int m = m0 + wm0 + 32 * i + 8 * g + 4 * (lane >> 5);
-          if (m >= a.M) continue;
+          if (m >= a.Mq) continue;
           f32x4 *p = reinterpret_cast<f32x4 *>(part + (size_t)n * a.Mq + m);
           f32x4 v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
                      acc[i][j][4 * g + 3]};
@@ -752,9 +813,9 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
         if (!DH) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            bad |= m + e < a.M && (d[e >> 1] >> (16 * (e & 1)) & EX) == EX;
+            bad |= (d[e >> 1] >> (16 * (e & 1)) & EX) == EX;
         }
-        put8(a.out + (int64_t)(DH ? a.idx[n] : n) * a.out_ld, m, a.M, d);
+        put_chunk(a.out + (int64_t)(DH ? a.idx[n] : n) * a.out_ld, m, a.M, d);
       });
   if (!DH && a.flag) flag_nonfinite(a.flag, bad);
 }
@@ -762,7 +823,7 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
 // Both gradients in one launch, dh's tiles in the first nh workgroups: neither waits
 // for the other's last tiles. The first wave also sums up the losses where they are
 // few, which saves a launch.
-constexpr int kSumHere = 1024;  // partial sums of 16 rows
+constexpr int kSumHere = 1024;  // partial sums
 struct SumArgs {
   const double *lsum;
   int32_t n;         // partial sums; 0: not here
@@ -852,8 +913,8 @@ __global__ __launch_bounds__(512) void xent_join_kernel(JoinArgs dh, JoinArgs dw
     for (int e = 0; e < 4; ++e) d[e] = pack2(v[2 * e] * mult, v[2 * e + 1] * mult, a.bf);
     const uint32_t ex = a.bf ? 0x7F80u : 0x7C00u;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) bad |= m + e < a.M && (d[e >> 1] >> (16 * (e & 1)) & ex) == ex;
-    put8(a.out + (a.idx ? a.idx[n] : n) * a.out_ld, m, a.M, d);
+    for (int e = 0; e < 8; ++e) bad |= (d[e >> 1] >> (16 * (e & 1)) & ex) == ex;
+    put_chunk(a.out + (a.idx ? a.idx[n] : n) * a.out_ld, m, a.M, d);
   }
   if (a.flag) flag_nonfinite(a.flag, bad);
 }
@@ -891,7 +952,7 @@ Shape pick_tile(int t, int64_t M, int64_t N, int64_t K, bool split, double &us_b
     auto round = [&](int j) { return j * work / rate[t][j - 1] + 2.0; };
     double us = full * round(occ[t]);
     if (rest) us += round((int)((rest + 255) / 256));
-    if (parts > 1) us += 3.0 + (double)parts * M * N * 8 / 4e6;
+    if (parts > 1) us += 6.0 + (double)parts * M * N * 8 / 4e6;
     if (us < us_best) us_best = us, best = {t, (int)parts, (int)kper};
   }
   return best;
@@ -901,7 +962,7 @@ struct Plan {
   int64_t T, H, V, Tp, Hp, Vp, Hq, Tc, pieces, nb, wh, w_ld;
   bool pad_w;
   Shape s1, s2, s3;
-  int64_t ntile;
+  int64_t ntile, slot;
   // workspace, bytes
   size_t count, wsum, wmax, found, idx, ctarget, cweight, hc, wc, stats, tlogit, e, pdh, pdw,
       lsum, total;
@@ -914,9 +975,9 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   p.T = d.rows, p.H = d.hidden, p.V = d.vocab;
   p.Tp = up(p.T, 256), p.Hp = up(p.H, 64), p.Vp = up(p.V, 64), p.Hq = up(p.H, 8);
   p.w_ld = d.w_ld ? d.w_ld : p.H;
-  p.pad_w = p.H % 8 != 0 || p.w_ld % 8 != 0;
-  p.wh = p.pad_w ? p.Hp : p.H;
-  if (p.pad_w) p.w_ld = p.Hp;
+  p.pad_w = p.H < 8;
+  p.wh = std::max<int64_t>(p.H, 8);
+  if (p.pad_w) p.w_ld = 8;
   p.nb = (p.T + kCount - 1) / kCount;
   const int64_t per_row = grad ? p.Vp * 2 : (p.V + 63) / 64 * 8;
   const int64_t most = std::max<int64_t>(256, kPieceBytes / per_row / 256 * 256);
@@ -949,7 +1010,8 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   p.idx = take(p.Tp * 4);
   p.ctarget = take(p.Tp * 4);
   p.cweight = take(p.Tp * 4);
-  p.lsum = take(p.pieces * (p.Tc / kSlot) * 8);
+  p.slot = p.T <= kFew ? 4 : 16;
+  p.lsum = take(p.pieces * (p.Tc / p.slot) * 8);
   // the products read whole tiles of rows: a tile past the last piece's rows too
   p.hc = take((size_t)p.pieces * p.Tc * p.Hp * 2);
   p.stats = take((size_t)p.ntile * p.Tc * 8);
@@ -959,7 +1021,7 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
     p.pdh = take(p.s2.ns > 1 ? (size_t)p.s2.ns * p.Tc * p.Hq * 4 : 0);
     p.pdw = take(p.s3.ns > 1 || p.pieces > 1 ? (size_t)p.s3.ns * p.V * p.Hq * 4 : 0);
   }
-  p.wc = take(p.pad_w ? (size_t)p.V * p.Hp * 2 : 0);
+  p.wc = take(p.pad_w ? (size_t)p.V * 16 : 0);
   p.total = at;
   return p;
 }
@@ -1066,19 +1128,17 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
   }
   const uint16_t *w = (const uint16_t *)c.w;
   if (p.pad_w && p.T) {
-    const int64_t chunks = p.V * (p.Hp / 8);
-    hipLaunchKernelGGL(xent_pad_kernel, dim3((uint32_t)std::min<int64_t>((chunks + 255) / 256, 8192)),
-                       dim3(256), 0, st, w, w_ld, (int32_t)p.H, (uint16_t *)at(p.wc), (int32_t)p.Hp,
-                       chunks);
+    hipLaunchKernelGGL(xent_pad_kernel, dim3((uint32_t)((p.V + 255) / 256)), dim3(256), 0, st, w,
+                       w_ld, (int32_t)p.H, (uint16_t *)at(p.wc), (int32_t)p.V);
     FG_TRY(hipGetLastError());
     w = (const uint16_t *)at(p.wc);
   }
-  const int32_t nsum = (int32_t)((p.T + kSlot - 1) / kSlot);
+  const int32_t nsum = (int32_t)((p.T + p.slot - 1) / p.slot);
   bool summed = false;
   for (int64_t i = 0; i < p.pieces; ++i) {
     const int64_t row0 = i * p.Tc, rows = std::min(p.Tc, p.T - row0);
     const uint16_t *hc = r.hc + (size_t)row0 * p.Hp;
-    double *lsum = (double *)at(p.lsum) + i * (p.Tc / kSlot);
+    double *lsum = (double *)at(p.lsum) + i * (p.Tc / p.slot);
     if (rows > 0) {
       LogitArgs l{};
       l.w = w, l.w_ld = p.w_ld, l.wh = (int32_t)p.wh, l.V = (int32_t)p.V;
@@ -1096,14 +1156,16 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       s.idx = r.idx + row0, s.ctarget = l.ctarget, s.cweight = r.cweight + row0;
       s.stats = l.stats, s.tlogit = l.tlogit, s.e = l.e;
       s.loss = c.loss, s.lse = c.lse, s.lsum = lsum;
-      // workgroups: at least 2048, where the classes give as many ranges of 2048
-      const int64_t blocks = (rows + kSlot - 1) / kSlot;
-      int64_t ny = c.grad ? std::min<int64_t>((p.Vp + 2047) / 2048,
+      // workgroups: 2048, where the classes give as many ranges of 512
+      const int64_t blocks = (rows + p.slot - 1) / p.slot;
+      int64_t ny = c.grad ? std::min<int64_t>((p.Vp + 511) / 512,
                                               std::max<int64_t>(1, 2048 / blocks)) : 1;
       s.vper = (int32_t)up((p.Vp + ny - 1) / ny, 512);
-      ny = (p.Vp + s.vper - 1) / s.vper;
-      hipLaunchKernelGGL(xent_softmax_kernel, dim3((uint32_t)blocks, c.grad ? (uint32_t)ny : 1),
-                         dim3(256), 0, st, s);
+      ny = c.grad ? (p.Vp + s.vper - 1) / s.vper : 1;
+      if (!c.grad && p.pieces == 1 && blocks <= kTickets)
+        s.totals = c.totals, s.nsum = nsum, summed = true;
+      hipLaunchKernelGGL(p.slot == 4 ? xent_softmax_kernel<4> : xent_softmax_kernel<16>,
+                         dim3((uint32_t)blocks, (uint32_t)ny), dim3(256), 0, st, s);
       FG_TRY(hipGetLastError());
     }
     if (!c.grad) continue;
@@ -1136,7 +1198,7 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       JoinArgs &q = g.jdw;
       const bool split = p.s3.ns > 1;
       g.nsdw = p.s3.ns;
-      b.a = hc, b.a_ld = p.Hp, b.a_rows = (int32_t)p.Tc, b.a_cols = (int32_t)p.Hp;
+      b.a = hc, b.a_ld = p.Hp, b.a_rows = (int32_t)p.Tc, b.a_cols = (int32_t)p.wh;
       b.N = (int32_t)p.Vp;
       b.K = (int32_t)p.Tc, b.kper = p.s3.kper;
       b.out = split || !last ? nullptr : (uint16_t *)c.dw;

@@ -170,10 +170,23 @@ def test_weights_and_strides(dt, mean):
 def test_odd_strides_and_addresses(dt):
     """Rows that no 16-byte access fits: odd strides, addresses off by an element."""
     h, w, t, wt = inputs(70, 48, 90, dt, 6, h_ld=51, w_ld=53)
-    one = torch.cat([h.new_zeros(1), h.reshape(-1)])[1:].view(70, 48)
-    assert one.data_ptr() % 16
-    out = call(one, w, t, wt, dh_ld=49, dw_ld=51)
-    check(out, one, w, t, wt, dt)
+    one = lambda x: torch.cat([x.new_zeros(1), x.reshape(-1)])[1:].view(x.shape)
+    h, w1 = one(h), one(w)
+    assert h.data_ptr() % 16 == w1.data_ptr() % 16 == 2
+    out = call(h, w, t, wt, dh_ld=49, dw_ld=51)
+    check(out, h, w, t, wt, dt)
+    check(call(h, w1, t, wt), h, w1, t, wt, dt)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("hidden", [7, 8, 9, 12, 15, 31, 65, 66, 127, 131])
+def test_any_width(dt, hidden):
+    """Widths around a chunk of 8 and a stage of 64, rows followed by NaN."""
+    for t, v, ld in ((40, 300, 0), (150, 50, hidden + 3)):
+        print(dt, hidden, t, v, ld, flush=True)
+        x = inputs(t, hidden, v, dt, hidden, h_ld=ld, w_ld=ld)
+        x[1][v // 2:, 0] = 4.0      # a neighbour's first element is not to be taken in
+        check(call(*x, scale=64.0, dw_ld=ld), *x, dt, scale=64.0)
 
 
 @pytest.mark.parametrize("share", [0.0, 0.97, 1.0])
