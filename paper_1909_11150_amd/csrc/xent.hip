@@ -24,6 +24,10 @@
 //            there are few tiles, and joined in a fixed order.
 // The gradients thus take three products of rows x hidden x classes; without the
 // numerators they would take four.
+//
+// Up to 256 classes (pixels' classes) one tile holds them all: a single kernel goes
+// from the features to losses and G, and rows stay where they are, masked ones being
+// left out by the DMA (an offset out of range reads zeros).
 #include <algorithm>
 
 #include "dma_pipe.h"
@@ -56,6 +60,9 @@ struct LogitTiles {
 struct ProdTiles {
   using T256 = Pipe<FG_P2>;
 };
+// Up to 64 classes: 64 x 256, 4 waves of 64 x 64, twice per CU: the features' stream
+// bounds it, and a workgroup reads the weights once for 256 rows.
+using PClass = Pipe<64, 2, 1, 4, 64, 256>;
 
 // What the first kernels find out, read by the others.
 struct Found {
@@ -82,6 +89,7 @@ struct RowArgs {
   Found *found;
   int32_t *idx, *ctarget;
   float *cweight;
+  uint64_t *mark;        // a bit per row: live (up to 256 classes)
   uint16_t *hc;
   float *loss, *lse;
   uint16_t *dh;          // null: no gradients of the features
@@ -107,7 +115,20 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
-// Live rows, their weights' sum and largest magnitude, per block of 1024 rows.
+// The totals, by one thread.
+__device__ __forceinline__ void put_found(const RowArgs &a, int live, double sum, float mx) {
+  // no live row, or weights that cancel: a mean of nothing has no gradient
+  const double den = a.mean ? sum : 1.0;
+  const float top = mx > 0.f ? mx : 1.f;
+  a.found->live = live;
+  a.found->wsum = (float)sum;
+  a.found->ticket = 0;
+  a.found->wmax_inv = 1.f / top;
+  a.found->mult = den != 0.0 ? (float)(a.scale / den * top / kUp) : 0.f;
+}
+
+// Live rows, their weights' sum and largest magnitude, per block of 1024 rows; the
+// totals too where there is one block.
 __global__ __launch_bounds__(256) void xent_count_kernel(RowArgs a) {
   __shared__ double ws[4];
   __shared__ float wm[4];
@@ -118,7 +139,11 @@ __global__ __launch_bounds__(256) void xent_count_kernel(RowArgs a) {
 #pragma unroll
   for (int k = 0; k < kCount / 256; ++k) {
     float w;
-    if (live_row(a, blockIdx.x * kCount + k * 256 + threadIdx.x, w)) {
+    const int r = blockIdx.x * kCount + k * 256 + threadIdx.x;
+    const bool on = live_row(a, r, w);
+    const uint64_t mark = __ballot(on);
+    if (a.mark && (threadIdx.x & 63) == 0 && r < a.T) a.mark[r >> 6] = mark;
+    if (on) {
       ++n;
       sum += w;
       mx = fmaxf(mx, fabsf(w));
@@ -133,22 +158,14 @@ __global__ __launch_bounds__(256) void xent_count_kernel(RowArgs a) {
   }
   __syncthreads();
   if (threadIdx.x == 0) {
-    a.count[blockIdx.x] = cn[0] + cn[1] + cn[2] + cn[3];
-    a.wsum[blockIdx.x] = (ws[0] + ws[1]) + (ws[2] + ws[3]);
-    a.wmax[blockIdx.x] = fmaxf(fmaxf(wm[0], wm[1]), fmaxf(wm[2], wm[3]));
+    n = cn[0] + cn[1] + cn[2] + cn[3];
+    sum = (ws[0] + ws[1]) + (ws[2] + ws[3]);
+    mx = fmaxf(fmaxf(wm[0], wm[1]), fmaxf(wm[2], wm[3]));
+    a.count[blockIdx.x] = n;
+    a.wsum[blockIdx.x] = sum;
+    a.wmax[blockIdx.x] = mx;
+    if (gridDim.x == 1) put_found(a, n, sum, mx);
   }
-}
-
-// The totals, by one thread.
-__device__ __forceinline__ void put_found(const RowArgs &a, int live, double sum, float mx) {
-  // no live row, or weights that cancel: a mean of nothing has no gradient
-  const double den = a.mean ? sum : 1.0;
-  const float top = mx > 0.f ? mx : 1.f;
-  a.found->live = live;
-  a.found->wsum = (float)sum;
-  a.found->ticket = 0;
-  a.found->wmax_inv = 1.f / top;
-  a.found->mult = den != 0.0 ? (float)(a.scale / den * top / kUp) : 0.f;
 }
 
 // One workgroup: counts become the live rows before each block; the totals.
@@ -392,6 +409,68 @@ __device__ __forceinline__ int piece_rows(const Found *f, int row0, int Tc) {
   return min(max(f->live - row0, 0), Tc);
 }
 
+// Classes past the last one, of a wave's classes from v0 on: logit -inf.
+template <class P>
+__device__ __forceinline__ void no_class(f32x16 (&acc)[P::FM][P::FN], int v0, int V, int lane) {
+#pragma unroll
+  for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+      if (v0 + 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3) >= V)
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j) acc[i][j][v] = -INFINITY;
+}
+
+// A tile of logits: oa, ob: this lane's first chunks in the weights' and the
+// features' buffers.
+template <class P>
+__device__ __forceinline__ void logit_sums(f32x16 (&acc)[P::FM][P::FN], const Ring &R,
+                                           __amdgpu_buffer_rsrc_t rs_w,
+                                           __amdgpu_buffer_rsrc_t rs_h,
+                                           const unsigned (&oa)[P::PA],
+                                           const unsigned (&ob)[P::PB], const KmSlot<P::PA> &as,
+                                           const KmSlot<P::PB> &bs, int wh, int wave, int wm0,
+                                           int wn0, int lane) {
+  constexpr int PA = P::PA, PB = P::PB, BK = P::BK;
+  const int nst = (wh + BK - 1) / BK;
+  auto issue = [&](int st, int slot) __attribute__((always_inline)) {
+    uint8_t *ta = R.a[slot], *tb = R.b[slot];
+    const int k0 = st * BK;
+    if (k0 + BK <= wh) {
+#pragma unroll
+      for (int jj = 0; jj < PB; ++jj) dma16(rs_h, tb + dma_dst<PB>(wave, jj), ob[jj] + 2u * k0);
+#pragma unroll
+      for (int jj = 0; jj < PA; ++jj) dma16(rs_w, ta + dma_dst<PA>(wave, jj), oa[jj] + 2u * k0);
+    } else {  // chunks past the end: zeros
+      auto tail = [&](unsigned o, int coff) __attribute__((always_inline)) {
+        return k0 + coff < wh ? o + 2u * (chunk_at(k0 + coff, wh) - coff) : kOOB;
+      };
+#pragma unroll
+      for (int jj = 0; jj < PB; ++jj)
+        dma16(rs_h, tb + dma_dst<PB>(wave, jj), tail(ob[jj], bs.coff[jj]));
+#pragma unroll
+      for (int jj = 0; jj < PA; ++jj)
+        dma16(rs_w, ta + dma_dst<PA>(wave, jj), tail(oa[jj], as.coff[jj]));
+    }
+  };
+  // the last chunk's repeated elements: zeros in both operands, whatever they are
+  auto fix = [&](Frags<P> &f, int it, int ks) __attribute__((always_inline)) {
+    if (it + 1 < nst || wh % 8 == 0) return;
+    const int over = it * BK + 16 * ks + 8 * (lane >> 5) + 8 - wh;  // 1 .. 7: that chunk
+    const int cut = over < 8 ? over : 0;
+    u32x4 m;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+      m[d] = (2 * d < cut ? 0u : 0xFFFFu) | (2 * d + 1 < cut ? 0u : 0xFFFF0000u);
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i) f.a[i] &= m;
+#pragma unroll
+    for (int j = 0; j < P::FN; ++j) f.b[j] &= m;
+  };
+  zero<P>(acc);
+  pipeline<P, true, true>(acc, R, nst, wm0, wn0, lane, issue, NoFold{}, fix);
+}
+
 template <class P, bool STORE>
 __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a, TileMap tm) {
   FG_DMA_RING(P, R);
@@ -416,55 +495,9 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
   for (int jj = 0; jj < PA; ++jj) oa[jj] = (unsigned)(as.row[jj] * (int)a.w_ld + as.coff[jj]) * 2u;
 #pragma unroll
   for (int jj = 0; jj < PB; ++jj) ob[jj] = (unsigned)(bs.row[jj] * a.Hp + bs.coff[jj]) * 2u;
-  const int nst = (a.wh + BK - 1) / BK;
-  auto issue = [&](int st, int slot) __attribute__((always_inline)) {
-    uint8_t *ta = R.a[slot], *tb = R.b[slot];
-    const int k0 = st * BK;
-    if (k0 + BK <= a.wh) {
-#pragma unroll
-      for (int jj = 0; jj < PB; ++jj) dma16(rs_h, tb + dma_dst<PB>(wave, jj), ob[jj] + 2u * k0);
-#pragma unroll
-      for (int jj = 0; jj < PA; ++jj) dma16(rs_w, ta + dma_dst<PA>(wave, jj), oa[jj] + 2u * k0);
-    } else {  // chunks past the end: zeros
-      auto tail = [&](unsigned o, int coff) __attribute__((always_inline)) {
-        return k0 + coff < a.wh ? o + 2u * (chunk_at(k0 + coff, a.wh) - coff) : kOOB;
-      };
-#pragma unroll
-      for (int jj = 0; jj < PB; ++jj)
-        dma16(rs_h, tb + dma_dst<PB>(wave, jj), tail(ob[jj], bs.coff[jj]));
-#pragma unroll
-      for (int jj = 0; jj < PA; ++jj)
-        dma16(rs_w, ta + dma_dst<PA>(wave, jj), tail(oa[jj], as.coff[jj]));
-    }
-  };
-  // the last chunk's repeated elements: zeros in both operands, whatever they are
-  auto fix = [&](Frags<P> &f, int it, int ks) __attribute__((always_inline)) {
-    if (it + 1 < nst || a.wh % 8 == 0) return;
-    const int over = it * BK + 16 * ks + 8 * (lane >> 5) + 8 - a.wh;  // 1 .. 7: that chunk
-    const int cut = over < 8 ? over : 0;
-    u32x4 m;
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-      m[d] = (2 * d < cut ? 0u : 0xFFFFu) | (2 * d + 1 < cut ? 0u : 0xFFFF0000u);
-#pragma unroll
-    for (int i = 0; i < P::FM; ++i) f.a[i] &= m;
-#pragma unroll
-    for (int j = 0; j < P::FN; ++j) f.b[j] &= m;
-  };
   f32x16 acc[P::FM][P::FN];
-  zero<P>(acc);
-  pipeline<P, true, true>(acc, R, nst, wm0, wn0, lane, issue, NoFold{}, fix);
-
-  // classes past the last one: logit -inf
-  if (m0 + P::TM > a.V) {
-#pragma unroll
-    for (int i = 0; i < P::FM; ++i)
-#pragma unroll
-      for (int v = 0; v < 16; ++v)
-        if (m0 + wm0 + 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3) >= a.V)
-#pragma unroll
-          for (int j = 0; j < P::FN; ++j) acc[i][j][v] = -INFINITY;
-  }
+  logit_sums<P>(acc, R, rs_w, rs_h, oa, ob, as, bs, a.wh, wave, wm0, wn0, lane);
+  if (m0 + P::TM > a.V) no_class<P>(acc, m0 + wm0, a.V, lane);
   __syncthreads();  // every wave is done reading the ring
   float *xm = reinterpret_cast<float *>(R.b[0]), *xs = xm + P::WGM * P::TN;
   static_assert(2 * P::WGM * P::TN * 4 <= P::B_BYTES, "exchange fits a stage");
@@ -540,6 +573,140 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
       sum += xs[k * P::TN + p];
     }
     if (n0 + p < rows) a.stats[(size_t)ty * a.Tc + n0 + p] = float2{-scale_of(m), sum};
+  }
+}
+
+// ---- few classes -------------------------------------------------------------------
+struct ClassArgs {
+  const uint16_t *w, *h;
+  int64_t w_ld, h_ld;
+  int32_t wh, V, T;
+  const Found *found;
+  const uint64_t *mark;
+  const int32_t *target;
+  const float *weight;
+  uint16_t *e;       // [T][Vp] 2^15 G, or null: losses only
+  int32_t Vp;
+  float *loss, *lse;
+  double *lsum;      // per tile of rows
+};
+
+// All classes in one tile: losses and G of TN rows.
+template <class P>
+__global__ __launch_bounds__(P::NT, P::WPE) void xent_classes_kernel(ClassArgs a) {
+  FG_DMA_RING(P, R);
+  constexpr int PA = P::PA, PB = P::PB, BK = P::BK, TN = P::TN;
+  const int n0 = blockIdx.x * TN;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / P::WGN, wm0 = wm * P::WM, wn0 = (wave % P::WGN) * P::WN;
+  const int hrows = min(TN, a.T - n0);
+  const __amdgpu_buffer_rsrc_t rs_w = rsrc(a.w, (uint32_t)((a.V - 1) * a.w_ld + a.wh) * 2u);
+  const __amdgpu_buffer_rsrc_t rs_h =
+      rsrc(a.h + n0 * a.h_ld, (uint32_t)((hrows - 1) * a.h_ld + a.wh) * 2u);
+  auto live = [&](int n) __attribute__((always_inline)) {
+    return n < a.T && (a.mark[n >> 6] >> (n & 63) & 1);
+  };
+  const KmSlot<PA> as = km_slots<BK, PA>(wave, lane);
+  const KmSlot<PB> bs = km_slots<BK, PB>(wave, lane);
+  unsigned oa[PA], ob[PB];
+#pragma unroll
+  for (int jj = 0; jj < PA; ++jj) oa[jj] = (unsigned)(as.row[jj] * (int)a.w_ld + as.coff[jj]) * 2u;
+#pragma unroll
+  for (int jj = 0; jj < PB; ++jj)  // masked rows: zeros
+    ob[jj] = live(n0 + bs.row[jj]) ? (unsigned)(bs.row[jj] * (int)a.h_ld + bs.coff[jj]) * 2u : kOOB;
+  f32x16 acc[P::FM][P::FN];
+  logit_sums<P>(acc, R, rs_w, rs_h, oa, ob, as, bs, a.wh, wave, wm0, wn0, lane);
+  if (P::TM > a.V) no_class<P>(acc, wm0, a.V, lane);
+  __syncthreads();  // every wave is done reading the ring
+  float *xm = reinterpret_cast<float *>(R.b[0]), *xs = xm + P::WGM * TN, *xt = xs + P::WGM * TN;
+  double *part = reinterpret_cast<double *>(xt + TN);
+  static_assert((2 * P::WGM + 1) * TN * 4 + P::NW * 8 <= P::B_BYTES, "exchange fits a stage");
+  int tg[P::FN];
+  float w[P::FN], up[P::FN], s[P::FN];
+#pragma unroll
+  for (int j = 0; j < P::FN; ++j) {
+    const int p = wn0 + 32 * j + (lane & 31), n = n0 + p;
+    const bool on = live(n);
+    tg[j] = on ? a.target[n] : -1;
+    w[j] = !on ? 0.f : a.weight ? a.weight[n] : 1.f;
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        m = fmaxf(m, acc[i][j][v]);
+        if (tg[j] == wm0 + 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) xt[p] = acc[i][j][v];
+      }
+    m = fmaxf(m, __shfl_xor(m, 32));
+    if (lane < 32) xm[wm * TN + p] = m;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < P::FN; ++j) {
+    const int p = wn0 + 32 * j + (lane & 31);
+    float m = xm[p];
+#pragma unroll
+    for (int k = 1; k < P::WGM; ++k) m = fmaxf(m, xm[k * TN + p]);
+    up[j] = scale_of(m);
+    s[j] = 0.f;
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        acc[i][j][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][v], kLog2e, up[j]));
+        s[j] += acc[i][j][v];
+      }
+    s[j] += __shfl_xor(s[j], 32);
+    if (lane < 32) xs[wm * TN + p] = s[j];
+  }
+  __syncthreads();
+  double sum = 0;
+  float f[P::FN], pt[P::FN];
+#pragma unroll
+  for (int j = 0; j < P::FN; ++j) {
+    const int p = wn0 + 32 * j + (lane & 31), n = n0 + p;
+    s[j] = xs[p];
+#pragma unroll
+    for (int k = 1; k < P::WGM; ++k) s[j] += xs[k * TN + p];
+    const bool on = tg[j] >= 0;
+    const float l2 = __log2f(s[j]) - up[j], d = on ? l2 * kLn2 - xt[p] : 0.f;
+    const float c = kUp * w[j] * a.found->wmax_inv;
+    f[j] = c / s[j];
+    pt[j] = c * expm1f(-d);  // 2^15 w (p - 1)
+    if (wm == 0 && lane < 32 && n < a.T) {
+      const float loss = on ? w[j] * d : 0.f;
+      a.loss[n] = loss;
+      if (a.lse) a.lse[n] = on ? l2 * kLn2 : 0.f;
+      sum += loss;
+    }
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) part[wave] = sum;
+  if (a.e) {
+    store16<P>(
+        wave_buf<P>(R, wave), lane,
+        [&](int i, int j, int g) __attribute__((always_inline)) {
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int v = wm0 + 32 * i + 8 * g + 4 * (lane >> 5) + e;
+            x[e] = acc[i][j][4 * g + e] * f[j];
+            if (v == tg[j]) x[e] = pt[j];
+            if (v >= a.V || tg[j] < 0) x[e] = 0.f;
+          }
+          return u32x2{pack2(x[0], x[1], P::BF), pack2(x[2], x[3], P::BF)};
+        },
+        [&](int r, int c, const u32x4 &d) __attribute__((always_inline)) {
+          const int n = n0 + wn0 + r, v = wm0 + c;
+          if (n < a.T && v < a.Vp) *reinterpret_cast<u32x4 *>(a.e + (size_t)n * a.Vp + v) = d;
+        });
+  }
+  __syncthreads();
+  if (tid == 0) {
+    double t = 0;
+    for (int k = 0; k < P::NW; ++k) t += part[k];
+    a.lsum[blockIdx.x] = t;
   }
 }
 
@@ -708,16 +875,19 @@ struct ProdArgs {
   int64_t pstride;           // elements of a part
   int32_t Mq, add;           // add: the sum is added to part's
   int32_t *flag;
+  const uint64_t *mark;      // rows in place: a bit per live one
 };
 
-template <class P, bool DH>
+// PLACE: rows in place (up to 256 classes); marks: LDS for a part's marks.
+constexpr int kMarks = 512;  // words of 64 rows
+template <class P, bool DH, bool PLACE>
 __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &tm, int block,
-                                             const Ring &R) {
+                                             const Ring &R, uint64_t *marks) {
   constexpr int PA = P::PA, PB = P::PB, BK = P::BK;
   int tx, ty, split;  // hidden, rows (classes), part
   if (!tm.decode(block, tx, ty, split)) return;
   const int m0 = tx * P::TM, n0 = ty * P::TN;
-  const int rows = piece_rows(a.found, a.row0, a.Tc);
+  const int rows = PLACE ? a.Tc : piece_rows(a.found, a.row0, a.Tc);
   if (DH && n0 >= rows) return;
   const int kbeg = split * a.kper, kend = min(min(a.K, DH ? a.K : rows), kbeg + a.kper);
   const int nst = kend > kbeg ? (kend - kbeg + BK - 1) / BK : 0;
@@ -748,8 +918,15 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
   const uint16_t *pa = a.a + kbeg * a.a_ld;
   const uint16_t *pb = DH ? a.b + n0 * a.b_ld + kbeg : a.b + kbeg * a.b_ld + n0;
   int left = max(min(a.a_rows, kend) - kbeg, 0), bleft = kend - kbeg;
-  auto issue = [&](int, int slot) __attribute__((always_inline)) {
+  constexpr bool MASK = PLACE && !DH;  // features of masked rows: zeros
+  static_assert(!MASK || BK == 64, "a word of marks per stage");
+  if constexpr (MASK) {
+    for (int i = tid; i < nst; i += P::NT) marks[i] = a.mark[kbeg / 64 + i];
+    __syncthreads();
+  }
+  auto issue = [&](int st, int slot) __attribute__((always_inline)) {
     uint8_t *ta = R.a[slot], *tb = R.b[slot];
+    const uint64_t mark = MASK ? marks[st] : 0;
     const int ra = min(left, BK), rb = min(bleft, BK);
     const __amdgpu_buffer_rsrc_t rs_a =
         rsrc(pa, ra > 0 ? (uint32_t)((ra - 1) * (int)a.a_ld + a.a_cols) * 2u : 0u);
@@ -759,7 +936,9 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
 #pragma unroll
     for (int jj = 0; jj < PB; ++jj) dma16(rs_b, tb + dma_dst<PB>(wave, jj), ob[jj]);
 #pragma unroll
-    for (int jj = 0; jj < PA; ++jj) dma16(rs_a, ta + dma_dst<PA>(wave, jj), oa[jj]);
+    for (int jj = 0; jj < PA; ++jj)
+      dma16(rs_a, ta + dma_dst<PA>(wave, jj),
+            !MASK || (mark >> as.krow[jj] & 1) ? oa[jj] : kOOB);
     pa += BK * a.a_ld;
     pb += DH ? BK : BK * a.b_ld;
     left -= BK;
@@ -815,7 +994,9 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
           for (int e = 0; e < 8; ++e)
             bad |= (d[e >> 1] >> (16 * (e & 1)) & EX) == EX;
         }
-        put_chunk(a.out + (int64_t)(DH ? a.idx[n] : n) * a.out_ld, m, a.M, d);
+        const bool on = !DH || !PLACE || (a.mark[n >> 6] >> (n & 63) & 1);
+        put_chunk(a.out + (int64_t)(DH && !PLACE ? a.idx[n] : n) * a.out_ld, m, a.M,
+                  on ? d : u32x4{0, 0, 0, 0});
       });
   if (!DH && a.flag) flag_nonfinite(a.flag, bad);
 }
@@ -830,11 +1011,12 @@ struct SumArgs {
   const Found *found;
   float *totals;
 };
-template <class P>
+template <class P, bool PLACE>
 __global__ __launch_bounds__(P::NT, P::WPE) void xent_products_kernel(ProdArgs dh, TileMap th,
                                                                       ProdArgs dw, TileMap tw,
                                                                       int nh, SumArgs sum) {
   FG_DMA_RING(P, R);
+  __shared__ uint64_t marks[PLACE ? kMarks : 1];
   const int block = blockIdx.x;
   if (sum.n && block == 0 && threadIdx.x < 64) {
     double s = 0;
@@ -847,9 +1029,9 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_products_kernel(ProdArgs d
     }
   }
   if (block < nh)
-    product_tile<P, true>(dh, th, block, R);
+    product_tile<P, true, PLACE>(dh, th, block, R, marks);
   else
-    product_tile<P, false>(dw, tw, block - nh, R);
+    product_tile<P, false, PLACE>(dw, tw, block - nh, R, marks);
 }
 
 // Joins the parts of a split sum, in their order: 8 columns of a row per lane.
@@ -861,6 +1043,7 @@ struct JoinArgs {
   int32_t row0, Tc;
   const Found *found;
   const int32_t *idx;
+  const uint64_t *mark;         // rows in place (dh)
   uint16_t *out;
   int64_t out_ld;
   int32_t bf;
@@ -914,6 +1097,7 @@ __global__ __launch_bounds__(512) void xent_join_kernel(JoinArgs dh, JoinArgs dw
     const uint32_t ex = a.bf ? 0x7F80u : 0x7C00u;
 #pragma unroll
     for (int e = 0; e < 8; ++e) bad |= (d[e >> 1] >> (16 * (e & 1)) & ex) == ex;
+    if (a.mark && !(a.mark[n >> 6] >> (n & 63) & 1)) d = u32x4{0, 0, 0, 0};
     put_chunk(a.out + (a.idx ? a.idx[n] : n) * a.out_ld, m, a.M, d);
   }
   if (a.flag) flag_nonfinite(a.flag, bad);
@@ -927,17 +1111,21 @@ constexpr int64_t kPieceBytes = (int64_t)1 << 30;
 
 constexpr int kTileOf[3] = {64, 128, 256};
 
-// Tile and number of parts for a product of M x N sums of length K. Estimated time of
-// the tiles in rounds of the workgroups that the chip holds, from the rates that a
-// CU reached with 1 .. 3 of them, and of writing and joining the parts.
+// Tile and number of parts for a product of M x N sums of length K: the least of the
+// times estimated for rounds of the workgroups that the chip holds. A round costs a
+// fixed time (first loads, store) and one per unit of K, by the tile and the
+// workgroups on a CU; measured over 56 shapes (1 .. 4096 rows, 64 .. 4096 hidden, 2000
+// .. 32000 classes), in which the tile chosen is within 20% of the best of the three.
 struct Shape {
   int tile, ns, kper;  // tile: index into kTileOf
 };
 // The best number of parts for one tile, and its time.
 Shape pick_tile(int t, int64_t M, int64_t N, int64_t K, bool split, double &us_best) {
-  // TFLOP/s of a CU with 1, 2, 3 workgroups of a tile
-  static const double rate[3][3] = {{1.0, 1.6, 2.0}, {2.6, 3.6, 3.6}, {4.7, 4.7, 4.7}};
   static const int occ[3] = {3, 2, 1};
+  static const double fixed[3][3] = {{2.0, 2.0, 2.0}, {3.5, 5.5, 5.5}, {9.0, 9.0, 9.0}};
+  const double more = t == 2 && split ? 5.0 : 0.0;  // the products' store of a large tile
+  static const double per_k[3][3] = {{.0055, .009, .0135}, {.0095, .0178, .0178},
+                                     {.0175, .0175, .0175}};
   Shape best{t, 1, 0};
   us_best = 1e300;
   const int64_t ts = kTileOf[t];
@@ -948,11 +1136,14 @@ Shape pick_tile(int t, int64_t M, int64_t N, int64_t K, bool split, double &us_b
     const int64_t parts = std::max<int64_t>(1, (K + kper - 1) / kper);
     const int64_t n = tiles * parts, slots = 256 * occ[t];
     const int64_t full = n / slots, rest = n - full * slots;
-    const double work = 2e-6 * ts * ts * kper;  // us at 1 TFLOP/s
-    auto round = [&](int j) { return j * work / rate[t][j - 1] + 2.0; };
-    double us = full * round(occ[t]);
-    if (rest) us += round((int)((rest + 255) / 256));
-    if (parts > 1) us += 6.0 + (double)parts * M * N * 8 / 4e6;
+    // a chip full of the largest tiles is slower per tile than a few of them
+    auto round = [&](int64_t m) {
+      const int j = (int)((m + 255) / 256) - 1;
+      return fixed[t][j] + more + kper * (per_k[t][j] + (t == 2 ? .0105 * m / 256 : 0.));
+    };
+    double us = full * round(slots);
+    if (rest) us += round(rest);
+    if (parts > 1) us += 5.0 + (double)parts * M * N * 8 / 8e6;
     if (us < us_best) us_best = us, best = {t, (int)parts, (int)kper};
   }
   return best;
@@ -960,11 +1151,11 @@ Shape pick_tile(int t, int64_t M, int64_t N, int64_t K, bool split, double &us_b
 
 struct Plan {
   int64_t T, H, V, Tp, Hp, Vp, Hq, Tc, pieces, nb, wh, w_ld;
-  bool pad_w;
+  bool pad_w, place;
   Shape s1, s2, s3;
   int64_t ntile, slot;
   // workspace, bytes
-  size_t count, wsum, wmax, found, idx, ctarget, cweight, hc, wc, stats, tlogit, e, pdh, pdw,
+  size_t count, wsum, wmax, found, mark, idx, ctarget, cweight, hc, wc, stats, tlogit, e, pdh, pdw,
       lsum, total;
 };
 
@@ -984,6 +1175,8 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   p.pieces = std::max<int64_t>(1, (p.Tp + most - 1) / most);
   p.Tc = std::max<int64_t>(256, up((p.T + p.pieces - 1) / p.pieces, 256));
   p.pieces = std::max<int64_t>(1, (p.T + p.Tc - 1) / p.Tc);
+  p.place = p.V <= kTileOf[2];
+  if (p.place) p.pieces = 1, p.Tc = std::max<int64_t>(256, p.Tp);
   const int64_t rows = std::min(p.T, p.Tc);
   double best = 1e300, us, us2;
   for (int t = 0; t < 3; ++t) {
@@ -992,11 +1185,17 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   }
   p.ntile = (p.V + kTileOf[p.s1.tile] - 1) / kTileOf[p.s1.tile];
   best = 1e300;  // one launch, one tile for both products
-  for (int t = 0; t < 3; ++t) {
+  for (int t = 0; t < (p.place ? 2 : 3); ++t) {  // in place: tiles of 64-deep stages
     const Shape a = pick_tile(t, p.H, rows, p.Vp, true, us);
     const Shape b = pick_tile(t, p.H, p.V, rows, true, us2);
     if (us + us2 < best) best = us + us2, p.s2 = a, p.s3 = b;
   }
+  if (p.place && p.s3.kper > 64 * kMarks) {
+    p.s3.kper = 64 * kMarks;
+    p.s3.ns = (int)((rows + p.s3.kper - 1) / p.s3.kper);
+  }
+  // rows of a workgroup of the kernel that finds the losses
+  p.slot = !p.place ? (p.T <= kFew ? 4 : 16) : p.V <= 64 ? 256 : p.V <= 128 ? 128 : 256;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t was = at;
@@ -1007,15 +1206,16 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   p.count = take(p.nb * 4);
   p.wsum = take(p.nb * 8);
   p.wmax = take(p.nb * 4);
-  p.idx = take(p.Tp * 4);
-  p.ctarget = take(p.Tp * 4);
-  p.cweight = take(p.Tp * 4);
-  p.slot = p.T <= kFew ? 4 : 16;
+  const int64_t moved = p.place ? 0 : 1;
+  p.idx = take(moved * p.Tp * 4);
+  p.ctarget = take(moved * p.Tp * 4);
+  p.cweight = take(moved * p.Tp * 4);
   p.lsum = take(p.pieces * (p.Tc / p.slot) * 8);
+  p.mark = take(p.place ? p.Tp / 8 : 0);
   // the products read whole tiles of rows: a tile past the last piece's rows too
-  p.hc = take((size_t)p.pieces * p.Tc * p.Hp * 2);
-  p.stats = take((size_t)p.ntile * p.Tc * 8);
-  p.tlogit = take(p.Tc * 4);
+  p.hc = take(p.place ? (p.pad_w ? (size_t)p.Tp * 16 : 0) : (size_t)p.pieces * p.Tc * p.Hp * 2);
+  p.stats = take(moved * (size_t)p.ntile * p.Tc * 8);
+  p.tlogit = take(moved * p.Tc * 4);
   if (grad) {
     p.e = take((size_t)p.Tc * p.Vp * 2);
     p.pdh = take(p.s2.ns > 1 ? (size_t)p.s2.ns * p.Tc * p.Hq * 4 : 0);
@@ -1046,6 +1246,7 @@ struct Products {
   JoinArgs jdh, jdw;
   int nsdh, nsdw;     // parts; 0: that gradient is not wanted
   int64_t rows;
+  bool place;
   SumArgs sum;
 };
 
@@ -1053,8 +1254,23 @@ template <class P>
 hipError_t launch_products(const Products &a, hipStream_t st) {
   const TileMap th = tile_map((a.dh.M + P::TM - 1) / P::TM, (a.rows + P::TN - 1) / P::TN, a.nsdh);
   const TileMap tw = tile_map((a.dw.M + P::TM - 1) / P::TM, (a.dw.V + P::TN - 1) / P::TN, a.nsdw);
-  hipLaunchKernelGGL((xent_products_kernel<P>), dim3(8 * (th.per + tw.per)), dim3(P::NT), 0, st,
-                     a.dh, th, a.dw, tw, 8 * th.per, a.sum);
+  const dim3 grid(8 * (th.per + tw.per)), block(P::NT);
+  if constexpr (P::BK == 64) {
+    if (a.place) {
+      hipLaunchKernelGGL((xent_products_kernel<P, true>), grid, block, 0, st, a.dh, th, a.dw, tw,
+                         8 * th.per, a.sum);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((xent_products_kernel<P, false>), grid, block, 0, st, a.dh, th, a.dw, tw,
+                     8 * th.per, a.sum);
+  return hipGetLastError();
+}
+
+template <class P>
+hipError_t launch_classes(const ClassArgs &a, hipStream_t st) {
+  hipLaunchKernelGGL(xent_classes_kernel<P>, dim3((uint32_t)((a.T + P::TN - 1) / P::TN)),
+                     dim3(P::NT), 0, st, a);
   return hipGetLastError();
 }
 
@@ -1113,7 +1329,15 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
   r.cweight = (float *)at(p.cweight);
   r.hc = (uint16_t *)at(p.hc);
   r.loss = c.loss, r.lse = c.lse;
-  if (p.T <= kDirect) {
+  r.mark = p.place ? (uint64_t *)at(p.mark) : nullptr;
+  if (p.place && p.T) {
+    hipLaunchKernelGGL(xent_count_kernel, dim3((uint32_t)p.nb), dim3(256), 0, st, r);
+    FG_TRY(hipGetLastError());
+    if (p.nb > 1) {
+      hipLaunchKernelGGL(xent_scan_kernel, dim3(1), dim3(1024), 0, st, r);
+      FG_TRY(hipGetLastError());
+    }
+  } else if (p.T <= kDirect) {
     r.nb = 0;  // a row per wave: a few rows are bound by one row's latency
     hipLaunchKernelGGL(xent_rows_kernel<1>, dim3((uint32_t)((p.T + 3) / 4 + 1)), dim3(256), 0, st,
                        r);
@@ -1133,13 +1357,33 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
     FG_TRY(hipGetLastError());
     w = (const uint16_t *)at(p.wc);
   }
+  const uint16_t *h = (const uint16_t *)c.h;  // rows in place
+  int64_t h_ld = r.h_ld;
+  if (p.place && p.pad_w && p.T) {
+    hipLaunchKernelGGL(xent_pad_kernel, dim3((uint32_t)((p.T + 255) / 256)), dim3(256), 0, st, h,
+                       h_ld, (int32_t)p.H, (uint16_t *)at(p.hc), (int32_t)p.T);
+    FG_TRY(hipGetLastError());
+    h = (const uint16_t *)at(p.hc);
+    h_ld = 8;
+  }
   const int32_t nsum = (int32_t)((p.T + p.slot - 1) / p.slot);
   bool summed = false;
   for (int64_t i = 0; i < p.pieces; ++i) {
     const int64_t row0 = i * p.Tc, rows = std::min(p.Tc, p.T - row0);
     const uint16_t *hc = r.hc + (size_t)row0 * p.Hp;
     double *lsum = (double *)at(p.lsum) + i * (p.Tc / p.slot);
-    if (rows > 0) {
+    if (p.place && rows > 0) {
+      ClassArgs l{};
+      l.w = w, l.h = h, l.w_ld = p.w_ld, l.h_ld = h_ld;
+      l.wh = (int32_t)p.wh, l.V = (int32_t)p.V, l.T = (int32_t)p.T;
+      l.found = r.found, l.mark = r.mark, l.target = c.target, l.weight = c.weight;
+      l.e = c.grad ? (uint16_t *)at(p.e) : nullptr, l.Vp = (int32_t)p.Vp;
+      l.loss = c.loss, l.lse = c.lse, l.lsum = lsum;
+      FG_TRY(p.V <= 64    ? (bf ? launch_classes<Bf16<PClass>>(l, st) : launch_classes<PClass>(l, st))
+             : p.V <= 128 ? (bf ? launch_classes<Bf16<P128>>(l, st) : launch_classes<P128>(l, st))
+                          : (bf ? launch_classes<Bf16<LogitTiles::T256>>(l, st)
+                                : launch_classes<LogitTiles::T256>(l, st)));
+    } else if (rows > 0) {
       LogitArgs l{};
       l.w = w, l.w_ld = p.w_ld, l.wh = (int32_t)p.wh, l.V = (int32_t)p.V;
       l.hc = hc, l.Hp = (int32_t)p.Hp;
@@ -1172,11 +1416,13 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
     const bool last = i + 1 == p.pieces;
     Products g{};
     g.rows = rows;
+    g.place = p.place;
     ProdArgs &a = g.dh;
     a.b = (const uint16_t *)at(p.e), a.b_ld = p.Vp;
     a.M = (int32_t)p.H, a.Mq = (int32_t)p.Hq;
-    a.row0 = (int32_t)row0, a.Tc = (int32_t)p.Tc, a.found = r.found;
+    a.row0 = (int32_t)row0, a.Tc = (int32_t)(p.place ? p.T : p.Tc), a.found = r.found;
     a.V = (int32_t)p.V;
+    a.mark = r.mark;
     JoinArgs &j = g.jdh;
     j.M = a.M, j.Mq = a.Mq, j.row0 = a.row0, j.Tc = a.Tc, j.found = r.found, j.bf = bf;
     g.dw = a, g.jdw = j;
@@ -1189,8 +1435,9 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       a.idx = r.idx + row0;
       a.out = split ? nullptr : (uint16_t *)c.dh, a.out_ld = r.dh_ld;
       a.part = split ? (float *)at(p.pdh) : nullptr, a.pstride = p.Tc * p.Hq;
-      j.part = a.part, j.pstride = a.pstride, j.nsplit = p.s2.ns, j.rows = -1;
-      j.idx = a.idx, j.out = (uint16_t *)c.dh, j.out_ld = a.out_ld;
+      j.part = a.part, j.pstride = a.pstride, j.nsplit = p.s2.ns;
+      j.rows = p.place ? (int32_t)p.T : -1;
+      j.idx = p.place ? nullptr : a.idx, j.mark = r.mark, j.out = (uint16_t *)c.dh, j.out_ld = a.out_ld;
       join_dh = split;
     }
     if (c.dw) {
@@ -1198,7 +1445,8 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       JoinArgs &q = g.jdw;
       const bool split = p.s3.ns > 1;
       g.nsdw = p.s3.ns;
-      b.a = hc, b.a_ld = p.Hp, b.a_rows = (int32_t)p.Tc, b.a_cols = (int32_t)p.wh;
+      b.a = p.place ? h : hc, b.a_ld = p.place ? h_ld : p.Hp;
+      b.a_rows = (int32_t)(p.place ? p.T : p.Tc), b.a_cols = (int32_t)p.wh;
       b.N = (int32_t)p.Vp;
       b.K = (int32_t)p.Tc, b.kper = p.s3.kper;
       b.out = split || !last ? nullptr : (uint16_t *)c.dw;
