@@ -412,24 +412,25 @@ def channel_slice_copy(src, src_ld, dst, dst_ld, npix, nch, gate=None, gate_ld=0
 
 
 # ---- classification head ----------------------------------------------------
-# A small call's time is the host's: checks look at each tensor once.
+# A small call's time is the host's: tensors that are just what is asked for pass one
+# look at type, shape and strides.
 _codes = {}      # torch element type -> code, filled on first use (torch may be absent)
-
-
-def _code(t):
-    if not _codes:
-        import torch
-        _codes.update({torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32,
-                       torch.int32: _I32})
-    return _codes.get(t.dtype)
-
-
+_types = {}      # and back
 _I32 = 100       # not a code of the library's
+
+
+def _known():
+    import torch
+    _codes.update({torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32,
+                   torch.int32: _I32})
+    _types.update({c: t for t, c in _codes.items()})
 
 
 def dtype_of(t):
     """Element type code (F16, BF16, F32) of a tensor."""
-    c = _code(t)
+    if not _codes:
+        _known()
+    c = _codes.get(t.dtype)
     if c is None or c == _I32:
         raise ValueError(f"element type {t.dtype} is not supported")
     return c
@@ -440,13 +441,12 @@ def _matrix(name, t, rows, cols, ld, dtype):
     shape (its last axis unit-strided, the others one stride) and row stride ld."""
     if t is None:
         return None
-    if _code(t) != dtype:
-        raise ValueError(f"{name}: element type {t.dtype} where the descriptor says another")
+    if not _types:
+        _known()
     shape, stride, ld = t.shape, t.stride(), ld or cols
-    if len(shape) == 2 and shape[0] == rows and shape[1] == cols:
-        if (cols > 1 and stride[1] != 1) or (rows > 1 and stride[0] != ld):
-            raise ValueError(f"{name}: strides {stride} where rows {ld} elements apart "
-                             "are needed")
+    if t.dtype is not _types.get(dtype):
+        raise ValueError(f"{name}: element type {t.dtype} where the descriptor says another")
+    if shape == (rows, cols) and stride == (ld, 1):
         return t.data_ptr()
     if t.numel() != rows * cols or (rows and (not shape or shape[-1] != cols)):
         raise ValueError(f"{name}: shape {tuple(shape)} where {rows} x {cols} is needed")
@@ -462,7 +462,10 @@ def _matrix(name, t, rows, cols, ld, dtype):
 def _vector(name, t, n, dtype):
     if t is None:
         return None
-    if _code(t) != dtype or t.numel() != n or not t.is_contiguous():
+    if not _types:
+        _known()
+    if t.dtype is not _types[dtype] or (t.shape != (n,) and t.numel() != n) or \
+            not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous "
                          f"{'int32' if dtype == _I32 else 'float32'} tensor of {n} elements")
     return t.data_ptr()
@@ -471,7 +474,9 @@ def _vector(name, t, n, dtype):
 def _counter(name, t):
     if t is None:
         return None
-    if _code(t) != _I32 or t.numel() < 1 or not t.is_contiguous():
+    if not _types:
+        _known()
+    if t.dtype is not _types[_I32] or t.numel() < 1 or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor")
     return t.data_ptr()
 

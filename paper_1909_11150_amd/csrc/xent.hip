@@ -115,16 +115,34 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
-// The totals, by one thread.
-__device__ __forceinline__ void put_found(const RowArgs &a, int live, double sum, float mx) {
+__device__ __forceinline__ Found make_found(int mean, double scale, int live, double sum,
+                                            float mx) {
   // no live row, or weights that cancel: a mean of nothing has no gradient
-  const double den = a.mean ? sum : 1.0;
+  const double den = mean ? sum : 1.0;
   const float top = mx > 0.f ? mx : 1.f;
-  a.found->live = live;
-  a.found->wsum = (float)sum;
-  a.found->ticket = 0;
-  a.found->wmax_inv = 1.f / top;
-  a.found->mult = den != 0.0 ? (float)(a.scale / den * top / kUp) : 0.f;
+  return {live, 1.f / top, den != 0.0 ? (float)(scale / den * top / kUp) : 0.f, (float)sum, 0};
+}
+__device__ __forceinline__ void put_found(const RowArgs &a, int live, double sum, float mx) {
+  *a.found = make_found(a.mean, a.scale, live, sum, mx);
+}
+
+// Up to 64 rows: they stay in place, and every kernel finds out by itself, a row per
+// lane, what the kernels above find for more.
+struct Tiny {
+  const int32_t *target;
+  const float *weight;
+  int32_t T, V, mean;  // T = 0: more rows
+  double scale;
+};
+__device__ __forceinline__ Found tiny_found(const Tiny &t, uint64_t &mark) {
+  const int r = threadIdx.x & 63;
+  float w = 1.f;
+  bool on = r < t.T && (uint32_t)t.target[r] < (uint32_t)t.V;
+  if (on && t.weight) w = t.weight[r];
+  on = on && w != 0.f;
+  mark = __ballot(on);
+  return make_found(t.mean, t.scale, __popcll(mark), wave_sum(on ? (double)w : 0.0),
+                    wave_max(on ? fabsf(w) : 0.f));
 }
 
 // Live rows, their weights' sum and largest magnitude, per block of 1024 rows; the
@@ -389,8 +407,9 @@ struct LogitArgs {
   int32_t wh;             // elements of a row (of w and of hc), at least 8
   int32_t V;
   const uint16_t *hc;     // the piece's first row
-  int32_t Hp;
-  const Found *found;
+  int32_t Hp;             // its stride
+  Found *found;
+  int32_t tiny;           // rows in place, all Tc of them
   int32_t row0, Tc;       // first live row of the piece, rows it may have
   const int32_t *ctarget;
   uint16_t *e;            // [Tc][Vp] numerators, fp16 (STORE)
@@ -481,8 +500,9 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
   int tx, ty, tz;  // rows, classes
   if (!tm.decode(blockIdx.x, tx, ty, tz)) return;
   const int n0 = tx * P::TN, m0 = ty * P::TM;
-  const int rows = piece_rows(a.found, a.row0, a.Tc);
+  const int rows = a.tiny ? a.Tc : piece_rows(a.found, a.row0, a.Tc);
   if (n0 >= rows) return;
+  if (a.tiny && blockIdx.x == 0 && threadIdx.x == 0) a.found->ticket = 0;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / P::WGN, wm0 = wm * P::WM, wn0 = (wave % P::WGN) * P::WN;
@@ -490,7 +510,10 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
   const int wrows = min(P::TM, a.V - m0);
   const __amdgpu_buffer_rsrc_t rs_w =
       rsrc(a.w + m0 * a.w_ld, (uint32_t)((wrows - 1) * a.w_ld + a.wh) * 2u);
-  const __amdgpu_buffer_rsrc_t rs_h = rsrc(a.hc + (size_t)n0 * a.Hp, (uint32_t)P::TN * a.Hp * 2u);
+  // (in place: to the last row's end; masked rows' logits are numbers no one reads)
+  const int hrows = a.tiny ? min(P::TN, rows - n0) : P::TN;
+  const __amdgpu_buffer_rsrc_t rs_h =
+      rsrc(a.hc + (size_t)n0 * a.Hp, (uint32_t)((hrows - 1) * a.Hp + a.wh) * 2u);
   const KmSlot<PA> as = km_slots<BK, PA>(wave, lane);
   const KmSlot<PB> bs = km_slots<BK, PB>(wave, lane);
   unsigned oa[PA], ob[PB];
@@ -515,7 +538,7 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
     if (lane < 32) xm[wm * P::TN + wn0 + 32 * j + lane] = m;
     // the target's logit, where it is one of this wave's classes
     const int n = n0 + wn0 + 32 * j + (lane & 31);
-    const int t = n < rows ? a.ctarget[n] - (m0 + wm0) : -1;
+    const int t = n < rows ? (int)((unsigned)a.ctarget[n] - (unsigned)(m0 + wm0)) : -1;
     if (__any(t >= 0 && t < P::WM)) {
 #pragma unroll
       for (int i = 0; i < P::FM; ++i)
@@ -728,6 +751,7 @@ struct SoftmaxArgs {
   double *lsum;                          // per RS rows
   float *totals;                         // null, or written by the last workgroup
   int32_t nsum;
+  Tiny tiny;                             // (then no idx, and ctarget is the target)
 };
 
 // RS rows' lse and losses from their tiles, then (gradients) a range of their
@@ -740,7 +764,9 @@ __global__ __launch_bounds__(256) void xent_softmax_kernel(SoftmaxArgs a) {
   __shared__ int tg[RS];
   __shared__ double part[RS], ws[4];
   __shared__ bool last;
-  const int rows = piece_rows(a.found, a.row0, a.Tc);
+  const int rows = a.tiny.T ? a.tiny.T : piece_rows(a.found, a.row0, a.Tc);
+  uint64_t mark = ~0ull;
+  const Found found = a.tiny.T ? tiny_found(a.tiny, mark) : *a.found;
   const int r0 = blockIdx.x * RS, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool first = blockIdx.y == 0;
   if (r0 < rows) {
@@ -772,13 +798,16 @@ __global__ __launch_bounds__(256) void xent_softmax_kernel(SoftmaxArgs a) {
       double d64 = 0;
       lse2[r] = l2;
       if (n < rows) {
-        const float w = a.cweight[n], d = l2 * kLn2 - a.tlogit[n];
-        tg[r] = a.ctarget[n];
-        wt[r] = kUp * w * a.found->wmax_inv;
+        const bool on = !a.tiny.T || (mark >> n & 1);
+        const float w = !on ? 0.f : a.cweight ? a.cweight[n] : 1.f;
+        const float d = on ? l2 * kLn2 - a.tlogit[n] : 0.f;
+        tg[r] = on ? a.ctarget[n] : -1;
+        wt[r] = kUp * w * found.wmax_inv;
         pt[r] = wt[r] * expm1f(-d);  // 2^15 w (p - 1)
         if (first) {
-          a.loss[a.idx[n]] = w * d;
-          if (a.lse) a.lse[a.idx[n]] = l2 * kLn2;
+          const int to = a.tiny.T ? n : a.idx[n];
+          a.loss[to] = w * d;
+          if (a.lse) a.lse[to] = on ? l2 * kLn2 : 0.f;
           d64 = w * d;
         }
       }
@@ -809,7 +838,7 @@ __global__ __launch_bounds__(256) void xent_softmax_kernel(SoftmaxArgs a) {
       __syncthreads();
       if (tid == 0) {
         a.totals[0] = (float)((ws[0] + ws[1]) + (ws[2] + ws[3]));
-        a.totals[1] = a.found->wsum;
+        a.totals[1] = found.wsum;
       }
     }
   }
@@ -831,7 +860,8 @@ __global__ __launch_bounds__(256) void xent_softmax_kernel(SoftmaxArgs a) {
       for (int e = 0; e < 8; ++e) {
         y[e] = h_to_f32((uint16_t)(x[e >> 1] >> (16 * (e & 1)))) * f;
         if (v + e == t) y[e] = p1;
-        if (v + e >= a.V) y[e] = 0.f;  // NaN rows keep the classes past the last at 0
+        // NaN rows keep the classes past the last at 0, masked ones every class
+        if (v + e >= a.V || t < 0) y[e] = 0.f;
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = pack2(y[2 * e], y[2 * e + 1], a.bf);
@@ -879,6 +909,7 @@ struct ProdArgs {
   int32_t Mq, add;           // add: the sum is added to part's
   int32_t *flag;
   const uint64_t *mark;      // rows in place: a bit per live one
+  Tiny tiny;                 // (without mark)
 };
 
 // PLACE: rows in place (up to 256 classes); marks: LDS for a part's marks.
@@ -897,6 +928,9 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm0 = (wave / P::WGN) * P::WM, wn0 = (wave % P::WGN) * P::WN;
+  uint64_t few = 0;  // the marks of a tiny call
+  float mult = 0.f;
+  if (PLACE && a.tiny.T) mult = tiny_found(a.tiny, few).mult;
 
   const MnSlot<PA> as = mn_slots<P::RBA, PA>(wave, lane);
   unsigned oa[PA], ob[PB];
@@ -924,7 +958,7 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
   constexpr bool MASK = PLACE && !DH;  // features of masked rows: zeros
   static_assert(!MASK || BK == 64, "a word of marks per stage");
   if constexpr (MASK) {
-    for (int i = tid; i < nst; i += P::NT) marks[i] = a.mark[kbeg / 64 + i];
+    for (int i = tid; i < nst; i += P::NT) marks[i] = a.mark ? a.mark[kbeg / 64 + i] : few;
     __syncthreads();
   }
   auto issue = [&](int st, int slot) __attribute__((always_inline)) {
@@ -979,7 +1013,7 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
     if (!a.out) return;
   }
   __syncthreads();  // every wave is done reading the ring
-  const float mult = a.found->mult;
+  if (!PLACE || !a.tiny.T) mult = a.found->mult;
   bool bad = false;
   store16<P>(
       wave_buf<P>(R, wave), lane,
@@ -997,7 +1031,7 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
           for (int e = 0; e < 8; ++e)
             bad |= (d[e >> 1] >> (16 * (e & 1)) & EX) == EX;
         }
-        const bool on = !DH || !PLACE || (a.mark[n >> 6] >> (n & 63) & 1);
+        const bool on = !DH || !PLACE || ((a.mark ? a.mark[n >> 6] : few) >> (n & 63) & 1);
         put_chunk(a.out + (int64_t)(DH && !PLACE ? a.idx[n] : n) * a.out_ld, m, a.M,
                   on ? d : u32x4{0, 0, 0, 0});
       });
@@ -1013,6 +1047,7 @@ struct SumArgs {
   int32_t n;         // partial sums; 0: not here
   const Found *found;
   float *totals;
+  Tiny tiny;
 };
 template <class P, bool PLACE>
 __global__ __launch_bounds__(P::NT, P::WPE) void xent_products_kernel(ProdArgs dh, TileMap th,
@@ -1026,9 +1061,11 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_products_kernel(ProdArgs d
 #pragma unroll 4
     for (int i = threadIdx.x; i < sum.n; i += 64) s += sum.lsum[i];
     s = wave_sum(s);
+    uint64_t mark;
+    const float w = sum.tiny.T ? tiny_found(sum.tiny, mark).wsum : sum.found->wsum;
     if (threadIdx.x == 0) {
       sum.totals[0] = (float)s;
-      sum.totals[1] = sum.found->wsum;
+      sum.totals[1] = w;
     }
   }
   if (block < nh)
@@ -1047,6 +1084,8 @@ struct JoinArgs {
   const Found *found;
   const int32_t *idx;
   const uint64_t *mark;         // rows in place (dh)
+  Tiny tiny;                    // (without mark)
+  int32_t masked;               // dh: masked rows are zeros
   uint16_t *out;
   int64_t out_ld;
   int32_t bf;
@@ -1062,6 +1101,8 @@ __global__ __launch_bounds__(512) void xent_join_kernel(JoinArgs dh, JoinArgs dw
   const int block = first ? blockIdx.x : blockIdx.x - nh;
   const int rows = a.rows < 0 ? piece_rows(a.found, a.row0, a.Tc) : a.rows;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint64_t few = ~0ull;
+  const float mult = a.tiny.T ? tiny_found(a.tiny, few).mult : a.found->mult;
   const bool shared = a.shared;
   const int64_t i = shared ? (int64_t)block * 64 + lane : (int64_t)block * 512 + threadIdx.x;
   const int c8 = a.Mq / 8;
@@ -1093,14 +1134,13 @@ __global__ __launch_bounds__(512) void xent_join_kernel(JoinArgs dh, JoinArgs dw
       for (int e = 0; e < 8; ++e) v[e] += sh[k][lane][e];
   }
   if (n < rows) {
-    const float mult = a.found->mult;
     u32x4 d;
 #pragma unroll
     for (int e = 0; e < 4; ++e) d[e] = pack2(v[2 * e] * mult, v[2 * e + 1] * mult, a.bf);
     const uint32_t ex = a.bf ? 0x7F80u : 0x7C00u;
 #pragma unroll
     for (int e = 0; e < 8; ++e) bad |= (d[e >> 1] >> (16 * (e & 1)) & ex) == ex;
-    if (a.mark && !(a.mark[n >> 6] >> (n & 63) & 1)) d = u32x4{0, 0, 0, 0};
+    if (a.masked && !((a.mark ? a.mark[n >> 6] : few) >> (n & 63) & 1)) d = u32x4{0, 0, 0, 0};
     put_chunk(a.out + (a.idx ? a.idx[n] : n) * a.out_ld, m, a.M, d);
   }
   if (a.flag) flag_nonfinite(a.flag, bad);
@@ -1146,7 +1186,7 @@ Shape pick_tile(int t, int64_t M, int64_t N, int64_t K, bool split, double &us_b
     };
     double us = full * round(slots);
     if (rest) us += round(rest);
-    if (parts > 1) us += 5.0 + (double)parts * M * N * 8 / 8e6;
+    if (parts > 1) us += 6.0 + (double)parts * M * N * 8 / 8e6;
     if (us < us_best) us_best = us, best = {t, (int)parts, (int)kper};
   }
   return best;
@@ -1154,7 +1194,7 @@ Shape pick_tile(int t, int64_t M, int64_t N, int64_t K, bool split, double &us_b
 
 struct Plan {
   int64_t T, H, V, Tp, Hp, Vp, Hq, Tc, pieces, nb, wh, w_ld;
-  bool pad_w, place;
+  bool pad_w, place, classes;  // rows in place; one tile holds all classes
   Shape s1, s2, s3;
   int64_t ntile, slot;
   // workspace, bytes
@@ -1178,7 +1218,8 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   p.pieces = std::max<int64_t>(1, (p.Tp + most - 1) / most);
   p.Tc = std::max<int64_t>(256, up((p.T + p.pieces - 1) / p.pieces, 256));
   p.pieces = std::max<int64_t>(1, (p.T + p.Tc - 1) / p.Tc);
-  p.place = p.V <= kTileOf[2];
+  p.classes = p.V <= kTileOf[2];
+  p.place = p.classes || p.T <= 64;
   if (p.place) p.pieces = 1, p.Tc = std::max<int64_t>(256, p.Tp);
   const int64_t rows = std::min(p.T, p.Tc);
   double best = 1e300, us, us2;
@@ -1198,7 +1239,7 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
     p.s3.ns = (int)((rows + p.s3.kper - 1) / p.s3.kper);
   }
   // rows of a workgroup of the kernel that finds the losses
-  p.slot = !p.place ? (p.T <= kFew ? 4 : 16) : p.V <= 64 ? 256 : p.V <= 128 ? 128 : 256;
+  p.slot = !p.classes ? (p.T <= kFew ? 4 : 16) : p.V <= 64 ? 256 : p.V <= 128 ? 128 : 256;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t was = at;
@@ -1214,11 +1255,11 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   p.ctarget = take(moved * p.Tp * 4);
   p.cweight = take(moved * p.Tp * 4);
   p.lsum = take(p.pieces * (p.Tc / p.slot) * 8);
-  p.mark = take(p.place ? p.Tp / 8 : 0);
+  p.mark = take(p.classes ? p.Tp / 8 : 0);
   // the products read whole tiles of rows: a tile past the last piece's rows too
   p.hc = take(p.place ? (p.pad_w ? (size_t)p.Tp * 16 : 0) : (size_t)p.pieces * p.Tc * p.Hp * 2);
-  p.stats = take(moved * (size_t)p.ntile * p.Tc * 8);
-  p.tlogit = take(moved * p.Tc * 4);
+  p.stats = take(p.classes ? 0 : (size_t)p.ntile * p.Tc * 8);
+  p.tlogit = take(p.classes ? 0 : p.Tc * 4);
   if (grad) {
     p.e = take((size_t)p.Tc * p.Vp * 2);
     p.pdh = take(p.s2.ns > 1 ? (size_t)p.s2.ns * p.Tc * p.Hq * 4 : 0);
@@ -1332,8 +1373,11 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
   r.cweight = (float *)at(p.cweight);
   r.hc = (uint16_t *)at(p.hc);
   r.loss = c.loss, r.lse = c.lse;
-  r.mark = p.place ? (uint64_t *)at(p.mark) : nullptr;
-  if (p.place && p.T) {
+  r.mark = p.classes ? (uint64_t *)at(p.mark) : nullptr;
+  const Tiny tiny = {c.target, c.weight, p.place && !p.classes ? (int32_t)p.T : 0, (int32_t)p.V,
+                     d.mean, d.scale};
+  if (tiny.T) {  // nothing to find out beforehand
+  } else if (p.classes && p.T) {
     hipLaunchKernelGGL(xent_count_kernel, dim3((uint32_t)p.nb), dim3(256), 0, st, r);
     FG_TRY(hipGetLastError());
     if (p.nb > 1) {
@@ -1375,7 +1419,7 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
     const int64_t row0 = i * p.Tc, rows = std::min(p.Tc, p.T - row0);
     const uint16_t *hc = r.hc + (size_t)row0 * p.Hp;
     double *lsum = (double *)at(p.lsum) + i * (p.Tc / p.slot);
-    if (p.place && rows > 0) {
+    if (p.classes && rows > 0) {
       ClassArgs l{};
       l.w = w, l.h = h, l.w_ld = p.w_ld, l.h_ld = h_ld;
       l.wh = (int32_t)p.wh, l.V = (int32_t)p.V, l.T = (int32_t)p.T;
@@ -1389,18 +1433,20 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
     } else if (rows > 0) {
       LogitArgs l{};
       l.w = w, l.w_ld = p.w_ld, l.wh = (int32_t)p.wh, l.V = (int32_t)p.V;
-      l.hc = hc, l.Hp = (int32_t)p.Hp;
-      l.found = r.found, l.row0 = (int32_t)row0, l.Tc = (int32_t)p.Tc;
-      l.ctarget = r.ctarget + row0;
+      l.hc = tiny.T ? h : hc, l.Hp = (int32_t)(tiny.T ? h_ld : p.Hp);
+      l.found = r.found, l.row0 = (int32_t)row0;
+      l.Tc = tiny.T ? tiny.T : (int32_t)p.Tc, l.tiny = tiny.T > 0;
+      l.ctarget = tiny.T ? c.target : r.ctarget + row0;
       l.e = c.grad ? (uint16_t *)at(p.e) : nullptr, l.Vp = (int32_t)p.Vp;
       l.stats = (float2 *)at(p.stats), l.tlogit = (float *)at(p.tlogit);
       FG_TRY(FG_XENT_TILE(launch_logits, LogitTiles, p.s1.tile, bf, l, rows, st));
       SoftmaxArgs s{};
-      s.found = r.found, s.row0 = (int32_t)row0, s.Tc = (int32_t)p.Tc;
+      s.found = r.found, s.row0 = (int32_t)row0, s.Tc = l.Tc, s.tiny = tiny;
       s.V = (int32_t)p.V, s.Vp = (int32_t)p.Vp;
       s.tlog = 6 + p.s1.tile, s.ntile = (int32_t)p.ntile;
       s.bf = bf;
-      s.idx = r.idx + row0, s.ctarget = l.ctarget, s.cweight = r.cweight + row0;
+      s.idx = r.idx + row0, s.ctarget = l.ctarget;
+      s.cweight = tiny.T ? c.weight : r.cweight + row0;
       s.stats = l.stats, s.tlogit = l.tlogit, s.e = l.e;
       s.loss = c.loss, s.lse = c.lse, s.lsum = lsum;
       // workgroups: 2048, where the classes give as many ranges of 512
@@ -1425,9 +1471,10 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
     a.M = (int32_t)p.H, a.Mq = (int32_t)p.Hq;
     a.row0 = (int32_t)row0, a.Tc = (int32_t)(p.place ? p.T : p.Tc), a.found = r.found;
     a.V = (int32_t)p.V;
-    a.mark = r.mark;
+    a.mark = r.mark, a.tiny = tiny;
     JoinArgs &j = g.jdh;
     j.M = a.M, j.Mq = a.Mq, j.row0 = a.row0, j.Tc = a.Tc, j.found = r.found, j.bf = bf;
+    j.tiny = tiny;
     g.dw = a, g.jdw = j;
     bool join_dh = false, join_dw = false;
     if (c.dh && rows > 0) {
@@ -1440,7 +1487,8 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       a.part = split ? (float *)at(p.pdh) : nullptr, a.pstride = p.Tc * p.Hq;
       j.part = a.part, j.pstride = a.pstride, j.nsplit = p.s2.ns;
       j.rows = p.place ? (int32_t)p.T : -1;
-      j.idx = p.place ? nullptr : a.idx, j.mark = r.mark, j.out = (uint16_t *)c.dh, j.out_ld = a.out_ld;
+      j.idx = p.place ? nullptr : a.idx, j.mark = r.mark, j.masked = p.place;
+      j.out = (uint16_t *)c.dh, j.out_ld = a.out_ld;
       join_dh = split;
     }
     if (c.dw) {
@@ -1463,7 +1511,7 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
     }
     if (!g.nsdh && !g.nsdw) continue;
     if (c.totals && last && nsum <= kSumHere) {
-      g.sum = {(const double *)at(p.lsum), nsum, r.found, c.totals};
+      g.sum = {(const double *)at(p.lsum), nsum, r.found, c.totals, tiny};
       summed = nsum > 0;
     }
     FG_TRY(FG_XENT_TILE(launch_products, ProdTiles, p.s2.tile, bf, g, st));
