@@ -393,7 +393,8 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, bool bf) {
     typedef __bf16 b2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, b2{(__bf16)a, (__bf16)b});
   }
-  return (uint32_t)f32_to_h(a) | ((uint32_t)f32_to_h(b) << 16);
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, h2{(_Float16)a, (_Float16)b});
 }
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void *p, uint32_t bytes) {
@@ -1094,11 +1095,7 @@ struct JoinArgs {
 // Where there are many, the workgroup's 8 waves share a sum, a run of the parts each
 // (12 x 512 sums of 256 parts took 42 us by single lanes). Both gradients' in one
 // launch, dh's in the first nh workgroups.
-__global__ __launch_bounds__(512) void xent_join_kernel(JoinArgs dh, JoinArgs dw, int nh) {
-  __shared__ float sh[8][64][8];
-  const bool first = (int)blockIdx.x < nh;
-  const JoinArgs &a = first ? dh : dw;
-  const int block = first ? blockIdx.x : blockIdx.x - nh;
+__device__ __forceinline__ void join_rows(const JoinArgs &a, int block, float (&sh)[8][64][8]) {
   const int rows = a.rows < 0 ? piece_rows(a.found, a.row0, a.Tc) : a.rows;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint64_t few = ~0ull;
@@ -1145,6 +1142,131 @@ __global__ __launch_bounds__(512) void xent_join_kernel(JoinArgs dh, JoinArgs dw
   }
   if (a.flag) flag_nonfinite(a.flag, bad);
 }
+__global__ __launch_bounds__(512) void xent_join_kernel(JoinArgs dh, JoinArgs dw, int nh) {
+  __shared__ float sh[8][64][8];
+  const bool first = (int)blockIdx.x < nh;
+  join_rows(first ? dh : dw, first ? blockIdx.x : blockIdx.x - nh, sh);
+}
+
+// dW of up to 64 rows: a sum of at most 64 terms per element, bound by writing dW. A
+// workgroup (8 waves of 64 x 32) keeps its 256 features of all rows in registers and
+// goes through a range of the classes, 64 at a time, whose G arrives while the ones
+// before are multiplied and stored. 3 rows of 2496 x 21696: 24.6 us (4.4 TB/s), 55 us by
+// the tiles of xent_products_kernel.
+// Below kOuter weights the launch it adds costs more: 11 rows of 128 x 1088 18.7 us in all
+// without it and 24.9 with it, 41 of 287 x 4039 22.8 and 25.1; 7 of 148 x 38444 33.5 and
+// 28.7, 7 of 2432 x 4032 41.9 and 35.4.
+constexpr int64_t kOuter = (int64_t)3 << 20;
+struct OuterArgs {
+  const uint16_t *h;
+  int64_t h_ld;
+  const uint16_t *g;         // [T][Vp]
+  int32_t Vp, V, H, wh;
+  int32_t per;               // chunks of 64 classes of a workgroup
+  uint16_t *out;
+  int64_t out_ld;
+  int32_t *flag;
+  Tiny tiny;
+};
+using POuter = Pipe<64, 2, 4, 2, 256, 64>;  // shapes only: 64 rows deep, 8 waves
+
+template <class P>
+__device__ __forceinline__ void outer_tile(const OuterArgs &a, int tm, int tv, uint8_t *stage) {
+  __shared__ __attribute__((aligned(1024))) uint8_t sA[P::A_BYTES], sB0[P::B_BYTES],
+      sB1[P::B_BYTES];
+  constexpr int PA = P::PA, PB = P::PB, KS = P::KS;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm0 = (wave / P::WGN) * P::WM, wn0 = (wave % P::WGN) * P::WN;
+  const int m0 = tm * P::TM, c0 = tv * a.per, c1 = min((a.Vp + 63) / 64, c0 + a.per);
+  if (c0 >= c1) return;
+  uint64_t mark;
+  const float mult = tiny_found(a.tiny, mark).mult;
+  const int T = a.tiny.T;
+  // rows past the last one, and of the features masked ones: zeros
+  const __amdgpu_buffer_rsrc_t rs_h = rsrc(a.h, (uint32_t)((T - 1) * (int)a.h_ld + a.wh) * 2u);
+  const __amdgpu_buffer_rsrc_t rs_g = rsrc(a.g, (uint32_t)(T * a.Vp) * 2u);
+  const MnSlot<PA> as = mn_slots<P::RBA, PA>(wave, lane);
+  const MnSlot<PB> bs = mn_slots<P::RBB, PB>(wave, lane);
+  auto issue = [&](int c, uint8_t *to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int jj = 0; jj < PB; ++jj)
+      dma16(rs_g, to + dma_dst<PB>(wave, jj),
+            bs.krow[jj] < T && 64 * c + bs.ncol[jj] < a.Vp
+                ? (unsigned)(bs.krow[jj] * a.Vp + 64 * c + bs.ncol[jj]) * 2u
+                : kOOB);
+  };
+  issue(c0, sB0);
+#pragma unroll
+  for (int jj = 0; jj < PA; ++jj)
+    dma16(rs_h, sA + dma_dst<PA>(wave, jj),
+          (mark >> as.krow[jj] & 1) && m0 + as.ncol[jj] < a.wh
+              ? (unsigned)(as.krow[jj] * (int)a.h_ld + chunk_at(m0 + as.ncol[jj], a.wh)) * 2u
+              : kOOB);
+  wait_vm<0>();
+  barrier_nofence();
+  u32x4 fa[KS][P::FM];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i) fa[ks][i] = frag<64, false, P::RBA>(sA, wm0 + 32 * i, ks, lane);
+  bool bad = false;
+  auto chunk = [&](int c, const uint8_t *here, uint8_t *next) __attribute__((always_inline)) {
+    if (c > c0) {  // this chunk has arrived, and every wave has read the one before
+      wait_vm<0>();
+      wait_lds();
+      barrier_nofence();
+    }
+    if (c + 1 < c1) issue(c + 1, next);
+    f32x16 acc[P::FM][P::FN];
+    zero<P>(acc);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if (16 * ks >= T) break;
+#pragma unroll
+      for (int j = 0; j < P::FN; ++j) {
+        const u32x4 fb = frag<64, false, P::RBB>(here, wn0 + 32 * j, ks, lane);
+#pragma unroll
+        for (int i = 0; i < P::FM; ++i)
+          acc[i][j] = P::BF ? mfma32_bf16(fa[ks][i], fb, acc[i][j]) : mfma32(fa[ks][i], fb, acc[i][j]);
+      }
+    }
+    store16<P>(
+        stage + wave * 64 * P::WM, lane,
+        [&](int i, int j, int g) __attribute__((always_inline)) {
+          const f32x16 &x = acc[i][j];
+          return u32x2{pack2(x[4 * g] * mult, x[4 * g + 1] * mult, P::BF),
+                       pack2(x[4 * g + 2] * mult, x[4 * g + 3] * mult, P::BF)};
+        },
+        [&](int r, int q, const u32x4 &d) __attribute__((always_inline)) {
+          const int v = 64 * c + wn0 + r, m = m0 + wm0 + q;
+          if (v >= a.V || m >= a.H) return;
+          constexpr uint32_t EX = P::BF ? 0x7F80u : 0x7C00u;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) bad |= (d[e >> 1] >> (16 * (e & 1)) & EX) == EX;
+          put_chunk(a.out + (int64_t)v * a.out_ld, m, a.H, d);
+        });
+  };
+  for (int c = c0; c < c1; c += 2) {
+    chunk(c, sB0, sB1);
+    if (c + 1 < c1) chunk(c + 1, sB1, sB0);
+  }
+  if (a.flag) flag_nonfinite(a.flag, bad);
+}
+
+// With the join of dh's parts in the first workgroups.
+template <class P>
+__global__ __launch_bounds__(P::NT) void xent_outer_kernel(OuterArgs a, int nm, JoinArgs dh,
+                                                           int nh) {
+  __shared__ __attribute__((aligned(1024))) uint8_t stage[P::NW * 64 * P::WM];
+  static_assert(P::NT == 512 && sizeof(stage) >= 16384, "room for the join's workgroups");
+  if ((int)blockIdx.x < nh) {
+    join_rows(dh, blockIdx.x, *reinterpret_cast<float(*)[8][64][8]>(stage));
+    return;
+  }
+  const int b = blockIdx.x - nh;
+  outer_tile<P>(a, b % nm, b / nm, stage);
+}
 
 // ---- host ------------------------------------------------------------------------------
 // The numerators of a piece of rows take at most this much of the workspace. Fewer,
@@ -1166,7 +1288,7 @@ struct Shape {
 Shape pick_tile(int t, int64_t M, int64_t N, int64_t K, bool split, double &us_best) {
   static const int occ[3] = {3, 2, 1};
   static const double fixed[3][3] = {{2.0, 2.0, 2.0}, {3.5, 5.5, 5.5}, {9.0, 9.0, 9.0}};
-  const double more = t == 2 && split ? 5.0 : 0.0;  // the products' store of a large tile
+  const double more = !split ? 0.0 : t == 2 ? 5.0 : t == 0 ? 1.0 : 0.0;  // the products' store
   static const double per_k[3][3] = {{.0055, .009, .0135}, {.0095, .0178, .0178},
                                      {.0175, .0175, .0175}};
   Shape best{t, 1, 0};
@@ -1194,7 +1316,8 @@ Shape pick_tile(int t, int64_t M, int64_t N, int64_t K, bool split, double &us_b
 
 struct Plan {
   int64_t T, H, V, Tp, Hp, Vp, Hq, Tc, pieces, nb, wh, w_ld;
-  bool pad_w, place, classes;  // rows in place; one tile holds all classes
+  bool pad_w, place, classes, outer;  // rows in place; one tile holds all classes; dW by
+                                      // xent_outer_kernel
   Shape s1, s2, s3;
   int64_t ntile, slot;
   // workspace, bytes
@@ -1220,6 +1343,7 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   p.pieces = std::max<int64_t>(1, (p.T + p.Tc - 1) / p.Tc);
   p.classes = p.V <= kTileOf[2];
   p.place = p.classes || p.T <= 64;
+  p.outer = p.place && !p.classes && p.T > 0 && p.V * p.H >= kOuter;
   if (p.place) p.pieces = 1, p.Tc = std::max<int64_t>(256, p.Tp);
   const int64_t rows = std::min(p.T, p.Tc);
   double best = 1e300, us, us2;
@@ -1232,6 +1356,7 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   for (int t = 0; t < (p.place ? 2 : 3); ++t) {  // in place: tiles of 64-deep stages
     const Shape a = pick_tile(t, p.H, rows, p.Vp, true, us);
     const Shape b = pick_tile(t, p.H, p.V, rows, true, us2);
+    if (p.outer) us2 = 0;
     if (us + us2 < best) best = us + us2, p.s2 = a, p.s3 = b;
   }
   if (p.place && p.s3.kper > 64 * kMarks) {
@@ -1263,6 +1388,7 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   if (grad) {
     p.e = take((size_t)p.Tc * p.Vp * 2);
     p.pdh = take(p.s2.ns > 1 ? (size_t)p.s2.ns * p.Tc * p.Hq * 4 : 0);
+    if (p.outer) p.s3.ns = 1;
     p.pdw = take(p.s3.ns > 1 || p.pieces > 1 ? (size_t)p.s3.ns * p.V * p.Hq * 4 : 0);
   }
   p.wc = take(p.pad_w ? (size_t)p.V * 16 : 0);
@@ -1292,6 +1418,7 @@ struct Products {
   int64_t rows;
   bool place;
   SumArgs sum;
+  OuterArgs outer;    // out: dW this way, not by dw
 };
 
 template <class P>
@@ -1318,16 +1445,30 @@ hipError_t launch_classes(const ClassArgs &a, hipStream_t st) {
   return hipGetLastError();
 }
 
+int join_blocks(JoinArgs &j, int64_t rows) {
+  const int64_t n = rows * (j.Mq / 8);
+  j.shared = j.nsplit >= 16;
+  return (int)((n + (j.shared ? 63 : 511)) / (j.shared ? 64 : 512));
+}
+
 hipError_t launch_join(Products &a, bool dh, bool dw, hipStream_t st) {
   if (!dh && !dw) return hipSuccess;
-  const auto blocks = [](JoinArgs &j, int64_t rows) {
-    const int64_t n = rows * (j.Mq / 8);
-    j.shared = j.nsplit >= 16;
-    return (int)((n + (j.shared ? 63 : 511)) / (j.shared ? 64 : 512));
-  };
-  const int nh = dh ? blocks(a.jdh, a.rows) : 0, nw = dw ? blocks(a.jdw, a.dw.V) : 0;
+  const int nh = dh ? join_blocks(a.jdh, a.rows) : 0, nw = dw ? join_blocks(a.jdw, a.dw.V) : 0;
   hipLaunchKernelGGL(xent_join_kernel, dim3((uint32_t)(nh + nw)), dim3(512), 0, st, a.jdh, a.jdw,
                      nh);
+  return hipGetLastError();
+}
+
+template <class P>
+hipError_t launch_outer(Products &a, bool dh, hipStream_t st) {
+  const int nh = dh ? join_blocks(a.jdh, a.rows) : 0;
+  const int nm = (a.outer.H + P::TM - 1) / P::TM, chunks = (a.outer.Vp + 63) / 64;
+  // some 1024 workgroups, two chunks each at least where there are as many
+  const int nv = std::max(1, std::min((chunks + 1) / 2, 1024 / nm));
+  a.outer.per = (chunks + nv - 1) / nv;
+  const int n = nm * ((chunks + a.outer.per - 1) / a.outer.per);
+  hipLaunchKernelGGL(xent_outer_kernel<P>, dim3((uint32_t)(nh + n)), dim3(P::NT), 0, st, a.outer,
+                     nm, a.jdh, nh);
   return hipGetLastError();
 }
 
@@ -1491,7 +1632,13 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       j.out = (uint16_t *)c.dh, j.out_ld = a.out_ld;
       join_dh = split;
     }
-    if (c.dw) {
+    if (c.dw && p.outer) {
+      OuterArgs &o = g.outer;
+      o.h = h, o.h_ld = h_ld, o.g = a.b, o.Vp = (int32_t)p.Vp, o.V = (int32_t)p.V;
+      o.H = (int32_t)p.H, o.wh = (int32_t)p.wh;
+      o.out = (uint16_t *)c.dw, o.out_ld = d.dw_ld ? d.dw_ld : d.hidden;
+      o.flag = c.flag, o.tiny = tiny;
+    } else if (c.dw) {
       ProdArgs &b = g.dw;
       JoinArgs &q = g.jdw;
       const bool split = p.s3.ns > 1;
@@ -1509,13 +1656,17 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       q.out = (uint16_t *)c.dw, q.out_ld = b.out_ld, q.flag = c.flag;
       join_dw = split && last;
     }
-    if (!g.nsdh && !g.nsdw) continue;
-    if (c.totals && last && nsum <= kSumHere) {
-      g.sum = {(const double *)at(p.lsum), nsum, r.found, c.totals, tiny};
-      summed = nsum > 0;
+    if (g.nsdh || g.nsdw) {
+      if (c.totals && last && nsum <= kSumHere) {
+        g.sum = {(const double *)at(p.lsum), nsum, r.found, c.totals, tiny};
+        summed = nsum > 0;
+      }
+      FG_TRY(FG_XENT_TILE(launch_products, ProdTiles, p.s2.tile, bf, g, st));
     }
-    FG_TRY(FG_XENT_TILE(launch_products, ProdTiles, p.s2.tile, bf, g, st));
-    FG_TRY(launch_join(g, join_dh, join_dw, st));
+    if (g.outer.out)
+      FG_TRY(bf ? launch_outer<Bf16<POuter>>(g, join_dh, st) : launch_outer<POuter>(g, join_dh, st));
+    else
+      FG_TRY(launch_join(g, join_dh, join_dw, st));
   }
   if (c.totals && !summed) {
     hipLaunchKernelGGL(xent_totals_kernel, dim3(1), dim3(1024), 0, st, (double *)at(p.lsum), nsum,
