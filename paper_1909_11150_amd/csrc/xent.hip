@@ -46,19 +46,18 @@ constexpr int kFew = 1024;      // rows up to which the softmax kernel takes 4 p
 constexpr int kCount = 1024;    // rows of a workgroup of the counting kernel
 constexpr int kDirect = 8192;   // rows up to which there is none
 
-#ifndef FG_P1
-#define FG_P1 64, 2, 2, 4, 256, 256
-#endif
-#ifndef FG_P2
-#define FG_P2 32, 5, 2, 4, 256, 256
-#endif
 using P128 = Pipe<64, 2, 2, 2, 128, 128>;  // 4 waves of 64 x 64
 using P64 = Pipe<64, 3, 2, 2, 64, 64>;     // 4 waves of 32 x 32
+// The largest, 8 waves of 128 x 64: 64-deep stages for the logits' operands, whose rows
+// lie along the sum (whole 128-byte lines: 8192 x 4096 x 131072 in two pieces 3.48 ms a
+// piece, 3.84 with 32-deep ones); 32-deep ones, five in the ring, for the products',
+// whose rows lie across it (7.0 ms, 7.4 with 64-deep ones). Smaller tiles twice per CU
+// (256 x 128) took 4.8 and 8.8 ms, 4 waves of 128 x 128 3.8 and 8.0.
 struct LogitTiles {
-  using T256 = Pipe<FG_P1>;
+  using T256 = Pipe<64, 2, 2, 4, 256, 256>;
 };
 struct ProdTiles {
-  using T256 = Pipe<FG_P2>;
+  using T256 = Pipe<32, 5, 2, 4, 256, 256>;
 };
 // Up to 64 classes: 64 x 256, 4 waves of 64 x 64, twice per CU: the features' stream
 // bounds it, and a workgroup reads the weights once for 256 rows.
@@ -276,14 +275,22 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
   int n = 0;
   double sum = 0;
   float mx = 0.f;
-#pragma unroll 8
-  for (int r = blk * kCount + threadIdx.x; r < min(r0, a.T); r += 256) {
-    float w;
-    if (live_row(a, r, w)) {
-      ++n;
-      if (totals) {
-        sum += w;
-        mx = fmaxf(mx, fabsf(w));
+  const int end = min(r0, a.T);
+  constexpr int B = 8;  // loads in flight
+  for (int r = blk * kCount + threadIdx.x; r < end; r += 256 * B) {
+    int32_t t[B];
+    float w[B];
+#pragma unroll
+    for (int k = 0; k < B; ++k) t[k] = a.target[min(r + 256 * k, a.T - 1)];
+#pragma unroll
+    for (int k = 0; k < B; ++k) w[k] = a.weight ? a.weight[min(r + 256 * k, a.T - 1)] : 1.f;
+#pragma unroll
+    for (int k = 0; k < B; ++k) {
+      const bool on = r + 256 * k < end && (uint32_t)t[k] < (uint32_t)a.V && w[k] != 0.f;
+      n += on;
+      if (totals && on) {
+        sum += w[k];
+        mx = fmaxf(mx, fabsf(w[k]));
       }
     }
   }
