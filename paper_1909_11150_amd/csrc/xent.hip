@@ -59,9 +59,10 @@ struct LogitTiles {
 struct ProdTiles {
   using T256 = Pipe<32, 5, 2, 4, 256, 256>;
 };
-// Up to 64 classes: 64 x 256, 4 waves of 64 x 64, twice per CU: the features' stream
-// bounds it, and a workgroup reads the weights once for 256 rows.
-using PClass = Pipe<64, 2, 1, 4, 64, 256>;
+// Up to 32 and 64 classes, by 128 rows: bound by the features' stream, of which two or
+// three stages are on their way in each of two workgroups per CU.
+using PClass32 = Pipe<64, 4, 1, 4, 32, 128>;
+using PClass64 = Pipe<64, 3, 1, 4, 64, 128>;
 
 // What the first kernels find out, read by the others.
 struct Found {
@@ -143,6 +144,33 @@ __device__ __forceinline__ Found tiny_found(const Tiny &t, uint64_t &mark) {
   return make_found(t.mean, t.scale, __popcll(mark), wave_sum(on ? (double)w : 0.0),
                     wave_max(on ? fabsf(w) : 0.f));
 }
+
+// Unweighted rows of few classes: the kernel that finds the losses also counts each
+// tile's live rows, and those after it add the counts up.
+constexpr int kTiles = 512;
+struct Counts {
+  const int32_t *live;
+  int32_t n, mean;  // n = 0: not so
+  double scale;
+};
+// The counts, a few per lane: loaded well before they are used.
+struct Counted {
+  int c[kTiles / 64];
+  __device__ __forceinline__ void load(const Counts &a) {
+#pragma unroll
+    for (int k = 0; k < kTiles / 64; ++k) {
+      const int i = 64 * k + (threadIdx.x & 63);
+      c[k] = i < a.n ? a.live[i] : 0;
+    }
+  }
+  __device__ __forceinline__ Found found(const Counts &a) const {
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < kTiles / 64; ++k) n += c[k];
+    n = wave_sum(n);
+    return make_found(a.mean, a.scale, n, (double)n, 1.f);
+  }
+};
 
 // Live rows, their weights' sum and largest magnitude, per block of 1024 rows; the
 // totals too where there is one block.
@@ -616,7 +644,8 @@ struct ClassArgs {
   int64_t w_ld, h_ld;
   int32_t wh, V, T;
   const Found *found;
-  const uint64_t *mark;
+  uint64_t *mark;
+  int32_t *count;    // per tile of rows: live ones, found here as the marks are; or null
   const int32_t *target;
   const float *weight;
   uint16_t *e;       // [T][Vp] 2^15 G, or null: losses only
@@ -639,7 +668,8 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_classes_kernel(ClassArgs a
   const __amdgpu_buffer_rsrc_t rs_h =
       rsrc(a.h + n0 * a.h_ld, (uint32_t)((hrows - 1) * a.h_ld + a.wh) * 2u);
   auto live = [&](int n) __attribute__((always_inline)) {
-    return n < a.T && (a.mark[n >> 6] >> (n & 63) & 1);
+    return n < a.T && (a.count ? (uint32_t)a.target[n] < (uint32_t)a.V
+                               : (a.mark[n >> 6] >> (n & 63) & 1) != 0);
   };
   const KmSlot<PA> as = km_slots<BK, PA>(wave, lane);
   const KmSlot<PB> bs = km_slots<BK, PB>(wave, lane);
@@ -655,7 +685,7 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_classes_kernel(ClassArgs a
   __syncthreads();  // every wave is done reading the ring
   float *xm = reinterpret_cast<float *>(R.b[0]), *xs = xm + P::WGM * TN, *xt = xs + P::WGM * TN;
   double *part = reinterpret_cast<double *>(xt + TN);
-  static_assert((2 * P::WGM + 1) * TN * 4 + P::NW * 8 <= P::B_BYTES, "exchange fits a stage");
+  static_assert((2 * P::WGM + 1) * TN * 4 + P::NW * 12 <= P::B_BYTES, "exchange fits a stage");
   int tg[P::FN];
   float w[P::FN], up[P::FN], s[P::FN];
 #pragma unroll
@@ -696,6 +726,7 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_classes_kernel(ClassArgs a
   }
   __syncthreads();
   double sum = 0;
+  const float wmax_inv = a.count ? 1.f : a.found->wmax_inv;
   float f[P::FN], pt[P::FN];
 #pragma unroll
   for (int j = 0; j < P::FN; ++j) {
@@ -705,7 +736,7 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_classes_kernel(ClassArgs a
     for (int k = 1; k < P::WGM; ++k) s[j] += xs[k * TN + p];
     const bool on = tg[j] >= 0;
     const float l2 = __log2f(s[j]) - up[j], d = on ? l2 * kLn2 - xt[p] : 0.f;
-    const float c = kUp * w[j] * a.found->wmax_inv;
+    const float c = kUp * w[j] * wmax_inv;
     f[j] = c / s[j];
     pt[j] = c * expm1f(-d);  // 2^15 w (p - 1)
     if (wm == 0 && lane < 32 && n < a.T) {
@@ -733,14 +764,29 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_classes_kernel(ClassArgs a
         },
         [&](int r, int c, const u32x4 &d) __attribute__((always_inline)) {
           const int n = n0 + wn0 + r, v = wm0 + c;
-          if (n < a.T && v < a.Vp) *reinterpret_cast<u32x4 *>(a.e + (size_t)n * a.Vp + v) = d;
+          if (n >= a.T || v >= a.Vp) return;
+          *reinterpret_cast<u32x4 *>(a.e + (size_t)n * a.Vp + v) = d;
+          if (P::TM < 64) *reinterpret_cast<u32x4 *>(a.e + (size_t)n * a.Vp + v + 32) = {0, 0, 0, 0};
         });
   }
+  int rows = 0;
+  if (a.count)
+    for (int g = wave; g < TN / 64; g += P::NW) {
+      const uint64_t mark = __ballot(live(n0 + 64 * g + lane));
+      rows += __popcll(mark);
+      if (lane == 0 && n0 + 64 * g < a.T) a.mark[(n0 >> 6) + g] = mark;
+    }
+  if (lane == 0) reinterpret_cast<int *>(part + P::NW)[wave] = rows;
   __syncthreads();
   if (tid == 0) {
     double t = 0;
-    for (int k = 0; k < P::NW; ++k) t += part[k];
+    int n = 0;
+    for (int k = 0; k < P::NW; ++k) {
+      t += part[k];
+      n += reinterpret_cast<int *>(part + P::NW)[k];
+    }
     a.lsum[blockIdx.x] = t;
+    if (a.count) a.count[blockIdx.x] = n;
   }
 }
 
@@ -878,22 +924,6 @@ __global__ __launch_bounds__(256) void xent_softmax_kernel(SoftmaxArgs a) {
   }
 }
 
-// One workgroup: the sums of the losses and of the weights.
-__global__ __launch_bounds__(1024) void xent_totals_kernel(const double *lsum, int32_t n,
-                                                           const Found *found, float *totals) {
-  __shared__ double ws[16];
-  double s = 0;
-  for (int i = threadIdx.x; i < n; i += 1024) s += lsum[i];
-  s = wave_sum(s);
-  if ((threadIdx.x & 63) == 0) ws[threadIdx.x >> 6] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int k = 1; k < 16; ++k) s += ws[k];
-    totals[0] = (float)s;
-    totals[1] = found->wsum;
-  }
-}
-
 // ---- products -------------------------------------------------------------------------
 // out[n][m] = mult * sum_k A[k][m] B(n, k), m < M (hidden), with A (the weights, or
 // the features) read row by row; B = G, rows n (dh, k: classes) or columns n (dW, k:
@@ -918,6 +948,7 @@ struct ProdArgs {
   int32_t *flag;
   const uint64_t *mark;      // rows in place: a bit per live one
   Tiny tiny;                 // (without mark)
+  Counts counts;
 };
 
 // PLACE: rows in place (up to 256 classes); marks: LDS for a part's marks.
@@ -939,6 +970,8 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
   uint64_t few = 0;  // the marks of a tiny call
   float mult = 0.f;
   if (PLACE && a.tiny.T) mult = tiny_found(a.tiny, few).mult;
+  Counted counted;
+  if constexpr (PLACE) counted.load(a.counts);
 
   const MnSlot<PA> as = mn_slots<P::RBA, PA>(wave, lane);
   unsigned oa[PA], ob[PB];
@@ -1021,7 +1054,10 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
     if (!a.out) return;
   }
   __syncthreads();  // every wave is done reading the ring
-  if (!PLACE || !a.tiny.T) mult = a.found->mult;
+  if (PLACE && a.counts.n)
+    mult = counted.found(a.counts).mult;
+  else if (!PLACE || !a.tiny.T)
+    mult = a.found->mult;
   bool bad = false;
   store16<P>(
       wave_buf<P>(R, wave), lane,
@@ -1056,7 +1092,19 @@ struct SumArgs {
   const Found *found;
   float *totals;
   Tiny tiny;
+  Counts counts;
 };
+// The weights' sum, by a wave.
+__device__ __forceinline__ float weights_sum(const Tiny &tiny, const Counts &counts,
+                                             const Found *found) {
+  if (counts.n) {
+    Counted c;
+    c.load(counts);
+    return c.found(counts).wsum;
+  }
+  uint64_t mark;
+  return tiny.T ? tiny_found(tiny, mark).wsum : found->wsum;
+}
 template <class P, bool PLACE>
 __global__ __launch_bounds__(P::NT, P::WPE) void xent_products_kernel(ProdArgs dh, TileMap th,
                                                                       ProdArgs dw, TileMap tw,
@@ -1069,8 +1117,7 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_products_kernel(ProdArgs d
 #pragma unroll 4
     for (int i = threadIdx.x; i < sum.n; i += 64) s += sum.lsum[i];
     s = wave_sum(s);
-    uint64_t mark;
-    const float w = sum.tiny.T ? tiny_found(sum.tiny, mark).wsum : sum.found->wsum;
+    const float w = weights_sum(sum.tiny, sum.counts, sum.found);
     if (threadIdx.x == 0) {
       sum.totals[0] = (float)s;
       sum.totals[1] = w;
@@ -1080,6 +1127,24 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_products_kernel(ProdArgs d
     product_tile<P, true, PLACE>(dh, th, block, R, marks);
   else
     product_tile<P, false, PLACE>(dw, tw, block - nh, R, marks);
+}
+
+// One workgroup: the sums of the losses and of the weights.
+__global__ __launch_bounds__(1024) void xent_totals_kernel(SumArgs a) {
+  __shared__ double ws[16];
+  double s = 0;
+  for (int i = threadIdx.x; i < a.n; i += 1024) s += a.lsum[i];
+  s = wave_sum(s);
+  if ((threadIdx.x & 63) == 0) ws[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const float w = weights_sum(a.tiny, a.counts, a.found);
+    for (int k = 1; k < 16; ++k) s += ws[k];
+    if (threadIdx.x == 0) {
+      a.totals[0] = (float)s;
+      a.totals[1] = w;
+    }
+  }
 }
 
 // Joins the parts of a split sum, in their order: 8 columns of a row per lane.
@@ -1093,6 +1158,7 @@ struct JoinArgs {
   const int32_t *idx;
   const uint64_t *mark;         // rows in place (dh)
   Tiny tiny;                    // (without mark)
+  Counts counts;
   int32_t masked;               // dh: masked rows are zeros
   uint16_t *out;
   int64_t out_ld;
@@ -1106,7 +1172,11 @@ __device__ __forceinline__ void join_rows(const JoinArgs &a, int block, float (&
   const int rows = a.rows < 0 ? piece_rows(a.found, a.row0, a.Tc) : a.rows;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint64_t few = ~0ull;
-  const float mult = a.tiny.T ? tiny_found(a.tiny, few).mult : a.found->mult;
+  Counted counted;
+  counted.load(a.counts);
+  const float mult = a.counts.n ? counted.found(a.counts).mult
+                     : a.tiny.T ? tiny_found(a.tiny, few).mult
+                                : a.found->mult;
   const bool shared = a.shared;
   const int64_t i = shared ? (int64_t)block * 64 + lane : (int64_t)block * 512 + threadIdx.x;
   const int c8 = a.Mq / 8;
@@ -1328,7 +1398,7 @@ struct Plan {
   Shape s1, s2, s3;
   int64_t ntile, slot;
   // workspace, bytes
-  size_t count, wsum, wmax, found, mark, idx, ctarget, cweight, hc, wc, stats, tlogit, e, pdh, pdw,
+  size_t count, wsum, wmax, found, mark, tcount, idx, ctarget, cweight, hc, wc, stats, tlogit, e, pdh, pdw,
       lsum, total;
 };
 
@@ -1371,7 +1441,7 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
     p.s3.ns = (int)((rows + p.s3.kper - 1) / p.s3.kper);
   }
   // rows of a workgroup of the kernel that finds the losses
-  p.slot = !p.classes ? (p.T <= kFew ? 4 : 16) : p.V <= 64 ? 256 : p.V <= 128 ? 128 : 256;
+  p.slot = !p.classes ? (p.T <= kFew ? 4 : 16) : p.V <= 128 ? 128 : 256;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t was = at;
@@ -1388,6 +1458,7 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   p.cweight = take(moved * p.Tp * 4);
   p.lsum = take(p.pieces * (p.Tc / p.slot) * 8);
   p.mark = take(p.classes ? p.Tp / 8 : 0);
+  p.tcount = take(p.classes ? kTiles * 4 : 0);
   // the products read whole tiles of rows: a tile past the last piece's rows too
   p.hc = take(p.place ? (p.pad_w ? (size_t)p.Tp * 16 : 0) : (size_t)p.pieces * p.Tc * p.Hp * 2);
   p.stats = take(p.classes ? 0 : (size_t)p.ntile * p.Tc * 8);
@@ -1524,7 +1595,11 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
   r.mark = p.classes ? (uint64_t *)at(p.mark) : nullptr;
   const Tiny tiny = {c.target, c.weight, p.place && !p.classes ? (int32_t)p.T : 0, (int32_t)p.V,
                      d.mean, d.scale};
-  if (tiny.T) {  // nothing to find out beforehand
+  const int32_t nsum = (int32_t)((p.T + p.slot - 1) / p.slot);
+  Counts counts{};
+  if (p.classes && !c.weight && nsum > 0 && nsum <= kTiles)
+    counts = {(int32_t *)at(p.tcount), nsum, d.mean, d.scale};
+  if (tiny.T || counts.n) {  // nothing to find out beforehand
   } else if (p.classes && p.T) {
     hipLaunchKernelGGL(xent_count_kernel, dim3((uint32_t)p.nb), dim3(256), 0, st, r);
     FG_TRY(hipGetLastError());
@@ -1561,7 +1636,7 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
     h = (const uint16_t *)at(p.hc);
     h_ld = 8;
   }
-  const int32_t nsum = (int32_t)((p.T + p.slot - 1) / p.slot);
+  const SumArgs sum = {(const double *)at(p.lsum), nsum, r.found, c.totals, tiny, counts};
   bool summed = false;
   for (int64_t i = 0; i < p.pieces; ++i) {
     const int64_t row0 = i * p.Tc, rows = std::min(p.Tc, p.T - row0);
@@ -1574,7 +1649,11 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       l.found = r.found, l.mark = r.mark, l.target = c.target, l.weight = c.weight;
       l.e = c.grad ? (uint16_t *)at(p.e) : nullptr, l.Vp = (int32_t)p.Vp;
       l.loss = c.loss, l.lse = c.lse, l.lsum = lsum;
-      FG_TRY(p.V <= 64    ? (bf ? launch_classes<Bf16<PClass>>(l, st) : launch_classes<PClass>(l, st))
+      l.count = counts.n ? (int32_t *)at(p.tcount) : nullptr;
+      FG_TRY(p.V <= 32    ? (bf ? launch_classes<Bf16<PClass32>>(l, st)
+                                : launch_classes<PClass32>(l, st))
+             : p.V <= 64  ? (bf ? launch_classes<Bf16<PClass64>>(l, st)
+                                : launch_classes<PClass64>(l, st))
              : p.V <= 128 ? (bf ? launch_classes<Bf16<P128>>(l, st) : launch_classes<P128>(l, st))
                           : (bf ? launch_classes<Bf16<LogitTiles::T256>>(l, st)
                                 : launch_classes<LogitTiles::T256>(l, st)));
@@ -1619,10 +1698,10 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
     a.M = (int32_t)p.H, a.Mq = (int32_t)p.Hq;
     a.row0 = (int32_t)row0, a.Tc = (int32_t)(p.place ? p.T : p.Tc), a.found = r.found;
     a.V = (int32_t)p.V;
-    a.mark = r.mark, a.tiny = tiny;
+    a.mark = r.mark, a.tiny = tiny, a.counts = counts;
     JoinArgs &j = g.jdh;
     j.M = a.M, j.Mq = a.Mq, j.row0 = a.row0, j.Tc = a.Tc, j.found = r.found, j.bf = bf;
-    j.tiny = tiny;
+    j.tiny = tiny, j.counts = counts;
     g.dw = a, g.jdw = j;
     bool join_dh = false, join_dw = false;
     if (c.dh && rows > 0) {
@@ -1665,7 +1744,7 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
     }
     if (g.nsdh || g.nsdw) {
       if (c.totals && last && nsum <= kSumHere) {
-        g.sum = {(const double *)at(p.lsum), nsum, r.found, c.totals, tiny};
+        g.sum = sum;
         summed = nsum > 0;
       }
       FG_TRY(FG_XENT_TILE(launch_products, ProdTiles, p.s2.tile, bf, g, st));
@@ -1676,8 +1755,7 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       FG_TRY(launch_join(g, join_dh, join_dw, st));
   }
   if (c.totals && !summed) {
-    hipLaunchKernelGGL(xent_totals_kernel, dim3(1), dim3(1024), 0, st, (double *)at(p.lsum), nsum,
-                       r.found, c.totals);
+    hipLaunchKernelGGL(xent_totals_kernel, dim3(1), dim3(1024), 0, st, sum);
     FG_TRY(hipGetLastError());
   }
   return hipSuccess;
