@@ -24,9 +24,10 @@ def threshold(p):
     return int(np.floor((1.0 - p) * 65536 + 0.5))
 
 
-def keep(n, seed, step, site, p):
-    """Truth value for each of n elements."""
-    b = np.arange((n + 7) // 8, dtype=np.uint64)
+def keep(n, seed, step, site, p, first=0):
+    """Truth value for each of n elements from `first` (a multiple of 8) on."""
+    assert first % 8 == 0
+    b = np.arange(first // 8, (first + n + 7) // 8, dtype=np.uint64)
     full = lambda v: np.full_like(b, v & 0xFFFFFFFF)
     w = philox((b & _LOW, b >> np.uint64(32), full(step), full(site)),
                (seed & 0xFFFFFFFF, seed >> 32), 7)

@@ -218,10 +218,16 @@ def _p(t):
     return t.data_ptr()
 
 
+_current_stream = None
+
+
 def _s(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        global _current_stream
+        if _current_stream is None:
+            import torch
+            _current_stream = torch.cuda.current_stream
+        return _current_stream().cuda_stream
     return stream
 
 
@@ -464,8 +470,9 @@ def _vector(name, t, n, dtype):
         return None
     if not _types:
         _known()
-    if t.dtype is not _types[dtype] or (t.shape != (n,) and t.numel() != n) or \
-            not t.is_contiguous():
+    if t.dtype is _types[dtype] and t.shape == (n,) and t.stride() == (1,):
+        return t.data_ptr()
+    if t.dtype is not _types[dtype] or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous "
                          f"{'int32' if dtype == _I32 else 'float32'} tensor of {n} elements")
     return t.data_ptr()
@@ -483,11 +490,12 @@ def _counter(name, t):
 
 def _dropout(fn, name, desc, x, y, z, z_name, step_count, stream):
     rows, cols, dtype = desc.rows, desc.cols, desc.dtype
-    _check(name, fn(
-        ctypes.byref(desc), _matrix("x", x, rows, cols, desc.x_ld, dtype),
-        _matrix(z_name, z, rows, cols, desc.z_ld, dtype),
-        _matrix("y", y, rows, cols, desc.y_ld, dtype), _counter("step_count", step_count),
-        _s(stream)))
+    st = fn(ctypes.byref(desc), _matrix("x", x, rows, cols, desc.x_ld, dtype),
+            None if z is None else _matrix(z_name, z, rows, cols, desc.z_ld, dtype),
+            _matrix("y", y, rows, cols, desc.y_ld, dtype),
+            None if step_count is None else _counter("step_count", step_count), _s(stream))
+    if st:
+        raise FgError(name, st)
 
 
 def dropout_fwd(desc, x, y, residual=None, step_count=None, stream=None):
@@ -511,9 +519,10 @@ def _xent_args(desc, h, w, target, loss, lse, totals, weight):
     n, hidden, dtype = desc.rows, desc.hidden, desc.dtype
     return (ctypes.byref(desc), _matrix("h", h, n, hidden, desc.h_ld, dtype),
             _matrix("w", w, desc.vocab, hidden, desc.w_ld, dtype),
-            _vector("target", target, n, _I32), _vector("weight", weight, n, F32),
-            _vector("loss", loss, n, F32), _vector("lse", lse, n, F32),
-            _vector("totals", totals, 2, F32))
+            _vector("target", target, n, _I32),
+            None if weight is None else _vector("weight", weight, n, F32),
+            _vector("loss", loss, n, F32), None if lse is None else _vector("lse", lse, n, F32),
+            None if totals is None else _vector("totals", totals, 2, F32))
 
 
 def linear_xent_fwd(desc, h, w, target, loss, lse=None, totals=None, weight=None, ws=None,

@@ -172,3 +172,22 @@ def test_many_elements_beyond_the_grid():
         fg.dropout_fwd(fg.DropoutDesc.make(rows, cols, 0.5, SEED, step=3), x, y)
         keep = D.keep(rows * cols, SEED, 3, 0, 0.5).reshape(rows, cols)
         same(y.cpu(), expect(x.cpu(), keep, 2))
+
+
+@pytest.mark.parametrize("cols,ld", [(1 << 16, 1 << 16), (65535, 65537)])
+def test_offsets_beyond_32_bits(cols, ld):
+    """More than 2^32 bytes (and 2^31 elements): the first and the last rows."""
+    rows = (1 << 31) // cols + 9
+    x = torch.empty(rows, ld, dtype=torch.float16, device="cuda")[:, :cols]
+    x.fill_(1.0)
+    y = torch.empty(rows, ld, dtype=torch.float16, device="cuda")[:, :cols]
+    d = fg.DropoutDesc.make(rows, cols, 0.5, SEED, site=3, step=1, x_ld=ld, y_ld=ld)
+    fg.dropout_fwd(d, x, y)
+    for r in (0, rows - 4):
+        first = r * cols // 8 * 8
+        keep = D.keep((r + 4) * cols - first, SEED, 1, 3, 0.5, first=first)[r * cols - first:]
+        same(y[r:r + 4].cpu(), expect(x[r:r + 4].cpu(), keep.reshape(4, cols), 2))
+    # about half of all elements are kept (five standard deviations)
+    kept = sum(int(torch.count_nonzero(y[i:i + 4096])) for i in range(0, rows, 4096))
+    n = rows * cols
+    assert abs(kept - n / 2) <= 5 * np.sqrt(n) / 2

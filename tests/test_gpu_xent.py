@@ -330,3 +330,67 @@ def test_gradients_against_differences():
         want = (real * g.double()).sum()
         # the difference's error is of third order in the step; the gradient's 2^-11
         assert abs(float(f1 - f0 - want)) <= 0.02 * abs(float(want)), (float(f1 - f0), float(want))
+
+
+def test_offsets_beyond_32_bits_in_rows():
+    """Features and their gradients of more than 2^32 bytes, few classes: rows at both ends
+    against 64 bits, the weights' gradient against a sum over pieces."""
+    t, h, v = 1_100_003, 2048, 11
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(t, h, generator=g, device="cuda", dtype=torch.bfloat16)
+    w = (torch.randn(v, h, generator=g, device="cuda") / 45).bfloat16()
+    target = torch.randint(-1, v, (t,), generator=g, device="cuda", dtype=torch.int32)
+    out = call(x, w, target, None, mean=False)
+    n = 0
+    dw = torch.zeros(v, h, dtype=torch.float64, device="cuda")
+    bound = torch.zeros_like(dw)
+    for i in range(0, t, 50_000):
+        sl = slice(i, min(t, i + 50_000))
+        o = xent(x[sl], w, target[sl], None, 1.0, False)
+        dw += o["dw"]
+        bound += o["dwa"]
+        n += int(o["live"].sum())
+        if i in (0, 1_100_000):
+            part = {k: out[k][sl] for k in ("loss", "lse", "dh")}
+            part.update(totals=o["totals"], dw=None, flag=out["flag"])
+            check(part, x[sl], w, target[sl], None, "bf16", mean=False, gpu_oracle=True)
+    assert float(out["totals"][1]) == n
+    # roundings of G, of the fp32 sums of a million rows (in parts), of the store
+    err = (out["dw"].double() - dw).abs()
+    assert bool((err <= bound * (2.0 ** -8 + 2.0 ** -11 + 4 * (t / 16 + 64) * U)
+                 + 2.0 ** -8 * dw.abs()).all())
+
+
+def test_offsets_beyond_32_bits_in_classes():
+    """Weights and their gradient of more than 2^32 bytes: classes at both ends."""
+    t, h, v = 9, 1024, 2_200_001
+    g = torch.Generator(device="cuda").manual_seed(2)
+    w = torch.empty(v, h, dtype=torch.float16, device="cuda")
+    for i in range(0, v, 1 << 18):
+        k = min(v, i + (1 << 18)) - i
+        w[i:i + k] = torch.randn(k, h, generator=g, device="cuda").half() / 32
+    x = torch.randn(t, h, generator=g, device="cuda").half()
+    target = torch.tensor([0, v - 1, -1, v, 5, v - 2, 1 << 21, 77, v // 2], dtype=torch.int32,
+                          device="cuda")
+    out = call(x, w, target, None, scale=1024.0)
+    live = (target >= 0) & (target < v)
+    z = torch.cat([x.double() @ w[i:i + (1 << 18)].double().t() for i in range(0, v, 1 << 18)], 1)
+    lse = torch.logsumexp(z, 1)
+    at = target.long().clamp(0, v - 1)[:, None]
+    nll = torch.where(live, lse - z.gather(1, at)[:, 0], torch.zeros_like(lse))
+    # logits of 64 fp32 steps of magnitude below 30, and 300 units of the sum
+    assert float((out["loss"].double() - nll).abs().max()) <= 1e-4
+    p = torch.exp(z - lse[:, None])
+    p.scatter_add_(1, at, -torch.ones_like(nll)[:, None])
+    p *= (live * (1024.0 / float(live.sum())))[:, None]
+    for sl in (slice(0, 300), slice(v - 300, v), slice((1 << 21) - 5, (1 << 21) + 5)):
+        want = p[:, sl].t() @ x.double()
+        mag = p[:, sl].abs().t() @ x.double().abs()
+        err = (out["dw"][sl].double() - want).abs()
+        assert bool((err <= mag * (2.0 ** -10 + 4e-4) + 2.0 ** -11 * want.abs() + 2.0 ** -24).all())
+    dh = sum(p[:, i:i + (1 << 18)] @ w[i:i + (1 << 18)].double() for i in range(0, v, 1 << 18))
+    mag = sum(p[:, i:i + (1 << 18)].abs() @ w[i:i + (1 << 18)].double().abs()
+              for i in range(0, v, 1 << 18))
+    # probabilities of 1 / v: their fp16 values keep all bits (2^15 / v > 2^-14)
+    assert bool(((out["dh"].double() - dh).abs() <= mag * 2e-3 + 2.0 ** -11 * dh.abs()
+                 + 2.0 ** -24).all())
