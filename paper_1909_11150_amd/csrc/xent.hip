@@ -1225,29 +1225,36 @@ __global__ __launch_bounds__(512) void xent_join_kernel(JoinArgs dh, JoinArgs dw
   join_rows(first ? dh : dw, first ? blockIdx.x : blockIdx.x - nh, sh);
 }
 
-// dW of up to 64 rows: a sum of at most 64 terms per element, bound by writing dW. A
-// workgroup (8 waves of 64 x 32) keeps its 256 features of all rows in registers and
-// goes through a range of the classes, 64 at a time, whose G arrives while the ones
-// before are multiplied and stored. 3 rows of 2496 x 21696: 24.6 us (4.4 TB/s), 55 us by
-// the tiles of xent_products_kernel.
+// Gradients that are sums of at most 64 terms per element, bound by being written: dW of
+// up to 64 rows, dh of up to 64 classes (DH). out[n][m] = mult sum_k A[k][m] G, with A
+// the features (weights). A workgroup (8 waves of 64 x 32) keeps 256 columns of A in
+// registers and goes through a range of the rows n, 64 at a time, whose G arrives while
+// the ones before are multiplied and stored. dW of 3 rows, 2496 x 21696: 24.6 us (4.4
+// TB/s), 55 by the tiles of xent_products_kernel; dh of 65536 x 512,
+// 12 classes: 15 us (5 TB/s), where both products by those tiles took 38 and dW's alone
+// take 14; 131073 x 331, 3 classes 105 -> 86 us in all.
 // Below kOuter weights the launch it adds costs more: 11 rows of 128 x 1088 18.7 us in all
 // without it and 24.9 with it, 41 of 287 x 4039 22.8 and 25.1; 7 of 148 x 38444 33.5 and
 // 28.7, 7 of 2432 x 4032 41.9 and 35.4.
 constexpr int64_t kOuter = (int64_t)3 << 20;
 struct OuterArgs {
-  const uint16_t *h;
-  int64_t h_ld;
-  const uint16_t *g;         // [T][Vp]
-  int32_t Vp, V, H, wh;
-  int32_t per;               // chunks of 64 classes of a workgroup
+  const uint16_t *a;
+  int64_t a_ld;
+  int32_t K, cols;           // terms; elements of a row of A, at least 8
+  const uint16_t *g;         // [rows][Vp]
+  int32_t Vp, N, H;          // output rows, columns
+  int32_t per;               // chunks of 64 output rows of a workgroup
   uint16_t *out;
   int64_t out_ld;
-  int32_t *flag;
-  Tiny tiny;
+  int32_t *flag;             // dW
+  const uint64_t *mark;      // dh
+  Tiny tiny;                 // dW: leaves masked rows out
+  Counts counts;
+  const Found *found;
 };
-using POuter = Pipe<64, 2, 4, 2, 256, 64>;  // shapes only: 64 rows deep, 8 waves
+using POuter = Pipe<64, 2, 4, 2, 256, 64>;  // shapes only: 64 terms deep, 8 waves
 
-template <class P>
+template <class P, bool DH>
 __device__ __forceinline__ void outer_tile(const OuterArgs &a, int tm, int tv, uint8_t *stage) {
   __shared__ __attribute__((aligned(1024))) uint8_t sA[P::A_BYTES], sB0[P::B_BYTES],
       sB1[P::B_BYTES];
@@ -1255,30 +1262,45 @@ __device__ __forceinline__ void outer_tile(const OuterArgs &a, int tm, int tv, u
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm0 = (wave / P::WGN) * P::WM, wn0 = (wave % P::WGN) * P::WN;
-  const int m0 = tm * P::TM, c0 = tv * a.per, c1 = min((a.Vp + 63) / 64, c0 + a.per);
+  const int m0 = tm * P::TM, c0 = tv * a.per, c1 = min((a.N + 63) / 64, c0 + a.per);
   if (c0 >= c1) return;
-  uint64_t mark;
-  const float mult = tiny_found(a.tiny, mark).mult;
-  const int T = a.tiny.T;
-  // rows past the last one, and of the features masked ones: zeros
-  const __amdgpu_buffer_rsrc_t rs_h = rsrc(a.h, (uint32_t)((T - 1) * (int)a.h_ld + a.wh) * 2u);
-  const __amdgpu_buffer_rsrc_t rs_g = rsrc(a.g, (uint32_t)(T * a.Vp) * 2u);
+  uint64_t on = ~0ull;  // rows of A that count
+  Counted counted;
+  float mult;
+  if (DH) {
+    counted.load(a.counts);
+    mult = a.counts.n ? counted.found(a.counts).mult : a.found->mult;
+  } else {
+    mult = tiny_found(a.tiny, on).mult;
+  }
+  // rows of A past the last one, and masked ones: zeros
+  const __amdgpu_buffer_rsrc_t rs_a = rsrc(a.a, (uint32_t)((a.K - 1) * (int)a.a_ld + a.cols) * 2u);
   const MnSlot<PA> as = mn_slots<P::RBA, PA>(wave, lane);
-  const MnSlot<PB> bs = mn_slots<P::RBB, PB>(wave, lane);
   auto issue = [&](int c, uint8_t *to) __attribute__((always_inline)) {
+    if constexpr (DH) {  // 64 rows of G, Vp = 64
+      const KmSlot<PB> bs = km_slots<64, PB>(wave, lane);
+      const __amdgpu_buffer_rsrc_t rs_g =
+          rsrc(a.g + (int64_t)64 * c * a.Vp, (uint32_t)(min(64, a.N - 64 * c) * a.Vp) * 2u);
 #pragma unroll
-    for (int jj = 0; jj < PB; ++jj)
-      dma16(rs_g, to + dma_dst<PB>(wave, jj),
-            bs.krow[jj] < T && 64 * c + bs.ncol[jj] < a.Vp
-                ? (unsigned)(bs.krow[jj] * a.Vp + 64 * c + bs.ncol[jj]) * 2u
-                : kOOB);
+      for (int jj = 0; jj < PB; ++jj)
+        dma16(rs_g, to + dma_dst<PB>(wave, jj), (unsigned)(bs.row[jj] * a.Vp + bs.coff[jj]) * 2u);
+    } else {  // 64 columns of G's K rows
+      const MnSlot<PB> bs = mn_slots<P::RBB, PB>(wave, lane);
+      const __amdgpu_buffer_rsrc_t rs_g = rsrc(a.g, (uint32_t)(a.K * a.Vp) * 2u);
+#pragma unroll
+      for (int jj = 0; jj < PB; ++jj)
+        dma16(rs_g, to + dma_dst<PB>(wave, jj),
+              bs.krow[jj] < a.K && 64 * c + bs.ncol[jj] < a.Vp
+                  ? (unsigned)(bs.krow[jj] * a.Vp + 64 * c + bs.ncol[jj]) * 2u
+                  : kOOB);
+    }
   };
   issue(c0, sB0);
 #pragma unroll
   for (int jj = 0; jj < PA; ++jj)
-    dma16(rs_h, sA + dma_dst<PA>(wave, jj),
-          (mark >> as.krow[jj] & 1) && m0 + as.ncol[jj] < a.wh
-              ? (unsigned)(as.krow[jj] * (int)a.h_ld + chunk_at(m0 + as.ncol[jj], a.wh)) * 2u
+    dma16(rs_a, sA + dma_dst<PA>(wave, jj),
+          (on >> as.krow[jj] & 1) && as.krow[jj] < a.K && m0 + as.ncol[jj] < a.cols
+              ? (unsigned)(as.krow[jj] * (int)a.a_ld + chunk_at(m0 + as.ncol[jj], a.cols)) * 2u
               : kOOB);
   wait_vm<0>();
   barrier_nofence();
@@ -1289,6 +1311,7 @@ __device__ __forceinline__ void outer_tile(const OuterArgs &a, int tm, int tv, u
     for (int i = 0; i < P::FM; ++i) fa[ks][i] = frag<64, false, P::RBA>(sA, wm0 + 32 * i, ks, lane);
   bool bad = false;
   auto chunk = [&](int c, const uint8_t *here, uint8_t *next) __attribute__((always_inline)) {
+    const uint64_t mark = DH ? a.mark[c] : ~0ull;
     if (c > c0) {  // this chunk has arrived, and every wave has read the one before
       wait_vm<0>();
       wait_lds();
@@ -1299,10 +1322,10 @@ __device__ __forceinline__ void outer_tile(const OuterArgs &a, int tm, int tv, u
     zero<P>(acc);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      if (16 * ks >= T) break;
+      if (16 * ks >= a.K) break;
 #pragma unroll
       for (int j = 0; j < P::FN; ++j) {
-        const u32x4 fb = frag<64, false, P::RBB>(here, wn0 + 32 * j, ks, lane);
+        const u32x4 fb = frag<64, DH, P::RBB>(here, wn0 + 32 * j, ks, lane);
 #pragma unroll
         for (int i = 0; i < P::FM; ++i)
           acc[i][j] = P::BF ? mfma32_bf16(fa[ks][i], fb, acc[i][j]) : mfma32(fa[ks][i], fb, acc[i][j]);
@@ -1316,33 +1339,36 @@ __device__ __forceinline__ void outer_tile(const OuterArgs &a, int tm, int tv, u
                        pack2(x[4 * g + 2] * mult, x[4 * g + 3] * mult, P::BF)};
         },
         [&](int r, int q, const u32x4 &d) __attribute__((always_inline)) {
-          const int v = 64 * c + wn0 + r, m = m0 + wm0 + q;
-          if (v >= a.V || m >= a.H) return;
+          const int n = 64 * c + wn0 + r, m = m0 + wm0 + q;
+          if (n >= a.N || m >= a.H) return;
           constexpr uint32_t EX = P::BF ? 0x7F80u : 0x7C00u;
+          if (!DH) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) bad |= (d[e >> 1] >> (16 * (e & 1)) & EX) == EX;
-          put_chunk(a.out + (int64_t)v * a.out_ld, m, a.H, d);
+            for (int e = 0; e < 8; ++e) bad |= (d[e >> 1] >> (16 * (e & 1)) & EX) == EX;
+          }
+          put_chunk(a.out + (int64_t)n * a.out_ld, m, a.H,
+                    mark >> (n & 63) & 1 ? d : u32x4{0, 0, 0, 0});
         });
   };
   for (int c = c0; c < c1; c += 2) {
     chunk(c, sB0, sB1);
     if (c + 1 < c1) chunk(c + 1, sB1, sB0);
   }
-  if (a.flag) flag_nonfinite(a.flag, bad);
+  if (!DH && a.flag) flag_nonfinite(a.flag, bad);
 }
 
-// With the join of dh's parts in the first workgroups.
-template <class P>
-__global__ __launch_bounds__(P::NT) void xent_outer_kernel(OuterArgs a, int nm, JoinArgs dh,
-                                                           int nh) {
+// With the join of the other gradient's parts in the first workgroups.
+template <class P, bool DH>
+__global__ __launch_bounds__(P::NT) void xent_outer_kernel(OuterArgs a, int nm, JoinArgs other,
+                                                           int nj) {
   __shared__ __attribute__((aligned(1024))) uint8_t stage[P::NW * 64 * P::WM];
   static_assert(P::NT == 512 && sizeof(stage) >= 16384, "room for the join's workgroups");
-  if ((int)blockIdx.x < nh) {
-    join_rows(dh, blockIdx.x, *reinterpret_cast<float(*)[8][64][8]>(stage));
+  if ((int)blockIdx.x < nj) {
+    join_rows(other, blockIdx.x, *reinterpret_cast<float(*)[8][64][8]>(stage));
     return;
   }
-  const int b = blockIdx.x - nh;
-  outer_tile<P>(a, b % nm, b / nm, stage);
+  const int b = blockIdx.x - nj;
+  outer_tile<P, DH>(a, b % nm, b / nm, stage);
 }
 
 // ---- host ------------------------------------------------------------------------------
@@ -1393,8 +1419,8 @@ Shape pick_tile(int t, int64_t M, int64_t N, int64_t K, bool split, double &us_b
 
 struct Plan {
   int64_t T, H, V, Tp, Hp, Vp, Hq, Tc, pieces, nb, wh, w_ld;
-  bool pad_w, place, classes, outer;  // rows in place; one tile holds all classes; dW by
-                                      // xent_outer_kernel
+  bool pad_w, place, classes, outer, spread;  // rows in place; one tile holds all classes;
+                                              // dW, dh by xent_outer_kernel
   Shape s1, s2, s3;
   int64_t ntile, slot;
   // workspace, bytes
@@ -1421,6 +1447,7 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   p.classes = p.V <= kTileOf[2];
   p.place = p.classes || p.T <= 64;
   p.outer = p.place && !p.classes && p.T > 0 && p.V * p.H >= kOuter;
+  p.spread = p.V <= 64 && p.T * p.H >= kOuter;
   if (p.place) p.pieces = 1, p.Tc = std::max<int64_t>(256, p.Tp);
   const int64_t rows = std::min(p.T, p.Tc);
   double best = 1e300, us, us2;
@@ -1434,6 +1461,7 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
     const Shape a = pick_tile(t, p.H, rows, p.Vp, true, us);
     const Shape b = pick_tile(t, p.H, p.V, rows, true, us2);
     if (p.outer) us2 = 0;
+    if (p.spread) us = 0;
     if (us + us2 < best) best = us + us2, p.s2 = a, p.s3 = b;
   }
   if (p.place && p.s3.kper > 64 * kMarks) {
@@ -1465,6 +1493,7 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   p.tlogit = take(p.classes ? 0 : p.Tc * 4);
   if (grad) {
     p.e = take((size_t)p.Tc * p.Vp * 2);
+    if (p.spread) p.s2.ns = 1;
     p.pdh = take(p.s2.ns > 1 ? (size_t)p.s2.ns * p.Tc * p.Hq * 4 : 0);
     if (p.outer) p.s3.ns = 1;
     p.pdw = take(p.s3.ns > 1 || p.pieces > 1 ? (size_t)p.s3.ns * p.V * p.Hq * 4 : 0);
@@ -1537,16 +1566,16 @@ hipError_t launch_join(Products &a, bool dh, bool dw, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <class P>
-hipError_t launch_outer(Products &a, bool dh, hipStream_t st) {
-  const int nh = dh ? join_blocks(a.jdh, a.rows) : 0;
-  const int nm = (a.outer.H + P::TM - 1) / P::TM, chunks = (a.outer.Vp + 63) / 64;
+template <class P, bool DH>
+hipError_t launch_outer(Products &a, bool join, hipStream_t st) {
+  const int nj = !join ? 0 : DH ? join_blocks(a.jdw, a.dw.V) : join_blocks(a.jdh, a.rows);
+  const int nm = (a.outer.H + P::TM - 1) / P::TM, chunks = (a.outer.N + 63) / 64;
   // some 1024 workgroups, two chunks each at least where there are as many
   const int nv = std::max(1, std::min((chunks + 1) / 2, 1024 / nm));
   a.outer.per = (chunks + nv - 1) / nv;
   const int n = nm * ((chunks + a.outer.per - 1) / a.outer.per);
-  hipLaunchKernelGGL(xent_outer_kernel<P>, dim3((uint32_t)(nh + n)), dim3(P::NT), 0, st, a.outer,
-                     nm, a.jdh, nh);
+  hipLaunchKernelGGL((xent_outer_kernel<P, DH>), dim3((uint32_t)(nj + n)), dim3(P::NT), 0, st,
+                     a.outer, nm, DH ? a.jdw : a.jdh, nj);
   return hipGetLastError();
 }
 
@@ -1704,7 +1733,13 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
     j.tiny = tiny, j.counts = counts;
     g.dw = a, g.jdw = j;
     bool join_dh = false, join_dw = false;
-    if (c.dh && rows > 0) {
+    if (c.dh && rows > 0 && p.spread) {
+      OuterArgs &o = g.outer;
+      o.a = w, o.a_ld = p.w_ld, o.K = (int32_t)p.V, o.cols = (int32_t)p.wh;
+      o.g = a.b, o.Vp = (int32_t)p.Vp, o.N = (int32_t)p.T, o.H = (int32_t)p.H;
+      o.out = (uint16_t *)c.dh, o.out_ld = r.dh_ld;
+      o.mark = r.mark, o.counts = counts, o.found = r.found;
+    } else if (c.dh && rows > 0) {
       const bool split = p.s2.ns > 1;
       g.nsdh = p.s2.ns;
       a.a = w, a.a_ld = p.w_ld, a.a_rows = (int32_t)p.V, a.a_cols = (int32_t)p.wh;
@@ -1720,8 +1755,8 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
     }
     if (c.dw && p.outer) {
       OuterArgs &o = g.outer;
-      o.h = h, o.h_ld = h_ld, o.g = a.b, o.Vp = (int32_t)p.Vp, o.V = (int32_t)p.V;
-      o.H = (int32_t)p.H, o.wh = (int32_t)p.wh;
+      o.a = h, o.a_ld = h_ld, o.K = tiny.T, o.cols = (int32_t)p.wh;
+      o.g = a.b, o.Vp = (int32_t)p.Vp, o.N = (int32_t)p.V, o.H = (int32_t)p.H;
       o.out = (uint16_t *)c.dw, o.out_ld = d.dw_ld ? d.dw_ld : d.hidden;
       o.flag = c.flag, o.tiny = tiny;
     } else if (c.dw) {
@@ -1749,8 +1784,10 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       }
       FG_TRY(FG_XENT_TILE(launch_products, ProdTiles, p.s2.tile, bf, g, st));
     }
-    if (g.outer.out)
-      FG_TRY(bf ? launch_outer<Bf16<POuter>>(g, join_dh, st) : launch_outer<POuter>(g, join_dh, st));
+    if (g.outer.out && p.spread)
+      FG_TRY((bf ? launch_outer<Bf16<POuter>, true> : launch_outer<POuter, true>)(g, join_dw, st));
+    else if (g.outer.out)
+      FG_TRY((bf ? launch_outer<Bf16<POuter>, false> : launch_outer<POuter, false>)(g, join_dh, st));
     else
       FG_TRY(launch_join(g, join_dh, join_dw, st));
   }
