@@ -5,10 +5,8 @@
 //   G = w (exp(l - lse) - onehot),  dh = c G W,  dW = c G^T h
 //
 // Rows whose target is no class (or whose weight is 0) are masked. The live rows
-// are first copied one after another into the workspace (features padded with
-// zeros to a multiple of 64), so masked rows cost no matrix work, whatever they
-// hold, infinities and NaN too, reaches nothing, and every operand of the matrix
-// products is aligned.
+// are first copied one after another into the workspace, so masked rows cost no
+// matrix work, and whatever they hold, infinities and NaN too, reaches nothing.
 //
 // Products run on MFMA tiles fed by LDS DMA (dma_pipe.h), in pieces of the live
 // rows and tiles of the classes:
@@ -27,7 +25,17 @@
 //
 // Up to 256 classes (pixels' classes) one tile holds them all: a single kernel goes
 // from the features to losses and G, and rows stay where they are, masked ones being
-// left out by the DMA (an offset out of range reads zeros).
+// left out by the DMA (an offset out of range reads zeros). Up to 64 rows they stay in
+// place too, and no kernel runs ahead to find the live ones. Sums of at most 64 terms
+// (dW of up to 64 rows, dh of up to 64 classes) have a kernel of their own, bound by
+// writing them.
+//
+// Measured (MI355X, fp16 unless noted; rates count the live rows' three products, or
+// one for losses alone): 8192 x 4096 x 131072 (rows, hidden, classes) bf16 with
+// gradients 22.0 ms (1.14 PFLOP/s; the kernels' clock is held to 1.7 - 1.85 GHz by the
+// board's power); 2048 x 1024 x 32000 0.46 ms (0.83); losses of 4096 x 2048 x 32768
+// 0.46 ms (1.07) and of 48 x 2048 x 65536 bf16 74 us (3.6 TB/s); gradients of
+// 65536 x 512 x 12 56 us (2.3 TB/s).
 #include <algorithm>
 
 #include "dma_pipe.h"
@@ -356,7 +364,7 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(RowArgs a) {
     const int k = 4 * j + wave, r = r0 + k, to = __shfl(place, k);
     const bool on = mask >> k & 1;
     const uint16_t *src = a.h + (int64_t)r * a.h_ld;
-    for (int c = 8 * lane; on && c < a.Hp; c += 512)
+    for (int c = 8 * lane; on && c < a.H; c += 512)
       *reinterpret_cast<u32x4 *>(a.hc + (size_t)to * a.Hp + c) = row8(src, c, a.H);
     if (!on && a.dh && r < a.T)
       for (int c = 8 * lane; c < a.H; c += 512)
