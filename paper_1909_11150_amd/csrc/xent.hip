@@ -72,6 +72,20 @@ struct ProdTiles {
 using PClass32 = Pipe<64, 4, 1, 4, 32, 128>;
 using PClass64 = Pipe<64, 3, 1, 4, 64, 128>;
 
+// Tiles of a band, see tile_map (8192 x 4096 x 131072: logits 3.50 -> 3.38 ms a piece and
+// products 6.94 -> 6.81 against bands of one; of eight 3.41 and 6.90).
+constexpr int kBand = 4;
+// Tile (x, y, part) of n1 tiles along y at place v of the order that tile_map lays down.
+__device__ __forceinline__ bool find_tile(const TileMap &tm, int block, int n1, int &x, int &y,
+                                          int &part) {
+  int i, z;
+  if (!tm.decode(block, i, x, z)) return false;
+  const int nb = (n1 + tm.n0 - 1) / tm.n0;
+  part = z / nb;
+  y = (z - part * nb) * tm.n0 + i;
+  return y < n1;
+}
+
 // What the first kernels find out, read by the others.
 struct Found {
   int32_t live;     // rows
@@ -542,7 +556,7 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
   FG_DMA_RING(P, R);
   constexpr int PA = P::PA, PB = P::PB, BK = P::BK;
   int tx, ty, tz;  // rows, classes
-  if (!tm.decode(blockIdx.x, tx, ty, tz)) return;
+  if (!find_tile(tm, blockIdx.x, (a.V + P::TM - 1) / P::TM, tx, ty, tz)) return;
   const int n0 = tx * P::TN, m0 = ty * P::TM;
   const int rows = a.tiny ? a.Tc : piece_rows(a.found, a.row0, a.Tc);
   if (n0 >= rows) return;
@@ -948,6 +962,7 @@ struct ProdArgs {
   const Found *found;
   const int32_t *idx;        // dh: row of the output
   int32_t V;                 // dW: rows of the output
+  int32_t ntile;             // tiles of rows n
   uint16_t *out;             // null: fp32 sums to part
   int64_t out_ld;
   float *part;               // [parts][rows][Mq]
@@ -966,7 +981,7 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
                                              const Ring &R, uint64_t *marks) {
   constexpr int PA = P::PA, PB = P::PB, BK = P::BK;
   int tx, ty, split;  // hidden, rows (classes), part
-  if (!tm.decode(block, tx, ty, split)) return;
+  if (!find_tile(tm, block, a.ntile, tx, ty, split)) return;
   const int m0 = tx * P::TM, n0 = ty * P::TN;
   const int rows = PLACE ? a.Tc : piece_rows(a.found, a.row0, a.Tc);
   if (DH && n0 >= rows) return;
@@ -1511,8 +1526,13 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   return p;
 }
 
+// Tiles in bands of up to kBand along the second axis (classes, or output rows), in which
+// the first axis comes next and the parts of a sum last: an XCD, which runs some 32
+// tiles at a time, then reads 4 + 8 panels of operands for them and not 16 + 2.
 TileMap tile_map(int64_t n0, int64_t n1, int64_t n2) {
-  return {(int32_t)n0, (int32_t)n1, (int32_t)n2, (int32_t)((n0 * n1 * n2 + 7) / 8), kOutputMajor};
+  const int64_t b = std::min<int64_t>(n1, kBand), nb = (n1 + b - 1) / b;
+  return {(int32_t)b, (int32_t)n0, (int32_t)(nb * n2), (int32_t)((b * n0 * nb * n2 + 7) / 8),
+          kOutputMajor};
 }
 
 template <class P>
@@ -1537,9 +1557,11 @@ struct Products {
 };
 
 template <class P>
-hipError_t launch_products(const Products &a, hipStream_t st) {
-  const TileMap th = tile_map((a.dh.M + P::TM - 1) / P::TM, (a.rows + P::TN - 1) / P::TN, a.nsdh);
-  const TileMap tw = tile_map((a.dw.M + P::TM - 1) / P::TM, (a.dw.V + P::TN - 1) / P::TN, a.nsdw);
+hipError_t launch_products(Products &a, hipStream_t st) {
+  a.dh.ntile = (int32_t)((a.rows + P::TN - 1) / P::TN);
+  a.dw.ntile = (a.dw.V + P::TN - 1) / P::TN;
+  const TileMap th = tile_map((a.dh.M + P::TM - 1) / P::TM, std::max(a.dh.ntile, 1), a.nsdh);
+  const TileMap tw = tile_map((a.dw.M + P::TM - 1) / P::TM, a.dw.ntile, a.nsdw);
   const dim3 grid(8 * (th.per + tw.per)), block(P::NT);
   if constexpr (P::BK == 64) {
     if (a.place) {
