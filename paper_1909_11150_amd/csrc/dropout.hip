@@ -9,15 +9,36 @@
 // its whole battery of tests. One block of 128 bits decides 8 elements, 16 bits
 // each: a 32-bit number per element would double the integer multiplies, which
 // run at a quarter of the VALU rate, for a finer p than 1/65536.
+//
+// Bound by memory: one read, one read of the residual or gate, one write. Measured
+// (MI355X): 65536 x 256 fp16 slices of 1024-wide buffers 11.2 us (6.0 TB/s, as much as a
+// copy of that size, which the caches serve in part), their gated gradients 17.5 us (5.7),
+// 16384 x 4096 bf16 with a residual 73 us (5.5; a 2 GiB copy runs at 5.0), 8191 rows of
+// 1023 of 1030 fp32 14.2 us (4.7).
 #include <algorithm>
 
 #include "dma_pipe.h"
 
 namespace fg {
-
-namespace {
+namespace dropout {
 
 constexpr int kThreads = 256;
+
+// Element types by their code.
+template <int DT>
+struct TypeOf;
+template <>
+struct TypeOf<FG_F16> {
+  using T = _Float16;
+};
+template <>
+struct TypeOf<FG_BF16> {
+  using T = __bf16;
+};
+template <>
+struct TypeOf<FG_F32> {
+  using T = float;
+};
 
 struct Args {
   const void *x, *z;
@@ -110,8 +131,9 @@ __device__ __forceinline__ float apply(float x, float z, bool keep, float scale)
 }
 
 // One block (8 elements) per lane and turn: rows whose blocks are aligned.
-template <class T, int Z>
+template <int DT, int Z>
 __global__ __launch_bounds__(kThreads) void dropout_kernel(Args a) {
+  using T = typename TypeOf<DT>::T;
   const uint32_t step = step_of(a);
   const uint64_t nb = (a.n + 7) / 8, stride = (uint64_t)gridDim.x * kThreads;
   for (uint64_t b = (uint64_t)blockIdx.x * kThreads + threadIdx.x; b < nb; b += stride) {
@@ -143,8 +165,9 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(Args a) {
 // block per lane, and then takes them 64 at a time, so that its accesses are
 // contiguous within a row; each lane fetches its decision from the lane that drew
 // it.
-template <class T, int Z>
+template <int DT, int Z>
 __global__ __launch_bounds__(kThreads) void dropout_any_kernel(Args a) {
+  using T = typename TypeOf<DT>::T;
   const uint32_t step = step_of(a);
   const int lane = threadIdx.x & 63;
   const uint64_t waves = (uint64_t)gridDim.x * (kThreads / 64);
@@ -167,28 +190,29 @@ __global__ __launch_bounds__(kThreads) void dropout_any_kernel(Args a) {
   }
 }
 
-template <class T, int Z>
+template <int DT, int Z>
 hipError_t launch(const Args &a, bool vec, hipStream_t st) {
   const uint64_t per = vec ? (uint64_t)kThreads * 8 : (uint64_t)kThreads / 64 * 512;
   const uint32_t grid = (uint32_t)std::min<uint64_t>((a.n + per - 1) / per, 256 * 32);
   if (vec)
-    hipLaunchKernelGGL((dropout_kernel<T, Z>), dim3(grid), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((dropout_kernel<DT, Z>), dim3(grid), dim3(kThreads), 0, st, a);
   else
-    hipLaunchKernelGGL((dropout_any_kernel<T, Z>), dim3(grid), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((dropout_any_kernel<DT, Z>), dim3(grid), dim3(kThreads), 0, st, a);
   return hipGetLastError();
 }
 
-template <class T>
+template <int DT>
 hipError_t launch_z(const Args &a, int z, bool vec, hipStream_t st) {
-  return z == kGate       ? launch<T, kGate>(a, vec, st)
-         : z == kResidual ? launch<T, kResidual>(a, vec, st)
-                          : launch<T, kPlain>(a, vec, st);
+  return z == kGate       ? launch<DT, kGate>(a, vec, st)
+         : z == kResidual ? launch<DT, kResidual>(a, vec, st)
+                          : launch<DT, kPlain>(a, vec, st);
 }
 
-}  // namespace
+}  // namespace dropout
 
 hipError_t launch_dropout(const fg_dropout_desc &d, const void *x, const void *z, bool gate,
                           void *y, const int32_t *step_count, hipStream_t st) {
+  using namespace dropout;
   Args a{};
   a.x = x, a.z = z, a.y = y, a.step_count = step_count;
   a.xl = d.x_ld ? d.x_ld : d.cols;
@@ -208,9 +232,9 @@ hipError_t launch_dropout(const fg_dropout_desc &d, const void *x, const void *z
   a.cols = vec && dense ? 0 : (uint32_t)d.cols;
   a.div = dma::make_fastdiv(!a.cols ? 1 : vec ? a.cols / 8 : a.cols);
   const int zk = !z ? kPlain : gate ? kGate : kResidual;
-  return d.dtype == FG_F32    ? launch_z<float>(a, zk, vec, st)
-         : d.dtype == FG_BF16 ? launch_z<__bf16>(a, zk, vec, st)
-                              : launch_z<_Float16>(a, zk, vec, st);
+  return d.dtype == FG_F32    ? launch_z<FG_F32>(a, zk, vec, st)
+         : d.dtype == FG_BF16 ? launch_z<FG_BF16>(a, zk, vec, st)
+                              : launch_z<FG_F16>(a, zk, vec, st);
 }
 
 }  // namespace fg
