@@ -62,7 +62,8 @@
  *     every sum is evaluated in a fixed order (no floating-point atomics). A
  *     gradient given less workspace than fg_conv_workspace_bytes() has an
  *     order of its own, also fixed (see there).
- *   - Tensor sizes must stay below 2^31 elements per tensor.
+ *   - Tensor sizes must stay below 2^31 elements per tensor, the classification
+ *     head's calls apart, which count in 64 bits and state limits of their own.
  */
 #ifndef FCNGRAD_H
 #define FCNGRAD_H

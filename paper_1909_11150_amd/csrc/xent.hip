@@ -32,10 +32,10 @@
 //
 // Measured (MI355X, fp16 unless noted; rates count the live rows' three products, or
 // one for losses alone): 8192 x 4096 x 131072 (rows, hidden, classes) bf16 with
-// gradients 22.0 ms (1.14 PFLOP/s; the kernels' clock is held to 1.7 - 1.85 GHz by the
+// gradients 21.5 ms (1.17 PFLOP/s; the kernels' clock is held to 1.6 - 1.85 GHz by the
 // board's power); 2048 x 1024 x 32000 0.46 ms (0.83); losses of 4096 x 2048 x 32768
 // 0.46 ms (1.07) and of 48 x 2048 x 65536 bf16 74 us (3.6 TB/s); gradients of
-// 65536 x 512 x 12 56 us (2.3 TB/s).
+// 65536 x 512 x 12 57 us (2.3 TB/s).
 #include <algorithm>
 
 #include "dma_pipe.h"
