@@ -32,7 +32,7 @@
 //
 // Measured (MI355X, fp16 unless noted; rates count the live rows' three products, or
 // one for losses alone): 8192 x 4096 x 131072 (rows, hidden, classes) bf16 with
-// gradients 21.5 ms (1.17 PFLOP/s; the kernels' clock is held to 1.6 - 1.85 GHz by the
+// gradients 21.1 ms (1.19 PFLOP/s; the kernels' clock is held to 1.6 - 1.85 GHz by the
 // board's power); 2048 x 1024 x 32000 0.46 ms (0.83); losses of 4096 x 2048 x 32768
 // 0.46 ms (1.07) and of 48 x 2048 x 65536 bf16 74 us (3.6 TB/s); gradients of
 // 65536 x 512 x 12 57 us (2.3 TB/s).
@@ -394,6 +394,14 @@ __global__ __launch_bounds__(256) void xent_pad_kernel(const uint16_t *w, int64_
 }
 
 // ---- tiles -----------------------------------------------------------------------
+// A barrier for what waves exchange in LDS: global stores on their way are not waited
+// for (__syncthreads does; at the end of a tile that is a trip to memory).
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("" ::: "memory");
+  wait_lds();
+  barrier_nofence();
+}
+
 // This wave's part of the ring, 64 WM bytes, once every wave is done reading it.
 template <class P>
 __device__ __forceinline__ uint8_t *wave_buf(const Ring &R, int wave) {
@@ -498,6 +506,20 @@ __device__ __forceinline__ void no_class(f32x16 (&acc)[P::FM][P::FN], int v0, in
         for (int j = 0; j < P::FN; ++j) acc[i][j][v] = -INFINITY;
 }
 
+// The logit of class t (counted from this wave's first) of this lane's row, if the lane
+// holds it: selected, one store at the caller's (a branch per element spills its masks).
+template <class P>
+__device__ __forceinline__ bool pick(const f32x16 (&acc)[P::FM][P::FN], int j, int t, int lane,
+                                     float &x) {
+  x = 0.f;
+#pragma unroll
+  for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+      x = t - 4 * (lane >> 5) == 32 * i + 8 * (v >> 2) + (v & 3) ? acc[i][j][v] : x;
+  return t >= 0 && t < P::WM && (t >> 2 & 1) == lane >> 5;
+}
+
 // A tile of logits: oa, ob: this lane's first chunks in the weights' and the
 // features' buffers.
 template <class P>
@@ -579,10 +601,16 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
   for (int jj = 0; jj < PA; ++jj) oa[jj] = (unsigned)(as.row[jj] * (int)a.w_ld + as.coff[jj]) * 2u;
 #pragma unroll
   for (int jj = 0; jj < PB; ++jj) ob[jj] = (unsigned)(bs.row[jj] * a.Hp + bs.coff[jj]) * 2u;
+  int target[P::FN];  // the rows' targets, counted from this wave's first class
+#pragma unroll
+  for (int j = 0; j < P::FN; ++j) {
+    const int n = n0 + wn0 + 32 * j + (lane & 31);
+    target[j] = n < rows ? (int)((unsigned)a.ctarget[n] - (unsigned)(m0 + wm0)) : -1;
+  }
   f32x16 acc[P::FM][P::FN];
   logit_sums<P>(acc, R, rs_w, rs_h, oa, ob, as, bs, a.wh, wave, wm0, wn0, lane);
   if (m0 + P::TM > a.V) no_class<P>(acc, m0 + wm0, a.V, lane);
-  __syncthreads();  // every wave is done reading the ring
+  lds_barrier();  // every wave is done reading the ring
   float *xm = reinterpret_cast<float *>(R.b[0]), *xs = xm + P::WGM * P::TN;
   static_assert(2 * P::WGM * P::TN * 4 <= P::B_BYTES, "exchange fits a stage");
 #pragma unroll
@@ -595,17 +623,13 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
     m = fmaxf(m, __shfl_xor(m, 32));
     if (lane < 32) xm[wm * P::TN + wn0 + 32 * j + lane] = m;
     // the target's logit, where it is one of this wave's classes
-    const int n = n0 + wn0 + 32 * j + (lane & 31);
-    const int t = n < rows ? (int)((unsigned)a.ctarget[n] - (unsigned)(m0 + wm0)) : -1;
+    const int n = n0 + wn0 + 32 * j + (lane & 31), t = target[j];
     if (__any(t >= 0 && t < P::WM)) {
-#pragma unroll
-      for (int i = 0; i < P::FM; ++i)
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (t == 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) a.tlogit[n] = acc[i][j][v];
+      float x;
+      if (pick<P>(acc, j, t, lane, x)) a.tlogit[n] = x;
     }
   }
-  __syncthreads();
+  lds_barrier();
   float up[P::FN], s[P::FN];
 #pragma unroll
   for (int j = 0; j < P::FN; ++j) {
@@ -648,7 +672,7 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
     s[j] += __shfl_xor(s[j], 32);
     if (lane < 32) xs[wm * P::TN + wn0 + 32 * j + lane] = s[j];
   }
-  __syncthreads();
+  lds_barrier();
   for (int p = tid; p < P::TN; p += P::NT) {
     float m = -INFINITY, sum = 0.f;
 #pragma unroll
@@ -701,33 +725,37 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_classes_kernel(ClassArgs a
 #pragma unroll
   for (int jj = 0; jj < PB; ++jj)  // masked rows: zeros
     ob[jj] = live(n0 + bs.row[jj]) ? (unsigned)(bs.row[jj] * (int)a.h_ld + bs.coff[jj]) * 2u : kOOB;
-  f32x16 acc[P::FM][P::FN];
-  logit_sums<P>(acc, R, rs_w, rs_h, oa, ob, as, bs, a.wh, wave, wm0, wn0, lane);
-  if (P::TM > a.V) no_class<P>(acc, wm0, a.V, lane);
-  __syncthreads();  // every wave is done reading the ring
-  float *xm = reinterpret_cast<float *>(R.b[0]), *xs = xm + P::WGM * TN, *xt = xs + P::WGM * TN;
-  double *part = reinterpret_cast<double *>(xt + TN);
-  static_assert((2 * P::WGM + 1) * TN * 4 + P::NW * 12 <= P::B_BYTES, "exchange fits a stage");
   int tg[P::FN];
   float w[P::FN], up[P::FN], s[P::FN];
 #pragma unroll
   for (int j = 0; j < P::FN; ++j) {
-    const int p = wn0 + 32 * j + (lane & 31), n = n0 + p;
+    const int n = n0 + wn0 + 32 * j + (lane & 31);
     const bool on = live(n);
     tg[j] = on ? a.target[n] : -1;
     w[j] = !on ? 0.f : a.weight ? a.weight[n] : 1.f;
+  }
+  const float wmax_inv = a.count ? 1.f : a.found->wmax_inv;
+  f32x16 acc[P::FM][P::FN];
+  logit_sums<P>(acc, R, rs_w, rs_h, oa, ob, as, bs, a.wh, wave, wm0, wn0, lane);
+  if (P::TM > a.V) no_class<P>(acc, wm0, a.V, lane);
+  lds_barrier();  // every wave is done reading the ring
+  float *xm = reinterpret_cast<float *>(R.b[0]), *xs = xm + P::WGM * TN, *xt = xs + P::WGM * TN;
+  double *part = reinterpret_cast<double *>(xt + TN);
+  static_assert((2 * P::WGM + 1) * TN * 4 + P::NW * 12 <= P::B_BYTES, "exchange fits a stage");
+#pragma unroll
+  for (int j = 0; j < P::FN; ++j) {
+    const int p = wn0 + 32 * j + (lane & 31);
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < P::FM; ++i)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        m = fmaxf(m, acc[i][j][v]);
-        if (tg[j] == wm0 + 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) xt[p] = acc[i][j][v];
-      }
+      for (int v = 0; v < 16; ++v) m = fmaxf(m, acc[i][j][v]);
+    float x;
+    if (pick<P>(acc, j, tg[j] - wm0, lane, x)) xt[p] = x;
     m = fmaxf(m, __shfl_xor(m, 32));
     if (lane < 32) xm[wm * TN + p] = m;
   }
-  __syncthreads();
+  lds_barrier();
 #pragma unroll
   for (int j = 0; j < P::FN; ++j) {
     const int p = wn0 + 32 * j + (lane & 31);
@@ -746,9 +774,8 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_classes_kernel(ClassArgs a
     s[j] += __shfl_xor(s[j], 32);
     if (lane < 32) xs[wm * TN + p] = s[j];
   }
-  __syncthreads();
+  lds_barrier();
   double sum = 0;
-  const float wmax_inv = a.count ? 1.f : a.found->wmax_inv;
   float f[P::FN], pt[P::FN];
 #pragma unroll
   for (int j = 0; j < P::FN; ++j) {
@@ -799,7 +826,7 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_classes_kernel(ClassArgs a
       if (lane == 0 && n0 + 64 * g < a.T) a.mark[(n0 >> 6) + g] = mark;
     }
   if (lane == 0) reinterpret_cast<int *>(part + P::NW)[wave] = rows;
-  __syncthreads();
+  lds_barrier();
   if (tid == 0) {
     double t = 0;
     int n = 0;
@@ -992,7 +1019,10 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
   const int wm0 = (wave / P::WGN) * P::WM, wn0 = (wave % P::WGN) * P::WN;
   uint64_t few = 0;  // the marks of a tiny call
   float mult = 0.f;
-  if (PLACE && a.tiny.T) mult = tiny_found(a.tiny, few).mult;
+  if (PLACE && a.tiny.T)
+    mult = tiny_found(a.tiny, few).mult;
+  else if (!PLACE || !a.counts.n)
+    mult = a.found->mult;
   Counted counted;
   if constexpr (PLACE) counted.load(a.counts);
 
@@ -1056,31 +1086,37 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
     for (int j = 0; j < P::FN; ++j) {
       const int n = n0 + wn0 + 32 * j + (lane & 31);
       if (n >= nrow) continue;
+      float *row = part + (size_t)n * a.Mq;
+      const int c = m0 + wm0 + 4 * (lane >> 5);
+      if (a.add) {  // every load on its way before the first sum
+        f32x4 v[P::FM][4];
+#pragma unroll
+        for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int m = c + 32 * i + 8 * g;
+            v[i][g] = *reinterpret_cast<const f32x4 *>(row + (m < a.Mq ? m : 0));
+          }
+#pragma unroll
+        for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] += v[i][r >> 2][r & 3];
+      }
+      if (a.out) continue;
 #pragma unroll
       for (int i = 0; i < P::FM; ++i)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const int m = m0 + wm0 + 32 * i + 8 * g + 4 * (lane >> 5);
-          if (m >= a.Mq) continue;
-          f32x4 *p = reinterpret_cast<f32x4 *>(part + (size_t)n * a.Mq + m);
-          f32x4 v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
-                     acc[i][j][4 * g + 3]};
-          if (a.add) v += *p;
-          if (!a.out) {
-            *p = v;
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] = v[e];
-          }
+          const int m = c + 32 * i + 8 * g;
+          if (m < a.Mq)
+            *reinterpret_cast<f32x4 *>(row + m) = f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1],
+                                                        acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
         }
     }
     if (!a.out) return;
   }
-  __syncthreads();  // every wave is done reading the ring
-  if (PLACE && a.counts.n)
-    mult = counted.found(a.counts).mult;
-  else if (!PLACE || !a.tiny.T)
-    mult = a.found->mult;
+  lds_barrier();  // every wave is done reading the ring
+  if (PLACE && a.counts.n) mult = counted.found(a.counts).mult;
   bool bad = false;
   store16<P>(
       wave_buf<P>(R, wave), lane,
@@ -1395,9 +1431,11 @@ __global__ __launch_bounds__(P::NT) void xent_outer_kernel(OuterArgs a, int nm, 
 }
 
 // ---- host ------------------------------------------------------------------------------
-// The numerators of a piece of rows take at most this much of the workspace. Fewer,
-// longer pieces add the fp32 sums of dW (8 bytes an element of the weights) less
-// often; a gibibyte holds 4096 rows of 131072 classes.
+// The numerators of a piece of rows take at most this much of the workspace; all rows are
+// one piece where theirs take no more than this and the fp32 sums of dW, which several
+// pieces need, would together. Fewer, longer pieces add those sums (8 bytes an element of
+// the weights) less often; a gibibyte holds 4096 rows of 131072 classes. (One piece
+// against two: 8192 x 4096 x 131072 21.1 and 22.2 ms, 5000 x 512 x 131072 2.73 and 3.05.)
 constexpr int64_t kPieceBytes = (int64_t)1 << 30;
 
 constexpr int kTileOf[3] = {64, 128, 256};
@@ -1463,7 +1501,8 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   if (p.pad_w) p.w_ld = 8;
   p.nb = (p.T + kCount - 1) / kCount;
   const int64_t per_row = grad ? p.Vp * 2 : (p.V + 63) / 64 * 8;
-  const int64_t most = std::max<int64_t>(256, kPieceBytes / per_row / 256 * 256);
+  int64_t most = std::max<int64_t>(256, kPieceBytes / per_row / 256 * 256);
+  if (grad && p.Tp * per_row <= kPieceBytes + p.V * p.Hq * 4) most = std::max(most, p.Tp);
   p.pieces = std::max<int64_t>(1, (p.Tp + most - 1) / most);
   p.Tc = std::max<int64_t>(256, up((p.T + p.pieces - 1) / p.pieces, 256));
   p.pieces = std::max<int64_t>(1, (p.T + p.Tc - 1) / p.Tc);
