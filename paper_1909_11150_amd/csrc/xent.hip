@@ -34,7 +34,7 @@
 // one for losses alone): 8192 x 4096 x 131072 (rows, hidden, classes) bf16 with
 // gradients 21.1 ms (1.19 PFLOP/s; the kernels' clock is held to 1.6 - 1.85 GHz by the
 // board's power); 2048 x 1024 x 32000 0.46 ms (0.83); losses of 4096 x 2048 x 32768
-// 0.46 ms (1.07) and of 48 x 2048 x 65536 bf16 74 us (3.6 TB/s); gradients of
+// 0.45 ms (1.09) and of 48 x 2048 x 65536 bf16 56 us (4.8 TB/s); gradients of
 // 65536 x 512 x 12 57 us (2.3 TB/s).
 #include <algorithm>
 
@@ -476,6 +476,7 @@ struct LogitArgs {
   int32_t Hp;             // its stride
   Found *found;
   int32_t tiny;           // rows in place, all Tc of them
+  int32_t stream;         // one tile of rows: each tile of classes begins its sum elsewhere
   int32_t row0, Tc;       // first live row of the piece, rows it may have
   const int32_t *ctarget;
   uint16_t *e;            // [Tc][Vp] numerators, fp16 (STORE)
@@ -506,6 +507,11 @@ __device__ __forceinline__ void no_class(f32x16 (&acc)[P::FM][P::FN], int v0, in
         for (int j = 0; j < P::FN; ++j) acc[i][j][v] = -INFINITY;
 }
 
+template <class P>
+__host__ __device__ __forceinline__ int stages(int wh) {
+  return (wh + P::BK - 1) / P::BK;
+}
+
 // The logit of class t (counted from this wave's first) of this lane's row, if the lane
 // holds it: selected, one store at the caller's (a branch per element spills its masks).
 template <class P>
@@ -521,17 +527,18 @@ __device__ __forceinline__ bool pick(const f32x16 (&acc)[P::FM][P::FN], int j, i
 }
 
 // A tile of logits: oa, ob: this lane's first chunks in the weights' and the
-// features' buffers.
-template <class P>
+// features' buffers. TURN: the sum begins at stage `first` and comes round to it.
+template <class P, bool TURN>
 __device__ __forceinline__ void logit_sums(f32x16 (&acc)[P::FM][P::FN], const Ring &R,
                                            __amdgpu_buffer_rsrc_t rs_w,
                                            __amdgpu_buffer_rsrc_t rs_h,
                                            const unsigned (&oa)[P::PA],
                                            const unsigned (&ob)[P::PB], const KmSlot<P::PA> &as,
-                                           const KmSlot<P::PB> &bs, int wh, int wave, int wm0,
-                                           int wn0, int lane) {
+                                           const KmSlot<P::PB> &bs, int wh, int first, int wave,
+                                           int wm0, int wn0, int lane) {
   constexpr int PA = P::PA, PB = P::PB, BK = P::BK;
-  const int nst = (wh + BK - 1) / BK;
+  const int nst = stages<P>(wh);
+  if (!TURN) first = 0;
   // offsets in the last stage: its last chunk may begin before its place, and chunks
   // past the end are zeros. Selected, not branched to: the main loop's scheduling
   // regions span whole steps (a branch cost 3.5% of the largest product).
@@ -546,8 +553,9 @@ __device__ __forceinline__ void logit_sums(f32x16 (&acc)[P::FM][P::FN], const Ri
   for (int jj = 0; jj < PB; ++jj) lb[jj] = tail(ob[jj], bs.coff[jj]);
   auto issue = [&](int st, int slot) __attribute__((always_inline)) {
     uint8_t *ta = R.a[slot], *tb = R.b[slot];
-    const bool last = st + 1 == nst;
-    const unsigned k0 = 2u * BK * st;
+    const int at = !TURN ? st : st + first < nst ? st + first : st + first - nst;
+    const bool last = at + 1 == nst;
+    const unsigned k0 = 2u * BK * at;
 #pragma unroll
     for (int jj = 0; jj < PB; ++jj)
       dma16(rs_h, tb + dma_dst<PB>(wave, jj), last ? lb[jj] : ob[jj] + k0);
@@ -557,8 +565,8 @@ __device__ __forceinline__ void logit_sums(f32x16 (&acc)[P::FM][P::FN], const Ri
   };
   // the last chunk's repeated elements: zeros in both operands, whatever they are
   auto fix = [&](Frags<P> &f, int it, int ks) __attribute__((always_inline)) {
-    if (it + 1 < nst || wh % 8 == 0) return;
-    const int over = it * BK + 16 * ks + 8 * (lane >> 5) + 8 - wh;  // 1 .. 7: that chunk
+    if (wh % 8 == 0 || it + first + 1 != nst) return;
+    const int over = (nst - 1) * BK + 16 * ks + 8 * (lane >> 5) + 8 - wh;  // 1 .. 7: that chunk
     const int cut = over < 8 ? over : 0;
     u32x4 m;
 #pragma unroll
@@ -608,7 +616,13 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
     target[j] = n < rows ? (int)((unsigned)a.ctarget[n] - (unsigned)(m0 + wm0)) : -1;
   }
   f32x16 acc[P::FM][P::FN];
-  logit_sums<P>(acc, R, rs_w, rs_h, oa, ob, as, bs, a.wh, wave, wm0, wn0, lane);
+  // With one tile of rows the weights stream from memory: where all workgroups read the
+  // same part of rows of a power of two bytes, few memory channels serve them. So each
+  // begins elsewhere: 48 x 2048 x 65536 73.7 -> 55.7 us (4.8 TB/s), 48 x 4096 x 65536 129
+  // -> 107. (Not in the largest tiles, whose products it slows by 2%.)
+  constexpr bool TURN = P::TN < 256;
+  const int first = TURN && a.stream ? (int)(blockIdx.x % (unsigned)stages<P>(a.wh)) : 0;
+  logit_sums<P, TURN>(acc, R, rs_w, rs_h, oa, ob, as, bs, a.wh, first, wave, wm0, wn0, lane);
   if (m0 + P::TM > a.V) no_class<P>(acc, m0 + wm0, a.V, lane);
   lds_barrier();  // every wave is done reading the ring
   float *xm = reinterpret_cast<float *>(R.b[0]), *xs = xm + P::WGM * P::TN;
@@ -657,7 +671,9 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
         [&](int r, int c, const u32x4 &d) __attribute__((always_inline)) {
           const int n = n0 + wn0 + r, v = m0 + wm0 + c;
           if (n < rows && v < a.Vp)
-            *reinterpret_cast<u32x4 *>(a.e + (size_t)n * a.Vp + v) = d;
+            // past the L2, which then keeps the next tiles' operands: 2048 x 1024 x
+            // 32000 in all 470 -> 465 us, 16384 x 768 x 16000 1416 -> 1355
+            __builtin_nontemporal_store(d, reinterpret_cast<u32x4 *>(a.e + (size_t)n * a.Vp + v));
         });
   } else {
 #pragma unroll
@@ -736,7 +752,7 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_classes_kernel(ClassArgs a
   }
   const float wmax_inv = a.count ? 1.f : a.found->wmax_inv;
   f32x16 acc[P::FM][P::FN];
-  logit_sums<P>(acc, R, rs_w, rs_h, oa, ob, as, bs, a.wh, wave, wm0, wn0, lane);
+  logit_sums<P, false>(acc, R, rs_w, rs_h, oa, ob, as, bs, a.wh, 0, wave, wm0, wn0, lane);
   if (P::TM > a.V) no_class<P>(acc, wm0, a.V, lane);
   lds_barrier();  // every wave is done reading the ring
   float *xm = reinterpret_cast<float *>(R.b[0]), *xs = xm + P::WGM * TN, *xt = xs + P::WGM * TN;
@@ -1575,7 +1591,8 @@ TileMap tile_map(int64_t n0, int64_t n1, int64_t n2) {
 }
 
 template <class P>
-hipError_t launch_logits(const LogitArgs &a, int64_t rows, hipStream_t st) {
+hipError_t launch_logits(LogitArgs a, int64_t rows, hipStream_t st) {
+  a.stream = rows <= P::TN;
   const TileMap tm = tile_map((rows + P::TN - 1) / P::TN, (a.V + P::TM - 1) / P::TM, 1);
   if (a.e)
     hipLaunchKernelGGL((xent_logits_kernel<P, true>), dim3(8 * tm.per), dim3(P::NT), 0, st, a, tm);
