@@ -163,7 +163,9 @@ __device__ __forceinline__ Found tiny_found(const Tiny &t, uint64_t &mark) {
   if (on && t.weight) w = t.weight[r];
   on = on && w != 0.f;
   mark = __ballot(on);
-  return make_found(t.mean, t.scale, __popcll(mark), wave_sum(on ? (double)w : 0.0),
+  const int live = __popcll(mark);
+  if (!t.weight) return make_found(t.mean, t.scale, live, (double)live, live ? 1.f : 0.f);
+  return make_found(t.mean, t.scale, live, wave_sum(on ? (double)w : 0.0),
                     wave_max(on ? fabsf(w) : 0.f));
 }
 
@@ -891,6 +893,11 @@ __global__ __launch_bounds__(256) void xent_softmax_kernel(SoftmaxArgs a) {
   if (r0 < rows) {
     const int r = tid / G, g = tid % G, n = r0 + r;
     float m = -INFINITY, s = 0.f;
+    // (loaded beside the tiles' sums, not after them)
+    const bool on = n < rows && (!a.tiny.T || (mark >> n & 1));
+    const float tl = on ? a.tlogit[n] : 0.f;
+    const float w = !on ? 0.f : a.cweight ? a.cweight[n] : 1.f;
+    const int t = on ? a.ctarget[n] : -1;
     if (n < rows)
       for (int p0 = g; p0 < a.ntile; p0 += G * kAhead) {
         float2 x[kAhead];
@@ -900,27 +907,25 @@ __global__ __launch_bounds__(256) void xent_softmax_kernel(SoftmaxArgs a) {
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
           if (p0 + G * k >= a.ntile || x[k].y == 0.f) continue;  // none, or all -inf
-          const float t = fmaxf(m, x[k].x);
-          s = s * __builtin_amdgcn_exp2f(m - t) + x[k].y * __builtin_amdgcn_exp2f(x[k].x - t);
-          m = t;
+          const float top = fmaxf(m, x[k].x);
+          s = s * __builtin_amdgcn_exp2f(m - top) + x[k].y * __builtin_amdgcn_exp2f(x[k].x - top);
+          m = top;
         }
       }
 #pragma unroll
     for (int o = G / 2; o; o >>= 1) {
-      const float m1 = __shfl_xor(m, o), s1 = __shfl_xor(s, o), t = fmaxf(m, m1);
-      s = (s != 0.f ? s * __builtin_amdgcn_exp2f(m - t) : 0.f) +
-          (s1 != 0.f ? s1 * __builtin_amdgcn_exp2f(m1 - t) : 0.f);
-      m = t;
+      const float m1 = __shfl_xor(m, o), s1 = __shfl_xor(s, o), top = fmaxf(m, m1);
+      s = (s != 0.f ? s * __builtin_amdgcn_exp2f(m - top) : 0.f) +
+          (s1 != 0.f ? s1 * __builtin_amdgcn_exp2f(m1 - top) : 0.f);
+      m = top;
     }
     if (g == 0) {
       const float l2 = m + __log2f(s);  // of a row with every logit -inf: -inf
       double d64 = 0;
       lse2[r] = l2;
       if (n < rows) {
-        const bool on = !a.tiny.T || (mark >> n & 1);
-        const float w = !on ? 0.f : a.cweight ? a.cweight[n] : 1.f;
-        const float d = on ? l2 * kLn2 - a.tlogit[n] : 0.f;
-        tg[r] = on ? a.ctarget[n] : -1;
+        const float d = on ? l2 * kLn2 - tl : 0.f;
+        tg[r] = t;
         wt[r] = kUp * w * found.wmax_inv;
         pt[r] = wt[r] * expm1f(-d);  // 2^15 w (p - 1)
         if (first) {
@@ -937,11 +942,13 @@ __global__ __launch_bounds__(256) void xent_softmax_kernel(SoftmaxArgs a) {
       double sum = 0;
       for (int k = 0; k < RS; ++k) sum += part[k];
       a.lsum[blockIdx.x] = sum;
+      if (a.totals && gridDim.x == 1) a.totals[0] = (float)sum, a.totals[1] = found.wsum;
     }
   } else if (first && tid == 0) {
     a.lsum[blockIdx.x] = 0;
+    if (a.totals && gridDim.x == 1) a.totals[0] = 0.f, a.totals[1] = found.wsum;
   }
-  if (a.totals) {  // losses only: the workgroup that comes last sums them up
+  if (a.totals && gridDim.x > 1) {  // losses only: the workgroup that comes last sums them up
     if (tid == 0) {
       __threadfence();
       last = atomicAdd(&a.found->ticket, 1u) + 1u == gridDim.x;
