@@ -189,6 +189,20 @@ def test_any_width(dt, hidden):
         check(call(*x, scale=64.0, dw_ld=ld), *x, dt, scale=64.0)
 
 
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("rows", [64, 65, 127, 200, 256, 257])
+def test_rows_around_those_kept_in_place(dt, rows):
+    """Rows that stay where they are, and that are copied first, with and without weights,
+    from no masked row to nothing else, in narrow rows too."""
+    for hidden, classes, share, weights in ((88, 513, 0.3, True), (3, 300, 0.1, False),
+                                            (200, 1000, 0.0, True), (64, 400, 1.0, True),
+                                            (72, 290, 0.98, False)):
+        print(dt, rows, hidden, classes, share, flush=True)
+        x = inputs(rows, hidden, classes, dt, rows, masked=share, weights=weights, h_ld=hidden + 5)
+        check(call(*x, scale=64.0), *x, dt, scale=64.0)
+        check(call(*x, mean=False, grad=False), *x, dt, mean=False)
+
+
 @pytest.mark.parametrize("share", [0.0, 0.97, 1.0])
 def test_masked_shares(share):
     """From no masked row to nothing else."""
