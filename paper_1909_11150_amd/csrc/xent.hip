@@ -67,10 +67,15 @@ struct LogitTiles {
 struct ProdTiles {
   using T256 = Pipe<32, 5, 2, 4, 256, 256>;
 };
-// Up to 32 and 64 classes, by 128 rows: bound by the features' stream, of which two or
-// three stages are on their way in each of two workgroups per CU.
-using PClass32 = Pipe<64, 4, 1, 4, 32, 128>;
-using PClass64 = Pipe<64, 3, 1, 4, 64, 128>;
+// Up to 32 and 64 classes, by 128 rows: bound by the features' stream. With a workgroup
+// per CU or less (kSparse rows) a deep ring keeps it going; with more, more workgroups
+// per CU and a ring of two: 8192 x 2048 x 20 losses 14.8 us (21.6 with two stages), 262144 x
+// 64 x 12 losses 23.5 (29.4 with four), gradients of 65536 x 512 x 12 46.8 (48.3).
+using PSparse32 = Pipe<64, 4, 1, 4, 32, 128>;
+using PSparse64 = Pipe<64, 3, 1, 4, 64, 128>;
+using PClass32 = Pipe<64, 2, 1, 4, 32, 128>;
+using PClass64 = Pipe<64, 2, 1, 4, 64, 128>;
+constexpr int kSparse = 256 * 128;
 
 // Tiles of a band, see tile_map (8192 x 4096 x 131072: logits 3.50 -> 3.38 ms a piece and
 // products 6.94 -> 6.81 against bands of one; of eight 3.41 and 6.90).
@@ -862,7 +867,6 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_classes_kernel(ClassArgs a
           const int n = n0 + wn0 + r, v = wm0 + c;
           if (n >= a.T || v >= a.Vp) return;
           *reinterpret_cast<u32x4 *>(a.e + (size_t)n * a.Vp + v) = d;
-          if (P::TM < 64) *reinterpret_cast<u32x4 *>(a.e + (size_t)n * a.Vp + v + 32) = {0, 0, 0, 0};
         });
   }
   int rows = 0;
@@ -1092,7 +1096,9 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
   for (int jj = 0; jj < PB; ++jj) {
     if constexpr (DH) {
       const KmSlot<PB> bs = km_slots<BK, PB>(wave, lane);
-      ob[jj] = (unsigned)(bs.row[jj] * (int)a.b_ld + bs.coff[jj]) * 2u;
+      ob[jj] = !PLACE || bs.coff[jj] < a.b_ld  // (rows of 32: half a stage)
+                   ? (unsigned)(bs.row[jj] * (int)a.b_ld + bs.coff[jj]) * 2u
+                   : kOOB;
     } else {
       const MnSlot<PB> bs = mn_slots<P::RBB, PB>(wave, lane);
       ob[jj] = n0 + bs.ncol[jj] < a.N ? (unsigned)(bs.krow[jj] * (int)a.b_ld + bs.ncol[jj]) * 2u
@@ -1391,13 +1397,14 @@ __device__ __forceinline__ void outer_tile(const OuterArgs &a, int tm, int tv, u
   const __amdgpu_buffer_rsrc_t rs_a = rsrc(a.a, (uint32_t)((a.K - 1) * (int)a.a_ld + a.cols) * 2u);
   const MnSlot<PA> as = mn_slots<P::RBA, PA>(wave, lane);
   auto issue = [&](int c, uint8_t *to) __attribute__((always_inline)) {
-    if constexpr (DH) {  // 64 rows of G, Vp = 64
+    if constexpr (DH) {  // 64 rows of G, Vp = 32 or 64
       const KmSlot<PB> bs = km_slots<64, PB>(wave, lane);
       const __amdgpu_buffer_rsrc_t rs_g =
           rsrc(a.g + (int64_t)64 * c * a.Vp, (uint32_t)(min(64, a.N - 64 * c) * a.Vp) * 2u);
 #pragma unroll
       for (int jj = 0; jj < PB; ++jj)
-        dma16(rs_g, to + dma_dst<PB>(wave, jj), (unsigned)(bs.row[jj] * a.Vp + bs.coff[jj]) * 2u);
+        dma16(rs_g, to + dma_dst<PB>(wave, jj),
+              bs.coff[jj] < a.Vp ? (unsigned)(bs.row[jj] * a.Vp + bs.coff[jj]) * 2u : kOOB);
     } else {  // 64 columns of G's K rows
       const MnSlot<PB> bs = mn_slots<P::RBB, PB>(wave, lane);
       const __amdgpu_buffer_rsrc_t rs_g = rsrc(a.g, (uint32_t)(a.K * a.Vp) * 2u);
@@ -1555,7 +1562,8 @@ int64_t up(int64_t n, int64_t unit) { return (n + unit - 1) / unit * unit; }
 Plan make_plan(const fg_xent_desc &d, bool grad) {
   Plan p{};
   p.T = d.rows, p.H = d.hidden, p.V = d.vocab;
-  p.Tp = up(p.T, 256), p.Hp = up(p.H, 64), p.Vp = up(p.V, 64), p.Hq = up(p.H, 8);
+  // (G of up to 32 classes in rows of 32: 262144 x 256 x 12 97.3 -> 89.6 us)
+  p.Tp = up(p.T, 256), p.Hp = up(p.H, 64), p.Vp = p.V <= 32 ? 32 : up(p.V, 64), p.Hq = up(p.H, 8);
   p.w_ld = d.w_ld ? d.w_ld : p.H;
   p.pad_w = p.H < 8;
   p.wh = std::max<int64_t>(p.H, 8);
@@ -1812,10 +1820,15 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       l.e = c.grad ? (uint16_t *)at(p.e) : nullptr, l.Vp = (int32_t)p.Vp;
       l.loss = c.loss, l.lse = c.lse, l.lsum = lsum;
       l.count = counts.n ? (int32_t *)at(p.tcount) : nullptr;
-      FG_TRY(p.V <= 32    ? (bf ? launch_classes<Bf16<PClass32>>(l, st)
-                                : launch_classes<PClass32>(l, st))
-             : p.V <= 64  ? (bf ? launch_classes<Bf16<PClass64>>(l, st)
-                                : launch_classes<PClass64>(l, st))
+      const bool sparse = p.T <= kSparse;
+      FG_TRY(p.V <= 32    ? sparse ? (bf ? launch_classes<Bf16<PSparse32>>(l, st)
+                                         : launch_classes<PSparse32>(l, st))
+                                   : (bf ? launch_classes<Bf16<PClass32>>(l, st)
+                                         : launch_classes<PClass32>(l, st))
+             : p.V <= 64  ? sparse ? (bf ? launch_classes<Bf16<PSparse64>>(l, st)
+                                         : launch_classes<PSparse64>(l, st))
+                                   : (bf ? launch_classes<Bf16<PClass64>>(l, st)
+                                         : launch_classes<PClass64>(l, st))
              : p.V <= 128 ? (bf ? launch_classes<Bf16<P128>>(l, st) : launch_classes<P128>(l, st))
                           : (bf ? launch_classes<Bf16<LogitTiles::T256>>(l, st)
                                 : launch_classes<LogitTiles::T256>(l, st)));
