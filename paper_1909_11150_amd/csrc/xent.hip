@@ -1249,18 +1249,34 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_products_kernel(ProdArgs d
     product_tile<P, false, PLACE>(dw, tw, block - nh, R, marks);
 }
 
-// One workgroup: the sums of the losses and of the weights.
-__global__ __launch_bounds__(1024) void xent_totals_kernel(SumArgs a) {
+// One workgroup: the sums of the losses and of the weights. With counts: unweighted rows of
+// few classes in more tiles than every workgroup adds up, whose live ones it counts for the
+// kernels after it.
+__global__ __launch_bounds__(1024) void xent_totals_kernel(SumArgs a, Counts counts, Found *found) {
   __shared__ double ws[16];
+  __shared__ int cn[16];
   double s = 0;
-  for (int i = threadIdx.x; i < a.n; i += 1024) s += a.lsum[i];
+  int n = 0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < a.n; i += 1024) {
+    s += a.lsum[i];
+    if (counts.n) n += counts.live[i];
+  }
   s = wave_sum(s);
-  if ((threadIdx.x & 63) == 0) ws[threadIdx.x >> 6] = s;
+  n = wave_sum(n);
+  if ((threadIdx.x & 63) == 0) ws[threadIdx.x >> 6] = s, cn[threadIdx.x >> 6] = n;
   __syncthreads();
   if (threadIdx.x < 64) {
-    const float w = weights_sum(a.tiny, a.counts, a.found);
-    for (int k = 1; k < 16; ++k) s += ws[k];
-    if (threadIdx.x == 0) {
+    for (int k = 1; k < 16; ++k) s += ws[k], n += cn[k];
+    float w;
+    if (counts.n) {
+      const Found f = make_found(counts.mean, counts.scale, n, (double)n, 1.f);
+      w = f.wsum;
+      if (threadIdx.x == 0) *found = f;
+    } else {
+      w = weights_sum(a.tiny, a.counts, a.found);
+    }
+    if (threadIdx.x == 0 && a.totals) {
       a.totals[0] = (float)s;
       a.totals[1] = w;
     }
@@ -1618,7 +1634,7 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
   p.cweight = take(moved * p.Tp * 4);
   p.lsum = take(p.pieces * (p.Tc / p.slot) * 8);
   p.mark = take(p.place ? p.Tp / 8 : 0);
-  p.tcount = take(p.classes ? kTiles * 4 : 0);
+  p.tcount = take(p.classes ? (p.T + p.slot - 1) / p.slot * 4 : 0);
   // the products read whole tiles of rows: a tile past the last piece's rows too
   p.hc = take(p.place ? (p.pad_w ? (size_t)p.Tp * 16 : 0) : (size_t)p.pieces * p.Tc * p.Hp * 2);
   p.stats = take(p.classes ? 0 : (size_t)p.ntile * p.Tc * 8);
@@ -1767,9 +1783,10 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
   const bool stay = p.place && !p.classes;
   const int32_t nsum = (int32_t)((p.T + p.slot - 1) / p.slot);
   Counts counts{};
-  if (p.classes && !c.weight && nsum > 0 && nsum <= kTiles)
-    counts = {(int32_t *)at(p.tcount), nsum, d.mean, d.scale};
-  if ((stay && p.T) || counts.n) {  // nothing to find out beforehand
+  Counts many{};  // counted by the classes' kernel, added up by one after it
+  if (p.classes && !c.weight && nsum > 0)
+    (nsum <= kTiles ? counts : many) = {(int32_t *)at(p.tcount), nsum, d.mean, d.scale};
+  if ((stay && p.T) || counts.n || many.n) {  // nothing to find out beforehand
   } else if (p.classes && p.T) {
     hipLaunchKernelGGL(xent_count_kernel, dim3((uint32_t)p.nb), dim3(256), 0, st, r);
     FG_TRY(hipGetLastError());
@@ -1819,7 +1836,7 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       l.found = r.found, l.mark = r.mark, l.target = c.target, l.weight = c.weight;
       l.e = c.grad ? (uint16_t *)at(p.e) : nullptr, l.Vp = (int32_t)p.Vp;
       l.loss = c.loss, l.lse = c.lse, l.lsum = lsum;
-      l.count = counts.n ? (int32_t *)at(p.tcount) : nullptr;
+      l.count = counts.n || many.n ? (int32_t *)at(p.tcount) : nullptr;
       const bool sparse = p.T <= kSparse;
       FG_TRY(p.V <= 32    ? sparse ? (bf ? launch_classes<Bf16<PSparse32>>(l, st)
                                          : launch_classes<PSparse32>(l, st))
@@ -1832,6 +1849,11 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
              : p.V <= 128 ? (bf ? launch_classes<Bf16<P128>>(l, st) : launch_classes<P128>(l, st))
                           : (bf ? launch_classes<Bf16<LogitTiles::T256>>(l, st)
                                 : launch_classes<LogitTiles::T256>(l, st)));
+      if (many.n) {
+        hipLaunchKernelGGL(xent_totals_kernel, dim3(1), dim3(1024), 0, st, sum, many, r.found);
+        FG_TRY(hipGetLastError());
+        summed = true;
+      }
     } else if (rows > 0) {
       LogitArgs l{};
       l.w = w, l.w_ld = p.w_ld, l.wh = (int32_t)p.wh, l.V = (int32_t)p.V;
@@ -1926,7 +1948,7 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       join_dw = split && last;
     }
     if (g.nsdh || g.nsdw) {
-      if (c.totals && last && nsum <= kSumHere) {
+      if (c.totals && last && !summed && nsum <= kSumHere) {
         g.sum = sum;
         summed = nsum > 0;
       }
@@ -1940,7 +1962,7 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
       FG_TRY(launch_join(g, join_dh, join_dw, st));
   }
   if (c.totals && !summed) {
-    hipLaunchKernelGGL(xent_totals_kernel, dim3(1), dim3(1024), 0, st, sum);
+    hipLaunchKernelGGL(xent_totals_kernel, dim3(1), dim3(1024), 0, st, sum, Counts{}, r.found);
     FG_TRY(hipGetLastError());
   }
   return hipSuccess;

@@ -203,6 +203,17 @@ def test_rows_around_those_kept_in_place(dt, rows):
         check(call(*x, mean=False, grad=False), *x, dt, mean=False)
 
 
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("classes", [9, 40, 90, 200])
+def test_many_pixels(dt, classes):
+    """More tiles of rows than every workgroup adds the counts of, and about as many."""
+    for rows, share in ((70_001, 0.3), (140_000, 1.0), (65_536, 0.1), (65_537, 0.1)):
+        print(dt, classes, rows, share, flush=True)
+        x = inputs(rows, 24, classes, dt, rows, masked=share)
+        check(call(*x, scale=64.0), *x, dt, scale=64.0, gpu_oracle=True)
+        check(call(*x, grad=False), *x, dt, gpu_oracle=True)
+
+
 @pytest.mark.parametrize("share", [0.0, 0.97, 1.0])
 def test_masked_shares(share):
     """From no masked row to nothing else."""
