@@ -76,6 +76,12 @@ using PSparse64 = Pipe<64, 3, 1, 4, 64, 128>;
 using PClass32 = Pipe<64, 2, 1, 4, 32, 128>;
 using PClass64 = Pipe<64, 2, 1, 4, 64, 128>;
 constexpr int kSparse = 256 * 128;
+// 65 .. 128 and .. 256 classes by 64 rows while those tiles fit the chip at once, two to a
+// CU: 8543 x 1024 x 86 losses 13.6 us (17.8 by 128 rows), 16000 x 1024 x 200 18.7 (28.9 by
+// 256 rows); 65536 x 512 x 200 would take 28.1, not 24.0.
+using PHalf128 = Pipe<64, 3, 2, 2, 128, 64>;
+using PHalf256 = Pipe<64, 2, 4, 2, 256, 64>;
+constexpr int kHalf = 512 * 64;
 
 // Tiles of a band, see tile_map (8192 x 4096 x 131072: logits 3.50 -> 3.38 ms a piece and
 // products 6.94 -> 6.81 against bands of one; of eight 3.41 and 6.90).
@@ -1617,7 +1623,10 @@ Plan make_plan(const fg_xent_desc &d, bool grad) {
     p.s3.ns = (int)((rows + p.s3.kper - 1) / p.s3.kper);
   }
   // rows of a workgroup of the kernel that finds the losses
-  p.slot = !p.classes ? (p.T <= kFew ? 4 : 16) : p.V <= 128 ? 128 : 256;
+  p.slot = !p.classes ? (p.T <= kFew ? 4 : 16)
+           : p.V > 64 && p.T <= kHalf ? 64
+           : p.V <= 128               ? 128
+                                      : 256;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t was = at;
@@ -1846,6 +1855,10 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
                                          : launch_classes<PSparse64>(l, st))
                                    : (bf ? launch_classes<Bf16<PClass64>>(l, st)
                                          : launch_classes<PClass64>(l, st))
+             : p.slot == 64 ? p.V <= 128 ? (bf ? launch_classes<Bf16<PHalf128>>(l, st)
+                                               : launch_classes<PHalf128>(l, st))
+                                         : (bf ? launch_classes<Bf16<PHalf256>>(l, st)
+                                               : launch_classes<PHalf256>(l, st))
              : p.V <= 128 ? (bf ? launch_classes<Bf16<P128>>(l, st) : launch_classes<P128>(l, st))
                           : (bf ? launch_classes<Bf16<LogitTiles::T256>>(l, st)
                                 : launch_classes<LogitTiles::T256>(l, st)));

@@ -207,7 +207,8 @@ def test_rows_around_those_kept_in_place(dt, rows):
 @pytest.mark.parametrize("classes", [9, 40, 90, 200])
 def test_many_pixels(dt, classes):
     """More tiles of rows than every workgroup adds the counts of, and about as many."""
-    for rows, share in ((70_001, 0.3), (140_000, 1.0), (65_536, 0.1), (65_537, 0.1)):
+    for rows, share in ((70_001, 0.3), (140_000, 1.0), (65_536, 0.1), (65_537, 0.1),
+                        (32_768, 0.2), (32_769, 0.2)):
         print(dt, classes, rows, share, flush=True)
         x = inputs(rows, 24, classes, dt, rows, masked=share)
         check(call(*x, scale=64.0), *x, dt, scale=64.0, gpu_oracle=True)
