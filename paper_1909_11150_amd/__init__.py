@@ -481,8 +481,6 @@ def _vector(name, t, n, dtype):
         return None
     if not _types:
         _known()
-    if t.dtype is _types[dtype] and t.shape == (n,) and t.stride() == (1,):
-        return t.data_ptr()
     if t.dtype is not _types[dtype] or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous "
                          f"{'int32' if dtype == _I32 else 'float32'} tensor of {n} elements")
