@@ -26,16 +26,16 @@
 // Up to 256 classes (pixels' classes) one tile holds them all: a single kernel goes
 // from the features to losses and G, and rows stay where they are, masked ones being
 // left out by the DMA (an offset out of range reads zeros). Up to 64 rows, and up to 256 of
-// small calls, they stay in place too, and no kernel runs ahead to find the live ones. Sums of at most 64 terms
-// (dW of up to 64 rows, dh of up to 64 classes) have a kernel of their own, bound by
-// writing them.
+// small calls, they stay in place too, and no kernel runs ahead to find the live ones. Sums
+// of at most 64 terms (dW of up to 64 rows, dh of up to 64 classes) have a kernel of their
+// own, bound by writing them.
 //
 // Measured (MI355X, fp16 unless noted; rates count the live rows' three products, or
 // one for losses alone): 8192 x 4096 x 131072 (rows, hidden, classes) bf16 with
-// gradients 21.1 ms (1.19 PFLOP/s; the kernels' clock is held to 1.6 - 1.85 GHz by the
-// board's power); 2048 x 1024 x 32000 0.46 ms (0.83); losses of 4096 x 2048 x 32768
+// gradients 20.6 ms (1.22 PFLOP/s; the kernels' clock is held to 1.6 - 1.85 GHz by the
+// board's power); 2048 x 1024 x 32000 0.45 ms (0.85); losses of 4096 x 2048 x 32768
 // 0.45 ms (1.09) and of 48 x 2048 x 65536 bf16 56 us (4.8 TB/s); gradients of
-// 65536 x 512 x 12 57 us (2.3 TB/s).
+// 65536 x 512 x 12 54 us (2.4 TB/s).
 #include <algorithm>
 
 #include "dma_pipe.h"
