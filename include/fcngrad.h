@@ -557,7 +557,8 @@ typedef struct {
  * 0 for an invalid or unsupported descriptor. For gradients it holds 16-bit softmax
  * numerators, of a piece of the rows at a time: at most 1 GiB or 256 rows' of them (up to
  * 256 classes: all rows'; all rows' too where they take no more than 1 GiB and fp32 sums
- * of dw together), and fp32 sums of dw where there is more than one piece or few tiles. Calls that may overlap in time need workspaces of their own. */
+ * of dw together), and fp32 sums of dw where there is more than one piece or few tiles.
+ * Calls that may overlap in time need workspaces of their own. */
 size_t fg_linear_xent_workspace_bytes(const fg_xent_desc *d, int grad);
 
 /* Losses. h: rows x hidden, w: vocab x hidden. target: int32 per row; a row whose

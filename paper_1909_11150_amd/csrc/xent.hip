@@ -1471,7 +1471,8 @@ __device__ __forceinline__ void outer_tile(const OuterArgs &a, int tm, int tv, u
         const u32x4 fb = frag<64, DH, P::RBB>(here, wn0 + 32 * j, ks, lane);
 #pragma unroll
         for (int i = 0; i < P::FM; ++i)
-          acc[i][j] = P::BF ? mfma32_bf16(fa[ks][i], fb, acc[i][j]) : mfma32(fa[ks][i], fb, acc[i][j]);
+          acc[i][j] = P::BF ? mfma32_bf16(fa[ks][i], fb, acc[i][j])
+                            : mfma32(fa[ks][i], fb, acc[i][j]);
       }
     }
     store16<P>(
@@ -1575,8 +1576,8 @@ struct Plan {
   Shape s1, s2, s3;
   int64_t ntile, slot;
   // workspace, bytes
-  size_t count, wsum, wmax, found, mark, tcount, idx, ctarget, cweight, hc, wc, stats, tlogit, e, pdh, pdw,
-      lsum, total;
+  size_t count, wsum, wmax, found, mark, tcount, idx, ctarget, cweight, hc, wc, stats, tlogit,
+      e, pdh, pdw, lsum, total;
 };
 
 int64_t up(int64_t n, int64_t unit) { return (n + unit - 1) / unit * unit; }
