@@ -420,3 +420,43 @@ def test_offsets_beyond_32_bits_in_classes():
     # probabilities of 1 / v: their fp16 values keep all bits (2^15 / v > 2^-14)
     assert bool(((out["dh"].double() - dh).abs() <= mag * 2e-3 + 2.0 ** -11 * dh.abs()
                  + 2.0 ** -24).all())
+
+
+def test_offsets_beyond_32_bits_in_numerators():
+    """One piece of more than 2^32 bytes of numerators (less than fp32 sums of the weights'
+    gradient would add): rows at both ends, and the gradient of some classes over all rows."""
+    t, h, v = 5376, 2048, 400_000
+    assert 2 * t * v > 1 << 32 and 2 * t * v <= (1 << 30) + 4 * v * h
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(t, h, generator=g, device="cuda", dtype=torch.bfloat16)
+    w = torch.empty(v, h, dtype=torch.bfloat16, device="cuda")
+    for i in range(0, v, 50_000):
+        w[i:i + 50_000] = torch.randn(50_000, h, generator=g, device="cuda").bfloat16() / 32
+    target = torch.randint(-20_000, v, (t,), generator=g, device="cuda", dtype=torch.int32)
+    pick = torch.tensor([0, 1, 255, 256, 199_999, v - 1], device="cuda")
+    target[::97] = pick[torch.arange(len(target[::97]), device="cuda") % 6].int()
+    d = fg.XentDesc.make(t, h, v, dtype=fg.BF16)
+    need = fg.linear_xent_workspace_bytes(d, True)
+    # one piece and no fp32 sums of dw (3.3 GB); parts of dh, rows and tiles' sums below 1 GiB
+    assert 2 * t * v < need < 2 * t * v + (1 << 30)
+    out = call(x, w, target, None, mean=False)
+    for sl in (slice(0, 6), slice(t - 10, t)):
+        part = {k: out[k][sl] for k in ("loss", "lse", "dh")}
+        part.update(totals=xent(x[sl], w, target[sl], None, 1.0, False)["totals"], dw=None)
+        check(part, x[sl], w, target[sl], None, "bf16", mean=False, gpu_oracle=True)
+    xd, wd = x.double(), w[pick].double()
+    lse = out["lse"].double()[:, None]
+    hot = (target[:, None] == pick).double()
+    r = ((target >= 0).double())[:, None]
+    G = r * (torch.exp(xd @ wd.t() - lse) - hot)
+    dl = 4 * (h / 16 + 16) * U * (xd.abs() @ wd.abs().t()).max()
+    dlse = dl + 300 * U + 4 * U * (lse.abs().max() + 32)
+    # as in check(); twice the error of lse, which the values here take from the output
+    dg = 2.0 ** -8 + 2.0 ** -11 + 2 * (dl + 2 * dlse) + 16 * U
+    b = G.abs().t() @ xd.abs() * (dg + 4 * (t / 16 + 64) * U + U) + \
+        2.0 ** -39 * xd.abs().sum(0) + (r * hot * (dl + 2 * dlse)).t() @ xd.abs()
+    want = G.t() @ xd
+    b = b * (1 + 2.0 ** -8) + 2.0 ** -8 * want.abs() + TINY["bf16"]
+    err = (out["dw"][pick].double() - want).abs()
+    print(f"dw: {float((err / b).max()):.3f} of the bound")
+    assert bool((err <= b).all())
