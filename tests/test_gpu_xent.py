@@ -460,3 +460,40 @@ def test_offsets_beyond_32_bits_in_numerators():
     err = (out["dw"][pick].double() - want).abs()
     print(f"dw: {float((err / b).max()):.3f} of the bound")
     assert bool((err <= b).all())
+
+
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("size", [(1, 64, 2000), (48, 96, 3000), (200, 64, 500), (900, 64, 300),
+                                  (9000, 64, 300), (3000, 40, 12), (70_000, 24, 100)], ids=str)
+def test_graph_replays_of_every_path(size, grad):
+    """Tickets, counts and marks are made anew by each replay, whatever the workspace holds,
+    and whatever the targets have become."""
+    t, h, v = size
+    x = inputs(t, h, v, "f16", 21)
+    d = fg.XentDesc.make(t, h, v, scale=64.0)
+    ws = torch.full((fg.linear_xent_workspace_bytes(d, grad),), 0xFF, dtype=torch.uint8,
+                    device="cuda")
+    f = lambda *s: torch.zeros(*s, device="cuda")
+    loss, lse, totals = f(t), f(t), f(2)
+    dh, dw = torch.zeros_like(x[0]), torch.zeros_like(x[1])
+    target = x[2].clone()
+    args = (d, x[0], x[1], target, loss)
+    kw = dict(lse=lse, totals=totals, ws=ws)
+    run = (lambda: fg.linear_xent_grad(*args, dh, dw, **kw)) if grad else \
+        (lambda: fg.linear_xent_fwd(*args, **kw))
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        run()
+    for k in range(3):
+        target.copy_(x[2])
+        target[k::5] = -1
+        ref = call(x[0], x[1], target, None, grad=grad, scale=64.0)
+        ws.fill_(255 - k)
+        for a in (loss, lse, totals, dh, dw):
+            a.fill_(5.0)
+        g.replay()
+        torch.cuda.synchronize()
+        got = dict(loss=loss, lse=lse, totals=totals, **(dict(dh=dh, dw=dw) if grad else {}))
+        for name, a in got.items():
+            assert torch.equal(a, ref[name]), (k, name)
