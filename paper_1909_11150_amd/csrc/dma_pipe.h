@@ -365,8 +365,9 @@ __device__ __forceinline__ void sched_mfma_reads_dma() {
 struct NoFold {
   __device__ __forceinline__ void operator()() const {}
 };
-// `fix` may change the fragments of stage it, step ks, before their MFMAs; it is
-// called in the last stages only (the last one among them; no-op by default).
+// `fix` may change the fragments of stage it, step ks, before their MFMAs (no-op by
+// default). It is called in the tail alone: of the stages, counted as they are issued, only
+// the last is sure to be there, so what has to be changed must lie in that one.
 struct NoFix {
   template <class F>
   __device__ __forceinline__ void operator()(F &, int, int) const {}

@@ -567,8 +567,16 @@ __device__ __forceinline__ bool pick(const f32x16 (&acc)[P::FM][P::FN], int j, i
   return t >= 0 && t < P::WM && (t >> 2 & 1) == lane >> 5;
 }
 
+// Stages whose order may turn: all, or all but the last, which `fix` below has to find among
+// the pipeline's last ones where the width is no multiple of 8.
+template <class P>
+__device__ __forceinline__ int turning(int wh) {
+  return stages<P>(wh) - (wh % 8 != 0);
+}
+
 // A tile of logits: oa, ob: this lane's first chunks in the weights' and the
-// features' buffers. TURN: the sum begins at stage `first` and comes round to it.
+// features' buffers. TURN: the sum begins at stage `first` of the turning ones and comes
+// round to it.
 template <class P, bool TURN>
 __device__ __forceinline__ void logit_sums(f32x16 (&acc)[P::FM][P::FN], const Ring &R,
                                            __amdgpu_buffer_rsrc_t rs_w,
@@ -578,8 +586,7 @@ __device__ __forceinline__ void logit_sums(f32x16 (&acc)[P::FM][P::FN], const Ri
                                            const KmSlot<P::PB> &bs, int wh, int first, int wave,
                                            int wm0, int wn0, int lane) {
   constexpr int PA = P::PA, PB = P::PB, BK = P::BK;
-  const int nst = stages<P>(wh);
-  if (!TURN) first = 0;
+  const int nst = stages<P>(wh), turn = turning<P>(wh);
   // offsets in the last stage: its last chunk may begin before its place, and chunks
   // past the end are zeros. Selected, not branched to: the main loop's scheduling
   // regions span whole steps (a branch cost 3.5% of the largest product).
@@ -594,7 +601,8 @@ __device__ __forceinline__ void logit_sums(f32x16 (&acc)[P::FM][P::FN], const Ri
   for (int jj = 0; jj < PB; ++jj) lb[jj] = tail(ob[jj], bs.coff[jj]);
   auto issue = [&](int st, int slot) __attribute__((always_inline)) {
     uint8_t *ta = R.a[slot], *tb = R.b[slot];
-    const int at = !TURN ? st : st + first < nst ? st + first : st + first - nst;
+    const int to = st + first;
+    const int at = !TURN || st >= turn ? st : to < turn ? to : to - turn;
     const bool last = at + 1 == nst;
     const unsigned k0 = 2u * BK * at;
 #pragma unroll
@@ -604,9 +612,10 @@ __device__ __forceinline__ void logit_sums(f32x16 (&acc)[P::FM][P::FN], const Ri
     for (int jj = 0; jj < PA; ++jj)
       dma16(rs_w, ta + dma_dst<PA>(wave, jj), last ? la[jj] : oa[jj] + k0);
   };
-  // the last chunk's repeated elements: zeros in both operands, whatever they are
+  // the last chunk's repeated elements: zeros in both operands, whatever they are (called
+  // in the pipeline's last stages alone: the chunk's stage is its last, turned or not)
   auto fix = [&](Frags<P> &f, int it, int ks) __attribute__((always_inline)) {
-    if (wh % 8 == 0 || it + first + 1 != nst) return;
+    if (wh % 8 == 0 || it + 1 != nst) return;
     const int over = (nst - 1) * BK + 16 * ks + 8 * (lane >> 5) + 8 - wh;  // 1 .. 7: that chunk
     const int cut = over < 8 ? over : 0;
     u32x4 m;
@@ -662,7 +671,8 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_logits_kernel(LogitArgs a,
   // begins elsewhere: 48 x 2048 x 65536 73.7 -> 55.7 us (4.8 TB/s), 48 x 4096 x 65536 129
   // -> 107. (Not in the largest tiles, whose products it slows by 2%.)
   constexpr bool TURN = P::TN < 256;
-  const int first = TURN && a.stream ? (int)(blockIdx.x % (unsigned)stages<P>(a.wh)) : 0;
+  const int first =
+      TURN && a.stream ? (int)(blockIdx.x % (unsigned)max(turning<P>(a.wh), 1)) : 0;
   logit_sums<P, TURN>(acc, R, rs_w, rs_h, oa, ob, as, bs, a.wh, first, wave, wm0, wn0, lane);
   if (m0 + P::TM > a.V) no_class<P>(acc, m0 + wm0, a.V, lane);
   lds_barrier();  // every wave is done reading the ring

@@ -497,3 +497,48 @@ def test_graph_replays_of_every_path(size, grad):
         got = dict(loss=loss, lse=lse, totals=totals, **(dict(dh=dh, dw=dw) if grad else {}))
         for name, a in got.items():
             assert torch.equal(a, ref[name]), (k, name)
+
+
+# One tile of rows: each tile of classes begins its sums elsewhere. Widths of up to 40 stages
+# of 64 that 8 does not divide (and some that it does), classes in more tiles than stages.
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("hidden", [193, 257, 333, 381, 384, 777, 1001, 1037, 2047, 2048, 2500])
+def test_few_rows_of_any_width(dt, hidden):
+    """Losses and gradients of 1 to 128 rows, dense and in wider buffers."""
+    for classes, ld in ((513, 0), (10007, hidden + 5)):
+        h, w, t, _ = inputs(128, hidden, classes, dt, hidden, h_ld=ld, w_ld=ld)
+        t[0], h[0] = classes - 1, h[0].nan_to_num()       # a call of one row has a live one
+        for rows in (1, 3, 48, 64, 65, 100, 128):
+            print(dt, hidden, classes, rows, flush=True)
+            x = (h[:rows], w, t[:rows], None)
+            check(call(*x, scale=64.0), *x, dt, scale=64.0, gpu_oracle=True)
+            check(call(*x, grad=False), *x, dt, gpu_oracle=True)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_few_rows_of_an_odd_width_and_many_classes(dt):
+    """Hundreds of tiles of classes, each starting stage many times."""
+    for rows, hidden, classes in ((48, 2047, 65536), (3, 2500, 21696), (10, 381, 51219),
+                                  (100, 777, 50000)):
+        print(dt, rows, hidden, classes, flush=True)
+        x = inputs(rows, hidden, classes, dt, rows)
+        check(call(*x, scale=64.0), *x, dt, scale=64.0, gpu_oracle=True)
+
+
+def test_equal_classes_have_equal_logits_in_every_tile():
+    """Every row of the weights the same, of small whole numbers, whose sums are exact: the
+    losses are log(classes), whichever tile a class is in."""
+    rng = np.random.default_rng(1)
+    for rows, hidden in ((1, 777), (64, 2047), (128, 333)):
+        h = torch.from_numpy(rng.integers(-3, 4, (rows, hidden)).astype(np.float32)).half().cuda()
+        one = torch.from_numpy(rng.integers(-1, 2, hidden).astype(np.float32)).half().cuda()
+        w = one.expand(20000, hidden).contiguous()
+        t = torch.arange(rows, dtype=torch.int32, device="cuda") * 150
+        out = call(h, w, t, None, grad=False)
+        logit = h.double() @ one.double()
+        # the roundings of lse (and of the loss's difference): 4 units of its magnitude, and
+        # 300 of the sum of exponentials
+        bound = 300 * U + 8 * U * (logit.abs() + 32)
+        err = (out["loss"].double() - float(np.log(20000))).abs()
+        print(rows, hidden, float((err / bound).max()), flush=True)
+        assert bool((err <= bound).all())
