@@ -580,8 +580,10 @@ fg_status linear_xent_fwd(const fg_xent_desc *d, const void *h, const void *w,
 /* Losses, as above, and the gradients of scale * L, each rounded once to dtype:
  * dh (rows x hidden; 0 in masked rows) and dw (vocab x hidden; e.g. a member's place in
  * its gradient group); either may be null. G = weight * (softmax - onehot) is rounded to
- * dtype for the products dh = G w and dw = G^T h, its largest magnitude being scaled to
- * 2^15; their sums are fp32. found_nonfinite (device int32, may be null) is set to 1 if
+ * dtype for the products dh = G w and dw = G^T h, the weights being taken times a power of
+ * two that brings the largest to 2^14 .. 2^15; their sums are fp32, and the factor that the
+ * power leaves, with scale (/ the weights' sum), is too: a bf16 gradient may lose bits where
+ * scale (/ the sum) times the largest |weight| is below 2^-124. found_nonfinite (device int32, may be null) is set to 1 if
  * an element of dw is infinite or NaN, never cleared. With mean and weights that sum to
  * 0 (or no live row) the gradients are 0, as dw is without rows. Deterministic: every
  * sum has a fixed order. Errors as above, and FG_EINVAL if both dh and dw are null. */

@@ -48,7 +48,7 @@ using namespace dma;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // Numerators and G are held times 2^15: the largest is then 2^15, within fp16, and
 // values down to 2^-29 of it keep all their bits (2^-14 otherwise).
-constexpr float kUp = 32768.f;
+constexpr int kUp = 15;
 constexpr int kTickets = 64;    // softmax workgroups up to which the last one sums up
 constexpr int kFew = 1024;      // rows up to which the softmax kernel takes 4 per workgroup
 constexpr int kCount = 1024;    // rows of a workgroup of the counting kernel
@@ -100,7 +100,7 @@ __device__ __forceinline__ bool find_tile(const TileMap &tm, int block, int n1, 
 // What the first kernels find out, read by the others.
 struct Found {
   int32_t live;     // rows
-  float wmax_inv;   // 1 / largest |weight|
+  int32_t wexp;     // weights are taken times 2^wexp: the largest in (2^14, 2^15]
   float mult;       // G W and G^T h times this are the gradients
   float wsum;
   uint32_t ticket;  // workgroups done (losses only)
@@ -152,8 +152,14 @@ __device__ __forceinline__ Found make_found(int mean, double scale, int live, do
                                             float mx) {
   // no live row, or weights that cancel: a mean of nothing has no gradient
   const double den = mean ? sum : 1.0;
-  const float top = mx > 0.f ? mx : 1.f;
-  return {live, 1.f / top, den != 0.0 ? (float)(scale / den * top / kUp) : 0.f, (float)sum, 0};
+  // Weights are brought up by a power of two, which rounds nothing and reaches the smallest
+  // (the reciprocal of one below 2^-128 is infinite). An infinite one leaves no gradient a
+  // number.
+  int e = 0;
+  if (mx > 0.f && frexpf(mx, &e) == 0.5f) --e;  // mx in (2^(e - 1), 2^e]
+  const int wexp = kUp - e;
+  const double mult = den != 0.0 ? ldexp(scale / den, -wexp) : 0.0;
+  return {live, wexp, mx == INFINITY ? NAN : (float)mult, (float)sum, 0};
 }
 __device__ __forceinline__ void put_found(const RowArgs &a, int live, double sum, float mx) {
   *a.found = make_found(a.mean, a.scale, live, sum, mx);
@@ -802,7 +808,7 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_classes_kernel(ClassArgs a
     tg[j] = on ? a.target[n] : -1;
     w[j] = !on ? 0.f : a.weight ? a.weight[n] : 1.f;
   }
-  const float wmax_inv = a.count ? 1.f : a.found->wmax_inv;
+  const int wexp = a.count ? kUp : a.found->wexp;
   f32x16 acc[P::FM][P::FN];
   logit_sums<P, false>(acc, R, rs_w, rs_h, oa, ob, as, bs, a.wh, 0, wave, wm0, wn0, lane);
   if (P::TM > a.V) no_class<P>(acc, wm0, a.V, lane);
@@ -853,7 +859,7 @@ __global__ __launch_bounds__(P::NT, P::WPE) void xent_classes_kernel(ClassArgs a
     for (int k = 1; k < P::WGM; ++k) s[j] += xs[k * TN + p];
     const bool on = tg[j] >= 0;
     const float l2 = __log2f(s[j]) - up[j], d = on ? l2 * kLn2 - xt[p] : 0.f;
-    const float c = kUp * w[j] * wmax_inv;
+    const float c = ldexpf(w[j], wexp);
     f[j] = c / s[j];
     pt[j] = c * expm1f(-d);  // 2^15 w (p - 1)
     if (wm == 0 && lane < 32 && n < a.T) {
@@ -978,7 +984,7 @@ __global__ __launch_bounds__(256) void xent_softmax_kernel(SoftmaxArgs a) {
       if (n < rows) {
         const float d = on ? l2 * kLn2 - tl : 0.f;
         tg[r] = t;
-        wt[r] = kUp * w * found.wmax_inv;
+        wt[r] = ldexpf(w, found.wexp);
         pt[r] = wt[r] * expm1f(-d);  // 2^15 w (p - 1)
         if (first) {
           const int to = a.place ? n : a.idx[n];

@@ -542,3 +542,28 @@ def test_equal_classes_have_equal_logits_in_every_tile():
         err = (out["loss"].double() - float(np.log(20000))).abs()
         print(rows, hidden, float((err / bound).max()), flush=True)
         assert bool((err <= bound).all())
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("size", [(40, 64, 300), (200, 64, 300), (900, 64, 300), (300, 64, 12),
+                                  (70_000, 24, 40)], ids=str)
+def test_weights_below_the_normal_range(dt, size):
+    """Weights of 2^-140 times eighths: a mean's gradients are those of the eighths, bit for
+    bit, since every factor that a common power of two changes is exact; so are the sum's with
+    a scale that takes the power back."""
+    h, w, t, _ = inputs(*size, dt, 17)
+    rng = np.random.default_rng(18)
+    wt = torch.from_numpy(rng.integers(1, 17, size[0]).astype(np.float32) / 8).cuda()
+    wt[::9] = 0.0
+    tiny = wt * 2.0 ** -140
+    assert float(tiny[1]) > 0
+    for mean, scale, back in ((True, 64.0, 1.0), (False, 0.5, 2.0 ** 140)):
+        ref = call(h, w, t, wt, mean=mean, scale=scale)
+        check(ref, h, w, t, wt, dt, mean=mean, scale=scale, gpu_oracle=True)
+        out = call(h, w, t, tiny, mean=mean, scale=scale * back)
+        assert int(out["flag"]) == 0
+        for k in ("lse", "dh", "dw"):
+            assert torch.equal(out[k], ref[k]), (mean, k)
+        # losses are rounded to the subnormal grid, 2^-149
+        err = (out["loss"].double() - ref["loss"].double() * 2.0 ** -140).abs()
+        assert float(err.max()) <= 2.0 ** -149
