@@ -53,6 +53,7 @@ constexpr int kTickets = 64;    // softmax workgroups up to which the last one s
 constexpr int kFew = 1024;      // rows up to which the softmax kernel takes 4 per workgroup
 constexpr int kCount = 1024;    // rows of a workgroup of the counting kernel
 constexpr int kDirect = 8192;   // rows up to which there is none
+constexpr int kWide = 1 << 27;  // rows beyond which a workgroup copies 32, not 16
 
 using P128 = Pipe<64, 2, 2, 2, 128, 128>;  // 4 waves of 64 x 64
 using P64 = Pipe<64, 3, 2, 2, 64, 64>;     // 4 waves of 32 x 32
@@ -1830,7 +1831,13 @@ hipError_t run(const fg_xent_desc &d, const Call &c, void *ws, hipStream_t st) {
     FG_TRY(hipGetLastError());
     hipLaunchKernelGGL(xent_scan_kernel, dim3(1), dim3(1024), 0, st, r);
     FG_TRY(hipGetLastError());
-    hipLaunchKernelGGL(xent_rows_kernel<4>, dim3((uint32_t)((p.T + 15) / 16)), dim3(256), 0, st, r);
+    // 16 rows a workgroup, 32 where 16 would make 2^32 work items, more than a launch holds
+    if (p.T <= kWide)
+      hipLaunchKernelGGL(xent_rows_kernel<4>, dim3((uint32_t)((p.T + 15) / 16)), dim3(256), 0, st,
+                         r);
+    else
+      hipLaunchKernelGGL(xent_rows_kernel<8>, dim3((uint32_t)((p.T + 31) / 32)), dim3(256), 0, st,
+                         r);
     FG_TRY(hipGetLastError());
   }
   const uint16_t *w = (const uint16_t *)c.w;

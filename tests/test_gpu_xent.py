@@ -567,3 +567,25 @@ def test_weights_below_the_normal_range(dt, size):
         # losses are rounded to the subnormal grid, 2^-149
         err = (out["loss"].double() - ref["loss"].double() * 2.0 ** -140).abs()
         assert float(err.max()) <= 2.0 ** -149
+
+
+@pytest.mark.parametrize("v", [11, 257])
+def test_most_rows(v):
+    """One row less than the largest number refused: rows at both ends, and the counts."""
+    t = (1 << 28) - 1
+    w = torch.linspace(-2, 2, v, device="cuda").half()[:, None].contiguous()
+    h = torch.ones(t, 1, dtype=torch.float16, device="cuda")
+    h[1::2] = -0.5
+    target = torch.full((t,), 7, dtype=torch.int32, device="cuda")
+    target[::4] = -1
+    target[-1] = v - 1
+    d = fg.XentDesc.make(t, 1, v)
+    ws = torch.empty(fg.linear_xent_workspace_bytes(d, False), dtype=torch.uint8, device="cuda")
+    loss, totals = torch.full((t,), 7.0, device="cuda"), torch.empty(2, device="cuda")
+    fg.linear_xent_fwd(d, h, w, target, loss, totals=totals, ws=ws)
+    n = 4096
+    for sl in (slice(0, n), slice(t // 2, t // 2 + n), slice(t - n, t)):
+        o = xent(h[sl], w, target[sl])
+        # as in check(): logits 4 * 16 * 2 units, the sum 300, lse (below 8) 4 * 40
+        assert float((loss[sl].double() - o["loss"]).abs().max()) <= 588 * U
+    assert float(totals[1]) == float(np.float32(t - (t + 3) // 4))
