@@ -446,7 +446,9 @@ class _DenseProgram:
         self._shape_ok(nf, L.x_shape)
         dnf = n.dNF["U1"]
         self._shape_ok(dnf, L.x_shape)
-        self._add("F1x1.xent", "xent_logits_kernel", 3 * L.flops, self._L.linear_xent_grad,
+        # up to 256 classes one kernel goes from the features to the losses
+        kernel = "xent_classes_kernel" if n.xent.vocab <= 256 else "xent_logits_kernel"
+        self._add("F1x1.xent", kernel, 3 * L.flops, self._L.linear_xent_grad,
                   (ctypes.byref(n.xent), nf.data_ptr(), n.w["F1x1"].data_ptr(),
                    target.data_ptr(), None, n.pixel_loss.data_ptr(), None,
                    n.totals.data_ptr(), dnf.data_ptr(), n.dw["F1x1"].data_ptr(), None,

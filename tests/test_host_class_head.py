@@ -67,3 +67,15 @@ def test_options_are_checked(no_cuda):  # noqa: F811
     net, t = _net("xent", 0.0)
     with pytest.raises(ValueError, match="int32"):
         net.program(t.long())
+
+
+@pytest.mark.parametrize("classes,kernel", [(5, "xent_classes_kernel"), (256, "xent_classes_kernel"),
+                                            (257, "xent_logits_kernel")])
+def test_class_head_names_the_kernel_it_launches(no_cuda, classes, kernel):  # noqa: F811
+    layers = synth.densenet_layers(n=1, h=32, c_in=32, c0=32, growth=32, levels=2, per_block=2,
+                                   classes=classes)
+    w = [torch.zeros(L.w_shape, dtype=torch.float16) for L in layers]
+    net = DenseNet(layers, w, torch.zeros(layers[0].x_shape, dtype=torch.float16), device="cpu",
+                   loss="xent")
+    calls = net.program(torch.zeros(1, 32, 32, dtype=torch.int32)).calls
+    assert [c.kernel for c in calls if c.label == "F1x1.xent"] == [kernel]
