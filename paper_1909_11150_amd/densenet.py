@@ -35,7 +35,9 @@ Options, both off by default:
     6.2), in place in its slice; its gradient is masked and gated by that output on the
     way out of G, in the pass that gates it by the ReLU otherwise. A layer's mask is a
     function of the seed, the layer's place and ``step_count`` (device int32: the
-    optimizer's, where there is one), drawn again in the backward pass.
+    optimizer's, where there is one), drawn again in the backward pass. Where none is
+    given the network makes one of 0 and leaves it so: masks change as the program that
+    trains it counts ``step_count`` up.
   * ``loss="xent"``: the 1x1 head has a channel per class (``synth.densenet_layers``'s
     classes), the target is an int32 class per pixel (any other number: unlabelled), and
     head, softmax cross entropy and the head's two gradients are one library call, which
@@ -140,6 +142,9 @@ class DenseNet:
         self.dropout, self.seed = float(dropout), int(seed)
         self.step_count = step_count if step_count is not None or not self.dropout else \
             torch.zeros(1, dtype=torch.int32, device=self.dev)
+        if step_count is not None and (not self._int32_here(step_count) or
+                                       step_count.numel() < 1):
+            raise ValueError(f"step_count must be a contiguous int32 tensor on {self.dev}")
         if loss == "xent":   # per-pixel losses; their sum and the labelled pixels' number
             n_, h, w, c = self.L["F1x1"].x_shape
             self.xent = XentDesc.make(n_ * h * w, c, self.L["F1x1"].y_shape[3],
@@ -215,6 +220,11 @@ class DenseNet:
             self.inp[f"{blk}.{l}"] = Slice(z, 0, ld, c0 + (l - 1) * k)
             self.out[f"{blk}.{l}"] = Slice(z, c0 + (l - 1) * k, ld, k) if l < per else \
                 Slice(self.NF[blk], (l - 1) * k, per * k, k)
+
+    def _int32_here(self, t):
+        """Whether kernels may read t's address as int32: its type, layout and device."""
+        return t.dtype == torch.int32 and t.is_contiguous() and \
+            t.device.type == self.dev.type and self.dev.index in (None, t.device.index)
 
     # ---- prepared calls ----------------------------------------------------------
     def program(self, target, streams=2):
@@ -441,8 +451,8 @@ class _DenseProgram:
         n = self.net
         L = n.L["F1x1"]
         npix = n.xent.rows
-        if target.dtype != torch.int32 or target.numel() != npix or not target.is_contiguous():
-            raise ValueError(f"the target must be {npix} contiguous int32 classes")
+        if not n._int32_here(target) or target.numel() != npix:
+            raise ValueError(f"the target must be {npix} contiguous int32 classes on {n.dev}")
         self._shape_ok(nf, L.x_shape)
         dnf = n.dNF["U1"]
         self._shape_ok(dnf, L.x_shape)

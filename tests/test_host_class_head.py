@@ -79,3 +79,15 @@ def test_class_head_names_the_kernel_it_launches(no_cuda, classes, kernel):  # n
                    loss="xent")
     calls = net.program(torch.zeros(1, 32, 32, dtype=torch.int32)).calls
     assert [c.kernel for c in calls if c.label == "F1x1.xent"] == [kernel]
+
+
+def test_addresses_that_kernels_read_are_on_the_device(no_cuda):  # noqa: F811
+    """A step count or a target of another type or device is refused, not read."""
+    for bad in (torch.zeros(1, dtype=torch.int64), torch.zeros(1), torch.zeros(0, dtype=torch.int32),
+                torch.zeros(1, dtype=torch.int32, device="meta")):
+        with pytest.raises(ValueError, match="step_count"):
+            _net("huber", 0.5, step_count=bad)
+    _net("huber", 0.5, step_count=torch.zeros(1, dtype=torch.int32))
+    net, t = _net("xent", 0.0)
+    with pytest.raises(ValueError, match="int32"):
+        net.program(t.to("meta"))
