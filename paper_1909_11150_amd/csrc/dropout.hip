@@ -14,7 +14,9 @@
 // (MI355X): 65536 x 256 fp16 slices of 1024-wide buffers 11.2 us (6.0 TB/s, as much as a
 // copy of that size, which the caches serve in part), their gated gradients 17.5 us (5.7),
 // 16384 x 4096 bf16 with a residual 73 us (5.5; a 2 GiB copy runs at 5.0), 8191 rows of
-// 1023 of 1030 fp32 14.2 us (4.7).
+// 1023 of 1030 fp32 to dense ones 14.2 us (4.7). Strided rows off the 16-byte grid take one
+// element per lane and access: 16383 rows of 4095 of 4099 fp32 131 us (4.1 TB/s), fp16 114 us
+// (2.4), bf16 with a residual 119 us (3.4).
 #include <algorithm>
 
 #include "dma_pipe.h"

@@ -46,8 +46,9 @@ namespace xent {
 using namespace dma;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// Numerators and G are held times 2^15: the largest is then 2^15, within fp16, and
-// values down to 2^-29 of it keep all their bits (2^-14 otherwise).
+// Numerators and G are held times 2^kUp: the largest is then 2^15 (between 2^14 and 2^15
+// where rows have weights), within fp16, and values down to 2^-29 of that keep all their
+// bits (2^-14 otherwise).
 constexpr int kUp = 15;
 constexpr int kTickets = 64;    // softmax workgroups up to which the last one sums up
 constexpr int kFew = 1024;      // rows up to which the softmax kernel takes 4 per workgroup
@@ -78,8 +79,10 @@ using PClass32 = Pipe<64, 2, 1, 4, 32, 128>;
 using PClass64 = Pipe<64, 2, 1, 4, 64, 128>;
 constexpr int kSparse = 256 * 128;
 // 65 .. 128 and .. 256 classes by 64 rows while those tiles fit the chip at once, two to a
-// CU: 8543 x 1024 x 86 losses 13.6 us (17.8 by 128 rows), 16000 x 1024 x 200 18.7 (28.9 by
-// 256 rows); 65536 x 512 x 200 would take 28.1, not 24.0.
+// CU (72 and 80 KiB of LDS each): 8543 x 1024 x 86 losses 13.6 us (17.8 by 128 rows), 32768 x
+// 1024 x 100 18.4 (21.0), 16000 x 1024 x 200 18.7 (28.9 by 256 rows), 17000, 24000 and 32768 x
+// 1024 x 200 20.9, 22.3 and 24.2 (29); beyond that 40000 x 1024 x 100 25.3, not 21.7, and
+// 40000 x 1024 x 200 34.8, not 29.7.
 using PHalf128 = Pipe<64, 3, 2, 2, 128, 64>;
 using PHalf256 = Pipe<64, 2, 4, 2, 256, 64>;
 constexpr int kHalf = 512 * 64;
@@ -214,7 +217,11 @@ __device__ __forceinline__ void find_rows(const Tiny &t, int lane, uint64_t *mar
 }
 
 // Unweighted rows of few classes: the kernel that finds the losses also counts each
-// tile's live rows, and those after it add the counts up.
+// tile's live rows, and those after it add the counts up, every workgroup by itself up to
+// kTiles tiles, beyond by one workgroup in a launch between. With the line at 256, 512 and
+// 1024 tiles, gradients of 12 classes: 32769 x 256 25.7, 23.5 and 24.2 us, 65536 x 512 47.0,
+// 46.0 and 46.0, 65537 x 512 46.6, 47.0 and 45.1, 131073 x 256 48.2, 48.4 and 49.0 (51.6 at
+// 2048).
 constexpr int kTiles = 512;
 struct Counts {
   const int32_t *live;
