@@ -260,7 +260,7 @@ def _checkpoint(x):
     top = wide.abs().amax(dim=2, keepdim=True)
     e = (torch.frexp(top).exponent - 1).clamp_min(-119)
     e = torch.where(top > 0, e, torch.full_like(e, -119))
-    step = torch.ldexp(torch.ones_like(top), e - 6)
+    step = torch.exp2((e - 6).float())      # exact; ldexp is not on the GPU
     q = (wide / step).round_().clamp_(-127, 127)
     return (q * step).view(rows, -1)[:, :cols]
 
