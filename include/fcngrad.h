@@ -592,6 +592,74 @@ fg_status linear_xent_grad(const fg_xent_desc *d, const void *h, const void *w,
                            float *totals, void *dh, void *dw, int32_t *found_nonfinite,
                            void *ws, size_t ws_bytes, hipStream_t stream);
 
+/* ---- residual blocks: 8-bit checkpoints, layer norm, linear ----------------
+ * Rows are pixels' channels (NHWC) or tokens' features; row strides in elements, 0: dense.
+ * rows = 0 is a call with nothing to do (gradients that are sums over the rows become 0)
+ * and per-row pointers may then be null. Offsets are 64-bit. Errors, unless a call says
+ * more: FG_EINVAL for a null pointer, rows < 0, cols < 1, a stride below the width, an
+ * unknown dtype, a pointer not aligned to its elements, an output overlapping another
+ * tensor; FG_EUNSUPPORTED for more than the sizes that a call states, rows * width (rounded
+ * up to 32) of 2^34 or a buffer that spans 2^60 bytes or more; FG_EWORKSPACE for a
+ * workspace that is short or not 16-byte aligned. */
+
+/* An activation kept from the forward to the backward pass in 8 bits. Each 32 consecutive
+ * columns of a row (the last ones may be fewer) share a step of 2^(max(E, -119) - 6), 2^E
+ * being the largest power of two up to their largest finite magnitude; a value is stored as
+ * round(x / step), halves to even, limited to -127 .. 127: off by at most half a step, or one
+ * step above 127.5 steps. Infinities and NaN come back as NaN. `packed` holds
+ * fg_act8_bytes(rows, cols) bytes, 16-byte aligned: the codes, rows of cols rounded up to 32
+ * bytes, then a byte for each 32 columns. */
+typedef struct {
+    int64_t rows, cols, x_ld;
+    int32_t dtype;             /* of x: FG_F16, FG_BF16 or FG_F32 */
+} fg_act8_desc;
+
+/* 0 for negative rows, cols < 1, or sizes beyond the limits above. */
+size_t fg_act8_bytes(int64_t rows, int64_t cols);
+
+/* cols below 2^31. */
+fg_status act8_pack(const fg_act8_desc *d, const void *x, void *packed, hipStream_t stream);
+
+/* The values back, into x; exact where dtype is 16 bits wide and that of the packed tensor, or
+ * FG_F32, else rounded once. */
+fg_status act8_unpack(const fg_act8_desc *d, const void *packed, void *x, hipStream_t stream);
+
+/* Layer norm of each row of up to 16384 columns. */
+typedef struct {
+    int64_t rows, cols;
+    int64_t x_ld, y_ld;        /* of x; of y and dy */
+    int64_t add_ld, dx_ld;
+    double eps;                /* > 0, in fp32 too, and finite */
+    int32_t dtype;             /* every tensor's: FG_F16, FG_BF16 or FG_F32 */
+} fg_norm_desc;
+
+/* y = (x - mean) * rstd * weight + bias, rstd = 1 / sqrt(mean((x - mean)^2) + eps), in fp32,
+ * rounded once. weight and bias (cols elements) may be null (1 and 0). stats (fp32 mean and
+ * rstd per row, 8-byte aligned) and packed (the 8-bit checkpoint of x) may be null. y may be x
+ * itself at the same stride. */
+fg_status layer_norm_fwd(const fg_norm_desc *d, const void *x, const void *weight,
+                         const void *bias, void *y, float *stats, void *packed,
+                         hipStream_t stream);
+
+/* Device workspace of layer_norm_bwd; 0 for an invalid or unsupported descriptor. Calls that
+ * may overlap in time need workspaces of their own. */
+size_t fg_layer_norm_workspace_bytes(const fg_norm_desc *d);
+
+/* The gradients: with g = dy * weight and xh = (x - mean) * rstd,
+ *   dx = add + rstd * (g - mean(g) - xh * mean(g * xh)),
+ *   dweight = sum over the rows of dy * xh, dbias = that of dy,
+ * x being given itself or as its checkpoint (one of x and packed is null), mean and rstd as
+ * layer_norm_fwd wrote them. weight may be null (1), add (another gradient of x) too, and any
+ * of the outputs, if not all. dx may be dy or add itself at the same stride. found_nonfinite
+ * (device int32, may be null) is set to 1 if an element of dweight or dbias is infinite or
+ * NaN, never cleared. Sums in fp32 in a fixed order, each result rounded once. ws may be null
+ * where neither dweight nor dbias is wanted. */
+fg_status layer_norm_bwd(const fg_norm_desc *d, const void *dy, const void *x,
+                         const void *packed, const float *stats, const void *weight,
+                         const void *add, void *dx, void *dweight, void *dbias,
+                         int32_t *found_nonfinite, void *ws, size_t ws_bytes,
+                         hipStream_t stream);
+
 /* Output spatial size: transpose = 0 gives the forward P, Q; 1 gives the
  * transposed convolution's output size. FG_EINVAL if it is not positive. */
 fg_status fg_conv_out_dims(const fg_conv_desc *d, int transpose, int32_t *p,

@@ -33,6 +33,8 @@ ENTRY_POINTS = (
     "conv2d_bwd_weight_noalloc", "fg_mfma_loop",
     "dropout_fwd", "dropout_bwd",
     "linear_xent_fwd", "linear_xent_grad", "fg_linear_xent_workspace_bytes",
+    "act8_pack", "act8_unpack", "fg_act8_bytes",
+    "layer_norm_fwd", "layer_norm_bwd", "fg_layer_norm_workspace_bytes",
 )
 MFMA_LOOP_MAX_WORK = 1 << 28  # blocks * iters accepted by fg_mfma_loop
 MFMA_LOOP_FLOPS_PER_BLOCK_ITER = 1 << 20
@@ -92,6 +94,27 @@ class XentDesc(ctypes.Structure):
     def make(cls, rows, hidden, vocab, dtype=F16, mean=True, scale=1.0, h_ld=0, w_ld=0,
              dh_ld=0, dw_ld=0):
         return cls(rows, h_ld, w_ld, dh_ld, dw_ld, scale, hidden, vocab, dtype, int(mean))
+
+
+class Act8Desc(ctypes.Structure):
+    """fg_act8_desc. Stride 0: dense."""
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("x_ld", ctypes.c_int64),
+                ("dtype", ctypes.c_int32)]
+
+    @classmethod
+    def make(cls, rows, cols, dtype=F16, x_ld=0):
+        return cls(rows, cols, x_ld, dtype)
+
+
+class NormDesc(ctypes.Structure):
+    """fg_norm_desc. Strides 0: dense."""
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("x_ld", ctypes.c_int64),
+                ("y_ld", ctypes.c_int64), ("add_ld", ctypes.c_int64),
+                ("dx_ld", ctypes.c_int64), ("eps", ctypes.c_double), ("dtype", ctypes.c_int32)]
+
+    @classmethod
+    def make(cls, rows, cols, eps=1e-5, dtype=F16, x_ld=0, y_ld=0, add_ld=0, dx_ld=0):
+        return cls(rows, cols, x_ld, y_ld, add_ld, dx_ld, eps, dtype)
 
 
 class LibraryNotBuilt(RuntimeError):
@@ -161,6 +184,10 @@ def lib():
         "dropout_bwd": [ctypes.POINTER(DropoutDesc), vp, vp, vp, vp, vp],
         "linear_xent_fwd": [ctypes.POINTER(XentDesc)] + [vp] * 8 + [sz, vp],
         "linear_xent_grad": [ctypes.POINTER(XentDesc)] + [vp] * 11 + [sz, vp],
+        "act8_pack": [ctypes.POINTER(Act8Desc), vp, vp, vp],
+        "act8_unpack": [ctypes.POINTER(Act8Desc), vp, vp, vp],
+        "layer_norm_fwd": [ctypes.POINTER(NormDesc)] + [vp] * 7,
+        "layer_norm_bwd": [ctypes.POINTER(NormDesc)] + [vp] * 11 + [sz, vp],
         "avg_pool2d_fwd": [vp, i32, i32, i32, i32, vp, vp],
         "avg_pool2d_bwd": [vp, vp, i32, i32, i32, i32, vp, vp],
         "channel_slice_copy": [vp, i32, vp, i32, vp, i32, ctypes.c_int64, i32, i32, vp],
@@ -190,6 +217,10 @@ def lib():
     L.fg_lars_adam_workspace_bytes.restype = ctypes.c_size_t
     L.fg_linear_xent_workspace_bytes.argtypes = [ctypes.POINTER(XentDesc), ctypes.c_int]
     L.fg_linear_xent_workspace_bytes.restype = ctypes.c_size_t
+    L.fg_act8_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64]
+    L.fg_act8_bytes.restype = ctypes.c_size_t
+    L.fg_layer_norm_workspace_bytes.argtypes = [ctypes.POINTER(NormDesc)]
+    L.fg_layer_norm_workspace_bytes.restype = ctypes.c_size_t
     L.fg_conv_workspace_bytes.argtypes = [pdesc, ctypes.c_int]
     L.fg_conv_workspace_bytes.restype = ctypes.c_size_t
     L.fg_conv_kernel_name.argtypes = [pdesc, ctypes.c_int]
@@ -555,6 +586,122 @@ def linear_xent_grad(desc, h, w, target, loss, dh, dw, lse=None, totals=None, we
         _matrix("dh", dh, desc.rows, desc.hidden, desc.dh_ld, desc.dtype),
         _matrix("dw", dw, desc.vocab, desc.hidden, desc.dw_ld, desc.dtype),
         _counter("found_nonfinite", found_nonfinite), wp, wb, _s(stream)))
+
+
+# ---- residual blocks ----------------------------------------------------------
+_device = None   # () -> index of the current device
+
+
+def _here(name, t):
+    """Refuses a tensor that is not on the device whose stream takes the call."""
+    global _device
+    if _device is None:
+        import torch
+        if torch.cuda.is_initialized() or torch.cuda.is_available():
+            _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        else:
+            raise ValueError(f"{name}: no GPU, and the tensor must be on one")
+    if t.get_device() != _device():
+        raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+
+
+def _rows_of(name, t, rows, cols, ld, dtype):
+    if t is None:
+        return None
+    p = _matrix(name, t, rows, cols, ld, dtype)
+    _here(name, t)
+    return p
+
+
+def _bytes(name, t, n):
+    if t is None:
+        return None
+    if t.element_size() != 1 or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous uint8 tensor of {n} bytes")
+    _here(name, t)
+    return t.data_ptr()
+
+
+def _per_channel(name, t, n, dtype):
+    if t is None:
+        return None
+    if not _types:
+        _known()
+    if t.dtype is not _types.get(dtype) or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of {n} elements of the "
+                         "descriptor's type")
+    _here(name, t)
+    return t.data_ptr()
+
+
+def _flag(name, t):
+    if t is None:
+        return None
+    p = _counter(name, t)
+    _here(name, t)
+    return p
+
+
+def act8_bytes(rows, cols):
+    """Bytes of an 8-bit checkpoint of rows x cols values."""
+    return lib().fg_act8_bytes(rows, cols)
+
+
+def _checkpoint(name, t, rows, cols):
+    return None if t is None else _bytes(name, t, lib().fg_act8_bytes(rows, cols))
+
+
+def act8_pack(desc, x, packed, stream=None):
+    """8-bit checkpoint of x (see include/fcngrad.h). packed: uint8 tensor of
+    act8_bytes(desc.rows, desc.cols)."""
+    _check("act8_pack", lib().act8_pack(
+        ctypes.byref(desc), _rows_of("x", x, desc.rows, desc.cols, desc.x_ld, desc.dtype),
+        _checkpoint("packed", packed, desc.rows, desc.cols), _s(stream)))
+
+
+def act8_unpack(desc, packed, x, stream=None):
+    """The values of an 8-bit checkpoint, into x."""
+    _check("act8_unpack", lib().act8_unpack(
+        ctypes.byref(desc), _checkpoint("packed", packed, desc.rows, desc.cols),
+        _rows_of("x", x, desc.rows, desc.cols, desc.x_ld, desc.dtype), _s(stream)))
+
+
+def layer_norm_workspace_bytes(desc):
+    return lib().fg_layer_norm_workspace_bytes(ctypes.byref(desc))
+
+
+def _stats(t, rows):
+    if t is None:
+        return None
+    p = _vector("stats", t, 2 * rows, F32)
+    _here("stats", t)
+    return p
+
+
+def layer_norm_fwd(desc, x, y, weight=None, bias=None, stats=None, packed=None, stream=None):
+    """Layer norm of each row (see include/fcngrad.h). stats: fp32 rows x 2, mean and rstd;
+    packed: the 8-bit checkpoint of x; both for layer_norm_bwd."""
+    n, c, dt = desc.rows, desc.cols, desc.dtype
+    _check("layer_norm_fwd", lib().layer_norm_fwd(
+        ctypes.byref(desc), _rows_of("x", x, n, c, desc.x_ld, dt),
+        _per_channel("weight", weight, c, dt), _per_channel("bias", bias, c, dt),
+        _rows_of("y", y, n, c, desc.y_ld, dt), _stats(stats, n),
+        _checkpoint("packed", packed, n, c), _s(stream)))
+
+
+def layer_norm_bwd(desc, dy, stats, x=None, packed=None, weight=None, add=None, dx=None,
+                   dweight=None, dbias=None, found_nonfinite=None, ws=None, stream=None):
+    """Gradients of layer_norm_fwd from x or its checkpoint `packed`; add: another gradient of
+    x, added to dx. ws: uint8 tensor of layer_norm_workspace_bytes(desc)."""
+    n, c, dt = desc.rows, desc.cols, desc.dtype
+    wp, wb = (None, 0) if ws is None else (_bytes("ws", ws, 0), ws.numel())
+    _check("layer_norm_bwd", lib().layer_norm_bwd(
+        ctypes.byref(desc), _rows_of("dy", dy, n, c, desc.y_ld, dt),
+        _rows_of("x", x, n, c, desc.x_ld, dt), _checkpoint("packed", packed, n, c),
+        _stats(stats, n), _per_channel("weight", weight, c, dt),
+        _rows_of("add", add, n, c, desc.add_ld, dt), _rows_of("dx", dx, n, c, desc.dx_ld, dt),
+        _per_channel("dweight", dweight, c, dt), _per_channel("dbias", dbias, c, dt),
+        _flag("found_nonfinite", found_nonfinite), wp, wb, _s(stream)))
 
 
 def grad_flags_clear(flags, stream=None):

@@ -1074,6 +1074,144 @@ fg_status linear_xent_grad(const fg_xent_desc *d, const void *h, const void *w,
                    ws_bytes, stream);
 }
 
+// ---- residual blocks ---------------------------------------------------------
+namespace {
+
+// A tensor of a call: n rows of `width` elements, `ld` apart.
+struct Region {
+  const void *p;
+  int64_t n, ld, width, esz;
+  bool out;
+  const void *self;  // an input that it may be, element for element
+};
+Region region(const void *p, int64_t n, int64_t ld, int64_t width, int64_t esz, bool out,
+              const void *self = nullptr) {
+  return {p, n, ld ? ld : width, width, esz, out, self};
+}
+
+// Whether a write to one may reach the other: rows of one buffer side by side do not.
+bool collide(const Region &a, const Region &b) {
+  if (!a.p || !b.p || !a.n || !b.n) return false;
+  const int64_t sa = a.ld * a.esz, sb = b.ld * b.esz;
+  if ((a.p == b.self || b.p == a.self) && a.p == b.p && a.width == b.width &&
+      (sa == sb || a.n == 1))
+    return false;
+  if (sa == sb) {
+    const int64_t d = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p), r = (d % sa + sa) % sa;
+    if (a.width * a.esz <= r && r + b.width * b.esz <= sa) return false;
+  }
+  return overlap(a.p, (size_t)((a.n - 1) * a.ld + a.width) * a.esz, b.p,
+                 (size_t)((b.n - 1) * b.ld + b.width) * b.esz);
+}
+
+// Strides, spans, alignment and overlaps of a call's tensors.
+fg_status regions_ok(const Region *t, int n) {
+  for (int i = 0; i < n; ++i)
+    if (t[i].ld < t[i].width || (uintptr_t)t[i].p % t[i].esz) return FG_EINVAL;
+  for (int i = 0; i < n; ++i)
+    if (t[i].n > 1 && t[i].ld >= ((int64_t)1 << 60) / t[i].esz / t[i].n) return FG_EUNSUPPORTED;
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < n; ++j)
+      if (i != j && t[i].out && collide(t[i], t[j])) return FG_EINVAL;
+  return FG_OK;
+}
+
+bool type_ok(int32_t dtype) { return dtype >= FG_F16 && dtype <= FG_F32; }
+int64_t type_size(int32_t dtype) { return dtype == FG_F32 ? 4 : 2; }
+
+// rows x cols, rounded up to a checkpoint's, within 2^34.
+bool act8_fits(int64_t rows, int64_t cols) {
+  return cols < kMaxElems && rows < ((int64_t)1 << 34) / ((cols + 31) / 32 * 32);
+}
+
+fg_status act8_call(const fg_act8_desc *d, const void *x, const void *packed, bool pack,
+                    hipStream_t stream) {
+  if (!d || d->rows < 0 || d->cols < 1 || !type_ok(d->dtype) ||
+      (d->x_ld && d->x_ld < d->cols))
+    return FG_EINVAL;
+  if (!act8_fits(d->rows, d->cols)) return FG_EUNSUPPORTED;
+  if (!d->rows) return FG_OK;
+  if (!x || !packed || ((uintptr_t)packed & 15)) return FG_EINVAL;
+  const Region t[] = {region(x, d->rows, d->x_ld, d->cols, type_size(d->dtype), !pack),
+                      region(packed, 1, 0, (int64_t)act8_size(d->rows, d->cols), 1, pack)};
+  const fg_status ok = regions_ok(t, 2);
+  if (ok != FG_OK) return ok;
+  return launch_status(launch_act8(*d, pack ? x : nullptr, pack ? nullptr : const_cast<void *>(x),
+                                   const_cast<void *>(packed), stream));
+}
+
+fg_status norm_desc_ok(const fg_norm_desc *d) {
+  if (!d || d->rows < 0 || d->cols < 1 || !type_ok(d->dtype) || !((float)d->eps > 0.f) ||
+      !std::isfinite((float)d->eps))
+    return FG_EINVAL;
+  for (int64_t ld : {d->x_ld, d->y_ld, d->add_ld, d->dx_ld})
+    if (ld && ld < d->cols) return FG_EINVAL;
+  return d->cols <= 16384 && act8_fits(d->rows, d->cols) ? FG_OK : FG_EUNSUPPORTED;
+}
+
+}  // namespace
+
+size_t fg_act8_bytes(int64_t rows, int64_t cols) {
+  return rows >= 0 && cols >= 1 && act8_fits(rows, cols) ? act8_size(rows, cols) : 0;
+}
+
+fg_status act8_pack(const fg_act8_desc *d, const void *x, void *packed, hipStream_t stream) {
+  return act8_call(d, x, packed, true, stream);
+}
+
+fg_status act8_unpack(const fg_act8_desc *d, const void *packed, void *x, hipStream_t stream) {
+  return act8_call(d, x, packed, false, stream);
+}
+
+fg_status layer_norm_fwd(const fg_norm_desc *d, const void *x, const void *weight,
+                         const void *bias, void *y, float *stats, void *packed,
+                         hipStream_t stream) {
+  const fg_status valid = norm_desc_ok(d);
+  if (valid != FG_OK) return valid;
+  if (!d->rows) return FG_OK;
+  if (!x || !y || ((uintptr_t)packed & 15)) return FG_EINVAL;
+  const int64_t n = d->rows, c = d->cols, es = type_size(d->dtype);
+  const Region t[] = {region(x, n, d->x_ld, c, es, false), region(weight, 1, 0, c, es, false),
+                      region(bias, 1, 0, c, es, false), region(y, n, d->y_ld, c, es, true, x),
+                      region(stats, 1, 0, n, 8, true),
+                      region(packed, 1, 0, (int64_t)act8_size(n, c), 1, true)};
+  const fg_status ok = regions_ok(t, 6);
+  if (ok != FG_OK) return ok;
+  return launch_status(launch_layer_norm_fwd(*d, x, weight, bias, y, stats, packed, stream));
+}
+
+size_t fg_layer_norm_workspace_bytes(const fg_norm_desc *d) {
+  return norm_desc_ok(d) == FG_OK ? layer_norm_ws_bytes(*d) : 0;
+}
+
+fg_status layer_norm_bwd(const fg_norm_desc *d, const void *dy, const void *x,
+                         const void *packed, const float *stats, const void *weight,
+                         const void *add, void *dx, void *dweight, void *dbias,
+                         int32_t *found_nonfinite, void *ws, size_t ws_bytes,
+                         hipStream_t stream) {
+  const fg_status valid = norm_desc_ok(d);
+  if (valid != FG_OK) return valid;
+  const bool sums = dweight || dbias;
+  if ((x && packed) || (!dx && !sums)) return FG_EINVAL;
+  if (d->rows && (!dy || !stats || (!x && !packed) || ((uintptr_t)packed & 15))) return FG_EINVAL;
+  const size_t need = sums ? layer_norm_ws_bytes(*d) : 0;
+  if (need && (!ws || ws_bytes < need || ((uintptr_t)ws & 15))) return FG_EWORKSPACE;
+  const int64_t n = d->rows, c = d->cols, es = type_size(d->dtype);
+  // dx may be dy or add: as either, it must be clear of the other
+  const Region t[] = {region(dy, n, d->y_ld, c, es, false), region(x, n, d->x_ld, c, es, false),
+                      region(packed, 1, 0, (int64_t)act8_size(n, c), 1, false),
+                      region(stats, 1, 0, n, 8, false), region(weight, 1, 0, c, es, false),
+                      region(add, n, d->add_ld, c, es, false),
+                      region(dx, n, d->dx_ld, c, es, true, dx == dy ? dy : add),
+                      region(dweight, 1, 0, c, es, true), region(dbias, 1, 0, c, es, true),
+                      region(found_nonfinite, 1, 0, 1, 4, true),
+                      region(need ? ws : nullptr, 1, 0, (int64_t)need, 1, true)};
+  const fg_status ok = regions_ok(t, sizeof(t) / sizeof(t[0]));
+  if (ok != FG_OK) return ok;
+  return launch_status(launch_layer_norm_bwd(*d, dy, x, packed, stats, weight, add, dx, dweight,
+                                             dbias, found_nonfinite, ws, stream));
+}
+
 fg_status relu_backward(const uint16_t *dy, const uint16_t *act,
                         uint64_t numel, uint16_t *out, hipStream_t stream) {
   if (!dy || !act || !out || numel == 0) return FG_EINVAL;

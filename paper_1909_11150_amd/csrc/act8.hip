@@ -1,0 +1,81 @@
+// Activations kept in 8 bits from the forward to the backward pass (format: rows.h).
+//
+// Bound by memory: an fp16 element is read in 2 bytes and written in 33/32, and back.
+#include "rows.h"
+
+namespace fg {
+namespace act8 {
+
+using namespace rows;
+
+constexpr int kThreads = 256;
+
+struct Args {
+  const void *x;
+  void *y;
+  int64_t ld;
+  Packed p;
+  uint32_t n;         // chunks of 8 columns
+  int32_t cols;
+  dma::FastDiv div;   // by a row's chunks
+};
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void act8_pack_kernel(Args a) {
+  using T = typename TypeOf<DT>::T;
+  const uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= a.n) return;  // (a.n is a multiple of 4: groups stay whole)
+  const uint32_t row = a.div.div((uint32_t)i);
+  const int c = 8 * (int)((uint32_t)i - row * (uint32_t)(a.p.wide / 8));
+  float v[8];
+  load8(static_cast<const T *>(a.x) + row * a.ld, c, a.cols, v);
+  pack8(a.p, row, c, v);
+}
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void act8_unpack_kernel(Args a) {
+  using T = typename TypeOf<DT>::T;
+  const uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= a.n) return;
+  const uint32_t row = a.div.div((uint32_t)i);
+  const int c = 8 * (int)((uint32_t)i - row * (uint32_t)(a.p.wide / 8));
+  if (c >= a.cols) return;
+  float v[8];
+  decode8(*reinterpret_cast<const u32x2 *>(a.p.codes + (int64_t)row * a.p.wide + c),
+          a.p.exps[(int64_t)row * (a.p.wide / 32) + c / 32], v);
+  store8(static_cast<T *>(a.y) + row * a.ld, c, a.cols, v);
+}
+
+template <int DT>
+hipError_t launch(const Args &a, bool pack, hipStream_t st) {
+  const dim3 grid((uint32_t)((a.n + (uint64_t)kThreads - 1) / kThreads)), block(kThreads);
+  if (pack)
+    hipLaunchKernelGGL(act8_pack_kernel<DT>, grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL(act8_unpack_kernel<DT>, grid, block, 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace act8
+
+size_t act8_size(int64_t rows, int64_t cols) {
+  const int64_t wide = rows::packed_cols(cols);
+  return (size_t)(rows * wide + rows * (wide / 32));
+}
+
+hipError_t launch_act8(const fg_act8_desc &d, const void *x, void *y, void *packed,
+                       hipStream_t st) {
+  act8::Args a{};
+  a.x = x, a.y = y;
+  a.ld = d.x_ld ? d.x_ld : d.cols;
+  a.p = rows::packed_at(packed, d.rows, d.cols);
+  a.n = (uint32_t)(d.rows * (a.p.wide / 8));
+  a.cols = (int32_t)d.cols;
+  a.div = dma::make_fastdiv((uint32_t)(a.p.wide / 8));
+  const bool pack = x != nullptr;
+  return d.dtype == FG_F16    ? act8::launch<FG_F16>(a, pack, st)
+         : d.dtype == FG_BF16 ? act8::launch<FG_BF16>(a, pack, st)
+                              : act8::launch<FG_F32>(a, pack, st);
+}
+
+}  // namespace fg

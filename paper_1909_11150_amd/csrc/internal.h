@@ -191,6 +191,19 @@ hipError_t launch_linear_xent(const fg_xent_desc &d, const void *h, const void *
                               float *lse, float *totals, void *dh, void *dw, int32_t *flag,
                               bool grad, void *ws, hipStream_t st);
 
+size_t act8_size(int64_t rows, int64_t cols);
+// Packs x, or (x null) unpacks into y.
+hipError_t launch_act8(const fg_act8_desc &d, const void *x, void *y, void *packed,
+                       hipStream_t st);
+hipError_t launch_layer_norm_fwd(const fg_norm_desc &d, const void *x, const void *weight,
+                                 const void *bias, void *y, float *stats, void *packed,
+                                 hipStream_t st);
+size_t layer_norm_ws_bytes(const fg_norm_desc &d);
+hipError_t launch_layer_norm_bwd(const fg_norm_desc &d, const void *dy, const void *x,
+                                 const void *packed, const float *stats, const void *weight,
+                                 const void *add, void *dx, void *dweight, void *dbias,
+                                 int32_t *flag, void *ws, hipStream_t st);
+
 // One-shot profiling events (fg_profile_next_launch): prof_begin records the
 // armed start event on the stream, prof_end the stop event, then disarms.
 // Both do nothing when no events are armed.

@@ -1,0 +1,118 @@
+// Layer norm of rows, and its gradients.
+//
+//   y = (x - mean) rstd w + b,  rstd = (mean((x - mean)^2) + eps)^(-1/2)
+//   g = dy w,  xh = (x - mean) rstd
+//   dx = add + rstd (g - mean(g) - xh mean(g xh)),  dw = sum dy xh,  db = sum dy
+//
+// Bound by memory. A team of lanes takes a row whole into registers, 8 columns a lane and
+// chunk: 8 to 64 lanes of a wave, then 2 to 8 waves. So a row is read once, its mean and the
+// squares about it are summed from registers (no difference of large sums), and the next
+// row's loads are on their way meanwhile. The gradients of weight and bias are summed down
+// the rows in registers, a team's columns being always the same, then over a workgroup's
+// teams in LDS; the workgroups' sums go to the workspace and a second kernel adds them in
+// order. Everything is summed in fp32 and in a fixed order.
+#include <algorithm>
+
+#include "norm.h"
+
+namespace fg {
+namespace norm {
+
+template <int DT, int TL, int W, int N>
+__global__ __launch_bounds__((Team<TL, W, N>::NT)) void norm_fwd_kernel(FwdArgs a) {
+  using T = typename TypeOf<DT>::T;
+  using M = Team<TL, W, N>;
+  __shared__ float red[W > 1 ? 2 * M::NT / 64 : 1];
+  const int t = threadIdx.x % M::TEAM, team = threadIdx.x / M::TEAM, cols = a.cols;
+  const T *x = static_cast<const T *>(a.x), *w = static_cast<const T *>(a.weight),
+          *b = static_cast<const T *>(a.bias);
+  T *y = static_cast<T *>(a.y);
+  Raw<T> rw[N], rb[N], next[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int c = M::col(t, n);
+    if (w) rw[n] = load_any(w, c, cols);
+    if (b) rb[n] = load_any(b, c, cols);
+  }
+  const int64_t step = (int64_t)gridDim.x * M::TEAMS;
+  int64_t r0 = (int64_t)blockIdx.x * M::TEAMS;
+  auto load = [&](int64_t r) __attribute__((always_inline)) {
+    const T *row = x + min(r, a.rows - 1) * a.x_ld;
+#pragma unroll
+    for (int n = 0; n < N; ++n) next[n] = load_any(row, M::col(t, n), cols);
+  };
+  load(r0 + team);
+  for (; r0 < a.rows; r0 += step) {
+    const int64_t r = r0 + team;
+    const bool on = r < a.rows;
+    float v[N][8], s = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      values<T>(next[n], M::col(t, n), cols, v[n]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += v[n][e];
+    }
+    if (r0 + step < a.rows) load(r + step);
+    if (a.packed.codes && on) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) pack8(a.packed, r, M::col(t, n), v[n]);
+    }
+    const float mean = team_sum<M>(s, red, 0) * a.inv;
+    float q = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[n][e] -= mean;
+        const float d = M::col(t, n) + e < cols ? v[n][e] : 0.f;
+        q = fmaf(d, d, q);
+      }
+    const float rstd = 1.f / sqrtf(team_sum<M>(q, red, 1) * a.inv + a.eps);
+    if (!on) continue;
+    if (a.stats && t == 0) a.stats[r] = float2{mean, rstd};
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int c = M::col(t, n);
+      float g[8], h[8];
+      if (w) values<T>(rw[n], c, cols, g);
+      if (b) values<T>(rb[n], c, cols, h);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float o = v[n][e] * rstd;
+        if (w) o *= g[e];
+        v[n][e] = b ? o + h[e] : o;
+      }
+      store8(y + r * a.y_ld, c, cols, v[n]);
+    }
+  }
+}
+
+struct Fwd {
+  const FwdArgs &a;
+  hipStream_t st;
+  template <int DT, int TL, int W, int N>
+  hipError_t go() const {
+    using M = Team<TL, W, N>;
+    const int64_t blocks = std::min<int64_t>((a.rows + M::TEAMS - 1) / M::TEAMS, kFwdBlocks);
+    hipLaunchKernelGGL((norm_fwd_kernel<DT, TL, W, N>), dim3((uint32_t)blocks), dim3(M::NT), 0,
+                       st, a);
+    return hipGetLastError();
+  }
+};
+
+}  // namespace norm
+
+hipError_t launch_layer_norm_fwd(const fg_norm_desc &d, const void *x, const void *weight,
+                                 const void *bias, void *y, float *stats, void *packed,
+                                 hipStream_t st) {
+  norm::FwdArgs a{};
+  a.x = x, a.weight = weight, a.bias = bias, a.y = y;
+  a.stats = reinterpret_cast<float2 *>(stats);
+  if (packed) a.packed = rows::packed_at(packed, d.rows, d.cols);
+  a.rows = d.rows, a.cols = (int32_t)d.cols;
+  a.x_ld = d.x_ld ? d.x_ld : d.cols, a.y_ld = d.y_ld ? d.y_ld : d.cols;
+  a.inv = (float)(1.0 / (double)d.cols), a.eps = (float)d.eps;
+  return norm::for_team(d.dtype, a.cols, norm::Fwd{a, st});
+}
+
+}  // namespace fg

@@ -1,0 +1,286 @@
+// Layer norm's gradients (formulas and layout: norm.hip).
+#include <algorithm>
+
+#include "norm.h"
+
+namespace fg {
+namespace norm {
+
+struct BwdArgs {
+  const void *dy, *x, *weight, *add;
+  void *dx;
+  const float2 *stats;
+  Packed packed;       // PACKED: x's place
+  float *part;         // [workgroup][2][wide] sums of dy xh and of dy; null: not wanted
+  int64_t rows, dy_ld, x_ld, add_ld, dx_ld;
+  int32_t cols;
+  float inv;
+};
+
+// 8 waves a workgroup.
+template <int TL, int W, int N>
+using Grad = Team<TL, W, N, 512>;
+
+// What a row's gradient needs, on its way.
+template <class T, int N, bool PACKED>
+struct Loads {
+  Raw<T> dy[N], add[N];
+  Raw<T> x[PACKED ? 1 : N];
+  u32x2 code[PACKED ? N : 1];
+  uint32_t exp[PACKED ? N : 1];
+  float2 stat;
+};
+
+template <int DT, int TL, int W, int N, bool PACKED>
+__global__ __launch_bounds__(512, 2) void norm_bwd_kernel(BwdArgs a) {
+  using T = typename TypeOf<DT>::T;
+  using M = Grad<TL, W, N>;
+  constexpr int FOLD = M::TEAMS / 2;  // teams whose sums wait in LDS at a time
+  constexpr int LDS = FOLD * M::TEAM * N * 16;
+  __shared__ __attribute__((aligned(16))) float lds[LDS > 64 ? LDS : 64];
+  const int t = threadIdx.x % M::TEAM, team = threadIdx.x / M::TEAM, cols = a.cols;
+  const T *dy = static_cast<const T *>(a.dy), *x = static_cast<const T *>(a.x),
+          *w = static_cast<const T *>(a.weight), *add = static_cast<const T *>(a.add);
+  T *dx = static_cast<T *>(a.dx);
+  Raw<T> rw[N];
+  float aw[N][8] = {}, ab[N][8] = {};
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+    if (w) rw[n] = load_any(w, M::col(t, n), cols);
+  Loads<T, N, PACKED> next;
+  auto load = [&](int64_t r) __attribute__((always_inline)) {
+    r = min(r, a.rows - 1);
+    next.stat = a.stats[r];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int c = M::col(t, n);
+      next.dy[n] = load_any(dy + r * a.dy_ld, c, cols);
+      if constexpr (PACKED) {
+        const int k = min(c, a.packed.wide - 8);
+        next.code[n] = *reinterpret_cast<const u32x2 *>(a.packed.codes + r * a.packed.wide + k);
+        next.exp[n] = a.packed.exps[r * (a.packed.wide / 32) + k / 32];
+      } else {
+        next.x[n] = load_any(x + r * a.x_ld, c, cols);
+      }
+      if (add) next.add[n] = load_any(add + r * a.add_ld, c, cols);
+    }
+  };
+  const int64_t step = (int64_t)gridDim.x * M::TEAMS;
+  int64_t r0 = (int64_t)blockIdx.x * M::TEAMS;
+  load(r0 + team);
+  int turn = 0;
+  for (; r0 < a.rows; r0 += step, turn ^= 1) {
+    const int64_t r = r0 + team;
+    const bool on = r < a.rows;
+    const Loads<T, N, PACKED> now = next;
+    if (r0 + step < a.rows) load(r + step);
+    float g[N][8], xh[N][8], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int c = M::col(t, n);
+      values<T>(now.dy[n], c, cols, g[n]);  // zeros past the row's end: no masks below
+      if constexpr (PACKED)
+        decode8(now.code[n], now.exp[n], xh[n]);
+      else
+        values<T>(now.x[n], c, cols, xh[n]);
+      float wv[8];
+      if (w) values<T>(rw[n], c, cols, wv);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        xh[n][e] = (xh[n][e] - now.stat.x) * now.stat.y;
+        if (!on) g[n][e] = xh[n][e] = 0.f;
+        aw[n][e] = fmaf(g[n][e], xh[n][e], aw[n][e]);
+        ab[n][e] += g[n][e];
+        if (w) g[n][e] *= wv[e];
+        s1 += g[n][e];
+        s2 = fmaf(g[n][e], xh[n][e], s2);
+      }
+    }
+    if (!dx) continue;  // (the same for all)
+    if constexpr (W == 1) {
+      s1 = team_sum<M>(s1, nullptr, 0) * a.inv;
+      s2 = team_sum<M>(s2, nullptr, 0) * a.inv;
+    } else {  // both in one exchange
+#pragma unroll
+      for (int o = 32; o; o >>= 1) {
+        s1 += __shfl_xor(s1, o);
+        s2 += __shfl_xor(s2, o);
+      }
+      float2 *at = reinterpret_cast<float2 *>(lds) + 8 * turn;
+      const int wave = threadIdx.x >> 6;
+      if ((threadIdx.x & 63) == 0) at[wave] = float2{s1, s2};
+      __syncthreads();
+      s1 = s2 = 0.f;
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        const float2 p = at[wave / W * W + k];
+        s1 += p.x;
+        s2 += p.y;
+      }
+      s1 *= a.inv;
+      s2 *= a.inv;
+    }
+    if (!on) continue;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int c = M::col(t, n);
+      float o[8];
+      if (add) values<T>(now.add[n], c, cols, o);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float d = (g[n][e] - s1 - xh[n][e] * s2) * now.stat.y;
+        o[e] = add ? o[e] + d : d;
+      }
+      store8(dx + r * a.dx_ld, c, cols, o);
+    }
+  }
+  if (!a.part) return;
+  // the workgroup's teams, halves onto halves
+  for (int half = M::TEAMS / 2; half; half >>= 1) {
+    __syncthreads();
+    f32x4 *at = reinterpret_cast<f32x4 *>(lds);
+    if (team >= half && team < 2 * half) {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float *v = k < 2 ? aw[n] + 4 * k : ab[n] + 4 * (k - 2);
+          at[((team - half) * N * 4 + 4 * n + k) * M::TEAM + t] = f32x4{v[0], v[1], v[2], v[3]};
+        }
+    }
+    __syncthreads();
+    if (team < half) {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float *v = k < 2 ? aw[n] + 4 * k : ab[n] + 4 * (k - 2);
+          const f32x4 q = at[(team * N * 4 + 4 * n + k) * M::TEAM + t];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] += q[e];
+        }
+    }
+  }
+  if (team) return;
+  float *out = a.part + (size_t)blockIdx.x * 2 * M::WIDE;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float *v = k < 2 ? aw[n] + 4 * k : ab[n] + 4 * (k - 2);
+      *reinterpret_cast<f32x4 *>(out + (k / 2) * M::WIDE + M::col(t, n) + 4 * (k & 1)) =
+          f32x4{v[0], v[1], v[2], v[3]};
+    }
+}
+
+// Sums the workgroups' parts, in order: 64 columns of one of the two gradients, 8 waves
+// a run of the parts each.
+struct JoinArgs {
+  const float *part;
+  void *dweight, *dbias;   // either may be null
+  int32_t n, wide, cols;
+  int32_t *flag;
+};
+template <int DT>
+__global__ __launch_bounds__(512) void norm_join_kernel(JoinArgs a) {
+  using T = typename TypeOf<DT>::T;
+  __shared__ float sh[8][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, which = blockIdx.y;
+  T *out = static_cast<T *>(which ? a.dbias : a.dweight);
+  if (!out) return;
+  const int c = blockIdx.x * 64 + lane, per = (a.n + 7) / 8;
+  const int k0 = wave * per, k1 = min(a.n, k0 + per);
+  const float *p = a.part + (size_t)which * a.wide + min(c, a.wide - 1);
+  float s = 0.f;
+#pragma unroll 8
+  for (int k = k0; k < k1; ++k) s += p[(size_t)k * 2 * a.wide];
+  sh[wave][lane] = s;
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int k = 1; k < 8; ++k) s += sh[k][lane];
+  bool bad = false;
+  if (c < a.cols) {
+    const T v = (T)s;
+    out[c] = v;
+    bad = !(fabsf((float)v) < INFINITY);
+  }
+  if (a.flag) flag_nonfinite(a.flag, bad);
+}
+
+struct Plan {
+  int64_t blocks, wide;
+};
+struct MakePlan {
+  int64_t rows;
+  Plan *p;
+  template <int DT, int TL, int W, int N>
+  hipError_t go() const {
+    using M = Grad<TL, W, N>;
+    p->wide = M::WIDE;
+    p->blocks = std::min<int64_t>((rows + M::TEAMS - 1) / M::TEAMS, M::WIDE <= 1024 ? 512 : 256);
+    return hipSuccess;
+  }
+};
+Plan make_plan(int64_t rows, int64_t cols) {
+  Plan p{};
+  (void)for_cols<FG_F16>((int)cols, MakePlan{rows, &p});
+  return p;
+}
+
+struct Bwd {
+  const BwdArgs &a;
+  int64_t blocks;
+  hipStream_t st;
+  template <int DT, int TL, int W, int N>
+  hipError_t go() const {
+    const dim3 grid((uint32_t)blocks), block(512);
+    if (a.packed.codes)
+      hipLaunchKernelGGL((norm_bwd_kernel<DT, TL, W, N, true>), grid, block, 0, st, a);
+    else
+      hipLaunchKernelGGL((norm_bwd_kernel<DT, TL, W, N, false>), grid, block, 0, st, a);
+    return hipGetLastError();
+  }
+};
+
+}  // namespace norm
+
+size_t layer_norm_ws_bytes(const fg_norm_desc &d) {
+  const norm::Plan p = norm::make_plan(d.rows, d.cols);
+  return (size_t)p.blocks * 2 * p.wide * 4;
+}
+
+hipError_t launch_layer_norm_bwd(const fg_norm_desc &d, const void *dy, const void *x,
+                                 const void *packed, const float *stats, const void *weight,
+                                 const void *add, void *dx, void *dweight, void *dbias,
+                                 int32_t *flag, void *ws, hipStream_t st) {
+  const norm::Plan p = norm::make_plan(d.rows, d.cols);
+  const bool sums = dweight || dbias;
+  const auto ld = [&](int64_t v) { return v ? v : d.cols; };
+  norm::BwdArgs a{};
+  a.dy = dy, a.x = x, a.weight = weight, a.add = add, a.dx = dx;
+  a.stats = reinterpret_cast<const float2 *>(stats);
+  if (packed) a.packed = rows::packed_at(packed, d.rows, d.cols);
+  a.part = sums ? static_cast<float *>(ws) : nullptr;
+  a.rows = d.rows;
+  a.dy_ld = ld(d.y_ld), a.x_ld = ld(d.x_ld), a.add_ld = ld(d.add_ld), a.dx_ld = ld(d.dx_ld);
+  a.cols = (int32_t)d.cols;
+  a.inv = (float)(1.0 / (double)d.cols);
+  if (d.rows) {
+    const hipError_t e = norm::for_team(d.dtype, a.cols, norm::Bwd{a, p.blocks, st});
+    if (e != hipSuccess) return e;
+  }
+  if (!sums) return hipSuccess;
+  const norm::JoinArgs j = {a.part, dweight, dbias, (int32_t)(d.rows ? p.blocks : 0),
+                            (int32_t)p.wide, a.cols, flag};
+  const dim3 grid((uint32_t)((d.cols + 63) / 64), 2), block(512);
+  if (d.dtype == FG_F16)
+    hipLaunchKernelGGL(norm::norm_join_kernel<FG_F16>, grid, block, 0, st, j);
+  else if (d.dtype == FG_BF16)
+    hipLaunchKernelGGL(norm::norm_join_kernel<FG_BF16>, grid, block, 0, st, j);
+  else
+    hipLaunchKernelGGL(norm::norm_join_kernel<FG_F32>, grid, block, 0, st, j);
+  return hipGetLastError();
+}
+
+}  // namespace fg

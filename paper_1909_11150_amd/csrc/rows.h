@@ -1,0 +1,196 @@
+// Rows of any width, stride and element alignment in chunks of 8 elements, and the 8-bit
+// checkpoint of an activation.
+#pragma once
+#include "common.h"
+#include "dma_pipe.h"
+
+namespace fg {
+namespace rows {
+
+// Element types by their code.
+template <int DT>
+struct TypeOf;
+template <>
+struct TypeOf<FG_F16> {
+  using T = _Float16;
+};
+template <>
+struct TypeOf<FG_BF16> {
+  using T = __bf16;
+};
+template <>
+struct TypeOf<FG_F32> {
+  using T = float;
+};
+
+// 16 bytes at any element's address: global memory is accessed in one instruction whatever
+// the alignment, only slower across lines.
+struct __attribute__((packed, aligned(2))) Any16 {
+  u32x4 v;
+};
+
+// 8 elements as they are in memory.
+template <class T>
+struct Raw {
+  u32x4 w[sizeof(T) / 2];
+};
+
+// Loads chunk c (a multiple of 8) of a row of at least 8 elements. Where the row ends within
+// or before the chunk, the last 8 elements come in its place; values() moves them. No branch:
+// several chunks' loads are on their way together.
+template <class T>
+__device__ __forceinline__ Raw<T> load_raw(const T *row, int c, int cols) {
+  Raw<T> r;
+  const T *p = row + min(c, cols - 8);
+#pragma unroll
+  for (int k = 0; k < (int)(sizeof(T) / 2); ++k)
+    r.w[k] = reinterpret_cast<const Any16 *>(p + 8 / (sizeof(T) / 2) * k)->v;
+  return r;
+}
+
+// ... of a row of fewer.
+template <class T>
+__device__ __forceinline__ Raw<T> load_narrow(const T *row, int c, int cols) {
+  T v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? row[c + e] : (T)0.f;
+  return __builtin_bit_cast(Raw<T>, v);
+}
+
+// The chunk's elements as fp32, zeros past the row's end.
+template <class T>
+__device__ __forceinline__ void values(const Raw<T> &r, int c, int cols, float (&v)[8]) {
+  typedef T t8 __attribute__((ext_vector_type(8)));
+  const t8 q = __builtin_bit_cast(t8, r);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = (float)q[e];
+  if (cols < 8) return;
+  if (cols % 8 == 0) {
+    if (c >= cols) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    }
+    return;
+  }
+  const int s = c - min(c, cols - 8);  // elements that belong before the chunk
+#pragma unroll
+  for (int b = 4; b; b >>= 1)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = s & b ? (e + b < 8 ? v[e + b] : 0.f) : v[e];
+  if (s >= 8) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.f;
+  }
+}
+
+template <class T>
+__device__ __forceinline__ Raw<T> load_any(const T *row, int c, int cols) {
+  return cols >= 8 ? load_raw(row, c, cols) : load_narrow(row, c, cols);
+}
+
+template <class T>
+__device__ __forceinline__ void load8(const T *row, int c, int cols, float (&v)[8]) {
+  values<T>(load_any(row, c, cols), c, cols, v);
+}
+
+// Rounds 8 values once to T and writes those within the row.
+template <class T>
+__device__ __forceinline__ void store8(T *row, int c, int cols, const float (&v)[8]) {
+  T q[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) q[e] = (T)v[e];
+  if (c + 8 <= cols) {
+    const Raw<T> r = __builtin_bit_cast(Raw<T>, q);
+#pragma unroll
+    for (int k = 0; k < (int)(sizeof(T) / 2); ++k)
+      reinterpret_cast<Any16 *>(row + c + 8 / (sizeof(T) / 2) * k)->v = r.w[k];
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (c + e < cols) row[c + e] = q[e];
+}
+
+// ---- 8-bit checkpoints ---------------------------------------------------------------
+// rows x cols values in row-major codes (signed bytes, rows padded with zeros to a multiple
+// of 32 columns), then one byte for each 32 columns of a row: the biased exponent b, at least
+// 8, of the largest magnitude; a code stands for code * 2^(b - 133), so the largest is 64 ..
+// 127 steps. A power of two makes packing exact but for the one rounding, and the value exact
+// in fp16 and bf16 where it came from that type: 7 bits, and no bit below the type's last one
+// (128 steps would leave fp16's range at its top: codes end at 127, one step's error there).
+// Infinities and NaN are the code -128, which comes back as NaN: what a checkpoint loses must
+// not hide an overflow from the gradients' check.
+struct Packed {
+  int8_t *codes;
+  uint8_t *exps;
+  int32_t wide;    // columns of a row of codes
+};
+__host__ __device__ inline int64_t packed_cols(int64_t cols) { return (cols + 31) / 32 * 32; }
+__host__ __device__ inline Packed packed_at(const void *p, int64_t rows, int64_t cols) {
+  const int64_t wide = packed_cols(cols);
+  int8_t *codes = static_cast<int8_t *>(const_cast<void *>(p));
+  return {codes, reinterpret_cast<uint8_t *>(codes + rows * wide), (int32_t)wide};
+}
+
+__device__ __forceinline__ uint32_t magnitude(float v) {  // 0 where v is no number
+  const uint32_t u = __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu;
+  return u < 0x7F800000u ? u : 0u;
+}
+// Of the largest magnitude of a group.
+__device__ __forceinline__ uint32_t group_exp(uint32_t top) { return max(top >> 23, 8u); }
+__device__ __forceinline__ float step_of(uint32_t b) {
+  return __builtin_bit_cast(float, (b - 6u) << 23);
+}
+__device__ __forceinline__ float steps_of(uint32_t b) {  // its reciprocal
+  return __builtin_bit_cast(float, (260u - b) << 23);
+}
+// Code in the low byte: adding 1.5 * 2^23 rounds to a whole number, halves to even, and
+// leaves it in the sum's low bits.
+__device__ __forceinline__ uint32_t code_of(float v, float inv) {
+  const float q = fminf(fmaxf(v * inv, -127.f), 127.f) + 12582912.f;
+  const bool number = (__builtin_bit_cast(uint32_t, v) & 0x7F800000u) != 0x7F800000u;
+  return number ? __builtin_bit_cast(uint32_t, q) : 0x80u;
+}
+__device__ __forceinline__ uint32_t bytes4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x0C0C0400u);
+  const uint32_t hi = __builtin_amdgcn_perm(d, c, 0x0C0C0400u);
+  return lo | hi << 16;
+}
+// 8 codes as values.
+__device__ __forceinline__ void decode8(const u32x2 &q, uint32_t b, float (&v)[8]) {
+  const float step = step_of(b);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int code = (int8_t)(q[e >> 2] >> (8 * (e & 3)));
+    v[e] = code == -128 ? __builtin_nanf("") : (float)code * step;
+  }
+}
+
+// Packs this lane's 8 values of a row, 4 lanes (a multiple of 4 and the next three) to a
+// group of 32 columns; every lane of the four takes part, those past the end with zeros.
+__device__ __forceinline__ void pack8(const Packed &p, int64_t row, int c, const float (&v)[8]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[e]));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+  if (c >= p.wide) return;
+  const uint32_t b = group_exp(top);
+  const float inv = steps_of(b);
+  uint32_t q[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) q[e] = code_of(v[e], inv);
+  *reinterpret_cast<u32x2 *>(p.codes + row * p.wide + c) =
+      u32x2{bytes4(q[0], q[1], q[2], q[3]), bytes4(q[4], q[5], q[6], q[7])};
+  if (c % 32 == 0) p.exps[row * (p.wide / 32) + c / 32] = (uint8_t)b;
+}
+
+template <class T>
+__device__ __forceinline__ T wave_sum(T v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+}  // namespace rows
+}  // namespace fg
