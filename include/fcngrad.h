@@ -660,6 +660,48 @@ fg_status layer_norm_bwd(const fg_norm_desc *d, const void *dy, const void *x,
                          int32_t *found_nonfinite, void *ws, size_t ws_bytes,
                          hipStream_t stream);
 
+/* Linear layer of each row (a 1x1 convolution), with bias, activation and residual. */
+enum { FG_ACT_NONE = 0, FG_ACT_RELU = 1, FG_ACT_GELU = 2 };
+
+typedef struct {
+    int64_t rows;
+    int64_t x_ld, w_ld;        /* of x; of w */
+    int64_t y_ld, r_ld, z_ld;  /* of y and dy; of the residual; of z */
+    int64_t dx_ld, dw_ld;
+    int32_t in, out;
+    int32_t dtype;             /* every tensor's: FG_F16 or FG_BF16 */
+    int32_t act;               /* FG_ACT_*; gelu(z) = z Phi(z), Phi the normal distribution's */
+} fg_linear_desc;
+
+/* Device workspace in bytes that linear_bwd (grad != 0) or linear_fwd needs; 0 for an invalid
+ * or unsupported descriptor, and where none is needed. For gradients it holds dz and x's
+ * values from its checkpoint in 16 bits, and fp32 parts of split sums. Calls that may overlap
+ * in time need workspaces of their own. */
+size_t fg_linear_workspace_bytes(const fg_linear_desc *d, int grad);
+
+/* y = residual + act(z), z = x w^T + bias: products and sums in fp32, one rounding. x: rows x
+ * in, w: out x in, bias: out (null: 0), residual: rows x out (null: 0). For the backward pass of
+ * an activation, z (rows x out, rounded) and packed_z (its 8-bit checkpoint) may be kept;
+ * either may be null, and both must be without one. y may be the residual itself at the same
+ * stride. Phi is within 1.2e-5 of itself. FG_EUNSUPPORTED also for FG_F32, rows of 2^28,
+ * in or out above 2^17, strides of 2^20, rows * in or rows * out of 2^34 or more. */
+fg_status linear_fwd(const fg_linear_desc *d, const void *x, const void *w, const void *bias,
+                     const void *residual, void *y, void *z, void *packed_z, void *ws,
+                     size_t ws_bytes, hipStream_t stream);
+
+/* The gradients from dy (rows x out): with dz = dy * act'(z), rounded to dtype for the products,
+ *   dx = dz w,  dw = dz^T x,  dbias = the sum of dz over the rows (before that rounding),
+ * sums in fp32 in a fixed order, each rounded once; any of the three may be null, if not all. w is
+ * read for dx; x, given itself or as its checkpoint packed_x, for dw; z, or its checkpoint
+ * packed_z, where there is an activation (of ReLU any tensor that is positive where z is, e.g. y
+ * without residual). What is not read may be null; x and packed_x, z and packed_z are not given
+ * both. relu'(0) = 0; a NaN in z reaches dz. found_nonfinite (device int32, may be null) is set
+ * to 1 if an element of dw or dbias is infinite or NaN, never cleared. Limits as linear_fwd. */
+fg_status linear_bwd(const fg_linear_desc *d, const void *dy, const void *x,
+                     const void *packed_x, const void *w, const void *z, const void *packed_z,
+                     void *dx, void *dw, void *dbias, int32_t *found_nonfinite, void *ws,
+                     size_t ws_bytes, hipStream_t stream);
+
 /* Output spatial size: transpose = 0 gives the forward P, Q; 1 gives the
  * transposed convolution's output size. FG_EINVAL if it is not positive. */
 fg_status fg_conv_out_dims(const fg_conv_desc *d, int transpose, int32_t *p,

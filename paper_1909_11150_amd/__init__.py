@@ -19,6 +19,7 @@ OP_FWD, OP_BWD_DATA, OP_BWD_WEIGHT, OP_CONVT = 0, 1, 2, 3
 MAX_SEGMENTS = 64
 GRAD_F32, GRAD_F16_SCALED = 0, 1
 F16, BF16, F32 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU = 0, 1, 2
 
 ENTRY_POINTS = (
     "conv2d_fwd", "conv2d_bwd_data", "conv2d_bwd_weight",
@@ -35,6 +36,7 @@ ENTRY_POINTS = (
     "linear_xent_fwd", "linear_xent_grad", "fg_linear_xent_workspace_bytes",
     "act8_pack", "act8_unpack", "fg_act8_bytes",
     "layer_norm_fwd", "layer_norm_bwd", "fg_layer_norm_workspace_bytes",
+    "linear_fwd", "linear_bwd", "fg_linear_workspace_bytes",
 )
 MFMA_LOOP_MAX_WORK = 1 << 28  # blocks * iters accepted by fg_mfma_loop
 MFMA_LOOP_FLOPS_PER_BLOCK_ITER = 1 << 20
@@ -117,6 +119,20 @@ class NormDesc(ctypes.Structure):
         return cls(rows, cols, x_ld, y_ld, add_ld, dx_ld, eps, dtype)
 
 
+class LinearDesc(ctypes.Structure):
+    """fg_linear_desc. Strides 0: dense."""
+    _fields_ = [("rows", ctypes.c_int64), ("x_ld", ctypes.c_int64), ("w_ld", ctypes.c_int64),
+                ("y_ld", ctypes.c_int64), ("r_ld", ctypes.c_int64), ("z_ld", ctypes.c_int64),
+                ("dx_ld", ctypes.c_int64), ("dw_ld", ctypes.c_int64),
+                ("fan_in", ctypes.c_int32), ("fan_out", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("act", ctypes.c_int32)]
+
+    @classmethod
+    def make(cls, rows, fan_in, fan_out, dtype=F16, act=ACT_NONE, x_ld=0, w_ld=0, y_ld=0, r_ld=0,
+             z_ld=0, dx_ld=0, dw_ld=0):
+        return cls(rows, x_ld, w_ld, y_ld, r_ld, z_ld, dx_ld, dw_ld, fan_in, fan_out, dtype, act)
+
+
 class LibraryNotBuilt(RuntimeError):
     pass
 
@@ -188,6 +204,8 @@ def lib():
         "act8_unpack": [ctypes.POINTER(Act8Desc), vp, vp, vp],
         "layer_norm_fwd": [ctypes.POINTER(NormDesc)] + [vp] * 7,
         "layer_norm_bwd": [ctypes.POINTER(NormDesc)] + [vp] * 11 + [sz, vp],
+        "linear_fwd": [ctypes.POINTER(LinearDesc)] + [vp] * 8 + [sz, vp],
+        "linear_bwd": [ctypes.POINTER(LinearDesc)] + [vp] * 11 + [sz, vp],
         "avg_pool2d_fwd": [vp, i32, i32, i32, i32, vp, vp],
         "avg_pool2d_bwd": [vp, vp, i32, i32, i32, i32, vp, vp],
         "channel_slice_copy": [vp, i32, vp, i32, vp, i32, ctypes.c_int64, i32, i32, vp],
@@ -221,6 +239,8 @@ def lib():
     L.fg_act8_bytes.restype = ctypes.c_size_t
     L.fg_layer_norm_workspace_bytes.argtypes = [ctypes.POINTER(NormDesc)]
     L.fg_layer_norm_workspace_bytes.restype = ctypes.c_size_t
+    L.fg_linear_workspace_bytes.argtypes = [ctypes.POINTER(LinearDesc), ctypes.c_int]
+    L.fg_linear_workspace_bytes.restype = ctypes.c_size_t
     L.fg_conv_workspace_bytes.argtypes = [pdesc, ctypes.c_int]
     L.fg_conv_workspace_bytes.restype = ctypes.c_size_t
     L.fg_conv_kernel_name.argtypes = [pdesc, ctypes.c_int]
@@ -694,13 +714,52 @@ def layer_norm_bwd(desc, dy, stats, x=None, packed=None, weight=None, add=None, 
     """Gradients of layer_norm_fwd from x or its checkpoint `packed`; add: another gradient of
     x, added to dx. ws: uint8 tensor of layer_norm_workspace_bytes(desc)."""
     n, c, dt = desc.rows, desc.cols, desc.dtype
-    wp, wb = (None, 0) if ws is None else (_bytes("ws", ws, 0), ws.numel())
+    wp, wb = _scratch(ws)
     _check("layer_norm_bwd", lib().layer_norm_bwd(
         ctypes.byref(desc), _rows_of("dy", dy, n, c, desc.y_ld, dt),
         _rows_of("x", x, n, c, desc.x_ld, dt), _checkpoint("packed", packed, n, c),
         _stats(stats, n), _per_channel("weight", weight, c, dt),
         _rows_of("add", add, n, c, desc.add_ld, dt), _rows_of("dx", dx, n, c, desc.dx_ld, dt),
         _per_channel("dweight", dweight, c, dt), _per_channel("dbias", dbias, c, dt),
+        _flag("found_nonfinite", found_nonfinite), wp, wb, _s(stream)))
+
+
+def linear_workspace_bytes(desc, grad):
+    return lib().fg_linear_workspace_bytes(ctypes.byref(desc), int(grad))
+
+
+def _scratch(ws):
+    return (None, 0) if ws is None else (_bytes("ws", ws, 0), ws.numel())
+
+
+def linear_fwd(desc, x, w, y, bias=None, residual=None, z=None, packed_z=None, ws=None,
+               stream=None):
+    """y = residual + act(x w^T + bias) (see include/fcngrad.h). z, packed_z: what an
+    activation's backward pass needs of z = x w^T + bias, in desc's type or in 8 bits. ws:
+    uint8 tensor of linear_workspace_bytes(desc, False)."""
+    n, k, m, dt = desc.rows, desc.fan_in, desc.fan_out, desc.dtype
+    wp, wb = _scratch(ws)
+    _check("linear_fwd", lib().linear_fwd(
+        ctypes.byref(desc), _rows_of("x", x, n, k, desc.x_ld, dt),
+        _rows_of("w", w, m, k, desc.w_ld, dt), _per_channel("bias", bias, m, dt),
+        _rows_of("residual", residual, n, m, desc.r_ld, dt), _rows_of("y", y, n, m, desc.y_ld, dt),
+        _rows_of("z", z, n, m, desc.z_ld, dt), _checkpoint("packed_z", packed_z, n, m), wp, wb,
+        _s(stream)))
+
+
+def linear_bwd(desc, dy, x=None, packed_x=None, w=None, z=None, packed_z=None, dx=None, dw=None,
+               dbias=None, found_nonfinite=None, ws=None, stream=None):
+    """Gradients of linear_fwd from dy: dx (reads w), dw (reads x or its checkpoint packed_x),
+    dbias; z or its checkpoint packed_z with an activation. ws: uint8 tensor of
+    linear_workspace_bytes(desc, True)."""
+    n, k, m, dt = desc.rows, desc.fan_in, desc.fan_out, desc.dtype
+    wp, wb = _scratch(ws)
+    _check("linear_bwd", lib().linear_bwd(
+        ctypes.byref(desc), _rows_of("dy", dy, n, m, desc.y_ld, dt),
+        _rows_of("x", x, n, k, desc.x_ld, dt), _checkpoint("packed_x", packed_x, n, k),
+        _rows_of("w", w, m, k, desc.w_ld, dt), _rows_of("z", z, n, m, desc.z_ld, dt),
+        _checkpoint("packed_z", packed_z, n, m), _rows_of("dx", dx, n, k, desc.dx_ld, dt),
+        _rows_of("dw", dw, m, k, desc.dw_ld, dt), _per_channel("dbias", dbias, m, dt),
         _flag("found_nonfinite", found_nonfinite), wp, wb, _s(stream)))
 
 

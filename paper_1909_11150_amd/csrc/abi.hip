@@ -1091,7 +1091,7 @@ Region region(const void *p, int64_t n, int64_t ld, int64_t width, int64_t esz, 
 
 // Whether a write to one may reach the other: rows of one buffer side by side do not.
 bool collide(const Region &a, const Region &b) {
-  if (!a.p || !b.p || !a.n || !b.n) return false;
+  if (!a.p || !b.p || !a.n || !b.n || !a.width || !b.width) return false;
   const int64_t sa = a.ld * a.esz, sb = b.ld * b.esz;
   if ((a.p == b.self || b.p == a.self) && a.p == b.p && a.width == b.width &&
       (sa == sb || a.n == 1))
@@ -1210,6 +1210,80 @@ fg_status layer_norm_bwd(const fg_norm_desc *d, const void *dy, const void *x,
   if (ok != FG_OK) return ok;
   return launch_status(launch_layer_norm_bwd(*d, dy, x, packed, stats, weight, add, dx, dweight,
                                              dbias, found_nonfinite, ws, stream));
+}
+
+static fg_status linear_desc_ok(const fg_linear_desc *d) {
+  if (!d || d->rows < 0 || d->in < 1 || d->out < 1 || !type_ok(d->dtype) ||
+      d->act < FG_ACT_NONE || d->act > FG_ACT_GELU)
+    return FG_EINVAL;
+  const struct {
+    int64_t ld, width;
+  } t[] = {{d->x_ld, d->in},  {d->w_ld, d->in},  {d->dx_ld, d->in}, {d->dw_ld, d->in},
+           {d->y_ld, d->out}, {d->r_ld, d->out}, {d->z_ld, d->out}};
+  for (const auto &s : t)
+    if (s.ld && s.ld < s.width) return FG_EINVAL;
+  for (const auto &s : t)
+    if (s.ld >= (int64_t)1 << 20) return FG_EUNSUPPORTED;
+  if (d->dtype == FG_F32 || d->rows >= (int64_t)1 << 28 || d->in > 1 << 17 || d->out > 1 << 17 ||
+      !act8_fits(d->rows, d->in) || !act8_fits(d->rows, d->out))
+    return FG_EUNSUPPORTED;
+  return FG_OK;
+}
+
+size_t fg_linear_workspace_bytes(const fg_linear_desc *d, int grad) {
+  return linear_desc_ok(d) == FG_OK ? linear_ws_bytes(*d, grad != 0) : 0;
+}
+
+fg_status linear_fwd(const fg_linear_desc *d, const void *x, const void *w, const void *bias,
+                     const void *residual, void *y, void *z, void *packed_z, void *ws,
+                     size_t ws_bytes, hipStream_t stream) {
+  const fg_status valid = linear_desc_ok(d);
+  if (valid != FG_OK) return valid;
+  if (d->act == FG_ACT_NONE && (z || packed_z)) return FG_EINVAL;
+  if (!d->rows) return FG_OK;
+  if (!x || !w || !y || ((uintptr_t)packed_z & 15)) return FG_EINVAL;
+  const size_t need = linear_ws_bytes(*d, false);
+  if (need && (!ws || ws_bytes < need || ((uintptr_t)ws & 15))) return FG_EWORKSPACE;
+  const int64_t n = d->rows, k = d->in, m = d->out;
+  const Region t[] = {region(x, n, d->x_ld, k, 2, false), region(w, m, d->w_ld, k, 2, false),
+                      region(bias, 1, 0, m, 2, false),
+                      region(residual, n, d->r_ld, m, 2, false),
+                      region(y, n, d->y_ld, m, 2, true, residual),
+                      region(z, n, d->z_ld, m, 2, true),
+                      region(packed_z, 1, 0, (int64_t)act8_size(n, m), 1, true),
+                      region(need ? ws : nullptr, 1, 0, (int64_t)need, 1, true)};
+  const fg_status ok = regions_ok(t, sizeof(t) / sizeof(t[0]));
+  if (ok != FG_OK) return ok;
+  return launch_status(launch_linear_fwd(*d, x, w, bias, residual, y, z, packed_z, ws, stream));
+}
+
+fg_status linear_bwd(const fg_linear_desc *d, const void *dy, const void *x,
+                     const void *packed_x, const void *w, const void *z, const void *packed_z,
+                     void *dx, void *dw, void *dbias, int32_t *found_nonfinite, void *ws,
+                     size_t ws_bytes, hipStream_t stream) {
+  const fg_status valid = linear_desc_ok(d);
+  if (valid != FG_OK) return valid;
+  if ((!dx && !dw && !dbias) || (x && packed_x) || (z && packed_z)) return FG_EINVAL;
+  if (d->act == FG_ACT_NONE && (z || packed_z)) return FG_EINVAL;
+  if (d->rows && (!dy || (dx && !w) || (dw && !x && !packed_x) ||
+                  (d->act != FG_ACT_NONE && !z && !packed_z) || ((uintptr_t)packed_x & 15) ||
+                  ((uintptr_t)packed_z & 15)))
+    return FG_EINVAL;
+  const size_t need = linear_ws_bytes(*d, true);
+  if (need && (!ws || ws_bytes < need || ((uintptr_t)ws & 15))) return FG_EWORKSPACE;
+  const int64_t n = d->rows, k = d->in, m = d->out;
+  const Region t[] = {region(dy, n, d->y_ld, m, 2, false), region(x, n, d->x_ld, k, 2, false),
+                      region(packed_x, 1, 0, (int64_t)act8_size(n, k), 1, false),
+                      region(w, m, d->w_ld, k, 2, false), region(z, n, d->z_ld, m, 2, false),
+                      region(packed_z, 1, 0, (int64_t)act8_size(n, m), 1, false),
+                      region(dx, n, d->dx_ld, k, 2, true), region(dw, m, d->dw_ld, k, 2, true),
+                      region(dbias, 1, 0, m, 2, true),
+                      region(found_nonfinite, 1, 0, 1, 4, true),
+                      region(need ? ws : nullptr, 1, 0, (int64_t)need, 1, true)};
+  const fg_status ok = regions_ok(t, sizeof(t) / sizeof(t[0]));
+  if (ok != FG_OK) return ok;
+  return launch_status(launch_linear_bwd(*d, dy, x, packed_x, w, z, packed_z, dx, dw, dbias,
+                                         found_nonfinite, ws, stream));
 }
 
 fg_status relu_backward(const uint16_t *dy, const uint16_t *act,

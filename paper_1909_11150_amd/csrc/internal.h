@@ -204,6 +204,15 @@ hipError_t launch_layer_norm_bwd(const fg_norm_desc &d, const void *dy, const vo
                                  const void *add, void *dx, void *dweight, void *dbias,
                                  int32_t *flag, void *ws, hipStream_t st);
 
+size_t linear_ws_bytes(const fg_linear_desc &d, bool grad);
+hipError_t launch_linear_fwd(const fg_linear_desc &d, const void *x, const void *w,
+                             const void *bias, const void *residual, void *y, void *z,
+                             void *packed_z, void *ws, hipStream_t st);
+hipError_t launch_linear_bwd(const fg_linear_desc &d, const void *dy, const void *x,
+                             const void *packed_x, const void *w, const void *z,
+                             const void *packed_z, void *dx, void *dw, void *dbias,
+                             int32_t *flag, void *ws, hipStream_t st);
+
 // One-shot profiling events (fg_profile_next_launch): prof_begin records the
 // armed start event on the stream, prof_end the stop event, then disarms.
 // Both do nothing when no events are armed.

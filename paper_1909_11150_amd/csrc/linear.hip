@@ -1,0 +1,917 @@
+// Linear layers with bias, activation and residual in the product's epilogue, and their
+// gradients.
+//
+//   z = x w^T + b,  y = residual + act(z)
+//   dz = dy act'(z),  dx = dz w,  dw = dz^T x,  db = sum of dz over the rows
+//
+// Products run on the MFMA tiles that dma_pipe.h feeds by LDS DMA. The forward tile holds
+// outputs x rows, so 32 consecutive outputs of a row lie in two lanes' registers: bias,
+// activation and the 8-bit checkpoint of z (a step for each 32 columns) are made there, and
+// one rounding writes y. Its operands' rows both lie along the sum. Backward, dz is formed
+// once (16 bits, the matrix pipes' type) while its columns are summed for db; dx and dw are
+// one launch, whose operands by rows of the sum are read with transposing LDS reads. Long
+// sums with few tiles are split and joined in order; the join does the epilogue then.
+#include <algorithm>
+
+#include "rows.h"
+#include "tiles.h"
+
+namespace fg {
+namespace linear {
+
+using namespace tiles;
+using rows::Packed;
+using rows::TypeOf;
+
+struct FwdTiles {
+  using T256 = Pipe<64, 2, 2, 4, 256, 256>;
+};
+struct BwdTiles {
+  using T256 = Pipe<32, 5, 2, 4, 256, 256>;
+};
+
+// ---- activations ---------------------------------------------------------------------
+// Phi(-|z|) = exp(-z^2 / 2) R(|z|), Phi the normal distribution's function: R as a polynomial
+// in t = 1 / (1 + c |z|), fitted here to its values (largest relative error 4.7e-6, where a
+// result's rounding to fp16 is 4.9e-4); relative, so that far negative z keep their digits.
+// One exponential and one reciprocal, some 16 instructions. -inf gives 0, NaN NaN.
+struct Gauss {
+  float below, bell;  // Phi(-|z|); exp(-z^2 / 2)
+  __device__ __forceinline__ explicit Gauss(float z) {
+    const float a = fabsf(z);
+    const float t = __builtin_amdgcn_rcpf(fmaf(a, 0.31f, 1.f));
+    bell = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+    float r = fmaf(t, -0.07392825f, 0.18044779f);
+    r = fmaf(r, t, 0.01574751f);
+    r = fmaf(r, t, 0.13342834f);
+    r = fmaf(r, t, 0.12044163f);
+    r = fmaf(r, t, 0.12386067f);
+    below = bell * (r * t);
+  }
+  __device__ __forceinline__ float phi(float z) const { return z > 0.f ? 1.f - below : below; }
+};
+__device__ __forceinline__ float gelu(float z) {
+  return fmaxf(z, -64.f) * Gauss(z).phi(z);
+}
+__device__ __forceinline__ float gelu_slope(float z) {
+  const Gauss g(z);
+  return fmaf(fminf(fmaxf(z, -64.f), 64.f) * 0.39894228f, g.bell, g.phi(z));
+}
+__device__ __forceinline__ float apply(float z, int act) {
+  return act == FG_ACT_RELU ? (z > 0.f || z != z ? z : 0.f) : act == FG_ACT_GELU ? gelu(z) : z;
+}
+
+__device__ __forceinline__ float to_f32(uint32_t half, bool bf) {
+  return bf ? __builtin_bit_cast(float, half << 16) : h_to_f32((uint16_t)half);
+}
+
+// ---- forward -------------------------------------------------------------------------
+struct Epilogue {
+  const uint16_t *bias, *residual;
+  uint16_t *y, *z;
+  int64_t y_ld, r_ld, z_ld;
+  Packed packed;
+  int32_t out, act;
+};
+struct FwdArgs {
+  const uint16_t *w, *x;
+  int64_t w_ld, x_ld;
+  int32_t K, kper;        // the sum's length (at least 8); of a part (a multiple of 64)
+  int64_t rows;
+  int32_t ntile;          // tiles of outputs
+  Epilogue e;
+  float *part;            // [parts][rows][Mq] or null
+  int64_t pstride;
+  int32_t Mq;
+};
+
+// A wave's block of y: residual and result go through this wave's buffer, 32 rows at a time,
+// 16-byte chunks permuted by the row, so that neighbouring lanes read and write one row's
+// consecutive bytes. One rounding of residual + act(z).
+template <class P>
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[P::FM][P::FN], uint8_t *buf,
+                                           int lane, const uint16_t *residual, int64_t r_ld,
+                                           uint16_t *y, int64_t y_ld, int64_t n0, int m0,
+                                           int64_t nrow, int out) {
+  constexpr int CPW = P::WM / 8, RB = P::WM * 2, SH = CPW == 16 ? 0 : CPW == 8 ? 1 : 2;
+  constexpr int RPI = 64 / CPW;
+  const int q = lane % CPW, m = m0 + 8 * q;
+  auto place = [&](int r, int c) __attribute__((always_inline)) {
+    return buf + r * RB + ((c ^ ((r >> SH) & (CPW - 1))) << 4);
+  };
+#pragma unroll
+  for (int j = 0; j < P::FN; ++j) {
+    if (residual) {
+      u32x4 d[32 / RPI];
+#pragma unroll
+      for (int k = 0; k < 32 / RPI; ++k) {
+        const int64_t n = n0 + 32 * j + k * RPI + lane / CPW;
+        d[k] = n < nrow && m < out ? row8(residual + n * r_ld, m, out) : u32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int k = 0; k < 32 / RPI; ++k)
+        *reinterpret_cast<u32x4 *>(place(k * RPI + lane / CPW, q)) = d[k];
+      wait_lds();
+      __builtin_amdgcn_wave_barrier();
+    }
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        u32x2 *at = reinterpret_cast<u32x2 *>(place(lane & 31, 4 * i + g) + 8 * (lane >> 5));
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * g + e];
+        if (residual) {
+          const u32x2 o = *at;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] += to_f32(o[e >> 1] >> (16 * (e & 1)) & 0xFFFFu, P::BF);
+        }
+        *at = u32x2{pack2(v[0], v[1], P::BF), pack2(v[2], v[3], P::BF)};
+      }
+    wait_lds();
+    __builtin_amdgcn_wave_barrier();
+    u32x4 d[32 / RPI];
+#pragma unroll
+    for (int k = 0; k < 32 / RPI; ++k)
+      d[k] = *reinterpret_cast<const u32x4 *>(place(k * RPI + lane / CPW, q));
+#pragma unroll
+    for (int k = 0; k < 32 / RPI; ++k) {
+      const int64_t n = n0 + 32 * j + k * RPI + lane / CPW;
+      if (n < nrow && m < out) put8(y + n * y_ld, m, out, d[k]);
+    }
+    wait_lds();
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// A wave's block of z as 8-bit codes: a group of 32 outputs of a row is 16 registers of this
+// lane and of the one 32 further, which exchange halves, so that each writes 16 bytes.
+template <class P>
+__device__ __forceinline__ void pack_block(const f32x16 (&acc)[P::FM][P::FN], const Packed &p,
+                                           int64_t n0, int m0, int64_t nrow, int lane) {
+  const bool up = lane >= 32;
+#pragma unroll
+  for (int j = 0; j < P::FN; ++j)
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) top = max(top, rows::magnitude(acc[i][j][v]));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+      const uint32_t b = rows::group_exp(top);
+      const float inv = rows::steps_of(b);
+      uint32_t q[4];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        uint32_t c[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = rows::code_of(acc[i][j][4 * g + e], inv);
+        q[g] = rows::bytes4(c[0], c[1], c[2], c[3]);
+      }
+      const uint32_t r0 = __shfl_xor((int)(up ? q[0] : q[2]), 32);
+      const uint32_t r1 = __shfl_xor((int)(up ? q[1] : q[3]), 32);
+      const int64_t n = n0 + 32 * j + (lane & 31);
+      const int m = m0 + 32 * i;
+      if (n < nrow && m < p.wide) {
+        *reinterpret_cast<u32x4 *>(p.codes + n * p.wide + m + (up ? 16 : 0)) =
+            up ? u32x4{r0, q[2], r1, q[3]} : u32x4{q[0], r0, q[1], r1};
+        if (!up) p.exps[n * (p.wide / 32) + m / 32] = (uint8_t)b;
+      }
+    }
+}
+
+// 4 elements of a vector of n from c on, zeros past its end.
+__device__ __forceinline__ void load4(const uint16_t *p, int c, int n, bool bf, float (&v)[4]) {
+  struct __attribute__((packed, aligned(2))) Any8 {
+    u32x2 v;
+  };
+  if (c + 4 <= n) {
+    const u32x2 q = reinterpret_cast<const Any8 *>(p + c)->v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = to_f32(q[e >> 1] >> (16 * (e & 1)) & 0xFFFFu, bf);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = c + e < n ? to_f32(p[c + e], bf) : 0.f;
+}
+
+template <class P>
+__device__ __forceinline__ void epilogue(f32x16 (&acc)[P::FM][P::FN], const Epilogue &a,
+                                         uint8_t *buf, int lane, int64_t n0, int m0,
+                                         int64_t nrow) {
+  if (a.bias) {
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        float b[4];
+        load4(a.bias, m0 + 32 * i + 8 * g + 4 * (lane >> 5), a.out, P::BF, b);
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] += b[e];
+      }
+  }
+  if (a.z) store_rows<P>(acc, buf, lane, nullptr, 0, a.z, a.z_ld, n0, m0, nrow, a.out);
+  if (a.packed.codes) {
+    if (m0 + P::WM > a.out) {  // (weights past the last output are zeros, but 0 x NaN is not)
+#pragma unroll
+      for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (m0 + 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3) >= a.out)
+#pragma unroll
+            for (int j = 0; j < P::FN; ++j) acc[i][j][v] = 0.f;
+    }
+    pack_block<P>(acc, a.packed, n0, m0, nrow, lane);
+  }
+  if (a.act != FG_ACT_NONE) {
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+      for (int j = 0; j < P::FN; ++j)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[i][j][v] = apply(acc[i][j][v], a.act);
+  }
+  store_rows<P>(acc, buf, lane, a.residual, a.r_ld, a.y, a.y_ld, n0, m0, nrow, a.out);
+}
+
+// fp32 sums of a wave's block to a part of a split sum.
+template <class P>
+__device__ __forceinline__ void store_part(const f32x16 (&acc)[P::FM][P::FN], float *part, int Mq,
+                                           int lane, int64_t n0, int m0, int64_t nrow) {
+#pragma unroll
+  for (int j = 0; j < P::FN; ++j) {
+    const int64_t n = n0 + 32 * j + (lane & 31);
+    if (n >= nrow) continue;
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int m = m0 + 32 * i + 8 * g + 4 * (lane >> 5);
+        if (m < Mq)
+          *reinterpret_cast<f32x4 *>(part + n * Mq + m) =
+              f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
+                    acc[i][j][4 * g + 3]};
+      }
+  }
+}
+
+template <class P>
+__global__ __launch_bounds__(P::NT, P::WPE) void linear_fwd_kernel(FwdArgs a, TileMap tm) {
+  FG_DMA_RING(P, R);
+  constexpr int PA = P::PA, PB = P::PB, BK = P::BK;
+  int tx, ty, split;  // rows, outputs, part
+  if (!find_tile(tm, blockIdx.x, a.ntile, tx, ty, split)) return;
+  const int64_t n0 = (int64_t)tx * P::TN;
+  const int m0 = ty * P::TM;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm0 = (wave / P::WGN) * P::WM, wn0 = (wave % P::WGN) * P::WN;
+  const int kbeg = split * a.kper, kend = min(a.K, kbeg + a.kper);
+  const int nst = kend > kbeg ? (kend - kbeg + BK - 1) / BK : 0;
+
+  const int wrows = min(P::TM, a.e.out - m0);
+  const int xrows = (int)min((int64_t)P::TN, a.rows - n0);
+  const __amdgpu_buffer_rsrc_t rs_w =
+      rsrc(a.w + m0 * a.w_ld, (uint32_t)((wrows - 1) * (int)a.w_ld + a.K) * 2u);
+  const __amdgpu_buffer_rsrc_t rs_x =
+      rsrc(a.x + n0 * a.x_ld, (uint32_t)((xrows - 1) * (int)a.x_ld + a.K) * 2u);
+  const KmSlot<PA> as = km_slots<BK, PA>(wave, lane);
+  const KmSlot<PB> bs = km_slots<BK, PB>(wave, lane);
+  unsigned oa[PA], ob[PB], la[PA], lb[PB];
+  // offsets in the last stage: its last chunk may begin before its place (both operands'
+  // alike), and chunks past the end are zeros
+  const int kl = kbeg + (nst - 1) * BK;
+  auto tail = [&](unsigned o, int coff) __attribute__((always_inline)) {
+    return kl + coff < a.K ? o + 2u * (chunk_at(kl + coff, a.K) - coff) : kOOB;
+  };
+#pragma unroll
+  for (int jj = 0; jj < PA; ++jj) {
+    oa[jj] = (unsigned)(as.row[jj] * (int)a.w_ld + as.coff[jj]) * 2u;
+    la[jj] = tail(oa[jj], as.coff[jj]);
+    oa[jj] += 2u * kbeg;
+  }
+#pragma unroll
+  for (int jj = 0; jj < PB; ++jj) {
+    ob[jj] = (unsigned)(bs.row[jj] * (int)a.x_ld + bs.coff[jj]) * 2u;
+    lb[jj] = tail(ob[jj], bs.coff[jj]);
+    ob[jj] += 2u * kbeg;
+  }
+  auto issue = [&](int st, int slot) __attribute__((always_inline)) {
+    uint8_t *ta = R.a[slot], *tb = R.b[slot];
+    const bool last = st + 1 == nst;
+    const unsigned k0 = 2u * BK * st;
+#pragma unroll
+    for (int jj = 0; jj < PB; ++jj)
+      dma16(rs_x, tb + dma_dst<PB>(wave, jj), last ? lb[jj] : ob[jj] + k0);
+#pragma unroll
+    for (int jj = 0; jj < PA; ++jj)
+      dma16(rs_w, ta + dma_dst<PA>(wave, jj), last ? la[jj] : oa[jj] + k0);
+  };
+  // the last chunk's repeated elements: zeros in both operands, whatever they are
+  auto fix = [&](Frags<P> &f, int it, int ks) __attribute__((always_inline)) {
+    if (a.K % 8 == 0 || it + 1 != nst) return;
+    const int over = kl + 16 * ks + 8 * (lane >> 5) + 8 - a.K;  // 1 .. 7: that chunk
+    const int cut = over < 8 ? over : 0;
+    u32x4 m;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+      m[d] = (2 * d < cut ? 0u : 0xFFFFu) | (2 * d + 1 < cut ? 0u : 0xFFFF0000u);
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i) f.a[i] &= m;
+#pragma unroll
+    for (int j = 0; j < P::FN; ++j) f.b[j] &= m;
+  };
+  f32x16 acc[P::FM][P::FN];
+  zero<P>(acc);
+  pipeline<P, true, true>(acc, R, nst, wm0, wn0, lane, issue, NoFold{}, fix);
+  if (a.part) {
+    store_part<P>(acc, a.part + split * a.pstride, a.Mq, lane, n0 + wn0, m0 + wm0, a.rows);
+    return;
+  }
+  lds_barrier();  // every wave is done reading the ring
+  epilogue<P>(acc, a.e, wave_buf<P>(R, wave), lane, n0 + wn0, m0 + wm0, a.rows);
+}
+
+// ---- the gradient of z -----------------------------------------------------------------
+struct DzArgs {
+  const uint16_t *dy, *z;
+  Packed packed;
+  uint16_t *dz;          // null: sums only
+  float *part;           // [row blocks][Mp] or null
+  int64_t rows, dy_ld, z_ld, per;   // rows of a workgroup
+  int32_t out, Mp, act, tlog;       // 2^tlog lanes side by side
+};
+
+// dz = dy act'(z), rounded to the type that the products take, in rows of a multiple of 8
+// with zeros behind them; its columns' fp32 sums per workgroup, before the rounding.
+template <int DT>
+__global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a) {
+  using T = typename TypeOf<DT>::T;
+  __shared__ float sums[256][9];
+  const int tl = 1 << a.tlog, t = threadIdx.x & (tl - 1), team = threadIdx.x >> a.tlog;
+  const int teams = 256 >> a.tlog;
+  const int c = 8 * ((int)blockIdx.x * tl + t);
+  const int64_t r0 = (int64_t)blockIdx.y * a.per, r1 = min(a.rows, r0 + a.per);
+  const T *dy = reinterpret_cast<const T *>(a.dy), *z = reinterpret_cast<const T *>(a.z);
+  T *dz = reinterpret_cast<T *>(a.dz);
+  float s[8] = {};
+  constexpr int B = 4;  // rows on their way
+  if (c < a.Mp)
+    for (int64_t r = r0 + team; r < r1; r += B * teams) {
+      rows::Raw<T> d[B], h[B];
+      u32x2 q[B];
+      uint32_t e[B];
+#pragma unroll
+      for (int k = 0; k < B; ++k) {
+        const int64_t n = min(r + k * teams, a.rows - 1);
+        d[k] = rows::load_any(dy + n * a.dy_ld, c, a.out);
+        if (a.act == FG_ACT_NONE) continue;
+        if (a.packed.codes) {
+          q[k] = *reinterpret_cast<const u32x2 *>(a.packed.codes + n * a.packed.wide + c);
+          e[k] = a.packed.exps[n * (a.packed.wide / 32) + c / 32];
+        } else {
+          h[k] = rows::load_any(z + n * a.z_ld, c, a.out);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < B; ++k) {
+        const int64_t n = r + k * teams;
+        if (n >= r1) break;
+        float g[8], v[8];
+        rows::values<T>(d[k], c, a.out, g);
+        if (a.act != FG_ACT_NONE) {
+          if (a.packed.codes)
+            rows::decode8(q[k], e[k], v);
+          else
+            rows::values<T>(h[k], c, a.out, v);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (a.act == FG_ACT_RELU)
+              g[i] = v[i] > 0.f ? g[i] : v[i] != v[i] ? v[i] : 0.f;
+            else
+              g[i] *= gelu_slope(v[i]);
+            if (c + i >= a.out) g[i] = 0.f;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] += g[i];
+        if (dz) rows::store8(dz + n * a.Mp, c, a.Mp, g);
+      }
+    }
+  if (!a.part) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sums[threadIdx.x][i] = s[i];
+  __syncthreads();
+  for (int k = threadIdx.x; k < 8 * tl; k += 256) {
+    const int col = 8 * (int)blockIdx.x * tl + k;
+    if (col >= a.Mp) break;
+    float v = 0.f;
+    for (int j = 0; j < teams; ++j) v += sums[(j << a.tlog) + k / 8][k % 8];
+    a.part[(int64_t)blockIdx.y * a.Mp + col] = v;
+  }
+}
+
+// The sums of the row blocks, in order: 64 columns a workgroup, 8 waves a run of them each.
+struct SumArgs {
+  const float *part;
+  uint16_t *out;
+  int32_t n, Mp, cols;
+  int32_t *flag;
+};
+template <int DT>
+__global__ __launch_bounds__(512) void linear_sum_kernel(SumArgs a) {
+  using T = typename TypeOf<DT>::T;
+  __shared__ float sh[8][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c = blockIdx.x * 64 + lane, per = (a.n + 7) / 8;
+  const int k0 = wave * per, k1 = min(a.n, k0 + per);
+  float s = 0.f;
+#pragma unroll 8
+  for (int k = k0; k < k1; ++k) s += a.part[(int64_t)k * a.Mp + min(c, a.Mp - 1)];
+  sh[wave][lane] = s;
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int k = 1; k < 8; ++k) s += sh[k][lane];
+  bool bad = false;
+  if (c < a.cols) {
+    const T v = (T)s;
+    reinterpret_cast<T *>(a.out)[c] = v;
+    bad = !(fabsf((float)v) < INFINITY);
+  }
+  if (a.flag) flag_nonfinite(a.flag, bad);
+}
+
+// ---- products of the gradients ---------------------------------------------------------
+// out[n][m] = sum_k A[k][m] B(n, k): A's rows (of w: outputs; of x: rows) lie across the sum;
+// dz is B, by rows n (dx, k: outputs) or columns n (dw, k: rows).
+struct ProdArgs {
+  const uint16_t *a;
+  int64_t a_ld;
+  int32_t a_cols;            // at least 8
+  const uint16_t *b;
+  int64_t b_ld;
+  int32_t b_cols;            // a multiple of 8
+  int64_t N, K;              // rows of the output; the sum's length
+  int64_t kper;              // of a part (a multiple of 64)
+  int32_t M, ntile;
+  uint16_t *out;             // null: fp32 sums to part
+  int64_t out_ld;
+  float *part;               // [parts][N][Mq]
+  int64_t pstride;
+  int32_t Mq;
+  int32_t *flag;
+};
+
+template <class P, bool DX>
+__device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &tm, int block,
+                                             const Ring &R) {
+  constexpr int PA = P::PA, PB = P::PB, BK = P::BK;
+  int tx, ty, split;  // columns m, rows n, part
+  if (!find_tile(tm, block, a.ntile, tx, ty, split)) return;
+  const int m0 = tx * P::TM;
+  const int64_t n0 = (int64_t)ty * P::TN;
+  const int64_t kbeg = split * a.kper, kend = min(a.K, kbeg + a.kper);
+  const int nst = kend > kbeg ? (int)((kend - kbeg + BK - 1) / BK) : 0;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm0 = (wave / P::WGN) * P::WM, wn0 = (wave % P::WGN) * P::WN;
+
+  const MnSlot<PA> as = mn_slots<P::RBA, PA>(wave, lane);
+  unsigned oa[PA], ob[PB], lb[PB];
+#pragma unroll
+  for (int jj = 0; jj < PA; ++jj)
+    oa[jj] = m0 + as.ncol[jj] < a.a_cols
+                 ? (unsigned)(as.krow[jj] * (int)a.a_ld + chunk_at(m0 + as.ncol[jj], a.a_cols)) * 2u
+                 : kOOB;
+  const uint16_t *pa = a.a + kbeg * a.a_ld, *pb = nullptr;
+  // dx: all of the tile's rows of dz; kend is their end but for the last part's
+  const int64_t kcol = min((int64_t)a.b_cols, kbeg + a.kper);
+  const int brows = (int)min((int64_t)P::TN, a.N - n0);
+  __amdgpu_buffer_rsrc_t rs_rows;
+  if constexpr (DX) {
+    const KmSlot<PB> bs = km_slots<BK, PB>(wave, lane);
+    rs_rows = rsrc(a.b + n0 * a.b_ld, (uint32_t)((brows - 1) * (int)a.b_ld + a.b_cols) * 2u);
+    const int kl = (int)kbeg + (nst - 1) * BK;
+#pragma unroll
+    for (int jj = 0; jj < PB; ++jj) {
+      const unsigned o = (unsigned)(bs.row[jj] * (int)a.b_ld + bs.coff[jj]) * 2u;
+      ob[jj] = o + 2u * (unsigned)kbeg;
+      lb[jj] = kl + bs.coff[jj] < kcol ? o + 2u * (unsigned)kl : kOOB;
+    }
+  } else {
+    const MnSlot<PB> bs = mn_slots<P::RBB, PB>(wave, lane);
+    pb = a.b + kbeg * a.b_ld + n0;
+#pragma unroll
+    for (int jj = 0; jj < PB; ++jj)
+      ob[jj] = n0 + bs.ncol[jj] < a.b_cols
+                   ? (unsigned)(bs.krow[jj] * (int)a.b_ld + bs.ncol[jj]) * 2u
+                   : kOOB;
+  }
+  int64_t left = kend - kbeg;
+  auto issue = [&](int st, int slot) __attribute__((always_inline)) {
+    uint8_t *ta = R.a[slot], *tb = R.b[slot];
+    const int r = (int)min(left, (int64_t)BK);
+    const __amdgpu_buffer_rsrc_t rs_a = rsrc(pa, (uint32_t)((r - 1) * (int)a.a_ld + a.a_cols) * 2u);
+    if constexpr (DX) {
+      const bool last = st + 1 == nst;
+      const unsigned k0 = 2u * BK * st;
+#pragma unroll
+      for (int jj = 0; jj < PB; ++jj)
+        dma16(rs_rows, tb + dma_dst<PB>(wave, jj), last ? lb[jj] : ob[jj] + k0);
+    } else {
+      const __amdgpu_buffer_rsrc_t rs_b =
+          rsrc(pb, (uint32_t)((r - 1) * (int)a.b_ld + a.b_cols - (int)n0) * 2u);
+#pragma unroll
+      for (int jj = 0; jj < PB; ++jj) dma16(rs_b, tb + dma_dst<PB>(wave, jj), ob[jj]);
+      pb += BK * a.b_ld;
+    }
+#pragma unroll
+    for (int jj = 0; jj < PA; ++jj) dma16(rs_a, ta + dma_dst<PA>(wave, jj), oa[jj]);
+    pa += BK * a.a_ld;
+    left -= BK;
+  };
+  f32x16 acc[P::FM][P::FN];
+  zero<P>(acc);
+  pipeline<P, false, DX>(acc, R, nst, wm0, wn0, lane, issue);
+  if (a.part) {
+    store_part<P>(acc, a.part + split * a.pstride, a.Mq, lane, n0 + wn0, m0 + wm0, a.N);
+    return;
+  }
+  lds_barrier();  // every wave is done reading the ring
+  bool bad = false;
+  store16<P>(
+      wave_buf<P>(R, wave), lane,
+      [&](int i, int j, int g) __attribute__((always_inline)) {
+        const f32x16 &c = acc[i][j];
+        return u32x2{pack2(c[4 * g], c[4 * g + 1], P::BF),
+                     pack2(c[4 * g + 2], c[4 * g + 3], P::BF)};
+      },
+      [&](int r, int c, const u32x4 &d) __attribute__((always_inline)) {
+        const int64_t n = n0 + wn0 + r;
+        const int m = m0 + wm0 + c;
+        if (n >= a.N || m >= a.M) return;
+        constexpr uint32_t EX = P::BF ? 0x7F80u : 0x7C00u;
+        if (!DX) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) bad |= (d[e >> 1] >> (16 * (e & 1)) & EX) == EX;
+        }
+        put_chunk(a.out + n * a.out_ld, m, a.M, d);
+      });
+  if (!DX && a.flag) flag_nonfinite(a.flag, bad);
+}
+
+// Both in one launch, dx's tiles in the first nx workgroups: neither waits for the other's
+// last tiles.
+template <class P>
+__global__ __launch_bounds__(P::NT, P::WPE) void linear_products_kernel(ProdArgs dx, TileMap tx,
+                                                                        ProdArgs dw, TileMap tw,
+                                                                        int nx) {
+  FG_DMA_RING(P, R);
+  const int block = blockIdx.x;
+  if (block < nx)
+    product_tile<P, true>(dx, tx, block, R);
+  else
+    product_tile<P, false>(dw, tw, block - nx, R);
+}
+
+// ---- joins -----------------------------------------------------------------------------
+// The parts of split sums, in their order: 8 columns of a row per lane.
+struct JoinArgs {
+  const float *part;
+  int64_t pstride, rows;
+  int32_t nsplit, M, Mq;
+  uint16_t *out;
+  int64_t out_ld;
+  int32_t *flag;
+};
+__device__ __forceinline__ void joined(const float *p, int nsplit, int64_t pstride, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < nsplit; ++s, p += pstride)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x4 x = *reinterpret_cast<const f32x4 *>(p + 4 * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * h + e] += x[e];
+    }
+}
+template <int DT>
+__device__ __forceinline__ u32x4 rounded(const float (&v)[8]) {
+  u32x4 d;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) d[e] = pack2(v[2 * e], v[2 * e + 1], DT == FG_BF16);
+  return d;
+}
+template <int DT>
+__global__ __launch_bounds__(256) void linear_join_kernel(JoinArgs dx, JoinArgs dw, int nx) {
+  const bool first = (int)blockIdx.x < nx;
+  const JoinArgs &a = first ? dx : dw;
+  const int64_t i = (int64_t)(first ? blockIdx.x : blockIdx.x - nx) * 256 + threadIdx.x;
+  const int c8 = a.Mq / 8;
+  const int64_t n = i / c8;
+  const int m = (int)(i - n * c8) * 8;
+  bool bad = false;
+  if (n < a.rows) {
+    float v[8];
+    joined(a.part + n * a.Mq + m, a.nsplit, a.pstride, v);
+    const u32x4 d = rounded<DT>(v);
+    constexpr uint32_t EX = DT == FG_BF16 ? 0x7F80u : 0x7C00u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bad |= (d[e >> 1] >> (16 * (e & 1)) & EX) == EX;
+    put_chunk(a.out + n * a.out_ld, m, a.M, d);
+  }
+  if (a.flag) flag_nonfinite(a.flag, bad);
+}
+
+// ... of the forward product, with its epilogue: lanes by columns, rounded up to a
+// checkpoint's groups.
+struct JoinFwd {
+  const float *part;
+  int64_t pstride, rows;
+  int32_t nsplit, Mq, wide;
+  Epilogue e;
+};
+template <int DT>
+__global__ __launch_bounds__(256) void linear_join_fwd_kernel(JoinFwd a) {
+  using T = typename TypeOf<DT>::T;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int c8 = a.wide / 8;
+  const int64_t n = i / c8;
+  const int m = (int)(i - n * c8) * 8;
+  if (n >= a.rows) return;  // (whole groups of 4 lanes)
+  const Epilogue &e = a.e;
+  float v[8] = {};
+  if (m < e.out) {
+    joined(a.part + n * a.Mq + m, a.nsplit, a.pstride, v);
+    if (e.bias) {
+      float b[8];
+      rows::load8(reinterpret_cast<const T *>(e.bias), m, e.out, b);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += b[k];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (m + k >= e.out) v[k] = 0.f;
+    if (e.z) rows::store8(reinterpret_cast<T *>(e.z) + n * e.z_ld, m, e.out, v);
+  }
+  if (e.packed.codes) rows::pack8(e.packed, n, m, v);
+  if (m >= e.out) return;
+  float r[8] = {};
+  if (e.residual)
+    rows::load8(reinterpret_cast<const T *>(e.residual) + n * e.r_ld, m, e.out, r);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    v[k] = apply(v[k], e.act);
+    if (e.residual) v[k] += r[k];
+  }
+  rows::store8(reinterpret_cast<T *>(e.y) + n * e.y_ld, m, e.out, v);
+}
+
+// Rows of fewer than 8 elements, padded with zeros to 8.
+__global__ __launch_bounds__(256) void linear_pad_kernel(const uint16_t *x, int64_t ld, int32_t n,
+                                                         uint16_t *to, int64_t rows) {
+  const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (r < rows) *reinterpret_cast<u32x4 *>(to + r * 8) = row8(x + r * ld, 0, n);
+}
+
+// ---- host ------------------------------------------------------------------------------
+struct Plan {
+  int64_t rows, in, out, in8, out8, K;   // K: columns of x and w as the products read them
+  bool narrow;                           // fewer than 8: padded copies
+  Shape s1, s2, s3;
+  int tlog;
+  int64_t cblocks, rblocks, per;         // of the kernel that forms dz
+  // workspace, bytes
+  size_t xpad, wpad, p1, xu, dz, db, pdx, pdw, total;
+};
+
+Plan make_plan(const fg_linear_desc &d, bool grad) {
+  Plan p{};
+  p.rows = d.rows, p.in = d.in, p.out = d.out;
+  p.in8 = up(p.in, 8), p.out8 = up(p.out, 8);
+  p.narrow = p.in < 8;
+  p.K = std::max<int64_t>(p.in, 8);
+  double best = 1e300, us, us2;
+  for (int t = 0; t < 3; ++t) {
+    const Shape a = pick_tile(t, p.out, p.rows, p.K, true, us);
+    if (us < best) best = us, p.s1 = a;
+  }
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t was = at;
+    at += (bytes + 255) / 256 * 256;
+    return was;
+  };
+  p.wpad = take(p.narrow ? (size_t)p.out * 16 : 0);
+  if (!grad) {
+    p.xpad = take(p.narrow ? (size_t)p.rows * 16 : 0);
+    p.p1 = take(p.s1.ns > 1 ? (size_t)p.s1.ns * p.rows * p.out8 * 4 : 0);
+    p.total = at;
+    return p;
+  }
+  best = 1e300;  // one launch, one tile for both products
+  for (int t = 0; t < 3; ++t) {
+    const Shape a = pick_tile(t, p.in, p.rows, p.out8, true, us);
+    const Shape b = pick_tile(t, p.in, p.out, p.rows, true, us2);
+    if (us + us2 < best) best = us + us2, p.s2 = a, p.s3 = b;
+  }
+  p.tlog = 0;
+  while (p.tlog < 6 && (8 << p.tlog) < p.out8) ++p.tlog;
+  p.cblocks = (p.out8 + (8 << p.tlog) - 1) / (8 << p.tlog);
+  const int64_t teams = 256 >> p.tlog;
+  p.rblocks = std::max<int64_t>(
+      1, std::min<int64_t>((p.rows + 4 * teams - 1) / (4 * teams), 2048 / p.cblocks));
+  p.per = up((std::max<int64_t>(p.rows, 1) + p.rblocks - 1) / p.rblocks, 4 * teams);
+  p.rblocks = std::max<int64_t>(1, (p.rows + p.per - 1) / p.per);
+  p.xu = take((size_t)p.rows * p.in8 * 2);
+  p.dz = take(d.act != FG_ACT_NONE || p.out % 8 ? (size_t)p.rows * p.out8 * 2 : 0);
+  p.db = take((size_t)p.rblocks * p.out8 * 4);
+  p.pdx = take(p.s2.ns > 1 ? (size_t)p.s2.ns * p.rows * p.in8 * 4 : 0);
+  p.pdw = take(p.s3.ns > 1 ? (size_t)p.s3.ns * p.out * p.in8 * 4 : 0);
+  p.total = at;
+  return p;
+}
+
+#define FG_TRY(x)                      \
+  do {                                 \
+    const hipError_t e_ = (x);         \
+    if (e_ != hipSuccess) return e_;   \
+  } while (0)
+
+#define FG_LINEAR_TILE(FN, TS, tile, bf, ...)                                        \
+  ((tile) == 2   ? ((bf) ? FN<Bf16<TS::T256>>(__VA_ARGS__) : FN<TS::T256>(__VA_ARGS__)) \
+   : (tile) == 1 ? ((bf) ? FN<Bf16<P128>>(__VA_ARGS__) : FN<P128>(__VA_ARGS__))       \
+                 : ((bf) ? FN<Bf16<P64>>(__VA_ARGS__) : FN<P64>(__VA_ARGS__)))
+
+template <class P>
+hipError_t launch_fwd(FwdArgs a, int ns, hipStream_t st) {
+  a.ntile = (a.e.out + P::TM - 1) / P::TM;
+  const TileMap tm = tile_map((a.rows + P::TN - 1) / P::TN, a.ntile, ns);
+  hipLaunchKernelGGL(linear_fwd_kernel<P>, dim3(8 * tm.per), dim3(P::NT), 0, st, a, tm);
+  return hipGetLastError();
+}
+
+template <class P>
+hipError_t launch_products(ProdArgs dx, int nsx, ProdArgs dw, int nsw, hipStream_t st) {
+  dx.ntile = (int32_t)((dx.N + P::TN - 1) / P::TN);
+  dw.ntile = (int32_t)((dw.N + P::TN - 1) / P::TN);
+  const TileMap none{1, 1, 0, 0, kOutputMajor};
+  const TileMap tx = nsx ? tile_map((dx.M + P::TM - 1) / P::TM, dx.ntile, nsx) : none;
+  const TileMap tw = nsw ? tile_map((dw.M + P::TM - 1) / P::TM, dw.ntile, nsw) : none;
+  hipLaunchKernelGGL(linear_products_kernel<P>, dim3(8 * (tx.per + tw.per)), dim3(P::NT), 0, st,
+                     dx, tx, dw, tw, 8 * tx.per);
+  return hipGetLastError();
+}
+
+hipError_t pad(const uint16_t *x, int64_t ld, int64_t n, uint16_t *to, int64_t rows,
+               hipStream_t st) {
+  hipLaunchKernelGGL(linear_pad_kernel, dim3((uint32_t)((rows + 255) / 256)), dim3(256), 0, st, x,
+                     ld, (int32_t)n, to, rows);
+  return hipGetLastError();
+}
+
+}  // namespace linear
+
+size_t linear_ws_bytes(const fg_linear_desc &d, bool grad) {
+  return linear::make_plan(d, grad).total;
+}
+
+hipError_t launch_linear_fwd(const fg_linear_desc &d, const void *x, const void *w,
+                             const void *bias, const void *residual, void *y, void *z,
+                             void *packed_z, void *ws, hipStream_t st) {
+  using namespace linear;
+  const Plan p = make_plan(d, false);
+  uint8_t *base = static_cast<uint8_t *>(ws);
+  const bool bf = d.dtype == FG_BF16;
+  FwdArgs a{};
+  a.w = (const uint16_t *)w, a.x = (const uint16_t *)x;
+  a.w_ld = d.w_ld ? d.w_ld : p.in, a.x_ld = d.x_ld ? d.x_ld : p.in;
+  if (p.narrow) {
+    uint16_t *wp = (uint16_t *)(base + p.wpad), *xp = (uint16_t *)(base + p.xpad);
+    FG_TRY(pad(a.w, a.w_ld, p.in, wp, p.out, st));
+    FG_TRY(pad(a.x, a.x_ld, p.in, xp, p.rows, st));
+    a.w = wp, a.x = xp, a.w_ld = a.x_ld = 8;
+  }
+  a.K = (int32_t)p.K, a.kper = p.s1.kper, a.rows = p.rows;
+  Epilogue &e = a.e;
+  e.bias = (const uint16_t *)bias, e.residual = (const uint16_t *)residual;
+  e.y = (uint16_t *)y, e.z = (uint16_t *)z;
+  const auto ld = [&](int64_t v) { return v ? v : p.out; };
+  e.y_ld = ld(d.y_ld), e.r_ld = ld(d.r_ld), e.z_ld = ld(d.z_ld);
+  if (packed_z) e.packed = rows::packed_at(packed_z, p.rows, p.out);
+  e.out = (int32_t)p.out, e.act = d.act;
+  a.Mq = (int32_t)p.out8, a.pstride = p.rows * p.out8;
+  const bool split = p.s1.ns > 1;
+  if (split) a.part = (float *)(base + p.p1);
+  FG_TRY(FG_LINEAR_TILE(launch_fwd, FwdTiles, p.s1.tile, bf, a, p.s1.ns, st));
+  if (!split) return hipSuccess;
+  const JoinFwd j = {a.part, a.pstride, p.rows, p.s1.ns, a.Mq, (int32_t)up(p.out, 32), e};
+  const dim3 grid((uint32_t)((p.rows * (j.wide / 8) + 255) / 256)), block(256);
+  if (bf)
+    hipLaunchKernelGGL(linear_join_fwd_kernel<FG_BF16>, grid, block, 0, st, j);
+  else
+    hipLaunchKernelGGL(linear_join_fwd_kernel<FG_F16>, grid, block, 0, st, j);
+  return hipGetLastError();
+}
+
+hipError_t launch_linear_bwd(const fg_linear_desc &d, const void *dy, const void *x,
+                             const void *packed_x, const void *w, const void *z,
+                             const void *packed_z, void *dx, void *dw, void *dbias,
+                             int32_t *flag, void *ws, hipStream_t st) {
+  using namespace linear;
+  const Plan p = make_plan(d, true);
+  uint8_t *base = static_cast<uint8_t *>(ws);
+  const bool bf = d.dtype == FG_BF16;
+  const auto ld = [&](int64_t v, int64_t width) { return v ? v : width; };
+
+  // dz, and the parts of its columns' sums
+  DzArgs z1{};
+  z1.dy = (const uint16_t *)dy, z1.dy_ld = ld(d.y_ld, p.out);
+  z1.z = (const uint16_t *)z, z1.z_ld = ld(d.z_ld, p.out);
+  if (packed_z) z1.packed = rows::packed_at(packed_z, p.rows, p.out);
+  const bool formed = (dx || dw) && (d.act != FG_ACT_NONE || p.out % 8);
+  z1.dz = formed ? (uint16_t *)(base + p.dz) : nullptr;
+  z1.part = dbias ? (float *)(base + p.db) : nullptr;
+  z1.rows = p.rows, z1.per = p.per;
+  z1.out = (int32_t)p.out, z1.Mp = (int32_t)p.out8, z1.act = d.act, z1.tlog = p.tlog;
+  if ((formed || dbias) && p.rows) {
+    const dim3 grid((uint32_t)p.cblocks, (uint32_t)p.rblocks), block(256);
+    if (bf)
+      hipLaunchKernelGGL(linear_dz_kernel<FG_BF16>, grid, block, 0, st, z1);
+    else
+      hipLaunchKernelGGL(linear_dz_kernel<FG_F16>, grid, block, 0, st, z1);
+    FG_TRY(hipGetLastError());
+  }
+  if (dbias) {
+    const SumArgs s = {z1.part, (uint16_t *)dbias, (int32_t)(p.rows ? p.rblocks : 0),
+                       (int32_t)p.out8, (int32_t)p.out, flag};
+    const dim3 grid((uint32_t)((p.out + 63) / 64)), block(512);
+    if (bf)
+      hipLaunchKernelGGL(linear_sum_kernel<FG_BF16>, grid, block, 0, st, s);
+    else
+      hipLaunchKernelGGL(linear_sum_kernel<FG_F16>, grid, block, 0, st, s);
+    FG_TRY(hipGetLastError());
+  }
+  if (!dx && !dw) return hipSuccess;
+
+  ProdArgs a{}, b{};
+  a.b = b.b = formed ? z1.dz : z1.dy;
+  a.b_ld = b.b_ld = formed ? p.out8 : z1.dy_ld;
+  a.b_cols = b.b_cols = (int32_t)p.out8;
+  a.a_cols = b.a_cols = (int32_t)p.K;
+  a.M = b.M = (int32_t)p.in, a.Mq = b.Mq = (int32_t)p.in8;
+  JoinArgs jx{}, jw{};
+  int nsx = 0, nsw = 0;
+  if (dx && p.rows) {
+    a.a = (const uint16_t *)w, a.a_ld = ld(d.w_ld, p.in);
+    if (p.narrow) {
+      uint16_t *to = (uint16_t *)(base + p.wpad);
+      FG_TRY(pad(a.a, a.a_ld, p.in, to, p.out, st));
+      a.a = to, a.a_ld = 8;
+    }
+    nsx = p.s2.ns;
+    a.N = p.rows, a.K = p.out, a.kper = p.s2.kper;
+    a.out_ld = ld(d.dx_ld, p.in);
+    a.pstride = p.rows * p.in8;
+    (nsx > 1 ? (void *&)a.part : (void *&)a.out) = nsx > 1 ? (void *)(base + p.pdx) : dx;
+    jx = {a.part, a.pstride, p.rows, nsx, a.M, a.Mq, (uint16_t *)dx, a.out_ld, nullptr};
+  }
+  if (dw) {
+    b.a = (const uint16_t *)x, b.a_ld = ld(d.x_ld, p.in);
+    if (packed_x && p.rows) {
+      const fg_act8_desc u = {p.rows, p.in, p.in8, d.dtype};
+      FG_TRY(launch_act8(u, nullptr, base + p.xu, const_cast<void *>(packed_x), st));
+      b.a = (const uint16_t *)(base + p.xu), b.a_ld = p.in8;
+    }
+    if (p.narrow && p.rows) {
+      uint16_t *to = (uint16_t *)(base + p.xu);  // (each row onto itself where it is there)
+      FG_TRY(pad(b.a, b.a_ld, p.in, to, p.rows, st));
+      b.a = to, b.a_ld = 8;
+    }
+    nsw = p.s3.ns;
+    b.N = p.out, b.K = p.rows, b.kper = p.s3.kper;
+    b.out_ld = ld(d.dw_ld, p.in);
+    b.pstride = p.out * p.in8;
+    (nsw > 1 ? (void *&)b.part : (void *&)b.out) = nsw > 1 ? (void *)(base + p.pdw) : dw;
+    b.flag = flag;
+    jw = {b.part, b.pstride, p.out, nsw, b.M, b.Mq, (uint16_t *)dw, b.out_ld, flag};
+  }
+  if (!nsx && !nsw) return hipSuccess;
+  FG_TRY(FG_LINEAR_TILE(launch_products, BwdTiles, p.s2.tile, bf, a, nsx, b, nsw, st));
+  const int64_t bx = nsx > 1 ? (p.rows * (p.in8 / 8) + 255) / 256 : 0;
+  const int64_t bw = nsw > 1 ? (p.out * (p.in8 / 8) + 255) / 256 : 0;
+  if (!bx && !bw) return hipSuccess;
+  const dim3 grid((uint32_t)(bx + bw)), block(256);
+  if (bf)
+    hipLaunchKernelGGL(linear_join_kernel<FG_BF16>, grid, block, 0, st, jx, jw, (int)bx);
+  else
+    hipLaunchKernelGGL(linear_join_kernel<FG_F16>, grid, block, 0, st, jx, jw, (int)bx);
+  return hipGetLastError();
+}
+
+}  // namespace fg

@@ -92,6 +92,61 @@ def test_layer_norm_bwd_refusals(L):
     assert call(rows=0, dy=None, x=None, stats=None, dw=None, db=None, ws=None) == fg.FG_OK
 
 
+def test_linear_fwd_refusals(L):
+    d0 = dict(rows=64, fan_in=40, fan_out=24, act=fg.ACT_GELU)
+
+    def call(none=False, x=at(0), w=at(1), b=at(2), r=at(3), y=at(4), z=at(5), packed=at(6),
+             ws=at(7), ws_bytes=1 << 24, **kw):
+        d = fg.LinearDesc.make(**{**d0, **kw})
+        return L.linear_fwd(None if none else ctypes.byref(d), x, w, b, r, y, z, packed, ws,
+                            ws_bytes, None)
+
+    assert call(none=True) == fg.FG_EINVAL
+    for bad in (dict(x=None), dict(w=None), dict(y=None), dict(rows=-1), dict(fan_in=0),
+                dict(fan_out=0), dict(dtype=3), dict(act=3), dict(act=-1), dict(act=fg.ACT_NONE),
+                dict(x_ld=39), dict(w_ld=39), dict(y_ld=23), dict(r_ld=23), dict(z_ld=23),
+                dict(dx_ld=39), dict(dw_ld=39), dict(x=at(0) + 1), dict(b=at(2) + 1),
+                dict(packed=at(6) + 8), dict(y=at(0)), dict(y=at(1)), dict(y=at(2)), dict(y=at(5)),
+                dict(z=at(3)), dict(y=at(3) + 2), dict(y=at(3), y_ld=32), dict(packed=at(1))):
+        assert call(**bad) == fg.FG_EINVAL, bad
+    for bad in (dict(dtype=fg.F32), dict(rows=1 << 28), dict(fan_in=(1 << 17) + 1),
+                dict(fan_out=(1 << 17) + 1), dict(x_ld=1 << 20), dict(rows=1 << 27, fan_out=1024)):
+        assert call(**bad) == fg.FG_EUNSUPPORTED, bad
+        assert fg.linear_workspace_bytes(fg.LinearDesc.make(
+            **{**d0, **{k: v for k, v in bad.items()}}), False) == 0
+    assert call(rows=0, x=None, y=None) == fg.FG_OK
+    split = dict(rows=64, fan_in=8000, fan_out=24)    # a long sum of few tiles, in parts
+    need = fg.linear_workspace_bytes(fg.LinearDesc.make(**split), False)
+    if need:
+        for bad in (dict(ws=None), dict(ws_bytes=need - 1), dict(ws=at(7) + 8)):
+            assert call(**split, **bad) == fg.FG_EWORKSPACE
+
+
+def test_linear_bwd_refusals(L):
+    d0 = dict(rows=64, fan_in=40, fan_out=24, act=fg.ACT_GELU)
+    need = fg.linear_workspace_bytes(fg.LinearDesc.make(**d0), True)
+    assert need > 0
+
+    def call(none=False, dy=at(0), x=at(1), px=None, w=at(2), z=at(3), pz=None, dx=at(4),
+             dw=at(5), db=at(6), flag=at(7), ws=at(8), ws_bytes=need, **kw):
+        d = fg.LinearDesc.make(**{**d0, **kw})
+        return L.linear_bwd(None if none else ctypes.byref(d), dy, x, px, w, z, pz, dx, dw, db,
+                            flag, ws, ws_bytes, None)
+
+    assert call(none=True) == fg.FG_EINVAL
+    for bad in (dict(dy=None), dict(x=None), dict(w=None), dict(z=None), dict(px=at(9)),
+                dict(pz=at(9)), dict(dx=None, dw=None, db=None), dict(act=fg.ACT_NONE),
+                dict(x=None, px=at(9) + 4), dict(z=None, pz=at(9) + 4), dict(dx=at(0)),
+                dict(dx=at(2)), dict(dw=at(1)), dict(dw=at(4)), dict(db=at(0)), dict(flag=at(6)),
+                dict(flag=at(7) + 1), dict(ws=at(0)), dict(dw=at(8)), dict(dx=at(4) + 1),
+                dict(rows=-1), dict(dx_ld=8), dict(x=None, px=at(4))):
+        assert call(**bad) == fg.FG_EINVAL, bad
+    for bad in (dict(ws=None), dict(ws_bytes=need - 1), dict(ws=at(8) + 8)):
+        assert call(**bad) == fg.FG_EWORKSPACE, bad
+    assert call(dtype=fg.F32) == fg.FG_EUNSUPPORTED
+    assert call(dw_ld=1 << 20) == fg.FG_EUNSUPPORTED
+
+
 def test_bindings_check_tensors():
     h = lambda *s: torch.zeros(*s, dtype=torch.float16)
     d = fg.NormDesc.make(24, 8)
