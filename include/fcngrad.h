@@ -683,7 +683,7 @@ size_t fg_linear_workspace_bytes(const fg_linear_desc *d, int grad);
  * in, w: out x in, bias: out (null: 0), residual: rows x out (null: 0). For the backward pass of
  * an activation, z (rows x out, rounded) and packed_z (its 8-bit checkpoint) may be kept;
  * either may be null, and both must be without one. y may be the residual itself at the same
- * stride. Phi is within 1.2e-5 of itself. FG_EUNSUPPORTED also for FG_F32, rows of 2^28,
+ * stride. Phi(-|z|) is within 1.2e-5 of itself up to |z| = 6, and of 1e-9 beyond. FG_EUNSUPPORTED also for FG_F32, rows of 2^28,
  * in or out above 2^17, strides of 2^20, rows * in or rows * out of 2^34 or more. */
 fg_status linear_fwd(const fg_linear_desc *d, const void *x, const void *w, const void *bias,
                      const void *residual, void *y, void *z, void *packed_z, void *ws,

@@ -31,34 +31,34 @@ struct BwdTiles {
 };
 
 // ---- activations ---------------------------------------------------------------------
-// Phi(-|z|) = exp(-z^2 / 2) R(|z|), Phi the normal distribution's function: R as a polynomial
-// in t = 1 / (1 + c |z|), fitted here to its values (largest relative error 4.7e-6, where a
-// result's rounding to fp16 is 4.9e-4); relative, so that far negative z keep their digits.
-// One exponential and one reciprocal, some 16 instructions. -inf gives 0, NaN NaN.
-struct Gauss {
-  float below, bell;  // Phi(-|z|); exp(-z^2 / 2)
-  __device__ __forceinline__ explicit Gauss(float z) {
-    const float a = fabsf(z);
-    const float t = __builtin_amdgcn_rcpf(fmaf(a, 0.31f, 1.f));
-    bell = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
-    float r = fmaf(t, -0.07392825f, 0.18044779f);
-    r = fmaf(r, t, 0.01574751f);
-    r = fmaf(r, t, 0.13342834f);
-    r = fmaf(r, t, 0.12044163f);
-    r = fmaf(r, t, 0.12386067f);
-    below = bell * (r * t);
-  }
-  __device__ __forceinline__ float phi(float z) const { return z > 0.f ? 1.f - below : below; }
-};
-__device__ __forceinline__ float gelu(float z) {
-  return fmaxf(z, -64.f) * Gauss(z).phi(z);
+// Phi(-|z|), Phi the normal distribution's function, as 2^P(|z|): the logarithm is smooth, so a
+// polynomial of degree 7 fitted here keeps 5.7e-6 of the value (fp32 steps included; a result's
+// rounding to fp16 is 4.9e-4) up to |z| = 6, and falls on beyond, where Phi(-|z|) < 1e-9. No
+// reciprocal, and the digits of far negative z stay: 14 instructions for gelu, of which the
+// exponential takes four turns.
+__device__ __forceinline__ float phi_below(float z) {
+  const float a = fabsf(z);
+  float r = fmaf(a, -1.83478636e-6f, 6.15977578e-5f);
+  r = fmaf(r, a, -9.30520317e-4f);
+  r = fmaf(r, a, 8.50787166e-3f);
+  r = fmaf(r, a, -5.39600260e-2f);
+  r = fmaf(r, a, -0.458464442f);
+  r = fmaf(r, a, -1.15125102f);
+  r = fmaf(r, a, -0.999995298f);
+  return __builtin_amdgcn_exp2f(r);
 }
+// z Phi(z) = max(z, 0) - |z| Phi(-|z|). Infinities give 0 and themselves, NaN NaN.
+__device__ __forceinline__ float gelu(float z) {
+  return fmaf(-fminf(fabsf(z), 64.f), phi_below(z), fmaxf(z, 0.f));
+}
+// Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi)
 __device__ __forceinline__ float gelu_slope(float z) {
-  const Gauss g(z);
-  return fmaf(fminf(fmaxf(z, -64.f), 64.f) * 0.39894228f, g.bell, g.phi(z));
+  const float bell = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+  const float phi = 0.5f + copysignf(0.5f - phi_below(z), z);
+  return fmaf(__builtin_amdgcn_fmed3f(z, -64.f, 64.f) * 0.39894228f, bell, phi);
 }
 __device__ __forceinline__ float apply(float z, int act) {
-  return act == FG_ACT_RELU ? (z > 0.f || z != z ? z : 0.f) : act == FG_ACT_GELU ? gelu(z) : z;
+  return act == FG_ACT_RELU ? (z < 0.f ? 0.f : z) : act == FG_ACT_GELU ? gelu(z) : z;
 }
 
 __device__ __forceinline__ float to_f32(uint32_t half, bool bf) {
@@ -155,20 +155,14 @@ __device__ __forceinline__ void pack_block(const f32x16 (&acc)[P::FM][P::FN], co
   for (int j = 0; j < P::FN; ++j)
 #pragma unroll
     for (int i = 0; i < P::FM; ++i) {
-      uint32_t top = 0;
+      float v[16];
 #pragma unroll
-      for (int v = 0; v < 16; ++v) top = max(top, rows::magnitude(acc[i][j][v]));
-      top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-      const uint32_t b = rows::group_exp(top);
-      const float inv = rows::steps_of(b);
+      for (int e = 0; e < 16; ++e) v[e] = acc[i][j][e];
       uint32_t q[4];
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        uint32_t c[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) c[e] = rows::code_of(acc[i][j][4 * g + e], inv);
-        q[g] = rows::bytes4(c[0], c[1], c[2], c[3]);
-      }
+      const uint32_t b =
+          rows::pack_group<16>(v, q, [](uint32_t top) __attribute__((always_inline)) {
+            return max(top, (uint32_t)__shfl_xor((int)top, 32));
+          });
       const uint32_t r0 = __shfl_xor((int)(up ? q[0] : q[2]), 32);
       const uint32_t r1 = __shfl_xor((int)(up ? q[1] : q[3]), 32);
       const int64_t n = n0 + 32 * j + (lane & 31);
@@ -335,6 +329,106 @@ __global__ __launch_bounds__(P::NT, P::WPE) void linear_fwd_kernel(FwdArgs a, Ti
   epilogue<P>(acc, a.e, wave_buf<P>(R, wave), lane, n0 + wn0, m0 + wm0, a.rows);
 }
 
+// ---- forward, few rows -----------------------------------------------------------------
+// Up to 16 NB rows (tokens served one by one): bound by reading the weights once. A workgroup
+// takes 16 outputs, its 8 waves a run of the sum each: both operands go straight from memory
+// to the MFMA's registers, kAhead steps of 32 at a time, and the waves' sums meet in LDS.
+constexpr int kFewRows = 64;
+template <bool BF>
+__device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
+  if (BF)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a),
+                                                   __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a),
+                                                __builtin_bit_cast(half8, b), c, 0, 0, 0);
+}
+// Elements c .. c + 7 of a row of K (at least 8), zeros past its end.
+__device__ __forceinline__ u32x4 ending(const uint16_t *row, int c, int K) {
+  const int s = c - min(c, K - 8);
+  const u32x4 r = reinterpret_cast<const Any16 *>(row + min(c, K - 8))->v;
+  const uint64_t lo = (uint64_t)r[1] << 32 | r[0], hi = (uint64_t)r[3] << 32 | r[2];
+  const int sh = 16 * (s & 3);
+  uint64_t a = lo, b = hi;
+  if (s & 4) a = hi, b = 0;
+  if (sh) a = a >> sh | b << (64 - sh), b >>= sh;
+  if (s >= 8) a = b = 0;
+  return u32x4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+}
+
+template <bool BF, int NB>
+__global__ __launch_bounds__(512) void linear_few_kernel(FwdArgs a) {
+  constexpr int kAhead = 8;
+  __shared__ f32x4 sums[8][NB][64];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m0 = blockIdx.x * 16, K = a.K, rows = (int)a.rows, out = a.e.out;
+  const int c0 = 8 * (lane >> 4);
+  const uint16_t *w = a.w + min(m0 + (lane & 15), out - 1) * a.w_ld + c0;
+  const uint16_t *x[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) x[b] = a.x + min(16 * b + (lane & 15), rows - 1) * a.x_ld + c0;
+  // what the end needs: lane's outputs m .. m + 3 of row n (on their way meanwhile)
+  const Epilogue &e = a.e;
+  const int n = 16 * wave + (lane & 15), m = m0 + 4 * (lane >> 4);
+  const bool mine = wave < NB && n < rows && m < out;
+  float bias[4] = {}, res[4] = {};
+  if (mine && e.bias) load4(e.bias, m, out, BF, bias);
+  if (mine && e.residual) load4(e.residual + n * e.r_ld, m, out, BF, res);
+  f32x4 acc[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int full = K / 32, per = (full + 7) / 8;
+  const int s1 = min(full, (wave + 1) * per);
+  for (int s0 = wave * per; s0 < s1; s0 += kAhead) {
+    u32x4 fa[kAhead], fb[kAhead][NB];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int s = min(s0 + k, s1 - 1);
+      fa[k] = reinterpret_cast<const Any16 *>(w + 32 * s)->v;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) fb[k][b] = reinterpret_cast<const Any16 *>(x[b] + 32 * s)->v;
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (s0 + k < s1) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[b] = mfma16<BF>(fa[k], fb[k][b], acc[b]);
+      }
+  }
+  if (wave == 7 && K % 32) {  // what is left of the sum
+    const u32x4 f = ending(w - c0, 32 * full + c0, K);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+      acc[b] = mfma16<BF>(f, ending(x[b] - c0, 32 * full + c0, K), acc[b]);
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b) sums[wave][b][lane] = acc[b];
+  __syncthreads();
+  if (!mine) return;
+  float v[4] = {};
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const f32x4 q = sums[k][wave][lane];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += q[i];
+  }
+  auto put = [&](uint16_t *row) __attribute__((always_inline)) {
+    const u32x2 q = {pack2(v[0], v[1], BF), pack2(v[2], v[3], BF)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (m + i < out) row[m + i] = (uint16_t)(q[i >> 1] >> (16 * (i & 1)));
+  };
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] += bias[i];
+  if (e.z) put(e.z + n * e.z_ld);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] = apply(v[i], e.act);
+    if (e.residual) v[i] += res[i];
+  }
+  put(e.y + n * e.y_ld);
+}
+
 // ---- the gradient of z -----------------------------------------------------------------
 struct DzArgs {
   const uint16_t *dy, *z;
@@ -346,61 +440,94 @@ struct DzArgs {
 };
 
 // dz = dy act'(z), rounded to the type that the products take, in rows of a multiple of 8
-// with zeros behind them; its columns' fp32 sums per workgroup, before the rounding.
-template <int DT>
+// with zeros behind them; its columns' fp32 sums per workgroup, before the rounding. Bound by
+// memory: the next kRows rows are on their way while these are worked on. KEPT: z in 16 bits
+// or (1) its checkpoint; EVEN: 8 divides the columns, no masks.
+constexpr int kRows = 4;
+template <class T, int ACT, int KEPT, bool EVEN>
+struct DzLoads {
+  rows::Raw<T> d[kRows], h[ACT && !KEPT ? kRows : 1];
+  u32x2 q[ACT && KEPT ? kRows : 1];
+  uint32_t e[ACT && KEPT ? kRows : 1];
+  static __device__ __forceinline__ rows::Raw<T> raw(const T *row, int c, int cols) {
+    if constexpr (EVEN)
+      return __builtin_bit_cast(rows::Raw<T>, reinterpret_cast<const Any16 *>(row + c)->v);
+    else
+      return rows::load_any(row, c, cols);
+  }
+  __device__ __forceinline__ void load(const DzArgs &a, int64_t r, int teams, int c) {
+    const T *dy = reinterpret_cast<const T *>(a.dy), *z = reinterpret_cast<const T *>(a.z);
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const int64_t n = min(r + k * teams, a.rows - 1);
+      d[k] = raw(dy + n * a.dy_ld, c, a.out);
+      if constexpr (ACT && KEPT) {
+        q[k] = *reinterpret_cast<const u32x2 *>(a.packed.codes + n * a.packed.wide + c);
+        e[k] = a.packed.exps[n * (a.packed.wide / 32) + c / 32];
+      } else if constexpr (ACT != 0) {
+        h[k] = raw(z + n * a.z_ld, c, a.out);
+      }
+    }
+  }
+  static __device__ __forceinline__ void numbers(const rows::Raw<T> &r, int c, int cols,
+                                                 float (&v)[8]) {
+    if constexpr (EVEN) {
+      typedef T t8 __attribute__((ext_vector_type(8)));
+      const t8 x = __builtin_bit_cast(t8, r);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = (float)x[i];
+    } else {
+      rows::values<T>(r, c, cols, v);
+    }
+  }
+};
+
+template <int DT, int ACT, int KEPT, bool EVEN>
 __global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a) {
   using T = typename TypeOf<DT>::T;
+  using Loads = DzLoads<T, ACT, KEPT, EVEN>;
   __shared__ float sums[256][9];
   const int tl = 1 << a.tlog, t = threadIdx.x & (tl - 1), team = threadIdx.x >> a.tlog;
   const int teams = 256 >> a.tlog;
   const int c = 8 * ((int)blockIdx.x * tl + t);
-  const int64_t r0 = (int64_t)blockIdx.y * a.per, r1 = min(a.rows, r0 + a.per);
-  const T *dy = reinterpret_cast<const T *>(a.dy), *z = reinterpret_cast<const T *>(a.z);
+  const int64_t r0 = (int64_t)blockIdx.y * a.per + team, r1 = min(a.rows, r0 - team + a.per);
   T *dz = reinterpret_cast<T *>(a.dz);
   float s[8] = {};
-  constexpr int B = 4;  // rows on their way
-  if (c < a.Mp)
-    for (int64_t r = r0 + team; r < r1; r += B * teams) {
-      rows::Raw<T> d[B], h[B];
-      u32x2 q[B];
-      uint32_t e[B];
+  if (c < a.Mp) {
+    Loads next;
+    next.load(a, r0, teams, c);
+    for (int64_t r = r0; r < r1; r += kRows * teams) {
+      const Loads now = next;
+      if (r + kRows * teams < r1) next.load(a, r + kRows * teams, teams, c);
 #pragma unroll
-      for (int k = 0; k < B; ++k) {
-        const int64_t n = min(r + k * teams, a.rows - 1);
-        d[k] = rows::load_any(dy + n * a.dy_ld, c, a.out);
-        if (a.act == FG_ACT_NONE) continue;
-        if (a.packed.codes) {
-          q[k] = *reinterpret_cast<const u32x2 *>(a.packed.codes + n * a.packed.wide + c);
-          e[k] = a.packed.exps[n * (a.packed.wide / 32) + c / 32];
-        } else {
-          h[k] = rows::load_any(z + n * a.z_ld, c, a.out);
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < B; ++k) {
+      for (int k = 0; k < kRows; ++k) {
         const int64_t n = r + k * teams;
         if (n >= r1) break;
         float g[8], v[8];
-        rows::values<T>(d[k], c, a.out, g);
-        if (a.act != FG_ACT_NONE) {
-          if (a.packed.codes)
-            rows::decode8(q[k], e[k], v);
+        Loads::numbers(now.d[k], c, a.out, g);
+        if constexpr (ACT != 0) {
+          if constexpr (KEPT)
+            rows::decode8(now.q[k], now.e[k], v);
           else
-            rows::values<T>(h[k], c, a.out, v);
+            Loads::numbers(now.h[k], c, a.out, v);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            if (a.act == FG_ACT_RELU)
+            if constexpr (ACT == FG_ACT_RELU)
               g[i] = v[i] > 0.f ? g[i] : v[i] != v[i] ? v[i] : 0.f;
             else
               g[i] *= gelu_slope(v[i]);
-            if (c + i >= a.out) g[i] = 0.f;
+            if (!EVEN && c + i >= a.out) g[i] = 0.f;
           }
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] += g[i];
-        if (dz) rows::store8(dz + n * a.Mp, c, a.Mp, g);
+        if (dz)
+          *reinterpret_cast<u32x4 *>(dz + n * a.Mp + c) =
+              u32x4{pack2(g[0], g[1], DT == FG_BF16), pack2(g[2], g[3], DT == FG_BF16),
+                    pack2(g[4], g[5], DT == FG_BF16), pack2(g[6], g[7], DT == FG_BF16)};
       }
     }
+  }
   if (!a.part) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) sums[threadIdx.x][i] = s[i];
@@ -414,7 +541,7 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a) {
   }
 }
 
-// The sums of the row blocks, in order: 64 columns a workgroup, 8 waves a run of them each.
+// The sums of the row blocks, in order: 16 columns a workgroup, 64 lanes' runs of them each.
 struct SumArgs {
   const float *part;
   uint16_t *out;
@@ -422,22 +549,13 @@ struct SumArgs {
   int32_t *flag;
 };
 template <int DT>
-__global__ __launch_bounds__(512) void linear_sum_kernel(SumArgs a) {
+__global__ __launch_bounds__(256) void linear_sum_kernel(SumArgs a) {
   using T = typename TypeOf<DT>::T;
-  __shared__ float sh[8][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int c = blockIdx.x * 64 + lane, per = (a.n + 7) / 8;
-  const int k0 = wave * per, k1 = min(a.n, k0 + per);
-  float s = 0.f;
-#pragma unroll 8
-  for (int k = k0; k < k1; ++k) s += a.part[(int64_t)k * a.Mp + min(c, a.Mp - 1)];
-  sh[wave][lane] = s;
-  __syncthreads();
-  if (wave) return;
-#pragma unroll
-  for (int k = 1; k < 8; ++k) s += sh[k][lane];
+  float s;
+  const int c = 16 * (int)blockIdx.x + (threadIdx.x & 15);
+  rows::sum_columns(a.part, a.n, a.Mp, 16 * (int)blockIdx.x, a.Mp, s);
   bool bad = false;
-  if (c < a.cols) {
+  if (threadIdx.x < 16 && c < a.cols) {
     const T v = (T)s;
     reinterpret_cast<T *>(a.out)[c] = v;
     bad = !(fabsf((float)v) < INFINITY);
@@ -756,6 +874,18 @@ hipError_t launch_fwd(FwdArgs a, int ns, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <bool BF>
+hipError_t launch_few(const FwdArgs &a, hipStream_t st) {
+  const dim3 grid((uint32_t)((a.e.out + 15) / 16)), block(512);
+  if (a.rows <= 16)
+    hipLaunchKernelGGL((linear_few_kernel<BF, 1>), grid, block, 0, st, a);
+  else if (a.rows <= 32)
+    hipLaunchKernelGGL((linear_few_kernel<BF, 2>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((linear_few_kernel<BF, 4>), grid, block, 0, st, a);
+  return hipGetLastError();
+}
+
 template <class P>
 hipError_t launch_products(ProdArgs dx, int nsx, ProdArgs dw, int nsw, hipStream_t st) {
   dx.ntile = (int32_t)((dx.N + P::TN - 1) / P::TN);
@@ -766,6 +896,24 @@ hipError_t launch_products(ProdArgs dx, int nsx, ProdArgs dw, int nsw, hipStream
   hipLaunchKernelGGL(linear_products_kernel<P>, dim3(8 * (tx.per + tw.per)), dim3(P::NT), 0, st,
                      dx, tx, dw, tw, 8 * tx.per);
   return hipGetLastError();
+}
+
+template <int DT, int ACT, int KEPT>
+hipError_t launch_dz_of(const DzArgs &a, const Plan &p, hipStream_t st) {
+  const dim3 grid((uint32_t)p.cblocks, (uint32_t)p.rblocks), block(256);
+  if (p.out % 8 == 0)
+    hipLaunchKernelGGL((linear_dz_kernel<DT, ACT, KEPT, true>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((linear_dz_kernel<DT, ACT, KEPT, false>), grid, block, 0, st, a);
+  return hipGetLastError();
+}
+template <int DT>
+hipError_t launch_dz(const DzArgs &a, const Plan &p, hipStream_t st) {
+  const bool kept = a.packed.codes != nullptr;
+  return a.act == FG_ACT_NONE ? launch_dz_of<DT, FG_ACT_NONE, 0>(a, p, st)
+         : a.act == FG_ACT_RELU
+             ? (kept ? launch_dz_of<DT, FG_ACT_RELU, 1> : launch_dz_of<DT, FG_ACT_RELU, 0>)(a, p, st)
+             : (kept ? launch_dz_of<DT, FG_ACT_GELU, 1> : launch_dz_of<DT, FG_ACT_GELU, 0>)(a, p, st);
 }
 
 hipError_t pad(const uint16_t *x, int64_t ld, int64_t n, uint16_t *to, int64_t rows,
@@ -805,6 +953,7 @@ hipError_t launch_linear_fwd(const fg_linear_desc &d, const void *x, const void 
   e.y_ld = ld(d.y_ld), e.r_ld = ld(d.r_ld), e.z_ld = ld(d.z_ld);
   if (packed_z) e.packed = rows::packed_at(packed_z, p.rows, p.out);
   e.out = (int32_t)p.out, e.act = d.act;
+  if (p.rows <= kFewRows && !packed_z) return bf ? launch_few<true>(a, st) : launch_few<false>(a, st);
   a.Mq = (int32_t)p.out8, a.pstride = p.rows * p.out8;
   const bool split = p.s1.ns > 1;
   if (split) a.part = (float *)(base + p.p1);
@@ -840,17 +989,12 @@ hipError_t launch_linear_bwd(const fg_linear_desc &d, const void *dy, const void
   z1.rows = p.rows, z1.per = p.per;
   z1.out = (int32_t)p.out, z1.Mp = (int32_t)p.out8, z1.act = d.act, z1.tlog = p.tlog;
   if ((formed || dbias) && p.rows) {
-    const dim3 grid((uint32_t)p.cblocks, (uint32_t)p.rblocks), block(256);
-    if (bf)
-      hipLaunchKernelGGL(linear_dz_kernel<FG_BF16>, grid, block, 0, st, z1);
-    else
-      hipLaunchKernelGGL(linear_dz_kernel<FG_F16>, grid, block, 0, st, z1);
-    FG_TRY(hipGetLastError());
+    FG_TRY((bf ? launch_dz<FG_BF16> : launch_dz<FG_F16>)(z1, p, st));
   }
   if (dbias) {
     const SumArgs s = {z1.part, (uint16_t *)dbias, (int32_t)(p.rows ? p.rblocks : 0),
                        (int32_t)p.out8, (int32_t)p.out, flag};
-    const dim3 grid((uint32_t)((p.out + 63) / 64)), block(512);
+    const dim3 grid((uint32_t)((p.out + 15) / 16)), block(256);
     if (bf)
       hipLaunchKernelGGL(linear_sum_kernel<FG_BF16>, grid, block, 0, st, s);
     else

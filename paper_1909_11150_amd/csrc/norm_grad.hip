@@ -173,8 +173,7 @@ __global__ __launch_bounds__(512, 2) void norm_bwd_kernel(BwdArgs a) {
     }
 }
 
-// Sums the workgroups' parts, in order: 64 columns of one of the two gradients, 8 waves
-// a run of the parts each.
+// Sums the workgroups' parts, in order: 16 columns of one of the two gradients a workgroup.
 struct JoinArgs {
   const float *part;
   void *dweight, *dbias;   // either may be null
@@ -182,25 +181,16 @@ struct JoinArgs {
   int32_t *flag;
 };
 template <int DT>
-__global__ __launch_bounds__(512) void norm_join_kernel(JoinArgs a) {
+__global__ __launch_bounds__(256) void norm_join_kernel(JoinArgs a) {
   using T = typename TypeOf<DT>::T;
-  __shared__ float sh[8][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, which = blockIdx.y;
-  T *out = static_cast<T *>(which ? a.dbias : a.dweight);
+  T *out = static_cast<T *>(blockIdx.y ? a.dbias : a.dweight);
   if (!out) return;
-  const int c = blockIdx.x * 64 + lane, per = (a.n + 7) / 8;
-  const int k0 = wave * per, k1 = min(a.n, k0 + per);
-  const float *p = a.part + (size_t)which * a.wide + min(c, a.wide - 1);
-  float s = 0.f;
-#pragma unroll 8
-  for (int k = k0; k < k1; ++k) s += p[(size_t)k * 2 * a.wide];
-  sh[wave][lane] = s;
-  __syncthreads();
-  if (wave) return;
-#pragma unroll
-  for (int k = 1; k < 8; ++k) s += sh[k][lane];
+  const int c = 16 * (int)blockIdx.x + (threadIdx.x & 15);
+  float s;
+  sum_columns(a.part + (int64_t)blockIdx.y * a.wide, a.n, 2 * (int64_t)a.wide,
+              16 * (int)blockIdx.x, a.wide, s);
   bool bad = false;
-  if (c < a.cols) {
+  if (threadIdx.x < 16 && c < a.cols) {
     const T v = (T)s;
     out[c] = v;
     bad = !(fabsf((float)v) < INFINITY);
@@ -273,7 +263,7 @@ hipError_t launch_layer_norm_bwd(const fg_norm_desc &d, const void *dy, const vo
   if (!sums) return hipSuccess;
   const norm::JoinArgs j = {a.part, dweight, dbias, (int32_t)(d.rows ? p.blocks : 0),
                             (int32_t)p.wide, a.cols, flag};
-  const dim3 grid((uint32_t)((d.cols + 63) / 64), 2), block(512);
+  const dim3 grid((uint32_t)((d.cols + 15) / 16), 2), block(256);
   if (d.dtype == FG_F16)
     hipLaunchKernelGGL(norm::norm_join_kernel<FG_F16>, grid, block, 0, st, j);
   else if (d.dtype == FG_BF16)

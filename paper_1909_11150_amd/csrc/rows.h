@@ -132,9 +132,13 @@ __host__ __device__ inline Packed packed_at(const void *p, int64_t rows, int64_t
   return {codes, reinterpret_cast<uint8_t *>(codes + rows * wide), (int32_t)wide};
 }
 
-__device__ __forceinline__ uint32_t magnitude(float v) {  // 0 where v is no number
-  const uint32_t u = __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu;
-  return u < 0x7F800000u ? u : 0u;
+constexpr uint32_t kInf = 0x7F800000u;
+__device__ __forceinline__ uint32_t magnitude(float v) {
+  return __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu;
+}
+__device__ __forceinline__ uint32_t finite_magnitude(float v) {  // 0 where v is no number
+  const uint32_t u = magnitude(v);
+  return u < kInf ? u : 0u;
 }
 // Of the largest magnitude of a group.
 __device__ __forceinline__ uint32_t group_exp(uint32_t top) { return max(top >> 23, 8u); }
@@ -144,44 +148,78 @@ __device__ __forceinline__ float step_of(uint32_t b) {
 __device__ __forceinline__ float steps_of(uint32_t b) {  // its reciprocal
   return __builtin_bit_cast(float, (260u - b) << 23);
 }
-// Code in the low byte: adding 1.5 * 2^23 rounds to a whole number, halves to even, and
-// leaves it in the sum's low bits.
+// A number's code in the low byte: adding 1.5 * 2^23 rounds to a whole number, halves to even,
+// and leaves it in the sum's low bits.
 __device__ __forceinline__ uint32_t code_of(float v, float inv) {
-  const float q = fminf(fmaxf(v * inv, -127.f), 127.f) + 12582912.f;
-  const bool number = (__builtin_bit_cast(uint32_t, v) & 0x7F800000u) != 0x7F800000u;
-  return number ? __builtin_bit_cast(uint32_t, q) : 0x80u;
+  constexpr float k = 12582912.f;
+  return __builtin_bit_cast(uint32_t,
+                            __builtin_amdgcn_fmed3f(fmaf(v, inv, k), k - 127.f, k + 127.f));
+}
+__device__ __forceinline__ uint32_t any_code_of(float v, float inv) {
+  return magnitude(v) < kInf ? code_of(v, inv) : 0x80u;
 }
 __device__ __forceinline__ uint32_t bytes4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x0C0C0400u);
   const uint32_t hi = __builtin_amdgcn_perm(d, c, 0x0C0C0400u);
   return lo | hi << 16;
 }
+
+// Packs a group of 32 values that lies in several lanes, N a lane: `widest` takes a lane's
+// largest magnitude to the group's. Returns the exponent; q: the codes, four a word. Groups
+// with infinities or NaN (rare) go a slower way, all lanes of the wave together.
+template <int N, class Widest>
+__device__ __forceinline__ uint32_t pack_group(const float (&v)[N], uint32_t (&q)[N / 4],
+                                               Widest &&widest) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < N; ++e) top = max(top, magnitude(v[e]));
+  top = widest(top);
+  if (__builtin_expect(__any(top >= kInf), 0)) {
+    top = 0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) top = max(top, finite_magnitude(v[e]));
+    top = widest(top);
+    const float inv = steps_of(group_exp(top));
+#pragma unroll
+    for (int g = 0; g < N / 4; ++g)
+      q[g] = bytes4(any_code_of(v[4 * g], inv), any_code_of(v[4 * g + 1], inv),
+                    any_code_of(v[4 * g + 2], inv), any_code_of(v[4 * g + 3], inv));
+    return group_exp(top);
+  }
+  const uint32_t b = group_exp(top);
+  const float inv = steps_of(b);
+#pragma unroll
+  for (int g = 0; g < N / 4; ++g)
+    q[g] = bytes4(code_of(v[4 * g], inv), code_of(v[4 * g + 1], inv), code_of(v[4 * g + 2], inv),
+                  code_of(v[4 * g + 3], inv));
+  return b;
+}
+
 // 8 codes as values.
 __device__ __forceinline__ void decode8(const u32x2 &q, uint32_t b, float (&v)[8]) {
   const float step = step_of(b);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int code = (int8_t)(q[e >> 2] >> (8 * (e & 3)));
-    v[e] = code == -128 ? __builtin_nanf("") : (float)code * step;
+  for (int e = 0; e < 8; ++e) v[e] = (float)(int8_t)(q[e >> 2] >> (8 * (e & 3))) * step;
+  // a byte 0x80 somewhere: the code of what is no number
+  const u32x2 u = {q[0] ^ 0x80808080u, q[1] ^ 0x80808080u};
+  const uint32_t z = ((u[0] - 0x01010101u) & ~u[0]) | ((u[1] - 0x01010101u) & ~u[1]);
+  if (__builtin_expect((z & 0x80808080u) != 0, 0)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if ((uint8_t)(u[e >> 2] >> (8 * (e & 3))) == 0) v[e] = __builtin_nanf("");
   }
 }
 
 // Packs this lane's 8 values of a row, 4 lanes (a multiple of 4 and the next three) to a
 // group of 32 columns; every lane of the four takes part, those past the end with zeros.
 __device__ __forceinline__ void pack8(const Packed &p, int64_t row, int c, const float (&v)[8]) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[e]));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+  uint32_t q[2];
+  const uint32_t b = pack_group<8>(v, q, [](uint32_t top) __attribute__((always_inline)) {
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+    return max(top, (uint32_t)__shfl_xor((int)top, 2));
+  });
   if (c >= p.wide) return;
-  const uint32_t b = group_exp(top);
-  const float inv = steps_of(b);
-  uint32_t q[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) q[e] = code_of(v[e], inv);
-  *reinterpret_cast<u32x2 *>(p.codes + row * p.wide + c) =
-      u32x2{bytes4(q[0], q[1], q[2], q[3]), bytes4(q[4], q[5], q[6], q[7])};
+  *reinterpret_cast<u32x2 *>(p.codes + row * p.wide + c) = u32x2{q[0], q[1]};
   if (c % 32 == 0) p.exps[row * (p.wide / 32) + c / 32] = (uint8_t)b;
 }
 
@@ -190,6 +228,27 @@ __device__ __forceinline__ T wave_sum(T v) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
   return v;
+}
+
+// Sums of n rows of fp32 parts, `stride` elements apart, over 16 columns from c0 on (fewer
+// where `wide`, a multiple of 4, ends): 256 threads, 4 columns and every 64th row each, then
+// the 64 sums of a column in order. The sum of column c0 + i is thread i's, i < 16.
+__device__ __forceinline__ void sum_columns(const float *part, int n, int64_t stride, int c0,
+                                            int wide, float &sum) {
+  __shared__ f32x4 sh[64][5];
+  const int t = threadIdx.x, c = min(c0 + 4 * (t & 3), wide - 4);
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int k = t >> 2; k < n; k += 64)
+    s += *reinterpret_cast<const f32x4 *>(part + k * stride + c);
+  sh[t >> 2][t & 3] = s;
+  __syncthreads();
+  sum = 0.f;
+  if (t < 16) {
+    const float *p = reinterpret_cast<const float *>(&sh[0][0]) + t;
+#pragma unroll 8
+    for (int k = 0; k < 64; ++k) sum += p[20 * k];
+  }
 }
 
 }  // namespace rows

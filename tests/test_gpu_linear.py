@@ -7,8 +7,8 @@ Bounds, with u = 2^-24, h = half a step of the type (relative, or of its subnorm
   sums     products of 16-bit values are exact; an fp32 sum of n of them runs in steps of 16,
            parts are joined: 4 (n/16 + 64) u times the sum of the magnitudes
   z        the sum's, and u (|z| + |bias|)
-  Phi      relative to Phi(-|z|) 5.3e-6 (the polynomial's 4.7e-6, ten roundings) + 2 u z^2 (the
-           exponent's rounding); 3 u absolute
+  Phi      relative to Phi(-|z|) 6.2e-6 (the polynomial's 5.7e-6, roundings) + 2 u z^2 (the
+           exponent's rounding) up to |z| = 6; beyond, where both are in 0 .. 1e-9, 1e-9; 3 u
   y        1.13 (gelu's largest slope) times z's, |z| times Phi's, 4 u |y|, and h
   dz       |dy| times the slope's error: Phi's, and |z| exp(-z^2/2) / sqrt(2 pi) (2 u z^2 + 8 u);
            2 u |dz|; for the products also h
@@ -95,7 +95,8 @@ def scratch(d, grad):
 
 def phi_tol(z):
     """Error of Phi(z), absolute."""
-    return torch.special.ndtr(-z.abs()) * (5.3e-6 + 2 * U * z * z) + 3 * U
+    return torch.special.ndtr(-z.abs()) * (6.2e-6 + 2 * U * z * z) + 3 * U + \
+        1e-9 * (z.abs() > 6)
 
 
 def slope_tol(z, act):
@@ -201,6 +202,25 @@ def test_matches_the_formulas(dt, act, shape):
         xx = B.checkpoint(x)[1] if eight else x
         check_grads(dy, xx, w, zz, act, t, dx, dw, db)
         assert untouched(dx) and untouched(dw) and int(flag) == 0
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 32, 33, 48, 64, 65])
+@pytest.mark.parametrize("k,m", [(1, 1), (7, 20), (8, 16), (31, 5), (32, 33), (33, 100),
+                                 (300, 17), (2048, 1000), (5001, 40)])
+def test_few_rows(dt, rows, k, m):
+    """Tokens served: sums of every length, and outputs that end inside a workgroup's."""
+    t = TYPES[dt]
+    mk = Maker(dt, rows * 31 + k * 7 + m, (rows + m) % 2 == 1)
+    x, w = mk(rows, k), mk(m, k, 1 / math.sqrt(k))
+    bias, residual = mk.vector(m, 0.5), mk(rows, m)
+    d = fg.LinearDesc.make(rows, k, m, dtype=fg.dtype_of(x), act=fg.ACT_GELU, x_ld=mk.ld(k),
+                           w_ld=mk.ld(k), y_ld=mk.ld(m), r_ld=mk.ld(m), z_ld=mk.ld(m))
+    y, z = mk.out(rows, m), mk.out(rows, m)
+    fg.linear_fwd(d, x, w, y, bias=bias, residual=residual, z=z, ws=scratch(d, False))
+    z64, tz = check_y(y, x, w, bias, residual, "gelu", t)
+    near(z, z64, tz + half(t, z64.abs() + tz), "z")
+    assert untouched(y) and untouched(z)
 
 
 @pytest.mark.parametrize("shape", [(40, 24, 17), (300, 520, 264)], ids=str)
