@@ -331,8 +331,10 @@ __global__ __launch_bounds__(P::NT, P::WPE) void linear_fwd_kernel(FwdArgs a, Ti
 
 // ---- forward, few rows -----------------------------------------------------------------
 // Up to 16 NB rows (tokens served one by one): bound by reading the weights once. A workgroup
-// takes 16 outputs, its 8 waves a run of the sum each: both operands go straight from memory
-// to the MFMA's registers, kAhead steps of 32 at a time, and the waves' sums meet in LDS.
+// takes 8 A8 outputs and NB blocks of 16 rows, its NW waves a run of the sum each. A wave
+// feeds itself: a ring of its own in LDS, whose stages of 64 columns come by DMA in whole
+// 128-byte lines, so that it waits for nothing but its oldest loads and some 100 KiB a CU are
+// always on their way. The waves' sums meet in LDS at the end, in order.
 constexpr int kFewRows = 64;
 template <bool BF>
 __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
@@ -342,91 +344,173 @@ __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const u32x4 &b, const f3
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a),
                                                 __builtin_bit_cast(half8, b), c, 0, 0, 0);
 }
-// Elements c .. c + 7 of a row of K (at least 8), zeros past its end.
-__device__ __forceinline__ u32x4 ending(const uint16_t *row, int c, int K) {
-  const int s = c - min(c, K - 8);
-  const u32x4 r = reinterpret_cast<const Any16 *>(row + min(c, K - 8))->v;
-  const uint64_t lo = (uint64_t)r[1] << 32 | r[0], hi = (uint64_t)r[3] << 32 | r[2];
-  const int sh = 16 * (s & 3);
-  uint64_t a = lo, b = hi;
-  if (s & 4) a = hi, b = 0;
-  if (sh) a = a >> sh | b << (64 - sh), b >>= sh;
-  if (s >= 8) a = b = 0;
-  return u32x4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+
+template <int A8_, int NB_, int NW_>
+struct Few {
+  static constexpr int A8 = A8_, OUT = 8 * A8;        // outputs
+  static constexpr int MB = (A8 + 1) / 2, NB = NB_, NW = NW_, NT = 64 * NW;
+  static constexpr int A = 1024 * A8, STAGE = A + 2048 * NB;  // bytes of 64 columns
+  static constexpr int LOADS = A8 + 2 * NB;                   // DMA instructions, 8 rows each
+  static constexpr int FIT = 152 * 1024 / (NW * STAGE), NS = FIT < 8 ? FIT : 8;
+  static_assert(NS >= 2 && (NS - 1) * LOADS < 64, "ring depth, vmcnt range");
+};
+
+// Waits until at most n of the wave's stages, and N of them, are on their way.
+template <class F, int N>
+__device__ __forceinline__ void wait_younger(int n) {
+  if constexpr (N == 0) {
+    wait_vm<0>();
+  } else {
+    if (n >= N)
+      wait_vm<N * F::LOADS>();
+    else
+      wait_younger<F, N - 1>(n);
+  }
 }
 
-template <bool BF, int NB>
-__global__ __launch_bounds__(512) void linear_few_kernel(FwdArgs a) {
-  constexpr int kAhead = 8;
-  __shared__ f32x4 sums[8][NB][64];
+template <bool BF, class F>
+__global__ __launch_bounds__(F::NT) void linear_few_kernel(FwdArgs a) {
+  constexpr int A8 = F::A8, MB = F::MB, NB = F::NB, NW = F::NW, NS = F::NS;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[NW * NS * F::STAGE];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int m0 = blockIdx.x * 16, K = a.K, rows = (int)a.rows, out = a.e.out;
-  const int c0 = 8 * (lane >> 4);
-  const uint16_t *w = a.w + min(m0 + (lane & 15), out - 1) * a.w_ld + c0;
-  const uint16_t *x[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) x[b] = a.x + min(16 * b + (lane & 15), rows - 1) * a.x_ld + c0;
-  // what the end needs: lane's outputs m .. m + 3 of row n (on their way meanwhile)
+  const int m0 = blockIdx.x * F::OUT, K = a.K, rows = (int)a.rows;
+  const int out = min(a.e.out, m0 + F::OUT);  // this workgroup's end
+  uint8_t *ring = lds + wave * NS * F::STAGE;
+  // what the end needs, on its way meanwhile: outputs m .. m + 3 of row n, a block of 16 x 16
+  // for each wave in turn
+  constexpr int NE = (MB * NB + NW - 1) / NW;
   const Epilogue &e = a.e;
-  const int n = 16 * wave + (lane & 15), m = m0 + 4 * (lane >> 4);
-  const bool mine = wave < NB && n < rows && m < out;
-  float bias[4] = {}, res[4] = {};
-  if (mine && e.bias) load4(e.bias, m, out, BF, bias);
-  if (mine && e.residual) load4(e.residual + n * e.r_ld, m, out, BF, res);
-  f32x4 acc[NB];
+  float bias[NE][4] = {}, res[NE][4] = {};
 #pragma unroll
-  for (int b = 0; b < NB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int full = K / 32, per = (full + 7) / 8;
-  const int s1 = min(full, (wave + 1) * per);
-  for (int s0 = wave * per; s0 < s1; s0 += kAhead) {
-    u32x4 fa[kAhead], fb[kAhead][NB];
+  for (int k = 0; k < NE; ++k) {
+    const int id = wave + NW * k, m = m0 + 16 * (id / NB) + 4 * (lane >> 4),
+              n = 16 * (id % NB) + (lane & 15);
+    if (id >= MB * NB || n >= rows || m >= out) continue;
+    if (e.bias) load4(e.bias, m, out, BF, bias[k]);
+    if (e.residual) load4(e.residual + n * e.r_ld, m, out, BF, res[k]);
+  }
+  const __amdgpu_buffer_rsrc_t rs_w =
+      rsrc(a.w + m0 * a.w_ld, (uint32_t)((out - m0 - 1) * (int)a.w_ld + K) * 2u);
+  const __amdgpu_buffer_rsrc_t rs_x = rsrc(a.x, (uint32_t)((rows - 1) * (int)a.x_ld + K) * 2u);
+  // a DMA instruction fills 8 rows; lane: row lane / 8, the chunk that belongs at its place
+  const int r8 = lane >> 3;
+  unsigned wo[A8], xo[2 * NB];
+  int ch[2];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int s = min(s0 + k, s1 - 1);
-      fa[k] = reinterpret_cast<const Any16 *>(w + 32 * s)->v;
+  for (int h = 0; h < 2; ++h) ch[h] = 8 * ((lane & 7) ^ kmaj_swz<64>(8 * h + r8));
 #pragma unroll
-      for (int b = 0; b < NB; ++b) fb[k][b] = reinterpret_cast<const Any16 *>(x[b] + 32 * s)->v;
-    }
+  for (int b = 0; b < A8; ++b) wo[b] = (unsigned)((8 * b + r8) * (int)a.w_ld) * 2u;
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-      if (s0 + k < s1) {
+  for (int b = 0; b < 2 * NB; ++b) xo[b] = (unsigned)((8 * b + r8) * (int)a.x_ld) * 2u;
+  const int stages = (K + 63) / 64, per = (stages + NW - 1) / NW;
+  const int first = wave * per, run = min(per, stages - first);
+  // Each workgroup begins its runs elsewhere: where all read the same part of rows of a power
+  // of two bytes, few memory channels serve them.
+  const int turn = run > 0 ? (int)(blockIdx.x % (unsigned)run) : 0;
+  auto column = [&](int st) __attribute__((always_inline)) {
+    const int to = st + turn;
+    return 64 * (first + (to < run ? to : to - run));
+  };
+  auto issue = [&](int st, int slot) __attribute__((always_inline)) {
+    uint8_t *to = ring + slot * F::STAGE;
+    const int k0 = column(st);
+    // a last chunk of fewer than 8 begins earlier, in both operands alike
+    auto at = [&](unsigned row, int c) __attribute__((always_inline)) {
+      return c < K ? row + 2u * chunk_at(c, K) : kOOB;
+    };
 #pragma unroll
-        for (int b = 0; b < NB; ++b) acc[b] = mfma16<BF>(fa[k], fb[k][b], acc[b]);
+    for (int b = 0; b < A8; ++b) dma16(rs_w, to + 1024 * b, at(wo[b], k0 + ch[b & 1]));
+#pragma unroll
+    for (int b = 0; b < 2 * NB; ++b) dma16(rs_x, to + F::A + 1024 * b, at(xo[b], k0 + ch[b & 1]));
+  };
+  f32x4 acc[MB][NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto stage = [&](int st, int slot) __attribute__((always_inline)) {
+    const uint8_t *at = ring + slot * F::STAGE;
+    const int k0 = column(st);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      const int c = 4 * ks + (lane >> 4);
+      u32x4 fa[MB], fb[NB];
+#pragma unroll
+      for (int b = 0; b < MB; ++b)
+        fa[b] = *reinterpret_cast<const u32x4 *>(
+            at + 2048 * b + kmaj_off<64>(lane & (A8 == 1 ? 7 : 15), c));
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        fb[b] = *reinterpret_cast<const u32x4 *>(at + F::A + 2048 * b + kmaj_off<64>(lane & 15, c));
+      if (K % 8 && k0 + 64 > K) {  // what the last chunk repeats: zeros, whatever it is
+        const int over = k0 + 8 * c + 8 - K, cut = over < 8 ? over : 0;
+        u32x4 m;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+          m[d] = (2 * d < cut ? 0u : 0xFFFFu) | (2 * d + 1 < cut ? 0u : 0xFFFF0000u);
+#pragma unroll
+        for (int b = 0; b < MB; ++b) fa[b] &= m;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) fb[b] &= m;
       }
-  }
-  if (wave == 7 && K % 32) {  // what is left of the sum
-    const u32x4 f = ending(w - c0, 32 * full + c0, K);
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
-      acc[b] = mfma16<BF>(f, ending(x[b] - c0, 32 * full + c0, K), acc[b]);
-  }
+      for (int i = 0; i < MB; ++i)
 #pragma unroll
-  for (int b = 0; b < NB; ++b) sums[wave][b][lane] = acc[b];
-  __syncthreads();
-  if (!mine) return;
-  float v[4] = {};
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const f32x4 q = sums[k][wave][lane];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += q[i];
-  }
-  auto put = [&](uint16_t *row) __attribute__((always_inline)) {
-    const u32x2 q = {pack2(v[0], v[1], BF), pack2(v[2], v[3], BF)};
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (m + i < out) row[m + i] = (uint16_t)(q[i >> 1] >> (16 * (i & 1)));
+        for (int j = 0; j < NB; ++j) acc[i][j] = mfma16<BF>(fa[i], fb[j], acc[i][j]);
+    }
   };
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] += bias[i];
-  if (e.z) put(e.z + n * e.z_ld);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = apply(v[i], e.act);
-    if (e.residual) v[i] += res[i];
+  for (int s = 0; s < NS - 1; ++s)
+    if (s < run) issue(s, s);
+  int slot = 0;
+  for (int st = 0; st < run; ++st) {
+    // this wave has read the slot that it fills now
+    wait_lds();
+    asm volatile("" ::: "memory");
+    if (st + NS - 1 < run) issue(st + NS - 1, slot ? slot - 1 : NS - 1);
+    wait_younger<F, NS - 1>(run - 1 - st);
+    asm volatile("" ::: "memory");
+    stage(st, slot);
+    slot = slot + 1 < NS ? slot + 1 : 0;
   }
-  put(e.y + n * e.y_ld);
+  wait_lds();
+  __syncthreads();
+  f32x4 *sums = reinterpret_cast<f32x4 *>(lds);
+  static_assert(NW * MB * NB * 1024 <= (int)sizeof(lds), "the sums take the rings' place");
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) sums[((i * NB + j) * NW + wave) * 64 + lane] = acc[i][j];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < NE; ++k) {
+    const int id = wave + NW * k, m = m0 + 16 * (id / NB) + 4 * (lane >> 4),
+              n = 16 * (id % NB) + (lane & 15);
+    if (id >= MB * NB || n >= rows || m >= out) continue;
+    float v[4] = {};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const f32x4 q = sums[(id * NW + w) * 64 + lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] += q[i];
+    }
+    auto put = [&](uint16_t *row) __attribute__((always_inline)) {
+      const u32x2 q = {pack2(v[0], v[1], BF), pack2(v[2], v[3], BF)};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (m + i < out) row[m + i] = (uint16_t)(q[i >> 1] >> (16 * (i & 1)));
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += bias[k][i];
+    if (e.z) put(e.z + n * e.z_ld);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[i] = apply(v[i], e.act);
+      if (e.residual) v[i] += res[k][i];
+    }
+    put(e.y + n * e.y_ld);
+  }
 }
 
 // ---- the gradient of z -----------------------------------------------------------------
@@ -874,16 +958,28 @@ hipError_t launch_fwd(FwdArgs a, int ns, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <bool BF, class F>
+hipError_t launch_few_of(const FwdArgs &a, hipStream_t st) {
+  hipLaunchKernelGGL((linear_few_kernel<BF, F>), dim3((uint32_t)((a.e.out + F::OUT - 1) / F::OUT)),
+                     dim3(F::NT), 0, st, a);
+  return hipGetLastError();
+}
 template <bool BF>
 hipError_t launch_few(const FwdArgs &a, hipStream_t st) {
-  const dim3 grid((uint32_t)((a.e.out + 15) / 16)), block(512);
+  const int out = a.e.out;
   if (a.rows <= 16)
-    hipLaunchKernelGGL((linear_few_kernel<BF, 1>), grid, block, 0, st, a);
-  else if (a.rows <= 32)
-    hipLaunchKernelGGL((linear_few_kernel<BF, 2>), grid, block, 0, st, a);
-  else
-    hipLaunchKernelGGL((linear_few_kernel<BF, 4>), grid, block, 0, st, a);
-  return hipGetLastError();
+    return out <= 2048   ? launch_few_of<BF, Few<1, 1, 8>>(a, st)
+           : out <= 4096 ? launch_few_of<BF, Few<2, 1, 8>>(a, st)
+           : out <= 8192 ? launch_few_of<BF, Few<4, 1, 4>>(a, st)
+                         : launch_few_of<BF, Few<8, 1, 4>>(a, st);
+  if (a.rows <= 32)
+    return out <= 2048   ? launch_few_of<BF, Few<1, 2, 8>>(a, st)
+           : out <= 4096 ? launch_few_of<BF, Few<2, 2, 8>>(a, st)
+           : out <= 8192 ? launch_few_of<BF, Few<4, 2, 4>>(a, st)
+                         : launch_few_of<BF, Few<8, 2, 4>>(a, st);
+  return out <= 2048   ? launch_few_of<BF, Few<1, 4, 4>>(a, st)
+         : out <= 4096 ? launch_few_of<BF, Few<2, 4, 4>>(a, st)
+                       : launch_few_of<BF, Few<4, 4, 4>>(a, st);
 }
 
 template <class P>
