@@ -11,6 +11,8 @@
 // once (16 bits, the matrix pipes' type) while its columns are summed for db; dx and dw are
 // one launch, whose operands by rows of the sum are read with transposing LDS reads. Long
 // sums with few tiles are split and joined in order; the join does the epilogue then.
+#include <string.h>
+
 #include <algorithm>
 
 #include "rows.h"
@@ -23,6 +25,9 @@ using namespace tiles;
 using rows::Packed;
 using rows::TypeOf;
 
+// 128 x 128 in a ring of four, for launches of a workgroup per CU or less: with two, each
+// stage waits for its loads (dx of 4096 x 1024 -> 4096 43.1 -> 35.8 us).
+using P128D = Pipe<64, 4, 2, 2, 128, 128>;
 struct FwdTiles {
   using T256 = Pipe<64, 2, 2, 4, 256, 256>;
 };
@@ -766,22 +771,25 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
   if (!DX && a.flag) flag_nonfinite(a.flag, bad);
 }
 
-// Both in one launch, dx's tiles in the first nx workgroups: neither waits for the other's
-// last tiles.
+// Both in one launch: neither waits for the other's last tiles. The one whose sums (their
+// parts) are longer takes the first workgroups, `first` of them.
 template <class P>
 __global__ __launch_bounds__(P::NT, P::WPE) void linear_products_kernel(ProdArgs dx, TileMap tx,
                                                                         ProdArgs dw, TileMap tw,
-                                                                        int nx) {
+                                                                        int first, int dx_first) {
   FG_DMA_RING(P, R);
   const int block = blockIdx.x;
-  if (block < nx)
-    product_tile<P, true>(dx, tx, block, R);
+  const bool leads = block < first;
+  const int at = leads ? block : block - first;
+  if (leads == (dx_first != 0))
+    product_tile<P, true>(dx, tx, at, R);
   else
-    product_tile<P, false>(dw, tw, block - nx, R);
+    product_tile<P, false>(dw, tw, at, R);
 }
 
 // ---- joins -----------------------------------------------------------------------------
-// The parts of split sums, in their order: 8 columns of a row per lane.
+// The parts of split sums, in their order: 8 columns of a row per lane, or per 2^slog lanes
+// with a run of the parts each, whose sums then meet in LDS.
 struct JoinArgs {
   const float *part;
   int64_t pstride, rows;
@@ -789,7 +797,10 @@ struct JoinArgs {
   uint16_t *out;
   int64_t out_ld;
   int32_t *flag;
+  int32_t slog;
 };
+// Lanes to a sum: 256 parts of 64 x 24 sums took 25 us by single lanes.
+inline int shared_log(int nsplit) { return nsplit < 16 ? 0 : nsplit < 64 ? 2 : 4; }
 __device__ __forceinline__ void joined(const float *p, int nsplit, int64_t pstride, float (&v)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = 0.f;
@@ -811,16 +822,28 @@ __device__ __forceinline__ u32x4 rounded(const float (&v)[8]) {
 }
 template <int DT>
 __global__ __launch_bounds__(256) void linear_join_kernel(JoinArgs dx, JoinArgs dw, int nx) {
+  __shared__ float sums[256][8];
   const bool first = (int)blockIdx.x < nx;
   const JoinArgs &a = first ? dx : dw;
-  const int64_t i = (int64_t)(first ? blockIdx.x : blockIdx.x - nx) * 256 + threadIdx.x;
+  const int wide = 256 >> a.slog, t = threadIdx.x & (wide - 1), share = threadIdx.x / wide;
+  const int64_t i = (int64_t)(first ? blockIdx.x : blockIdx.x - nx) * wide + t;
   const int c8 = a.Mq / 8;
   const int64_t n = i / c8;
   const int m = (int)(i - n * c8) * 8;
+  const int per = (a.nsplit + (1 << a.slog) - 1) >> a.slog, s0 = share * per;
   bool bad = false;
-  if (n < a.rows) {
-    float v[8];
-    joined(a.part + n * a.Mq + m, a.nsplit, a.pstride, v);
+  float v[8] = {};
+  if (n < a.rows)
+    joined(a.part + s0 * a.pstride + n * a.Mq + m, min(per, a.nsplit - s0), a.pstride, v);
+  if (a.slog) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[threadIdx.x][e] = v[e];
+    __syncthreads();
+    for (int k = 1; !share && k < 1 << a.slog; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += sums[k * wide + t][e];
+  }
+  if (n < a.rows && !share) {
     const u32x4 d = rounded<DT>(v);
     constexpr uint32_t EX = DT == FG_BF16 ? 0x7F80u : 0x7C00u;
 #pragma unroll
@@ -882,6 +905,73 @@ __global__ __launch_bounds__(256) void linear_pad_kernel(const uint16_t *x, int6
 }
 
 // ---- host ------------------------------------------------------------------------------
+// Tile and number of parts for up to two products of a launch: the least of the times
+// estimated for rounds of the workgroups that the chip holds. A round of m workgroups whose
+// sums are k long takes f + e x + k (g + h x), x = m / (256 occ): its beginning and end, and
+// each stage, both longer where the chip is full. Fitted to 420 timings (22 shapes of 100 ..
+// 65536 rows and 64 .. 8000 columns, each pass by every tile in 1 .. 64 parts): within 11% of
+// them (rms), and the choice within 1.5% of the best on average, 21% at worst.
+struct Cost {
+  int occ;
+  double f, e, g, h;
+};
+constexpr int kTiles = 4;
+constexpr int kSide[kTiles] = {64, 128, 256, 128};
+constexpr Cost kCost[kTiles] = {{3, 0.0, 2.2, .0029, .0043},
+                                {2, 0.6, 3.5, .0068, .0053},
+                                {1, 7.6, 0.0, .0151, .0020},
+                                {1, 2.2, 1.6, .0060, .0012}};
+struct Need {
+  int64_t M, N, K;
+};
+double round_of(const Cost &c, double m, double k) {
+  const double x = m / (256.0 * c.occ);
+  return c.f + c.e * x + k * (c.g + c.h * x);
+}
+// n workgroups of k on average, the longest first.
+double rounds(const Cost &c, double n, double k, double longest) {
+  const double slots = 256.0 * c.occ, full = (double)(int64_t)(n / slots), rest = n - full * slots;
+  return std::max(full * round_of(c, slots, k) + (rest > 0 ? round_of(c, rest, k) : 0.0),
+                  round_of(c, std::min(n, slots), longest));
+}
+struct Parts {
+  double n, k, join;   // workgroups; length of a part; time to join
+  int ns, kper;
+};
+// The numbers of parts worth a look.
+int parts_of(const Need &p, int t, Parts (&out)[10]) {
+  const int64_t side = kSide[t];
+  const int64_t tiles = ((p.M + side - 1) / side) * ((p.N + side - 1) / side);
+  int n = 0;
+  for (int ns = 1; ns <= 512; ns *= 2) {
+    const int64_t kper = std::max<int64_t>(64, ((p.K + ns - 1) / ns + 63) / 64 * 64);
+    const int64_t parts = std::max<int64_t>(1, (p.K + kper - 1) / kper);
+    if (ns > 1 && (kper < 128 || tiles * parts > 4096)) break;
+    out[n++] = {(double)(tiles * parts), (double)kper,
+                parts > 1 ? (double)parts * p.M * p.N * 8 / 6.2e6 : 0.0, (int)parts, (int)kper};
+  }
+  return n;
+}
+void pick(const Need *p, int np, Shape *s) {
+  double best = 1e300;
+  for (int t = 0; t < kTiles; ++t) {
+    Parts a[10], b[10];
+    const int na = parts_of(p[0], t, a), nb = np > 1 ? parts_of(p[1], t, b) : 1;
+    if (np == 1) b[0] = {0, 0, 0, 0, 0};
+    for (int i = 0; i < na; ++i)
+      for (int j = 0; j < nb; ++j) {
+        const double n = a[i].n + b[j].n;
+        double us = rounds(kCost[t], n, (a[i].n * a[i].k + b[j].n * b[j].k) / n,
+                           std::max(a[i].k, b[j].k)) + a[i].join + b[j].join;
+        if (a[i].join + b[j].join > 0) us += 3.75;
+        if (us >= best) continue;
+        best = us;
+        s[0] = {t, a[i].ns, a[i].kper};
+        if (np > 1) s[1] = {t, b[j].ns, b[j].kper};
+      }
+  }
+}
+
 struct Plan {
   int64_t rows, in, out, in8, out8, K;   // K: columns of x and w as the products read them
   bool narrow;                           // fewer than 8: padded copies
@@ -892,17 +982,17 @@ struct Plan {
   size_t xpad, wpad, p1, xu, dz, db, pdx, pdw, total;
 };
 
-Plan make_plan(const fg_linear_desc &d, bool grad) {
+Plan find_plan(const fg_linear_desc &d, bool grad) {
   Plan p{};
   p.rows = d.rows, p.in = d.in, p.out = d.out;
   p.in8 = up(p.in, 8), p.out8 = up(p.out, 8);
   p.narrow = p.in < 8;
   p.K = std::max<int64_t>(p.in, 8);
-  double best = 1e300, us, us2;
-  for (int t = 0; t < 3; ++t) {
-    const Shape a = pick_tile(t, p.out, p.rows, p.K, true, us);
-    if (us < best) best = us, p.s1 = a;
-  }
+  const Need fwd = {p.out, p.rows, p.K}, bwd[2] = {{p.in, p.rows, p.out8}, {p.in, p.out, p.rows}};
+  if (!grad) pick(&fwd, 1, &p.s1);
+  Shape both[2] = {};  // one launch, one tile for both products
+  if (grad) pick(bwd, 2, both);
+  p.s2 = both[0], p.s3 = both[1];
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t was = at;
@@ -915,12 +1005,6 @@ Plan make_plan(const fg_linear_desc &d, bool grad) {
     p.p1 = take(p.s1.ns > 1 ? (size_t)p.s1.ns * p.rows * p.out8 * 4 : 0);
     p.total = at;
     return p;
-  }
-  best = 1e300;  // one launch, one tile for both products
-  for (int t = 0; t < 3; ++t) {
-    const Shape a = pick_tile(t, p.in, p.rows, p.out8, true, us);
-    const Shape b = pick_tile(t, p.in, p.out, p.rows, true, us2);
-    if (us + us2 < best) best = us + us2, p.s2 = a, p.s3 = b;
   }
   p.tlog = 0;
   while (p.tlog < 6 && (8 << p.tlog) < p.out8) ++p.tlog;
@@ -939,6 +1023,27 @@ Plan make_plan(const fg_linear_desc &d, bool grad) {
   return p;
 }
 
+// A function of the descriptor alone, remembered for a few of them by each host thread: a call
+// asks for it twice, and a look at every tile takes longer than a launch.
+Plan make_plan(const fg_linear_desc &d, bool grad) {
+  struct Entry {
+    fg_linear_desc d;
+    int grad;  // 0: empty
+    Plan p;
+  };
+  constexpr int kPlans = 32;
+  static thread_local Entry kept[kPlans] = {};
+  static thread_local unsigned next = 0;
+  const int g = grad ? 2 : 1;
+  for (const Entry &e : kept)
+    if (e.grad == g && !memcmp(&e.d, &d, sizeof(d))) return e.p;
+  Entry &e = kept[next++ % kPlans];
+  e.p = find_plan(d, grad);
+  e.d = d;
+  e.grad = g;
+  return e.p;
+}
+
 #define FG_TRY(x)                      \
   do {                                 \
     const hipError_t e_ = (x);         \
@@ -946,7 +1051,8 @@ Plan make_plan(const fg_linear_desc &d, bool grad) {
   } while (0)
 
 #define FG_LINEAR_TILE(FN, TS, tile, bf, ...)                                        \
-  ((tile) == 2   ? ((bf) ? FN<Bf16<TS::T256>>(__VA_ARGS__) : FN<TS::T256>(__VA_ARGS__)) \
+  ((tile) == 3   ? ((bf) ? FN<Bf16<P128D>>(__VA_ARGS__) : FN<P128D>(__VA_ARGS__))     \
+   : (tile) == 2 ? ((bf) ? FN<Bf16<TS::T256>>(__VA_ARGS__) : FN<TS::T256>(__VA_ARGS__)) \
    : (tile) == 1 ? ((bf) ? FN<Bf16<P128>>(__VA_ARGS__) : FN<P128>(__VA_ARGS__))       \
                  : ((bf) ? FN<Bf16<P64>>(__VA_ARGS__) : FN<P64>(__VA_ARGS__)))
 
@@ -989,8 +1095,9 @@ hipError_t launch_products(ProdArgs dx, int nsx, ProdArgs dw, int nsw, hipStream
   const TileMap none{1, 1, 0, 0, kOutputMajor};
   const TileMap tx = nsx ? tile_map((dx.M + P::TM - 1) / P::TM, dx.ntile, nsx) : none;
   const TileMap tw = nsw ? tile_map((dw.M + P::TM - 1) / P::TM, dw.ntile, nsw) : none;
+  const int dx_first = !nsw || (nsx && dx.kper >= dw.kper);
   hipLaunchKernelGGL(linear_products_kernel<P>, dim3(8 * (tx.per + tw.per)), dim3(P::NT), 0, st,
-                     dx, tx, dw, tw, 8 * tx.per);
+                     dx, tx, dw, tw, 8 * (dx_first ? tx.per : tw.per), dx_first);
   return hipGetLastError();
 }
 
@@ -1119,7 +1226,8 @@ hipError_t launch_linear_bwd(const fg_linear_desc &d, const void *dy, const void
     a.out_ld = ld(d.dx_ld, p.in);
     a.pstride = p.rows * p.in8;
     (nsx > 1 ? (void *&)a.part : (void *&)a.out) = nsx > 1 ? (void *)(base + p.pdx) : dx;
-    jx = {a.part, a.pstride, p.rows, nsx, a.M, a.Mq, (uint16_t *)dx, a.out_ld, nullptr};
+    jx = {a.part, a.pstride, p.rows, nsx, a.M, a.Mq, (uint16_t *)dx, a.out_ld, nullptr,
+          shared_log(nsx)};
   }
   if (dw) {
     b.a = (const uint16_t *)x, b.a_ld = ld(d.x_ld, p.in);
@@ -1139,12 +1247,16 @@ hipError_t launch_linear_bwd(const fg_linear_desc &d, const void *dy, const void
     b.pstride = p.out * p.in8;
     (nsw > 1 ? (void *&)b.part : (void *&)b.out) = nsw > 1 ? (void *)(base + p.pdw) : dw;
     b.flag = flag;
-    jw = {b.part, b.pstride, p.out, nsw, b.M, b.Mq, (uint16_t *)dw, b.out_ld, flag};
+    jw = {b.part, b.pstride, p.out, nsw, b.M, b.Mq, (uint16_t *)dw, b.out_ld, flag,
+          shared_log(nsw)};
   }
   if (!nsx && !nsw) return hipSuccess;
   FG_TRY(FG_LINEAR_TILE(launch_products, BwdTiles, p.s2.tile, bf, a, nsx, b, nsw, st));
-  const int64_t bx = nsx > 1 ? (p.rows * (p.in8 / 8) + 255) / 256 : 0;
-  const int64_t bw = nsw > 1 ? (p.out * (p.in8 / 8) + 255) / 256 : 0;
+  const auto blocks = [&](int64_t n, const JoinArgs &j) {
+    const int wide = 256 >> j.slog;
+    return (n * (p.in8 / 8) + wide - 1) / wide;
+  };
+  const int64_t bx = nsx > 1 ? blocks(p.rows, jx) : 0, bw = nsw > 1 ? blocks(p.out, jw) : 0;
   if (!bx && !bw) return hipSuccess;
   const dim3 grid((uint32_t)(bx + bw)), block(256);
   if (bf)

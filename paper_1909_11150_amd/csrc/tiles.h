@@ -1,6 +1,5 @@
 // What the tiled matrix products of the classification head (xent.hip) and of linear layers
-// (linear.hip) share: rows of any width in chunks of 8, stores, tile order, the choice of a
-// tile.
+// (linear.hip) share: rows of any width in chunks of 8, stores, tile order.
 #pragma once
 #include <algorithm>
 
@@ -117,7 +116,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void *p, uint32_t b
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, kRsrcFlags);
 }
 
-// ---- order and choice of tiles --------------------------------------------------------
+// ---- tile order -----------------------------------------------------------------------
 // Tiles of a band, see tile_map (8192 x 4096 x 131072: logits 3.50 -> 3.38 ms a piece and
 // products 6.94 -> 6.81 against bands of one; of eight 3.41 and 6.90).
 constexpr int kBand = 4;
@@ -144,44 +143,9 @@ inline TileMap tile_map(int64_t n0, int64_t n1, int64_t n2) {
 }
 
 constexpr int kTileOf[3] = {64, 128, 256};
-
-// Tile and number of parts for a product of M x N sums of length K: the least of the
-// times estimated for rounds of the workgroups that the chip holds. A round costs a
-// fixed time (first loads, store) and one per unit of K, by the tile and the
-// workgroups on a CU; measured over 56 shapes (1 .. 4096 rows, 64 .. 4096 hidden, 2000
-// .. 32000 classes), in which the tile chosen is within 20% of the best of the three.
 struct Shape {
-  int tile, ns, kper;  // tile: index into kTileOf
+  int tile, ns, kper;  // tile: index; parts of the sum, length of one
 };
-// The best number of parts for one tile, and its time.
-inline Shape pick_tile(int t, int64_t M, int64_t N, int64_t K, bool split, double &us_best) {
-  static const int occ[3] = {3, 2, 1};
-  static const double fixed[3][3] = {{2.0, 2.0, 2.0}, {3.5, 5.5, 5.5}, {9.0, 9.0, 9.0}};
-  const double more = !split ? 0.0 : t == 2 ? 5.0 : t == 0 ? 1.0 : 0.0;  // the products' store
-  static const double per_k[3][3] = {{.0055, .009, .0135}, {.0095, .0178, .0178},
-                                     {.0175, .0175, .0175}};
-  Shape best{t, 1, 0};
-  us_best = 1e300;
-  const int64_t ts = kTileOf[t];
-  const int64_t tiles = ((M + ts - 1) / ts) * ((N + ts - 1) / ts);
-  for (int ns = 1; ns <= (split ? 512 : 1); ns *= 2) {
-    const int64_t kper = std::max<int64_t>(64, ((K + ns - 1) / ns + 63) / 64 * 64);
-    if (ns > 1 && kper < 256) break;
-    const int64_t parts = std::max<int64_t>(1, (K + kper - 1) / kper);
-    const int64_t n = tiles * parts, slots = 256 * occ[t];
-    const int64_t full = n / slots, rest = n - full * slots;
-    // a chip full of the largest tiles is slower per tile than a few of them
-    auto round = [&](int64_t m) {
-      const int j = (int)((m + 255) / 256) - 1;
-      return fixed[t][j] + more + kper * (per_k[t][j] + (t == 2 ? .0105 * m / 256 : 0.));
-    };
-    double us = full * round(slots);
-    if (rest) us += round(rest);
-    if (parts > 1) us += 6.0 + (double)parts * M * N * 8 / 8e6;
-    if (us < us_best) us_best = us, best = {t, (int)parts, (int)kper};
-  }
-  return best;
-}
 
 }  // namespace tiles
 }  // namespace fg

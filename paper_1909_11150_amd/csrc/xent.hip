@@ -1432,6 +1432,41 @@ constexpr int64_t kInPlace = (int64_t)1 << 32;
 // against two: 8192 x 4096 x 131072 21.1 and 22.2 ms, 5000 x 512 x 131072 2.73 and 3.05.)
 constexpr int64_t kPieceBytes = (int64_t)1 << 30;
 
+// Tile and number of parts for a product of M x N sums of length K: the least of the
+// times estimated for rounds of the workgroups that the chip holds. A round costs a
+// fixed time (first loads, store) and one per unit of K, by the tile and the
+// workgroups on a CU; measured over 56 shapes (1 .. 4096 rows, 64 .. 4096 hidden, 2000
+// .. 32000 classes), in which the tile chosen is within 20% of the best of the three.
+// The best number of parts for one tile, and its time.
+Shape pick_tile(int t, int64_t M, int64_t N, int64_t K, bool split, double &us_best) {
+  static const int occ[3] = {3, 2, 1};
+  static const double fixed[3][3] = {{2.0, 2.0, 2.0}, {3.5, 5.5, 5.5}, {9.0, 9.0, 9.0}};
+  const double more = !split ? 0.0 : t == 2 ? 5.0 : t == 0 ? 1.0 : 0.0;  // the products' store
+  static const double per_k[3][3] = {{.0055, .009, .0135}, {.0095, .0178, .0178},
+                                     {.0175, .0175, .0175}};
+  Shape best{t, 1, 0};
+  us_best = 1e300;
+  const int64_t ts = kTileOf[t];
+  const int64_t tiles = ((M + ts - 1) / ts) * ((N + ts - 1) / ts);
+  for (int ns = 1; ns <= (split ? 512 : 1); ns *= 2) {
+    const int64_t kper = std::max<int64_t>(64, ((K + ns - 1) / ns + 63) / 64 * 64);
+    if (ns > 1 && kper < 256) break;
+    const int64_t parts = std::max<int64_t>(1, (K + kper - 1) / kper);
+    const int64_t n = tiles * parts, slots = 256 * occ[t];
+    const int64_t full = n / slots, rest = n - full * slots;
+    // a chip full of the largest tiles is slower per tile than a few of them
+    auto round = [&](int64_t m) {
+      const int j = (int)((m + 255) / 256) - 1;
+      return fixed[t][j] + more + kper * (per_k[t][j] + (t == 2 ? .0105 * m / 256 : 0.));
+    };
+    double us = full * round(slots);
+    if (rest) us += round(rest);
+    if (parts > 1) us += 6.0 + (double)parts * M * N * 8 / 8e6;
+    if (us < us_best) us_best = us, best = {t, (int)parts, (int)kper};
+  }
+  return best;
+}
+
 struct Plan {
   int64_t T, H, V, Tp, Hp, Vp, Hq, Tc, pieces, nb, wh, w_ld;
   bool pad_w, place, tiny, classes, outer, spread;  // rows in place, up to 64 of many classes;
