@@ -90,10 +90,25 @@ struct FwdArgs {
   int32_t Mq;
 };
 
+// Keeps the compiler from working on more of the accumulators at once than it has registers
+// for: without it the largest tiles spill 465 of them (65536 x 256 -> 1024 in 149 us, not 60).
+__device__ __forceinline__ void apart() { __builtin_amdgcn_sched_barrier(0); }
+
+// Rows n0 .. of a matrix of nrow rows as a buffer: what lies past the last row reads zeros and
+// is not written.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const void *p, int64_t n0, int64_t ld,
+                                                            int64_t nrow, int width, int esz) {
+  const int left = (int)min((int64_t)256, nrow - n0);
+  return rsrc(static_cast<const uint8_t *>(p) + n0 * ld * esz,
+              left > 0 ? (uint32_t)((left - 1) * (int)ld + width) * (uint32_t)esz : 0u);
+}
+
 // A wave's block of y: residual and result go through this wave's buffer, 32 rows at a time,
 // 16-byte chunks permuted by the row, so that neighbouring lanes read and write one row's
-// consecutive bytes. One rounding of residual + act(z).
-template <class P>
+// consecutive bytes. One rounding of residual + act(z). EVEN: 8 divides the columns; the
+// buffers' range checks then take the place of branches around every access, with which the
+// epilogue takes as long as a sum of 1000.
+template <class P, bool EVEN>
 __device__ __forceinline__ void store_rows(const f32x16 (&acc)[P::FM][P::FN], uint8_t *buf,
                                            int lane, const uint16_t *residual, int64_t r_ld,
                                            uint16_t *y, int64_t y_ld, int64_t n0, int m0,
@@ -104,14 +119,23 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[P::FM][P::FN], ui
   auto place = [&](int r, int c) __attribute__((always_inline)) {
     return buf + r * RB + ((c ^ ((r >> SH) & (CPW - 1))) << 4);
   };
+  const int64_t first = n0 + lane / CPW;
+  const __amdgpu_buffer_rsrc_t rs_y = rows_from(y, n0, y_ld, nrow, out, 2);
+  const __amdgpu_buffer_rsrc_t rs_r = rows_from(residual, n0, r_ld, nrow, out, 2);
+  unsigned yo = m < out ? (unsigned)(lane / CPW * (int)y_ld + m) * 2u : kOOB;
+  unsigned ro = m < out ? (unsigned)(lane / CPW * (int)r_ld + m) * 2u : kOOB;
 #pragma unroll
   for (int j = 0; j < P::FN; ++j) {
     if (residual) {
       u32x4 d[32 / RPI];
 #pragma unroll
       for (int k = 0; k < 32 / RPI; ++k) {
-        const int64_t n = n0 + 32 * j + k * RPI + lane / CPW;
-        d[k] = n < nrow && m < out ? row8(residual + n * r_ld, m, out) : u32x4{0, 0, 0, 0};
+        const int64_t n = first + 32 * j + k * RPI;
+        if constexpr (EVEN)
+          d[k] = __builtin_amdgcn_raw_buffer_load_b128(
+              rs_r, (int)(ro + (unsigned)((32 * j + k * RPI) * (int)r_ld) * 2u), 0, 0);
+        else
+          d[k] = n < nrow && m < out ? row8(residual + n * r_ld, m, out) : u32x4{0, 0, 0, 0};
       }
 #pragma unroll
       for (int k = 0; k < 32 / RPI; ++k)
@@ -133,6 +157,7 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[P::FM][P::FN], ui
           for (int e = 0; e < 4; ++e) v[e] += to_f32(o[e >> 1] >> (16 * (e & 1)) & 0xFFFFu, P::BF);
         }
         *at = u32x2{pack2(v[0], v[1], P::BF), pack2(v[2], v[3], P::BF)};
+        if (g == 3) apart();
       }
     wait_lds();
     __builtin_amdgcn_wave_barrier();
@@ -142,8 +167,12 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[P::FM][P::FN], ui
       d[k] = *reinterpret_cast<const u32x4 *>(place(k * RPI + lane / CPW, q));
 #pragma unroll
     for (int k = 0; k < 32 / RPI; ++k) {
-      const int64_t n = n0 + 32 * j + k * RPI + lane / CPW;
-      if (n < nrow && m < out) put8(y + n * y_ld, m, out, d[k]);
+      const int64_t n = first + 32 * j + k * RPI;
+      if constexpr (EVEN)
+        __builtin_amdgcn_raw_buffer_store_b128(
+            d[k], rs_y, (int)(yo + (unsigned)((32 * j + k * RPI) * (int)y_ld) * 2u), 0, 0);
+      else if (n < nrow && m < out)
+        put8(y + n * y_ld, m, out, d[k]);
     }
     wait_lds();
     __builtin_amdgcn_wave_barrier();
@@ -156,6 +185,8 @@ template <class P>
 __device__ __forceinline__ void pack_block(const f32x16 (&acc)[P::FM][P::FN], const Packed &p,
                                            int64_t n0, int m0, int64_t nrow, int lane) {
   const bool up = lane >= 32;
+  const __amdgpu_buffer_rsrc_t rs_q = rows_from(p.codes, n0, p.wide, nrow, p.wide, 1);
+  const __amdgpu_buffer_rsrc_t rs_e = rows_from(p.exps, n0, p.wide / 32, nrow, p.wide / 32, 1);
 #pragma unroll
   for (int j = 0; j < P::FN; ++j)
 #pragma unroll
@@ -170,21 +201,23 @@ __device__ __forceinline__ void pack_block(const f32x16 (&acc)[P::FM][P::FN], co
           });
       const uint32_t r0 = __shfl_xor((int)(up ? q[0] : q[2]), 32);
       const uint32_t r1 = __shfl_xor((int)(up ? q[1] : q[3]), 32);
-      const int64_t n = n0 + 32 * j + (lane & 31);
-      const int m = m0 + 32 * i;
-      if (n < nrow && m < p.wide) {
-        *reinterpret_cast<u32x4 *>(p.codes + n * p.wide + m + (up ? 16 : 0)) =
-            up ? u32x4{r0, q[2], r1, q[3]} : u32x4{q[0], r0, q[1], r1};
-        if (!up) p.exps[n * (p.wide / 32) + m / 32] = (uint8_t)b;
-      }
+      const int r = 32 * j + (lane & 31), m = m0 + 32 * i;
+      const bool in = m < p.wide;
+      __builtin_amdgcn_raw_buffer_store_b128(
+          up ? u32x4{r0, q[2], r1, q[3]} : u32x4{q[0], r0, q[1], r1}, rs_q,
+          in ? r * p.wide + m + (up ? 16 : 0) : (int)kOOB, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b8((uint8_t)b, rs_e,
+                                           in && !up ? r * (p.wide / 32) + m / 32 : (int)kOOB, 0,
+                                           0);
+      apart();
     }
 }
 
 // 4 elements of a vector of n from c on, zeros past its end.
+struct __attribute__((packed, aligned(2))) Any8 {
+  u32x2 v;
+};
 __device__ __forceinline__ void load4(const uint16_t *p, int c, int n, bool bf, float (&v)[4]) {
-  struct __attribute__((packed, aligned(2))) Any8 {
-    u32x2 v;
-  };
   if (c + 4 <= n) {
     const u32x2 q = reinterpret_cast<const Any8 *>(p + c)->v;
 #pragma unroll
@@ -195,26 +228,38 @@ __device__ __forceinline__ void load4(const uint16_t *p, int c, int n, bool bf, 
   for (int e = 0; e < 4; ++e) v[e] = c + e < n ? to_f32(p[c + e], bf) : 0.f;
 }
 
-template <class P>
+template <class P, bool EVEN>
 __device__ __forceinline__ void epilogue(f32x16 (&acc)[P::FM][P::FN], const Epilogue &a,
                                          uint8_t *buf, int lane, int64_t n0, int m0,
                                          int64_t nrow) {
   if (a.bias) {
 #pragma unroll
-    for (int i = 0; i < P::FM; ++i)
+    for (int i = 0; i < P::FM; ++i) {
+      u32x2 q[4];
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        float b[4];
-        load4(a.bias, m0 + 32 * i + 8 * g + 4 * (lane >> 5), a.out, P::BF, b);
+        const int m = m0 + 32 * i + 8 * g + 4 * (lane >> 5);
+        if constexpr (EVEN) {
+          q[g] = m < a.out ? reinterpret_cast<const Any8 *>(a.bias + m)->v : u32x2{0, 0};
+        } else {
+          uint32_t h[4];
 #pragma unroll
-        for (int j = 0; j < P::FN; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] += b[e];
+          for (int e = 0; e < 4; ++e) h[e] = m + e < a.out ? a.bias[m + e] : 0;
+          q[g] = u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
+        }
       }
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const float b = to_f32(q[v >> 2][v >> 1 & 1] >> (16 * (v & 1)) & 0xFFFFu, P::BF);
+#pragma unroll
+        for (int j = 0; j < P::FN; ++j) acc[i][j][v] += b;
+      }
+      apart();
+    }
   }
-  if (a.z) store_rows<P>(acc, buf, lane, nullptr, 0, a.z, a.z_ld, n0, m0, nrow, a.out);
+  if (a.z) store_rows<P, EVEN>(acc, buf, lane, nullptr, 0, a.z, a.z_ld, n0, m0, nrow, a.out);
   if (a.packed.codes) {
-    if (m0 + P::WM > a.out) {  // (weights past the last output are zeros, but 0 x NaN is not)
+    if (m0 + P::WM > a.out) {  // (weights past the end are zeros, but 0 x NaN is not)
 #pragma unroll
       for (int i = 0; i < P::FM; ++i)
 #pragma unroll
@@ -225,15 +270,24 @@ __device__ __forceinline__ void epilogue(f32x16 (&acc)[P::FM][P::FN], const Epil
     }
     pack_block<P>(acc, a.packed, n0, m0, nrow, lane);
   }
-  if (a.act != FG_ACT_NONE) {
+  if (a.act == FG_ACT_RELU) {
 #pragma unroll
     for (int i = 0; i < P::FM; ++i)
 #pragma unroll
       for (int j = 0; j < P::FN; ++j)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) acc[i][j][v] = apply(acc[i][j][v], a.act);
+        for (int v = 0; v < 16; ++v) acc[i][j][v] = acc[i][j][v] < 0.f ? 0.f : acc[i][j][v];
+  } else if (a.act == FG_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < P::FM; ++i)
+#pragma unroll
+      for (int j = 0; j < P::FN; ++j) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[i][j][v] = gelu(acc[i][j][v]);
+        apart();
+      }
   }
-  store_rows<P>(acc, buf, lane, a.residual, a.r_ld, a.y, a.y_ld, n0, m0, nrow, a.out);
+  store_rows<P, EVEN>(acc, buf, lane, a.residual, a.r_ld, a.y, a.y_ld, n0, m0, nrow, a.out);
 }
 
 // fp32 sums of a wave's block to a part of a split sum.
@@ -257,7 +311,7 @@ __device__ __forceinline__ void store_part(const f32x16 (&acc)[P::FM][P::FN], fl
   }
 }
 
-template <class P>
+template <class P, bool EVEN>
 __global__ __launch_bounds__(P::NT, P::WPE) void linear_fwd_kernel(FwdArgs a, TileMap tm) {
   FG_DMA_RING(P, R);
   constexpr int PA = P::PA, PB = P::PB, BK = P::BK;
@@ -331,7 +385,7 @@ __global__ __launch_bounds__(P::NT, P::WPE) void linear_fwd_kernel(FwdArgs a, Ti
     return;
   }
   lds_barrier();  // every wave is done reading the ring
-  epilogue<P>(acc, a.e, wave_buf<P>(R, wave), lane, n0 + wn0, m0 + wm0, a.rows);
+  epilogue<P, EVEN>(acc, a.e, wave_buf<P>(R, wave), lane, n0 + wn0, m0 + wm0, a.rows);
 }
 
 // ---- forward, few rows -----------------------------------------------------------------
@@ -1060,7 +1114,10 @@ template <class P>
 hipError_t launch_fwd(FwdArgs a, int ns, hipStream_t st) {
   a.ntile = (a.e.out + P::TM - 1) / P::TM;
   const TileMap tm = tile_map((a.rows + P::TN - 1) / P::TN, a.ntile, ns);
-  hipLaunchKernelGGL(linear_fwd_kernel<P>, dim3(8 * tm.per), dim3(P::NT), 0, st, a, tm);
+  if (a.e.out % 8 == 0)
+    hipLaunchKernelGGL((linear_fwd_kernel<P, true>), dim3(8 * tm.per), dim3(P::NT), 0, st, a, tm);
+  else
+    hipLaunchKernelGGL((linear_fwd_kernel<P, false>), dim3(8 * tm.per), dim3(P::NT), 0, st, a, tm);
   return hipGetLastError();
 }
 
