@@ -105,10 +105,10 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const void *p, int64
 
 // A wave's block of y: residual and result go through this wave's buffer, 32 rows at a time,
 // 16-byte chunks permuted by the row, so that neighbouring lanes read and write one row's
-// consecutive bytes. One rounding of residual + act(z). EVEN: 8 divides the columns; the
-// buffers' range checks then take the place of branches around every access, with which the
-// epilogue takes as long as a sum of 1000.
-template <class P, bool EVEN>
+// consecutive bytes. One rounding of residual + act(z). The buffers' range checks take the
+// place of branches around every access, with which the epilogue takes as long as a sum of
+// 1000; a row's last chunk, where 8 does not divide it, goes element by element.
+template <class P>
 __device__ __forceinline__ void store_rows(const f32x16 (&acc)[P::FM][P::FN], uint8_t *buf,
                                            int lane, const uint16_t *residual, int64_t r_ld,
                                            uint16_t *y, int64_t y_ld, int64_t n0, int m0,
@@ -122,20 +122,20 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[P::FM][P::FN], ui
   const int64_t first = n0 + lane / CPW;
   const __amdgpu_buffer_rsrc_t rs_y = rows_from(y, n0, y_ld, nrow, out, 2);
   const __amdgpu_buffer_rsrc_t rs_r = rows_from(residual, n0, r_ld, nrow, out, 2);
-  unsigned yo = m < out ? (unsigned)(lane / CPW * (int)y_ld + m) * 2u : kOOB;
-  unsigned ro = m < out ? (unsigned)(lane / CPW * (int)r_ld + m) * 2u : kOOB;
+  const unsigned yo = m + 8 <= out ? (unsigned)(lane / CPW * (int)y_ld + m) * 2u : kOOB;
+  const unsigned ro = m + 8 <= out ? (unsigned)(lane / CPW * (int)r_ld + m) * 2u : kOOB;
+  const bool edge = out % 8 && m0 + P::WM > out;       // (of the wave)
+  const bool tail = edge && m < out && m + 8 > out;
 #pragma unroll
   for (int j = 0; j < P::FN; ++j) {
     if (residual) {
       u32x4 d[32 / RPI];
 #pragma unroll
       for (int k = 0; k < 32 / RPI; ++k) {
+        d[k] = __builtin_amdgcn_raw_buffer_load_b128(
+            rs_r, (int)(ro + (unsigned)((32 * j + k * RPI) * (int)r_ld) * 2u), 0, 0);
         const int64_t n = first + 32 * j + k * RPI;
-        if constexpr (EVEN)
-          d[k] = __builtin_amdgcn_raw_buffer_load_b128(
-              rs_r, (int)(ro + (unsigned)((32 * j + k * RPI) * (int)r_ld) * 2u), 0, 0);
-        else
-          d[k] = n < nrow && m < out ? row8(residual + n * r_ld, m, out) : u32x4{0, 0, 0, 0};
+        if (edge && tail && n < nrow) d[k] = row8(residual + n * r_ld, m, out);
       }
 #pragma unroll
       for (int k = 0; k < 32 / RPI; ++k)
@@ -167,12 +167,10 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[P::FM][P::FN], ui
       d[k] = *reinterpret_cast<const u32x4 *>(place(k * RPI + lane / CPW, q));
 #pragma unroll
     for (int k = 0; k < 32 / RPI; ++k) {
+      __builtin_amdgcn_raw_buffer_store_b128(
+          d[k], rs_y, (int)(yo + (unsigned)((32 * j + k * RPI) * (int)y_ld) * 2u), 0, 0);
       const int64_t n = first + 32 * j + k * RPI;
-      if constexpr (EVEN)
-        __builtin_amdgcn_raw_buffer_store_b128(
-            d[k], rs_y, (int)(yo + (unsigned)((32 * j + k * RPI) * (int)y_ld) * 2u), 0, 0);
-      else if (n < nrow && m < out)
-        put8(y + n * y_ld, m, out, d[k]);
+      if (edge && tail && n < nrow) put8(y + n * y_ld, m, out, d[k]);
     }
     wait_lds();
     __builtin_amdgcn_wave_barrier();
@@ -228,7 +226,7 @@ __device__ __forceinline__ void load4(const uint16_t *p, int c, int n, bool bf, 
   for (int e = 0; e < 4; ++e) v[e] = c + e < n ? to_f32(p[c + e], bf) : 0.f;
 }
 
-template <class P, bool EVEN>
+template <class P>
 __device__ __forceinline__ void epilogue(f32x16 (&acc)[P::FM][P::FN], const Epilogue &a,
                                          uint8_t *buf, int lane, int64_t n0, int m0,
                                          int64_t nrow) {
@@ -239,14 +237,11 @@ __device__ __forceinline__ void epilogue(f32x16 (&acc)[P::FM][P::FN], const Epil
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int m = m0 + 32 * i + 8 * g + 4 * (lane >> 5);
-        if constexpr (EVEN) {
-          q[g] = m < a.out ? reinterpret_cast<const Any8 *>(a.bias + m)->v : u32x2{0, 0};
-        } else {
-          uint32_t h[4];
+        q[g] = m + 4 <= a.out ? reinterpret_cast<const Any8 *>(a.bias + m)->v : u32x2{0, 0};
+        if (m0 + P::WM > a.out && m < a.out && m + 4 > a.out)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) h[e] = m + e < a.out ? a.bias[m + e] : 0;
-          q[g] = u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
-        }
+          for (int e = 0; e < 3; ++e)
+            if (m + e < a.out) q[g][e >> 1] |= (uint32_t)a.bias[m + e] << (16 * (e & 1));
       }
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
@@ -257,7 +252,7 @@ __device__ __forceinline__ void epilogue(f32x16 (&acc)[P::FM][P::FN], const Epil
       apart();
     }
   }
-  if (a.z) store_rows<P, EVEN>(acc, buf, lane, nullptr, 0, a.z, a.z_ld, n0, m0, nrow, a.out);
+  if (a.z) store_rows<P>(acc, buf, lane, nullptr, 0, a.z, a.z_ld, n0, m0, nrow, a.out);
   if (a.packed.codes) {
     if (m0 + P::WM > a.out) {  // (weights past the end are zeros, but 0 x NaN is not)
 #pragma unroll
@@ -287,7 +282,7 @@ __device__ __forceinline__ void epilogue(f32x16 (&acc)[P::FM][P::FN], const Epil
         apart();
       }
   }
-  store_rows<P, EVEN>(acc, buf, lane, a.residual, a.r_ld, a.y, a.y_ld, n0, m0, nrow, a.out);
+  store_rows<P>(acc, buf, lane, a.residual, a.r_ld, a.y, a.y_ld, n0, m0, nrow, a.out);
 }
 
 // fp32 sums of a wave's block to a part of a split sum.
@@ -311,7 +306,7 @@ __device__ __forceinline__ void store_part(const f32x16 (&acc)[P::FM][P::FN], fl
   }
 }
 
-template <class P, bool EVEN>
+template <class P>
 __global__ __launch_bounds__(P::NT, P::WPE) void linear_fwd_kernel(FwdArgs a, TileMap tm) {
   FG_DMA_RING(P, R);
   constexpr int PA = P::PA, PB = P::PB, BK = P::BK;
@@ -385,7 +380,7 @@ __global__ __launch_bounds__(P::NT, P::WPE) void linear_fwd_kernel(FwdArgs a, Ti
     return;
   }
   lds_barrier();  // every wave is done reading the ring
-  epilogue<P, EVEN>(acc, a.e, wave_buf<P>(R, wave), lane, n0 + wn0, m0 + wm0, a.rows);
+  epilogue<P>(acc, a.e, wave_buf<P>(R, wave), lane, n0 + wn0, m0 + wm0, a.rows);
 }
 
 // ---- forward, few rows -----------------------------------------------------------------
@@ -684,19 +679,19 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a) {
   }
 }
 
-// The sums of the row blocks, in order: 16 columns a workgroup, 64 lanes' runs of them each.
+// The sums of the row blocks, in order: 16 columns a workgroup, 64 lanes' runs of them each. In
+// the products' launch, where there is one.
 struct SumArgs {
   const float *part;
   uint16_t *out;
   int32_t n, Mp, cols;
   int32_t *flag;
 };
-template <int DT>
-__global__ __launch_bounds__(256) void linear_sum_kernel(SumArgs a) {
-  using T = typename TypeOf<DT>::T;
+template <class T>
+__device__ __forceinline__ void sum_block(const SumArgs &a, int block, void *lds) {
+  const int c = 16 * block + (threadIdx.x & 15);
   float s;
-  const int c = 16 * (int)blockIdx.x + (threadIdx.x & 15);
-  rows::sum_columns(a.part, a.n, a.Mp, 16 * (int)blockIdx.x, a.Mp, s);
+  rows::sum_columns(a.part, a.n, a.Mp, 16 * block, a.Mp, lds, s);
   bool bad = false;
   if (threadIdx.x < 16 && c < a.cols) {
     const T v = (T)s;
@@ -704,6 +699,11 @@ __global__ __launch_bounds__(256) void linear_sum_kernel(SumArgs a) {
     bad = !(fabsf((float)v) < INFINITY);
   }
   if (a.flag) flag_nonfinite(a.flag, bad);
+}
+template <int DT>
+__global__ __launch_bounds__(256) void linear_sum_kernel(SumArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[rows::kSumLds];
+  sum_block<typename TypeOf<DT>::T>(a, blockIdx.x, lds);
 }
 
 // ---- products of the gradients ---------------------------------------------------------
@@ -804,6 +804,7 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
   }
   lds_barrier();  // every wave is done reading the ring
   bool bad = false;
+  const __amdgpu_buffer_rsrc_t rs_out = rows_from(a.out, n0 + wn0, a.out_ld, a.N, a.M, 2);
   store16<P>(
       wave_buf<P>(R, wave), lane,
       [&](int i, int j, int g) __attribute__((always_inline)) {
@@ -814,25 +815,38 @@ __device__ __forceinline__ void product_tile(const ProdArgs &a, const TileMap &t
       [&](int r, int c, const u32x4 &d) __attribute__((always_inline)) {
         const int64_t n = n0 + wn0 + r;
         const int m = m0 + wm0 + c;
-        if (n >= a.N || m >= a.M) return;
+        const bool in = n < a.N && m < a.M;
         constexpr uint32_t EX = P::BF ? 0x7F80u : 0x7C00u;
         if (!DX) {
+          bool inf = false;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) bad |= (d[e >> 1] >> (16 * (e & 1)) & EX) == EX;
+          for (int e = 0; e < 8; ++e) inf |= (d[e >> 1] >> (16 * (e & 1)) & EX) == EX;
+          bad |= inf && in;
         }
-        put_chunk(a.out + n * a.out_ld, m, a.M, d);
+        if (a.M >= 8)
+          __builtin_amdgcn_raw_buffer_store_b128(
+              d, rs_out, in ? (r * (int)a.out_ld + chunk_at(m, a.M)) * 2 : (int)kOOB, 0, 0);
+        else if (in)
+          put8(a.out + n * a.out_ld, m, a.M, d);
       });
   if (!DX && a.flag) flag_nonfinite(a.flag, bad);
 }
 
 // Both in one launch: neither waits for the other's last tiles. The one whose sums (their
-// parts) are longer takes the first workgroups, `first` of them.
+// parts) are longer takes the first workgroups, `first` of them; the last ones sum up dbias.
 template <class P>
 __global__ __launch_bounds__(P::NT, P::WPE) void linear_products_kernel(ProdArgs dx, TileMap tx,
                                                                         ProdArgs dw, TileMap tw,
-                                                                        int first, int dx_first) {
+                                                                        SumArgs sum, int first,
+                                                                        int both, int dx_first) {
   FG_DMA_RING(P, R);
   const int block = blockIdx.x;
+  if (block >= both) {
+    static_assert(P::A_BYTES >= rows::kSumLds, "room for the sums");
+    using T = typename TypeOf<P::BF ? FG_BF16 : FG_F16>::T;
+    sum_block<T>(sum, block - both, R.a[0]);
+    return;
+  }
   const bool leads = block < first;
   const int at = leads ? block : block - first;
   if (leads == (dx_first != 0))
@@ -1114,10 +1128,7 @@ template <class P>
 hipError_t launch_fwd(FwdArgs a, int ns, hipStream_t st) {
   a.ntile = (a.e.out + P::TM - 1) / P::TM;
   const TileMap tm = tile_map((a.rows + P::TN - 1) / P::TN, a.ntile, ns);
-  if (a.e.out % 8 == 0)
-    hipLaunchKernelGGL((linear_fwd_kernel<P, true>), dim3(8 * tm.per), dim3(P::NT), 0, st, a, tm);
-  else
-    hipLaunchKernelGGL((linear_fwd_kernel<P, false>), dim3(8 * tm.per), dim3(P::NT), 0, st, a, tm);
+  hipLaunchKernelGGL(linear_fwd_kernel<P>, dim3(8 * tm.per), dim3(P::NT), 0, st, a, tm);
   return hipGetLastError();
 }
 
@@ -1146,15 +1157,17 @@ hipError_t launch_few(const FwdArgs &a, hipStream_t st) {
 }
 
 template <class P>
-hipError_t launch_products(ProdArgs dx, int nsx, ProdArgs dw, int nsw, hipStream_t st) {
+hipError_t launch_products(ProdArgs dx, int nsx, ProdArgs dw, int nsw, const SumArgs &sum,
+                           hipStream_t st) {
   dx.ntile = (int32_t)((dx.N + P::TN - 1) / P::TN);
   dw.ntile = (int32_t)((dw.N + P::TN - 1) / P::TN);
   const TileMap none{1, 1, 0, 0, kOutputMajor};
   const TileMap tx = nsx ? tile_map((dx.M + P::TM - 1) / P::TM, dx.ntile, nsx) : none;
   const TileMap tw = nsw ? tile_map((dw.M + P::TM - 1) / P::TM, dw.ntile, nsw) : none;
   const int dx_first = !nsw || (nsx && dx.kper >= dw.kper);
-  hipLaunchKernelGGL(linear_products_kernel<P>, dim3(8 * (tx.per + tw.per)), dim3(P::NT), 0, st,
-                     dx, tx, dw, tw, 8 * (dx_first ? tx.per : tw.per), dx_first);
+  const int both = 8 * (tx.per + tw.per), sums = sum.out ? (sum.cols + 15) / 16 : 0;
+  hipLaunchKernelGGL(linear_products_kernel<P>, dim3(both + sums), dim3(P::NT), 0, st, dx, tx, dw,
+                     tw, sum, 8 * (dx_first ? tx.per : tw.per), both, dx_first);
   return hipGetLastError();
 }
 
@@ -1251,17 +1264,18 @@ hipError_t launch_linear_bwd(const fg_linear_desc &d, const void *dy, const void
   if ((formed || dbias) && p.rows) {
     FG_TRY((bf ? launch_dz<FG_BF16> : launch_dz<FG_F16>)(z1, p, st));
   }
-  if (dbias) {
-    const SumArgs s = {z1.part, (uint16_t *)dbias, (int32_t)(p.rows ? p.rblocks : 0),
-                       (int32_t)p.out8, (int32_t)p.out, flag};
+  SumArgs sum{};
+  if (dbias)
+    sum = {z1.part, (uint16_t *)dbias, (int32_t)(p.rows ? p.rblocks : 0), (int32_t)p.out8,
+           (int32_t)p.out, flag};
+  if (dbias && !dw && !(dx && p.rows)) {  // no product's launch to join
     const dim3 grid((uint32_t)((p.out + 15) / 16)), block(256);
     if (bf)
-      hipLaunchKernelGGL(linear_sum_kernel<FG_BF16>, grid, block, 0, st, s);
+      hipLaunchKernelGGL(linear_sum_kernel<FG_BF16>, grid, block, 0, st, sum);
     else
-      hipLaunchKernelGGL(linear_sum_kernel<FG_F16>, grid, block, 0, st, s);
-    FG_TRY(hipGetLastError());
+      hipLaunchKernelGGL(linear_sum_kernel<FG_F16>, grid, block, 0, st, sum);
+    return hipGetLastError();
   }
-  if (!dx && !dw) return hipSuccess;
 
   ProdArgs a{}, b{};
   a.b = b.b = formed ? z1.dz : z1.dy;
@@ -1308,7 +1322,7 @@ hipError_t launch_linear_bwd(const fg_linear_desc &d, const void *dy, const void
           shared_log(nsw)};
   }
   if (!nsx && !nsw) return hipSuccess;
-  FG_TRY(FG_LINEAR_TILE(launch_products, BwdTiles, p.s2.tile, bf, a, nsx, b, nsw, st));
+  FG_TRY(FG_LINEAR_TILE(launch_products, BwdTiles, p.s2.tile, bf, a, nsx, b, nsw, sum, st));
   const auto blocks = [&](int64_t n, const JoinArgs &j) {
     const int wide = 256 >> j.slog;
     return (n * (p.in8 / 8) + wide - 1) / wide;

@@ -186,9 +186,10 @@ __global__ __launch_bounds__(256) void norm_join_kernel(JoinArgs a) {
   T *out = static_cast<T *>(blockIdx.y ? a.dbias : a.dweight);
   if (!out) return;
   const int c = 16 * (int)blockIdx.x + (threadIdx.x & 15);
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kSumLds];
   float s;
   sum_columns(a.part + (int64_t)blockIdx.y * a.wide, a.n, 2 * (int64_t)a.wide,
-              16 * (int)blockIdx.x, a.wide, s);
+              16 * (int)blockIdx.x, a.wide, lds, s);
   bool bad = false;
   if (threadIdx.x < 16 && c < a.cols) {
     const T v = (T)s;

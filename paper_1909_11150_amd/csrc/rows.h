@@ -232,16 +232,18 @@ __device__ __forceinline__ T wave_sum(T v) {
 
 // Sums of n rows of fp32 parts, `stride` elements apart, over 16 columns from c0 on (fewer
 // where `wide`, a multiple of 4, ends): 256 threads, 4 columns and every 64th row each, then
-// the 64 sums of a column in order. The sum of column c0 + i is thread i's, i < 16.
+// the 64 sums of a column in order. The sum of column c0 + i is thread i's, i < 16. (Threads
+// past the 256th wait only.)
+constexpr int kSumLds = 64 * 5 * 16;
 __device__ __forceinline__ void sum_columns(const float *part, int n, int64_t stride, int c0,
-                                            int wide, float &sum) {
-  __shared__ f32x4 sh[64][5];
+                                            int wide, void *lds, float &sum) {
+  f32x4(*sh)[5] = static_cast<f32x4(*)[5]>(lds);
   const int t = threadIdx.x, c = min(c0 + 4 * (t & 3), wide - 4);
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-  for (int k = t >> 2; k < n; k += 64)
+  for (int k = t >> 2; k < n && t < 256; k += 64)
     s += *reinterpret_cast<const f32x4 *>(part + k * stride + c);
-  sh[t >> 2][t & 3] = s;
+  if (t < 256) sh[t >> 2][t & 3] = s;
   __syncthreads();
   sum = 0.f;
   if (t < 16) {
