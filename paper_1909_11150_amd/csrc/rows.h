@@ -57,30 +57,45 @@ __device__ __forceinline__ Raw<T> load_narrow(const T *row, int c, int cols) {
   return __builtin_bit_cast(Raw<T>, v);
 }
 
+// Elements that belong before chunk c where the row's last 8 came in its place; 8 and more: all.
+__device__ __forceinline__ int before(int c, int cols) { return c - min(c, cols - 8); }
+
 // The chunk's elements as fp32, zeros past the row's end.
 template <class T>
 __device__ __forceinline__ void values(const Raw<T> &r, int c, int cols, float (&v)[8]) {
   typedef T t8 __attribute__((ext_vector_type(8)));
-  const t8 q = __builtin_bit_cast(t8, r);
+  Raw<T> x = r;
+  if (cols >= 8) {
+    const int s = before(c, cols);
+    if (cols % 8 == 0) {
+#pragma unroll
+      for (int k = 0; k < (int)(sizeof(T) / 2); ++k)
+        if (s) x.w[k] = u32x4{0, 0, 0, 0};
+    } else if constexpr (sizeof(T) == 2) {
+      // whole words by selection, the odd element by a shift across words
+      u32x4 w = x.w[0];
+      w = s & 8 || s >= 16 ? u32x4{0, 0, 0, 0} : w;
+      w = s & 4 ? u32x4{w[2], w[3], 0, 0} : w;
+      w = s & 2 ? u32x4{w[1], w[2], w[3], 0} : w;
+      const uint32_t sh = 16 * (s & 1);
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+        x.w[0][d] = __builtin_amdgcn_alignbit(d < 3 ? w[d + 1] : 0u, w[d], sh);
+    } else {
+      uint32_t w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = s >= 8 ? 0u : r.w[e / 4][e % 4];
+#pragma unroll
+      for (int b = 4; b; b >>= 1)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = s & b ? (e + b < 8 ? w[e + b] : 0u) : w[e];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x.w[e / 4][e % 4] = w[e];
+    }
+  }
+  const t8 q = __builtin_bit_cast(t8, x);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = (float)q[e];
-  if (cols < 8) return;
-  if (cols % 8 == 0) {
-    if (c >= cols) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = 0.f;
-    }
-    return;
-  }
-  const int s = c - min(c, cols - 8);  // elements that belong before the chunk
-#pragma unroll
-  for (int b = 4; b; b >>= 1)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = s & b ? (e + b < 8 ? v[e + b] : 0.f) : v[e];
-  if (s >= 8) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 0.f;
-  }
 }
 
 template <class T>
@@ -93,22 +108,59 @@ __device__ __forceinline__ void load8(const T *row, int c, int cols, float (&v)[
   values<T>(load_any(row, c, cols), c, cols, v);
 }
 
-// Rounds 8 values once to T and writes those within the row.
+// Rounds 8 values once to T and writes those within the row: its last ones, where they are
+// fewer, in pieces of 4, 2 and 1.
 template <class T>
 __device__ __forceinline__ void store8(T *row, int c, int cols, const float (&v)[8]) {
   T q[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) q[e] = (T)v[e];
+  const Raw<T> r = __builtin_bit_cast(Raw<T>, q);
+  T *p = row + c;
   if (c + 8 <= cols) {
-    const Raw<T> r = __builtin_bit_cast(Raw<T>, q);
 #pragma unroll
     for (int k = 0; k < (int)(sizeof(T) / 2); ++k)
-      reinterpret_cast<Any16 *>(row + c + 8 / (sizeof(T) / 2) * k)->v = r.w[k];
+      reinterpret_cast<Any16 *>(p + 8 / (sizeof(T) / 2) * k)->v = r.w[k];
     return;
   }
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (c + e < cols) row[c + e] = q[e];
+  const int n = cols - c;
+  if (n <= 0) return;
+  typedef uint16_t bits;
+  struct __attribute__((packed, aligned(2))) Any8 {
+    u32x2 v;
+  };
+  struct __attribute__((packed, aligned(2))) Any4 {
+    uint32_t v;
+  };
+  if constexpr (sizeof(T) == 2) {
+    u32x2 w = {r.w[0][0], r.w[0][1]};
+    if (n & 4) {
+      reinterpret_cast<Any8 *>(p)->v = w;
+      w = u32x2{r.w[0][2], r.w[0][3]};
+      p += 4;
+    }
+    uint32_t h = w[0];
+    if (n & 2) {
+      reinterpret_cast<Any4 *>(p)->v = h;
+      h = w[1];
+      p += 2;
+    }
+    if (n & 1) *reinterpret_cast<bits *>(p) = (bits)h;
+  } else {
+    u32x4 w = r.w[0];
+    if (n & 4) {
+      reinterpret_cast<Any16 *>(p)->v = w;
+      w = r.w[1];
+      p += 4;
+    }
+    uint32_t h = w[0];
+    if (n & 2) {
+      reinterpret_cast<Any8 *>(p)->v = u32x2{w[0], w[1]};
+      h = w[2];
+      p += 2;
+    }
+    if (n & 1) reinterpret_cast<Any4 *>(p)->v = h;
+  }
 }
 
 // ---- 8-bit checkpoints ---------------------------------------------------------------
