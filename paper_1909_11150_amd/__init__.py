@@ -609,57 +609,72 @@ def linear_xent_grad(desc, h, w, target, loss, dh, dw, lse=None, totals=None, we
 
 
 # ---- residual blocks ----------------------------------------------------------
+# Tensors have to be on the device whose current stream takes the call.
 _device = None   # () -> index of the current device
 
 
-def _here(name, t):
-    """Refuses a tensor that is not on the device whose stream takes the call."""
-    global _device
+def _current():
+    """Index of the current device; no tensor's where there is no GPU."""
     if _device is None:
-        import torch
-        if torch.cuda.is_initialized() or torch.cuda.is_available():
-            _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-        else:
-            raise ValueError(f"{name}: no GPU, and the tensor must be on one")
-    if t.get_device() != _device():
+        return _find_device()
+    return _device()
+
+
+def _find_device():
+    global _device
+    import torch
+    if not _types:
+        _known()
+    if not (torch.cuda.is_initialized() or torch.cuda.is_available()):
+        return -2
+    _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return _device()
+
+
+def _here(name, t, cur):
+    if t.get_device() != cur:
         raise ValueError(f"{name} is on {t.device}, not on the current GPU")
 
 
-def _rows_of(name, t, rows, cols, ld, dtype):
+def _rows_of(name, t, rows, cols, ld, dtype, cur):
+    """Address of a rows x cols matrix; None stays."""
     if t is None:
         return None
+    if (t.get_device() == cur and t.dtype is _types.get(dtype) and t.shape == (rows, cols)
+            and t.stride() == (ld or cols, 1)):
+        return t.data_ptr()
     p = _matrix(name, t, rows, cols, ld, dtype)
-    _here(name, t)
+    _here(name, t, cur)
     return p
 
 
-def _bytes(name, t, n):
-    if t is None:
-        return None
+def _bytes(name, t, n, cur):
     if t.element_size() != 1 or t.numel() < n or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous uint8 tensor of {n} bytes")
-    _here(name, t)
+    _here(name, t, cur)
     return t.data_ptr()
 
 
-def _per_channel(name, t, n, dtype):
+def _per_channel(name, t, n, dtype, cur):
     if t is None:
         return None
-    if not _types:
-        _known()
     if t.dtype is not _types.get(dtype) or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous tensor of {n} elements of the "
                          "descriptor's type")
-    _here(name, t)
+    _here(name, t, cur)
     return t.data_ptr()
 
 
-def _flag(name, t):
+def _flag(name, t, cur):
     if t is None:
         return None
     p = _counter(name, t)
-    _here(name, t)
+    _here(name, t, cur)
     return p
+
+
+def _scratch(ws, cur):
+    return (None, 0) if ws is None else (_bytes("ws", ws, 0, cur), ws.numel())
 
 
 def act8_bytes(rows, cols):
@@ -667,69 +682,76 @@ def act8_bytes(rows, cols):
     return lib().fg_act8_bytes(rows, cols)
 
 
-def _checkpoint(name, t, rows, cols):
-    return None if t is None else _bytes(name, t, lib().fg_act8_bytes(rows, cols))
+def _checkpoint(name, t, rows, cols, cur):
+    return None if t is None else _bytes(name, t, lib().fg_act8_bytes(rows, cols), cur)
 
 
 def act8_pack(desc, x, packed, stream=None):
     """8-bit checkpoint of x (see include/fcngrad.h). packed: uint8 tensor of
     act8_bytes(desc.rows, desc.cols)."""
-    _check("act8_pack", lib().act8_pack(
-        ctypes.byref(desc), _rows_of("x", x, desc.rows, desc.cols, desc.x_ld, desc.dtype),
-        _checkpoint("packed", packed, desc.rows, desc.cols), _s(stream)))
+    n, c, cur = desc.rows, desc.cols, _current()
+    st = lib().act8_pack(
+        ctypes.byref(desc), _rows_of("x", x, n, c, desc.x_ld, desc.dtype, cur),
+        _checkpoint("packed", packed, n, c, cur), _s(stream))
+    if st:
+        raise FgError("act8_pack", st)
 
 
 def act8_unpack(desc, packed, x, stream=None):
     """The values of an 8-bit checkpoint, into x."""
-    _check("act8_unpack", lib().act8_unpack(
-        ctypes.byref(desc), _checkpoint("packed", packed, desc.rows, desc.cols),
-        _rows_of("x", x, desc.rows, desc.cols, desc.x_ld, desc.dtype), _s(stream)))
+    n, c, cur = desc.rows, desc.cols, _current()
+    st = lib().act8_unpack(
+        ctypes.byref(desc), _checkpoint("packed", packed, n, c, cur),
+        _rows_of("x", x, n, c, desc.x_ld, desc.dtype, cur), _s(stream))
+    if st:
+        raise FgError("act8_unpack", st)
 
 
 def layer_norm_workspace_bytes(desc):
     return lib().fg_layer_norm_workspace_bytes(ctypes.byref(desc))
 
 
-def _stats(t, rows):
+def _stats(t, rows, cur):
     if t is None:
         return None
     p = _vector("stats", t, 2 * rows, F32)
-    _here("stats", t)
+    _here("stats", t, cur)
     return p
 
 
 def layer_norm_fwd(desc, x, y, weight=None, bias=None, stats=None, packed=None, stream=None):
     """Layer norm of each row (see include/fcngrad.h). stats: fp32 rows x 2, mean and rstd;
     packed: the 8-bit checkpoint of x; both for layer_norm_bwd."""
-    n, c, dt = desc.rows, desc.cols, desc.dtype
-    _check("layer_norm_fwd", lib().layer_norm_fwd(
-        ctypes.byref(desc), _rows_of("x", x, n, c, desc.x_ld, dt),
-        _per_channel("weight", weight, c, dt), _per_channel("bias", bias, c, dt),
-        _rows_of("y", y, n, c, desc.y_ld, dt), _stats(stats, n),
-        _checkpoint("packed", packed, n, c), _s(stream)))
+    n, c, dt, cur = desc.rows, desc.cols, desc.dtype, _current()
+    st = lib().layer_norm_fwd(
+        ctypes.byref(desc), _rows_of("x", x, n, c, desc.x_ld, dt, cur),
+        _per_channel("weight", weight, c, dt, cur), _per_channel("bias", bias, c, dt, cur),
+        _rows_of("y", y, n, c, desc.y_ld, dt, cur), _stats(stats, n, cur),
+        _checkpoint("packed", packed, n, c, cur), _s(stream))
+    if st:
+        raise FgError("layer_norm_fwd", st)
 
 
 def layer_norm_bwd(desc, dy, stats, x=None, packed=None, weight=None, add=None, dx=None,
                    dweight=None, dbias=None, found_nonfinite=None, ws=None, stream=None):
     """Gradients of layer_norm_fwd from x or its checkpoint `packed`; add: another gradient of
     x, added to dx. ws: uint8 tensor of layer_norm_workspace_bytes(desc)."""
-    n, c, dt = desc.rows, desc.cols, desc.dtype
-    wp, wb = _scratch(ws)
-    _check("layer_norm_bwd", lib().layer_norm_bwd(
-        ctypes.byref(desc), _rows_of("dy", dy, n, c, desc.y_ld, dt),
-        _rows_of("x", x, n, c, desc.x_ld, dt), _checkpoint("packed", packed, n, c),
-        _stats(stats, n), _per_channel("weight", weight, c, dt),
-        _rows_of("add", add, n, c, desc.add_ld, dt), _rows_of("dx", dx, n, c, desc.dx_ld, dt),
-        _per_channel("dweight", dweight, c, dt), _per_channel("dbias", dbias, c, dt),
-        _flag("found_nonfinite", found_nonfinite), wp, wb, _s(stream)))
+    n, c, dt, cur = desc.rows, desc.cols, desc.dtype, _current()
+    wp, wb = _scratch(ws, cur)
+    st = lib().layer_norm_bwd(
+        ctypes.byref(desc), _rows_of("dy", dy, n, c, desc.y_ld, dt, cur),
+        _rows_of("x", x, n, c, desc.x_ld, dt, cur), _checkpoint("packed", packed, n, c, cur),
+        _stats(stats, n, cur), _per_channel("weight", weight, c, dt, cur),
+        _rows_of("add", add, n, c, desc.add_ld, dt, cur),
+        _rows_of("dx", dx, n, c, desc.dx_ld, dt, cur),
+        _per_channel("dweight", dweight, c, dt, cur), _per_channel("dbias", dbias, c, dt, cur),
+        _flag("found_nonfinite", found_nonfinite, cur), wp, wb, _s(stream))
+    if st:
+        raise FgError("layer_norm_bwd", st)
 
 
 def linear_workspace_bytes(desc, grad):
     return lib().fg_linear_workspace_bytes(ctypes.byref(desc), int(grad))
-
-
-def _scratch(ws):
-    return (None, 0) if ws is None else (_bytes("ws", ws, 0), ws.numel())
 
 
 def linear_fwd(desc, x, w, y, bias=None, residual=None, z=None, packed_z=None, ws=None,
@@ -737,14 +759,16 @@ def linear_fwd(desc, x, w, y, bias=None, residual=None, z=None, packed_z=None, w
     """y = residual + act(x w^T + bias) (see include/fcngrad.h). z, packed_z: what an
     activation's backward pass needs of z = x w^T + bias, in desc's type or in 8 bits. ws:
     uint8 tensor of linear_workspace_bytes(desc, False)."""
-    n, k, m, dt = desc.rows, desc.fan_in, desc.fan_out, desc.dtype
-    wp, wb = _scratch(ws)
-    _check("linear_fwd", lib().linear_fwd(
-        ctypes.byref(desc), _rows_of("x", x, n, k, desc.x_ld, dt),
-        _rows_of("w", w, m, k, desc.w_ld, dt), _per_channel("bias", bias, m, dt),
-        _rows_of("residual", residual, n, m, desc.r_ld, dt), _rows_of("y", y, n, m, desc.y_ld, dt),
-        _rows_of("z", z, n, m, desc.z_ld, dt), _checkpoint("packed_z", packed_z, n, m), wp, wb,
-        _s(stream)))
+    n, k, m, dt, cur = desc.rows, desc.fan_in, desc.fan_out, desc.dtype, _current()
+    wp, wb = _scratch(ws, cur)
+    st = lib().linear_fwd(
+        ctypes.byref(desc), _rows_of("x", x, n, k, desc.x_ld, dt, cur),
+        _rows_of("w", w, m, k, desc.w_ld, dt, cur), _per_channel("bias", bias, m, dt, cur),
+        _rows_of("residual", residual, n, m, desc.r_ld, dt, cur),
+        _rows_of("y", y, n, m, desc.y_ld, dt, cur), _rows_of("z", z, n, m, desc.z_ld, dt, cur),
+        _checkpoint("packed_z", packed_z, n, m, cur), wp, wb, _s(stream))
+    if st:
+        raise FgError("linear_fwd", st)
 
 
 def linear_bwd(desc, dy, x=None, packed_x=None, w=None, z=None, packed_z=None, dx=None, dw=None,
@@ -752,15 +776,19 @@ def linear_bwd(desc, dy, x=None, packed_x=None, w=None, z=None, packed_z=None, d
     """Gradients of linear_fwd from dy: dx (reads w), dw (reads x or its checkpoint packed_x),
     dbias; z or its checkpoint packed_z with an activation. ws: uint8 tensor of
     linear_workspace_bytes(desc, True)."""
-    n, k, m, dt = desc.rows, desc.fan_in, desc.fan_out, desc.dtype
-    wp, wb = _scratch(ws)
-    _check("linear_bwd", lib().linear_bwd(
-        ctypes.byref(desc), _rows_of("dy", dy, n, m, desc.y_ld, dt),
-        _rows_of("x", x, n, k, desc.x_ld, dt), _checkpoint("packed_x", packed_x, n, k),
-        _rows_of("w", w, m, k, desc.w_ld, dt), _rows_of("z", z, n, m, desc.z_ld, dt),
-        _checkpoint("packed_z", packed_z, n, m), _rows_of("dx", dx, n, k, desc.dx_ld, dt),
-        _rows_of("dw", dw, m, k, desc.dw_ld, dt), _per_channel("dbias", dbias, m, dt),
-        _flag("found_nonfinite", found_nonfinite), wp, wb, _s(stream)))
+    n, k, m, dt, cur = desc.rows, desc.fan_in, desc.fan_out, desc.dtype, _current()
+    wp, wb = _scratch(ws, cur)
+    st = lib().linear_bwd(
+        ctypes.byref(desc), _rows_of("dy", dy, n, m, desc.y_ld, dt, cur),
+        _rows_of("x", x, n, k, desc.x_ld, dt, cur),
+        _checkpoint("packed_x", packed_x, n, k, cur),
+        _rows_of("w", w, m, k, desc.w_ld, dt, cur), _rows_of("z", z, n, m, desc.z_ld, dt, cur),
+        _checkpoint("packed_z", packed_z, n, m, cur),
+        _rows_of("dx", dx, n, k, desc.dx_ld, dt, cur),
+        _rows_of("dw", dw, m, k, desc.dw_ld, dt, cur), _per_channel("dbias", dbias, m, dt, cur),
+        _flag("found_nonfinite", found_nonfinite, cur), wp, wb, _s(stream))
+    if st:
+        raise FgError("linear_bwd", st)
 
 
 def grad_flags_clear(flags, stream=None):

@@ -195,14 +195,16 @@ __device__ __forceinline__ void pack_block(const f32x16 (&acc)[P::FM][P::FN], co
       uint32_t q[4];
       const uint32_t b =
           rows::pack_group<16>(v, q, [](uint32_t top) __attribute__((always_inline)) {
-            return max(top, (uint32_t)__shfl_xor((int)top, 32));
+            const auto p = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+            return max(p[0], p[1]);
           });
-      const uint32_t r0 = __shfl_xor((int)(up ? q[0] : q[2]), 32);
-      const uint32_t r1 = __shfl_xor((int)(up ? q[1] : q[3]), 32);
+      // the lower lane's words 2 and 3 for the upper one's 0 and 1
+      const auto s0 = __builtin_amdgcn_permlane32_swap(q[0], q[2], false, false);
+      const auto s1 = __builtin_amdgcn_permlane32_swap(q[1], q[3], false, false);
       const int r = 32 * j + (lane & 31), m = m0 + 32 * i;
       const bool in = m < p.wide;
       __builtin_amdgcn_raw_buffer_store_b128(
-          up ? u32x4{r0, q[2], r1, q[3]} : u32x4{q[0], r0, q[1], r1}, rs_q,
+          u32x4{s0[0], s0[1], s1[0], s1[1]}, rs_q,
           in ? r * p.wide + m + (up ? 16 : 0) : (int)kOOB, 0, 0);
       __builtin_amdgcn_raw_buffer_store_b8((uint8_t)b, rs_e,
                                            in && !up ? r * (p.wide / 32) + m / 32 : (int)kOOB, 0,

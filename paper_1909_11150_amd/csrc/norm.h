@@ -15,22 +15,32 @@ struct Team {
   static __device__ __forceinline__ int col(int t, int n) { return 8 * (t + TEAM * n); }
 };
 
-// The team's sum, in every lane. red: LDS of NT / 64 floats for each of the alternating
-// places (W > 1), so that one barrier per sum is enough.
+// The team's sums of R values, in every lane. red: LDS of R * NT / 64 floats (W > 1) that no
+// other exchange uses before the next barrier.
+template <class M, int R>
+__device__ __forceinline__ void team_sums(float (&v)[R], float *red) {
+#pragma unroll
+  for (int k = 0; k < R; ++k) v[k] = sum_lanes<M::TL>(v[k]);
+  if constexpr (M::W > 1) {
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int k = 0; k < R; ++k) red[wave * R + k] = v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < R; ++k) v[k] = 0.f;
+#pragma unroll
+    for (int i = 0; i < M::W; ++i)
+#pragma unroll
+      for (int k = 0; k < R; ++k) v[k] += red[(wave / M::W * M::W + i) * R + k];
+  }
+}
 template <class M>
 __device__ __forceinline__ float team_sum(float v, float *red, int place) {
-#pragma unroll
-  for (int o = M::TL / 2; o; o >>= 1) v += __shfl_xor(v, o);
-  if constexpr (M::W > 1) {
-    float *at = red + place * (M::NT / 64);
-    const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) at[wave] = v;
-    __syncthreads();
-    v = 0.f;
-#pragma unroll
-    for (int k = 0; k < M::W; ++k) v += at[wave / M::W * M::W + k];
-  }
-  return v;
+  float s[1] = {v};
+  team_sums<M, 1>(s, red + place * (M::NT / 64));
+  return s[0];
 }
 
 struct FwdArgs {
@@ -43,27 +53,34 @@ struct FwdArgs {
   float inv, eps;    // 1 / cols
 };
 
-constexpr int kFwdBlocks = 2048;
-constexpr int kMaxCols = 16384;
+// Workgroups of the forward pass: some more than the chip holds at once, so that each takes
+// several rows with the next one's loads on their way (16384 x 1024 fp16: 16.6 us with 2048,
+// 17.1 with 1280, 15.4 with 1024; one row to a team without the loop 17.4 and more).
+constexpr int kFwdBlocks = 1024;
 
-// f.go<type, TL, W, N>() for the smallest team that holds a row.
-template <int DT, class F>
+// f.go<type, TL, W, N>() for the team that takes a row. Backward, where 16 sums a chunk stay in
+// registers, wide rows take more waves with a chunk to a lane each (16384 x 1024 fp16 27.5 us,
+// 31.1 with two); forward, two chunks and half the exchanges (8192 x 4096 bf16 27.4 us, 39 with
+// one).
+enum Pass { kForward, kGrad };
+template <int DT, Pass P, class F>
 hipError_t for_cols(int cols, const F &f) {
+  constexpr int W = P == kForward ? 1 : 2, N = P == kForward ? 2 : 1;
   return cols <= 64     ? f.template go<DT, 8, 1, 1>()
          : cols <= 128  ? f.template go<DT, 16, 1, 1>()
          : cols <= 256  ? f.template go<DT, 32, 1, 1>()
          : cols <= 512  ? f.template go<DT, 64, 1, 1>()
-         : cols <= 1024 ? f.template go<DT, 64, 1, 2>()
-         : cols <= 2048 ? f.template go<DT, 64, 2, 2>()
-         : cols <= 4096 ? f.template go<DT, 64, 4, 2>()
+         : cols <= 1024 ? f.template go<DT, 64, W, N>()
+         : cols <= 2048 ? f.template go<DT, 64, 2 * W, N>()
+         : cols <= 4096 ? f.template go<DT, 64, 4 * W, N>()
          : cols <= 8192 ? f.template go<DT, 64, 8, 2>()
-                        : f.template go<DT, 64, 8, 4>();
+                        : f.template go<DT, 64, 16, 2>();
 }
-template <class F>
+template <Pass P, class F>
 hipError_t for_team(int dtype, int cols, const F &f) {
-  return dtype == FG_F16    ? for_cols<FG_F16>(cols, f)
-         : dtype == FG_BF16 ? for_cols<FG_BF16>(cols, f)
-                            : for_cols<FG_F32>(cols, f);
+  return dtype == FG_F16    ? for_cols<FG_F16, P>(cols, f)
+         : dtype == FG_BF16 ? for_cols<FG_BF16, P>(cols, f)
+                            : for_cols<FG_F32, P>(cols, f);
 }
 
 }  // namespace norm

@@ -112,7 +112,7 @@ hipError_t launch_layer_norm_fwd(const fg_norm_desc &d, const void *x, const voi
   a.rows = d.rows, a.cols = (int32_t)d.cols;
   a.x_ld = d.x_ld ? d.x_ld : d.cols, a.y_ld = d.y_ld ? d.y_ld : d.cols;
   a.inv = (float)(1.0 / (double)d.cols), a.eps = (float)d.eps;
-  return norm::for_team(d.dtype, a.cols, norm::Fwd{a, st});
+  return norm::for_team<norm::kForward>(d.dtype, a.cols, norm::Fwd{a, st});
 }
 
 }  // namespace fg

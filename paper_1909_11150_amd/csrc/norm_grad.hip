@@ -17,9 +17,9 @@ struct BwdArgs {
   float inv;
 };
 
-// 8 waves a workgroup.
+// 8 waves a workgroup, or a row's 16.
 template <int TL, int W, int N>
-using Grad = Team<TL, W, N, 512>;
+using Grad = Team<TL, W, N, W <= 8 ? 512 : 64 * W>;
 
 // What a row's gradient needs, on its way.
 template <class T, int N, bool PACKED>
@@ -32,12 +32,13 @@ struct Loads {
 };
 
 template <int DT, int TL, int W, int N, bool PACKED>
-__global__ __launch_bounds__(512, 2) void norm_bwd_kernel(BwdArgs a) {
+__global__ __launch_bounds__((Grad<TL, W, N>::NT), 2) void norm_bwd_kernel(BwdArgs a) {
   using T = typename TypeOf<DT>::T;
   using M = Grad<TL, W, N>;
   constexpr int FOLD = M::TEAMS / 2;  // teams whose sums wait in LDS at a time
   constexpr int LDS = FOLD * M::TEAM * N * 16;
-  __shared__ __attribute__((aligned(16))) float lds[LDS > 64 ? LDS : 64];
+  constexpr int EX = 4 * (M::NT / 64);  // the sums' exchange, two of them in turn
+  __shared__ __attribute__((aligned(16))) float lds[LDS > EX ? LDS : EX];
   const int t = threadIdx.x % M::TEAM, team = threadIdx.x / M::TEAM, cols = a.cols;
   const T *dy = static_cast<const T *>(a.dy), *x = static_cast<const T *>(a.x),
           *w = static_cast<const T *>(a.weight), *add = static_cast<const T *>(a.add);
@@ -56,9 +57,9 @@ __global__ __launch_bounds__(512, 2) void norm_bwd_kernel(BwdArgs a) {
       const int c = M::col(t, n);
       next.dy[n] = load_any(dy + r * a.dy_ld, c, cols);
       if constexpr (PACKED) {
-        const int k = min(c, a.packed.wide - 8);
-        next.code[n] = *reinterpret_cast<const u32x2 *>(a.packed.codes + r * a.packed.wide + k);
-        next.exp[n] = a.packed.exps[r * (a.packed.wide / 32) + k / 32];
+        const int q = min(c, a.packed.wide - 8);
+        next.code[n] = *reinterpret_cast<const u32x2 *>(a.packed.codes + r * a.packed.wide + q);
+        next.exp[n] = a.packed.exps[r * (a.packed.wide / 32) + q / 32];
       } else {
         next.x[n] = load_any(x + r * a.x_ld, c, cols);
       }
@@ -71,10 +72,10 @@ __global__ __launch_bounds__(512, 2) void norm_bwd_kernel(BwdArgs a) {
   int turn = 0;
   for (; r0 < a.rows; r0 += step, turn ^= 1) {
     const int64_t r = r0 + team;
-    const bool on = r < a.rows;
+    const bool on = r < a.rows, ragged = r0 + M::TEAMS > a.rows;  // (the latter for all alike)
     const Loads<T, N, PACKED> now = next;
     if (r0 + step < a.rows) load(r + step);
-    float g[N][8], xh[N][8], s1 = 0.f, s2 = 0.f;
+    float g[N][8], xh[N][8], s[2] = {0.f, 0.f};
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const int c = M::col(t, n);
@@ -87,40 +88,20 @@ __global__ __launch_bounds__(512, 2) void norm_bwd_kernel(BwdArgs a) {
       if (w) values<T>(rw[n], c, cols, wv);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        xh[n][e] = (xh[n][e] - now.stat.x) * now.stat.y;
-        if (!on) g[n][e] = xh[n][e] = 0.f;
-        aw[n][e] = fmaf(g[n][e], xh[n][e], aw[n][e]);
-        ab[n][e] += g[n][e];
-        if (w) g[n][e] *= wv[e];
-        s1 += g[n][e];
-        s2 = fmaf(g[n][e], xh[n][e], s2);
+        float &gv = g[n][e], &xv = xh[n][e];
+        xv = (xv - now.stat.x) * now.stat.y;
+        if (ragged && !on) gv = xv = 0.f;
+        aw[n][e] = fmaf(gv, xv, aw[n][e]);
+        ab[n][e] += gv;
+        if (w) gv *= wv[e];
+        s[0] += gv;
+        s[1] = fmaf(gv, xv, s[1]);
       }
     }
     if (!dx) continue;  // (the same for all)
-    if constexpr (W == 1) {
-      s1 = team_sum<M>(s1, nullptr, 0) * a.inv;
-      s2 = team_sum<M>(s2, nullptr, 0) * a.inv;
-    } else {  // both in one exchange
-#pragma unroll
-      for (int o = 32; o; o >>= 1) {
-        s1 += __shfl_xor(s1, o);
-        s2 += __shfl_xor(s2, o);
-      }
-      float2 *at = reinterpret_cast<float2 *>(lds) + 8 * turn;
-      const int wave = threadIdx.x >> 6;
-      if ((threadIdx.x & 63) == 0) at[wave] = float2{s1, s2};
-      __syncthreads();
-      s1 = s2 = 0.f;
-#pragma unroll
-      for (int k = 0; k < W; ++k) {
-        const float2 p = at[wave / W * W + k];
-        s1 += p.x;
-        s2 += p.y;
-      }
-      s1 *= a.inv;
-      s2 *= a.inv;
-    }
+    team_sums<M, 2>(s, lds + 2 * (M::NT / 64) * turn);
     if (!on) continue;
+    const float s1 = s[0] * a.inv, s2 = s[1] * a.inv;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const int c = M::col(t, n);
@@ -215,7 +196,7 @@ struct MakePlan {
 };
 Plan make_plan(int64_t rows, int64_t cols) {
   Plan p{};
-  (void)for_cols<FG_F16>((int)cols, MakePlan{rows, &p});
+  (void)for_cols<FG_F16, kGrad>((int)cols, MakePlan{rows, &p});
   return p;
 }
 
@@ -223,14 +204,18 @@ struct Bwd {
   const BwdArgs &a;
   int64_t blocks;
   hipStream_t st;
+  template <int DT, int TL, int W, int N, bool PACKED>
+  hipError_t launch() const {
+    hipLaunchKernelGGL((norm_bwd_kernel<DT, TL, W, N, PACKED>), dim3((uint32_t)blocks),
+                       dim3(Grad<TL, W, N>::NT), 0, st, a);
+    return hipGetLastError();
+  }
   template <int DT, int TL, int W, int N>
   hipError_t go() const {
-    const dim3 grid((uint32_t)blocks), block(512);
-    if (a.packed.codes)
-      hipLaunchKernelGGL((norm_bwd_kernel<DT, TL, W, N, true>), grid, block, 0, st, a);
-    else
-      hipLaunchKernelGGL((norm_bwd_kernel<DT, TL, W, N, false>), grid, block, 0, st, a);
-    return hipGetLastError();
+    // (8192 x 4096 bf16: from x 50 us by 8 waves to a row, 45 by 4; packed 49.6 and 51.5)
+    if constexpr (W == 8 && N == 1)
+      if (!a.packed.codes) return launch<DT, TL, 4, 2, false>();
+    return a.packed.codes ? launch<DT, TL, W, N, true>() : launch<DT, TL, W, N, false>();
   }
 };
 
@@ -258,7 +243,7 @@ hipError_t launch_layer_norm_bwd(const fg_norm_desc &d, const void *dy, const vo
   a.cols = (int32_t)d.cols;
   a.inv = (float)(1.0 / (double)d.cols);
   if (d.rows) {
-    const hipError_t e = norm::for_team(d.dtype, a.cols, norm::Bwd{a, p.blocks, st});
+    const hipError_t e = norm::for_team<norm::kGrad>(d.dtype, a.cols, norm::Bwd{a, p.blocks, st});
     if (e != hipSuccess) return e;
   }
   if (!sums) return hipSuccess;

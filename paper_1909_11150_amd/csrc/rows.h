@@ -163,6 +163,45 @@ __device__ __forceinline__ void store8(T *row, int c, int cols, const float (&v)
   }
 }
 
+// ---- across lanes ----------------------------------------------------------------------
+// The value of the lane whose number differs in bit O, for values that agree within groups of
+// O lanes (a mirrored row then is as good as an exchange): VALU moves, no trip through LDS.
+template <int O>
+__device__ __forceinline__ uint32_t across(uint32_t v) {
+  static_assert(O == 1 || O == 2 || O == 4 || O == 8, "within a row of 16 lanes");
+  constexpr int kCtrl = O == 1 ? 0xB1 : O == 2 ? 0x4E : O == 4 ? 0x141 : 0x140;
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, kCtrl, 0xF, 0xF, true);
+}
+// Joins each lane's value with those of the TL - 1 lanes beside it, in all of them.
+template <int TL, class Join>
+__device__ __forceinline__ uint32_t join_lanes(uint32_t v, Join &&join) {
+  if constexpr (TL >= 2) v = join(v, across<1>(v));
+  if constexpr (TL >= 4) v = join(v, across<2>(v));
+  if constexpr (TL >= 8) v = join(v, across<4>(v));
+  if constexpr (TL >= 16) v = join(v, across<8>(v));
+  if constexpr (TL >= 32) {
+    const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = join(p[0], p[1]);
+  }
+  if constexpr (TL >= 64) {
+    const auto p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = join(p[0], p[1]);
+  }
+  return v;
+}
+template <int TL>
+__device__ __forceinline__ float sum_lanes(float v) {
+  return __builtin_bit_cast(
+      float, join_lanes<TL>(__builtin_bit_cast(uint32_t, v), [](uint32_t a, uint32_t b) {
+        return __builtin_bit_cast(
+            uint32_t, __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b));
+      }));
+}
+template <int TL>
+__device__ __forceinline__ uint32_t max_lanes(uint32_t v) {
+  return join_lanes<TL>(v, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+
 // ---- 8-bit checkpoints ---------------------------------------------------------------
 // rows x cols values in row-major codes (signed bytes, rows padded with zeros to a multiple
 // of 32 columns), then one byte for each 32 columns of a row: the biased exponent b, at least
@@ -266,20 +305,11 @@ __device__ __forceinline__ void decode8(const u32x2 &q, uint32_t b, float (&v)[8
 // group of 32 columns; every lane of the four takes part, those past the end with zeros.
 __device__ __forceinline__ void pack8(const Packed &p, int64_t row, int c, const float (&v)[8]) {
   uint32_t q[2];
-  const uint32_t b = pack_group<8>(v, q, [](uint32_t top) __attribute__((always_inline)) {
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-    return max(top, (uint32_t)__shfl_xor((int)top, 2));
-  });
+  const uint32_t b = pack_group<8>(
+      v, q, [](uint32_t top) __attribute__((always_inline)) { return max_lanes<4>(top); });
   if (c >= p.wide) return;
   *reinterpret_cast<u32x2 *>(p.codes + row * p.wide + c) = u32x2{q[0], q[1]};
   if (c % 32 == 0) p.exps[row * (p.wide / 32) + c / 32] = (uint8_t)b;
-}
-
-template <class T>
-__device__ __forceinline__ T wave_sum(T v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  return v;
 }
 
 // Sums of n rows of fp32 parts, `stride` elements apart, over 16 columns from c0 on (fewer
