@@ -32,7 +32,7 @@ struct Loads {
 };
 
 template <int DT, int TL, int W, int N, bool PACKED>
-__global__ __launch_bounds__((Grad<TL, W, N>::NT), 2) void norm_bwd_kernel(BwdArgs a) {
+__global__ __launch_bounds__((Grad<TL, W, N>::NT), N == 1 ? 4 : 2) void norm_bwd_kernel(BwdArgs a) {
   using T = typename TypeOf<DT>::T;
   using M = Grad<TL, W, N>;
   constexpr int FOLD = M::TEAMS / 2;  // teams whose sums wait in LDS at a time
