@@ -634,6 +634,7 @@ def _find_device():
 def _here(name, t, cur):
     if t.get_device() != cur:
         raise ValueError(f"{name} is on {t.device}, not on the current GPU")
+    return t.data_ptr()
 
 
 def _rows_of(name, t, rows, cols, ld, dtype, cur):
@@ -658,11 +659,12 @@ def _bytes(name, t, n, cur):
 def _per_channel(name, t, n, dtype, cur):
     if t is None:
         return None
+    if (t.get_device() == cur and t.dtype is _types.get(dtype) and t.numel() == n
+            and t.is_contiguous()):
+        return t.data_ptr()
     if t.dtype is not _types.get(dtype) or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous tensor of {n} elements of the "
-                         "descriptor's type")
-    _here(name, t, cur)
-    return t.data_ptr()
+        raise ValueError(f"{name} must be a contiguous {_types.get(dtype)} tensor of {n} elements")
+    return _here(name, t, cur)
 
 
 def _flag(name, t, cur):
@@ -711,14 +713,6 @@ def layer_norm_workspace_bytes(desc):
     return lib().fg_layer_norm_workspace_bytes(ctypes.byref(desc))
 
 
-def _stats(t, rows, cur):
-    if t is None:
-        return None
-    p = _vector("stats", t, 2 * rows, F32)
-    _here("stats", t, cur)
-    return p
-
-
 def layer_norm_fwd(desc, x, y, weight=None, bias=None, stats=None, packed=None, stream=None):
     """Layer norm of each row (see include/fcngrad.h). stats: fp32 rows x 2, mean and rstd;
     packed: the 8-bit checkpoint of x; both for layer_norm_bwd."""
@@ -726,7 +720,7 @@ def layer_norm_fwd(desc, x, y, weight=None, bias=None, stats=None, packed=None, 
     st = lib().layer_norm_fwd(
         ctypes.byref(desc), _rows_of("x", x, n, c, desc.x_ld, dt, cur),
         _per_channel("weight", weight, c, dt, cur), _per_channel("bias", bias, c, dt, cur),
-        _rows_of("y", y, n, c, desc.y_ld, dt, cur), _stats(stats, n, cur),
+        _rows_of("y", y, n, c, desc.y_ld, dt, cur), _per_channel("stats", stats, 2 * n, F32, cur),
         _checkpoint("packed", packed, n, c, cur), _s(stream))
     if st:
         raise FgError("layer_norm_fwd", st)
@@ -741,7 +735,8 @@ def layer_norm_bwd(desc, dy, stats, x=None, packed=None, weight=None, add=None, 
     st = lib().layer_norm_bwd(
         ctypes.byref(desc), _rows_of("dy", dy, n, c, desc.y_ld, dt, cur),
         _rows_of("x", x, n, c, desc.x_ld, dt, cur), _checkpoint("packed", packed, n, c, cur),
-        _stats(stats, n, cur), _per_channel("weight", weight, c, dt, cur),
+        _per_channel("stats", stats, 2 * n, F32, cur),
+        _per_channel("weight", weight, c, dt, cur),
         _rows_of("add", add, n, c, desc.add_ld, dt, cur),
         _rows_of("dx", dx, n, c, desc.dx_ld, dt, cur),
         _per_channel("dweight", dweight, c, dt, cur), _per_channel("dbias", dbias, c, dt, cur),
