@@ -54,7 +54,9 @@ __device__ __forceinline__ float phi_below(float z) {
 }
 // z Phi(z) = max(z, 0) - |z| Phi(-|z|). Infinities give 0 and themselves, NaN NaN.
 __device__ __forceinline__ float gelu(float z) {
-  return fmaf(-fminf(fabsf(z), 64.f), phi_below(z), fmaxf(z, 0.f));
+  // (medians: fminf and fmaxf would first quiet their NaN, two instructions more)
+  return fmaf(-__builtin_amdgcn_fmed3f(fabsf(z), 0.f, 64.f), phi_below(z),
+              __builtin_amdgcn_fmed3f(z, 0.f, INFINITY));
 }
 // Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi)
 __device__ __forceinline__ float gelu_slope(float z) {
@@ -94,6 +96,21 @@ struct FwdArgs {
 // for: without it the largest tiles spill 465 of them (65536 x 256 -> 1024 in 149 us, not 60).
 __device__ __forceinline__ void apart() { __builtin_amdgcn_sched_barrier(0); }
 
+// A block's activation, into registers of its own: changed in place under a branch, the whole
+// tile's accumulators would be copied, and some spilled.
+__device__ __forceinline__ void activate(float (&v)[16], const f32x16 &z, int act) {
+  if (act == FG_ACT_GELU) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = gelu(z[e]);
+  } else if (act == FG_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = z[e] < 0.f ? 0.f : z[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = z[e];
+  }
+}
+
 // Rows n0 .. of a matrix of nrow rows as a buffer: what lies past the last row reads zeros and
 // is not written.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const void *p, int64_t n0, int64_t ld,
@@ -110,7 +127,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const void *p, int64
 // 1000; a row's last chunk, where 8 does not divide it, goes element by element.
 template <class P>
 __device__ __forceinline__ void store_rows(const f32x16 (&acc)[P::FM][P::FN], uint8_t *buf,
-                                           int lane, const uint16_t *residual, int64_t r_ld,
+                                           int lane, int act, const uint16_t *residual,
+                                           int64_t r_ld,
                                            uint16_t *y, int64_t y_ld, int64_t n0, int m0,
                                            int64_t nrow, int out) {
   constexpr int CPW = P::WM / 8, RB = P::WM * 2, SH = CPW == 16 ? 0 : CPW == 8 ? 1 : 2;
@@ -144,21 +162,22 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[P::FM][P::FN], ui
       __builtin_amdgcn_wave_barrier();
     }
 #pragma unroll
-    for (int i = 0; i < P::FM; ++i)
+    for (int i = 0; i < P::FM; ++i) {
+      float v[16];
+      activate(v, acc[i][j], act);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         u32x2 *at = reinterpret_cast<u32x2 *>(place(lane & 31, 4 * i + g) + 8 * (lane >> 5));
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * g + e];
+        float *o = v + 4 * g;
         if (residual) {
-          const u32x2 o = *at;
+          const u32x2 q = *at;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] += to_f32(o[e >> 1] >> (16 * (e & 1)) & 0xFFFFu, P::BF);
+          for (int e = 0; e < 4; ++e) o[e] += to_f32(q[e >> 1] >> (16 * (e & 1)) & 0xFFFFu, P::BF);
         }
-        *at = u32x2{pack2(v[0], v[1], P::BF), pack2(v[2], v[3], P::BF)};
-        if (g == 3) apart();
+        *at = u32x2{pack2(o[0], o[1], P::BF), pack2(o[2], o[3], P::BF)};
       }
+      apart();
+    }
     wait_lds();
     __builtin_amdgcn_wave_barrier();
     u32x4 d[32 / RPI];
@@ -181,7 +200,7 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[P::FM][P::FN], ui
 // lane and of the one 32 further, which exchange halves, so that each writes 16 bytes.
 template <class P>
 __device__ __forceinline__ void pack_block(const f32x16 (&acc)[P::FM][P::FN], const Packed &p,
-                                           int64_t n0, int m0, int64_t nrow, int lane) {
+                                           int64_t n0, int m0, int64_t nrow, int out, int lane) {
   const bool up = lane >= 32;
   const __amdgpu_buffer_rsrc_t rs_q = rows_from(p.codes, n0, p.wide, nrow, p.wide, 1);
   const __amdgpu_buffer_rsrc_t rs_e = rows_from(p.exps, n0, p.wide / 32, nrow, p.wide / 32, 1);
@@ -192,6 +211,11 @@ __device__ __forceinline__ void pack_block(const f32x16 (&acc)[P::FM][P::FN], co
       float v[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) v[e] = acc[i][j][e];
+      if (m0 + 32 * i + 32 > out) {  // (weights past the end are zeros, but 0 x NaN is not)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (m0 + 32 * i + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3) >= out) v[e] = 0.f;
+      }
       uint32_t q[4];
       const uint32_t b =
           rows::pack_group<16>(v, q, [](uint32_t top) __attribute__((always_inline)) {
@@ -232,59 +256,32 @@ template <class P>
 __device__ __forceinline__ void epilogue(f32x16 (&acc)[P::FM][P::FN], const Epilogue &a,
                                          uint8_t *buf, int lane, int64_t n0, int m0,
                                          int64_t nrow) {
-  if (a.bias) {
 #pragma unroll
-    for (int i = 0; i < P::FM; ++i) {
-      u32x2 q[4];
+  for (int i = 0; i < P::FM; ++i) {
+    u32x2 q[4] = {};
+    if (a.bias) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int m = m0 + 32 * i + 8 * g + 4 * (lane >> 5);
-        q[g] = m + 4 <= a.out ? reinterpret_cast<const Any8 *>(a.bias + m)->v : u32x2{0, 0};
+        if (m + 4 <= a.out) q[g] = reinterpret_cast<const Any8 *>(a.bias + m)->v;
         if (m0 + P::WM > a.out && m < a.out && m + 4 > a.out)
 #pragma unroll
           for (int e = 0; e < 3; ++e)
             if (m + e < a.out) q[g][e >> 1] |= (uint32_t)a.bias[m + e] << (16 * (e & 1));
       }
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const float b = to_f32(q[v >> 2][v >> 1 & 1] >> (16 * (v & 1)) & 0xFFFFu, P::BF);
-#pragma unroll
-        for (int j = 0; j < P::FN; ++j) acc[i][j][v] += b;
-      }
-      apart();
     }
-  }
-  if (a.z) store_rows<P>(acc, buf, lane, nullptr, 0, a.z, a.z_ld, n0, m0, nrow, a.out);
-  if (a.packed.codes) {
-    if (m0 + P::WM > a.out) {  // (weights past the end are zeros, but 0 x NaN is not)
 #pragma unroll
-      for (int i = 0; i < P::FM; ++i)
+    for (int v = 0; v < 16; ++v) {
+      const float b = to_f32(q[v >> 2][v >> 1 & 1] >> (16 * (v & 1)) & 0xFFFFu, P::BF);
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (m0 + 32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3) >= a.out)
-#pragma unroll
-            for (int j = 0; j < P::FN; ++j) acc[i][j][v] = 0.f;
+      for (int j = 0; j < P::FN; ++j) acc[i][j][v] += b;
     }
-    pack_block<P>(acc, a.packed, n0, m0, nrow, lane);
+    apart();
   }
-  if (a.act == FG_ACT_RELU) {
-#pragma unroll
-    for (int i = 0; i < P::FM; ++i)
-#pragma unroll
-      for (int j = 0; j < P::FN; ++j)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) acc[i][j][v] = acc[i][j][v] < 0.f ? 0.f : acc[i][j][v];
-  } else if (a.act == FG_ACT_GELU) {
-#pragma unroll
-    for (int i = 0; i < P::FM; ++i)
-#pragma unroll
-      for (int j = 0; j < P::FN; ++j) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) acc[i][j][v] = gelu(acc[i][j][v]);
-        apart();
-      }
-  }
-  store_rows<P>(acc, buf, lane, a.residual, a.r_ld, a.y, a.y_ld, n0, m0, nrow, a.out);
+  if (a.z)
+    store_rows<P>(acc, buf, lane, FG_ACT_NONE, nullptr, 0, a.z, a.z_ld, n0, m0, nrow, a.out);
+  if (a.packed.codes) pack_block<P>(acc, a.packed, n0, m0, nrow, a.out, lane);
+  store_rows<P>(acc, buf, lane, a.act, a.residual, a.r_ld, a.y, a.y_ld, n0, m0, nrow, a.out);
 }
 
 // fp32 sums of a wave's block to a part of a split sum.
