@@ -673,10 +673,10 @@ typedef struct {
     int32_t act;               /* FG_ACT_*; gelu(z) = z Phi(z), Phi the normal distribution's */
 } fg_linear_desc;
 
-/* Device workspace in bytes that linear_bwd (grad != 0) or linear_fwd needs; 0 for an invalid
- * or unsupported descriptor, and where none is needed. For gradients it holds dz and x's
- * values from its checkpoint in 16 bits, and fp32 parts of split sums. Calls that may overlap
- * in time need workspaces of their own. */
+/* Device workspace in bytes that linear_fwd needs, or (grad != 0) linear_bwd and linear_fwd
+ * one after the other; 0 for an invalid or unsupported descriptor, and where none is needed.
+ * For gradients it holds dz and x's values from its checkpoint in 16 bits, and fp32 parts of
+ * split sums. Calls that may overlap in time need workspaces of their own. */
 size_t fg_linear_workspace_bytes(const fg_linear_desc *d, int grad);
 
 /* y = residual + act(z), z = x w^T + bias: products and sums in fp32, one rounding. x: rows x

@@ -1197,8 +1197,10 @@ hipError_t pad(const uint16_t *x, int64_t ld, int64_t n, uint16_t *to, int64_t r
 
 }  // namespace linear
 
+// (a training step's workspace serves its forward pass too)
 size_t linear_ws_bytes(const fg_linear_desc &d, bool grad) {
-  return linear::make_plan(d, grad).total;
+  const size_t fwd = linear::make_plan(d, false).total;
+  return grad ? std::max(fwd, linear::make_plan(d, true).total) : fwd;
 }
 
 hipError_t launch_linear_fwd(const fg_linear_desc &d, const void *x, const void *w,

@@ -1,6 +1,8 @@
 """Argument checks of the residual block's calls that need no GPU: every call below fails (or
 has nothing to do) before any device call."""
 import ctypes
+import math
+import random
 
 import pytest
 import torch
@@ -120,6 +122,16 @@ def test_linear_fwd_refusals(L):
     if need:
         for bad in (dict(ws=None), dict(ws_bytes=need - 1), dict(ws=at(7) + 8)):
             assert call(**split, **bad) == fg.FG_EWORKSPACE
+
+
+def test_a_training_steps_workspace_serves_its_forward_pass():
+    """Whatever the sizes: long sums of few tiles are split forward too."""
+    rng = random.Random(3)
+    for _ in range(300):
+        size = lambda hi: int(math.exp(rng.uniform(0, math.log(hi))))
+        for act in (fg.ACT_NONE, fg.ACT_GELU):
+            d = fg.LinearDesc.make(size(70000), size(20000), size(20000), act=act)
+            assert fg.linear_workspace_bytes(d, True) >= fg.linear_workspace_bytes(d, False)
 
 
 def test_linear_bwd_refusals(L):

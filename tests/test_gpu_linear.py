@@ -334,6 +334,28 @@ def test_rows_that_are_no_numbers(act, rows):
             assert torch.isnan(dx[2]).all() and torch.isnan(db).all()
 
 
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("rows", [3, 200])
+def test_subnormal_operands(dt, rows):
+    """Operands below the type's normal numbers count in full."""
+    k, m, t = 72, 40, TYPES[dt]
+    mk = Maker(dt, 12, False)
+    x, dy = mk(rows, k, torch.finfo(t).tiny / 8), mk(rows, m, torch.finfo(t).tiny / 8)
+    w = mk(m, k, 8.0)
+    assert bool(((x != 0) & (x.abs() < torch.finfo(t).tiny)).any())
+    d = fg.LinearDesc.make(rows, k, m, dtype=fg.dtype_of(x))
+    y, dx, dw = mk.out(rows, m), mk.out(rows, k), mk.out(m, k)
+    fg.linear_fwd(d, x, w, y, ws=scratch(d, False))
+    want, _, mag = B.linear(x, w)
+    # (fp32's own subnormals: products and sums below 2^-126 may lose bits of 2^-149)
+    tol = sum_tol(k) * mag + k * 2.0 ** -126 * (dt == "bf16")
+    near(y, want, tol + half(t, want.abs() + tol), "y")
+    fg.linear_bwd(d, dy, x=mk(rows, k), w=w, dx=dx, dw=dw, ws=scratch(d, True))
+    o = B.linear_grad(dy, None, w)
+    tol = sum_tol(m) * o["ax"] + m * 2.0 ** -126 * (dt == "bf16")
+    near(dx, o["dx"], tol + half(t, o["dx"].abs() + tol), "dx")
+
+
 @pytest.mark.parametrize("m", [8, 300])
 def test_far_pre_activations(m):
     """gelu of large and infinite z: 0, z, and no NaN but of NaN."""
