@@ -617,7 +617,7 @@ typedef struct {
 /* 0 for negative rows, cols < 1, or sizes beyond the limits above. */
 size_t fg_act8_bytes(int64_t rows, int64_t cols);
 
-/* cols below 2^31. */
+/* cols up to 2^31 - 32. */
 fg_status act8_pack(const fg_act8_desc *d, const void *x, void *packed, hipStream_t stream);
 
 /* The values back, into x; exact where dtype is 16 bits wide and that of the packed tensor, or
@@ -683,8 +683,9 @@ size_t fg_linear_workspace_bytes(const fg_linear_desc *d, int grad);
  * in, w: out x in, bias: out (null: 0), residual: rows x out (null: 0). For the backward pass of
  * an activation, z (rows x out, rounded) and packed_z (its 8-bit checkpoint) may be kept;
  * either may be null, and both must be without one. y may be the residual itself at the same
- * stride. Phi(-|z|) is within 1.2e-5 of itself up to |z| = 6, and of 1e-9 beyond. FG_EUNSUPPORTED also for FG_F32, rows of 2^28,
- * in or out above 2^17, strides of 2^20, rows * in or rows * out of 2^34 or more. */
+ * stride. Phi(-|z|) is within 1.2e-5 of itself up to |z| = 6, and of 1e-9 beyond.
+ * FG_EUNSUPPORTED also for FG_F32, rows of 2^28, in or out above 2^17, strides of 2^20, rows *
+ * in or rows * out of 2^34 or more. */
 fg_status linear_fwd(const fg_linear_desc *d, const void *x, const void *w, const void *bias,
                      const void *residual, void *y, void *z, void *packed_z, void *ws,
                      size_t ws_bytes, hipStream_t stream);

@@ -1119,9 +1119,10 @@ fg_status regions_ok(const Region *t, int n) {
 bool type_ok(int32_t dtype) { return dtype >= FG_F16 && dtype <= FG_F32; }
 int64_t type_size(int32_t dtype) { return dtype == FG_F32 ? 4 : 2; }
 
-// rows x cols, rounded up to a checkpoint's, within 2^34.
+// cols, rounded up to a checkpoint's, within 31 bits, and rows of them within 2^34.
 bool act8_fits(int64_t rows, int64_t cols) {
-  return cols < kMaxElems && rows < ((int64_t)1 << 34) / ((cols + 31) / 32 * 32);
+  if (cols > kMaxElems - 32) return false;
+  return rows < ((int64_t)1 << 34) / ((cols + 31) / 32 * 32);
 }
 
 fg_status act8_call(const fg_act8_desc *d, const void *x, const void *packed, bool pack,

@@ -47,6 +47,16 @@ def test_act8_sizes_and_refusals(L):
         assert call(rows=0, x=None, p=None) == fg.FG_OK
 
 
+def test_act8_widths_whose_rounding_up_passes_31_bits(L):
+    top = (1 << 31) - 32
+    assert fg.act8_bytes(1, top) == top + top // 32
+    for cols in (top + 1, (1 << 31) - 1):
+        assert fg.act8_bytes(1, cols) == 0
+        d = fg.Act8Desc.make(rows=1, cols=cols)
+        for fn in (L.act8_pack, L.act8_unpack):
+            assert fn(ctypes.byref(d), None, None, None) == fg.FG_EUNSUPPORTED
+
+
 def test_layer_norm_fwd_refusals(L):
     def call(none=False, x=at(0), w=at(1), b=at(2), y=at(3), stats=at(4), packed=at(5), **kw):
         d = fg.NormDesc.make(**{**dict(rows=64, cols=40), **kw})
