@@ -4,6 +4,10 @@
 //   z = x w^T + b,  y = residual + act(z)
 //   dz = dy act'(z),  dx = dz w,  dw = dz^T x,  db = sum of dz over the rows
 //
+// Bound by the matrix pipes where all three sizes are long (forward, fp32 sums included, 462 us
+// of 16384 x 2048 -> 8192 bf16, 1.19 PFLOP/s; with bias, gelu and checkpoint 546), by memory
+// where the sum is short (65536 x 256 -> 1024: 58 us, 93 with them) or the rows are few.
+//
 // Products run on the MFMA tiles that dma_pipe.h feeds by LDS DMA. The forward tile holds
 // outputs x rows, so 32 consecutive outputs of a row lie in two lanes' registers: bias,
 // activation and the 8-bit checkpoint of z (a step for each 32 columns) are made there, and
@@ -128,9 +132,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const void *p, int64
 template <class P>
 __device__ __forceinline__ void store_rows(const f32x16 (&acc)[P::FM][P::FN], uint8_t *buf,
                                            int lane, int act, const uint16_t *residual,
-                                           int64_t r_ld,
-                                           uint16_t *y, int64_t y_ld, int64_t n0, int m0,
-                                           int64_t nrow, int out) {
+                                           int64_t r_ld, uint16_t *y, int64_t y_ld, int64_t n0,
+                                           int m0, int64_t nrow, int out) {
   constexpr int CPW = P::WM / 8, RB = P::WM * 2, SH = CPW == 16 ? 0 : CPW == 8 ? 1 : 2;
   constexpr int RPI = 64 / CPW;
   const int q = lane % CPW, m = m0 + 8 * q;
@@ -388,7 +391,11 @@ __global__ __launch_bounds__(P::NT, P::WPE) void linear_fwd_kernel(FwdArgs a, Ti
 // feeds itself: a ring of its own in LDS, whose stages of 64 columns come by DMA in whole
 // 128-byte lines, so that it waits for nothing but its oldest loads and some 100 KiB a CU are
 // always on their way. The waves' sums meet in LDS at the end, in order.
-constexpr int kFewRows = 64;
+// (A 24 x 4096 -> 4096 in 11.6 us with its weights from memory, of 6.7 that a copy needs; tiles
+// 13.9. One row, 2048 -> 8192: 9.5 and 13.0; 8192 -> 32768: 99 and 117, of 107.)
+// More than 32 rows of more than 8192 outputs are the tiles' (64 x 4096 -> 16384 36.3 us, 40.2
+// here; 64 x 512 -> 16384 8.5 and 10.7; 64 x 2048 -> 8192 15.3 and 11.9).
+inline bool few_rows(int64_t rows, int64_t out) { return rows <= (out <= 8192 ? 64 : 32); }
 template <bool BF>
 __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
   if (BF)
@@ -580,6 +587,7 @@ struct DzArgs {
 // with zeros behind them; its columns' fp32 sums per workgroup, before the rounding. Bound by
 // memory: the next kRows rows are on their way while these are worked on. KEPT: z in 16 bits
 // or (1) its checkpoint; EVEN: 8 divides the columns, no masks.
+// 16384 x 8192 bf16 from z's checkpoint, gelu: 161 us, 4.2 TB/s; 65536 x 1024 fp16 74 us, 4.5.
 constexpr int kRows = 4;
 template <class T, int ACT, int KEPT, bool EVEN>
 struct DzLoads {
@@ -707,7 +715,10 @@ __global__ __launch_bounds__(256) void linear_sum_kernel(SumArgs a) {
 
 // ---- products of the gradients ---------------------------------------------------------
 // out[n][m] = sum_k A[k][m] B(n, k): A's rows (of w: outputs; of x: rows) lie across the sum;
-// dz is B, by rows n (dx, k: outputs) or columns n (dw, k: rows).
+// dz is B, by rows n (dx, k: outputs) or columns n (dw, k: rows). Bound by the matrix pipes: both
+// gradients of 16384 x 2048 -> 8192 bf16 take 845 us, 1.30 PFLOP/s at 74% of the pipes' cycles
+// and 1.7 GHz, which the board's power allows. 65536 x 256 -> 1024, 103 us, is a third of them:
+// dz is read twice, and a product's tiles have sums of 256 or a share of 65536.
 struct ProdArgs {
   const uint16_t *a;
   int64_t a_ld;
@@ -1139,6 +1150,9 @@ hipError_t launch_few_of(const FwdArgs &a, hipStream_t st) {
 }
 template <bool BF>
 hipError_t launch_few(const FwdArgs &a, hipStream_t st) {
+  // Outputs of a workgroup: at most some 2 workgroups a CU, and no more of them than fill the
+  // chip. 1 row of 2048 -> 2048 by 8, 16, 32, 64: 4.5, 4.4, 5.3, 6.1 us; of 4096 -> 4096 12.0,
+  // 9.2, 10.4, 13.9; of 2048 -> 8192 14.6, 10.6, 9.2, 9.7; of 2048 -> 16384 32: 16.8, 64: 15.6.
   const int out = a.e.out;
   if (a.rows <= 16)
     return out <= 2048   ? launch_few_of<BF, Few<1, 1, 8>>(a, st)
@@ -1152,7 +1166,7 @@ hipError_t launch_few(const FwdArgs &a, hipStream_t st) {
                          : launch_few_of<BF, Few<8, 2, 4>>(a, st);
   return out <= 2048   ? launch_few_of<BF, Few<1, 4, 4>>(a, st)
          : out <= 4096 ? launch_few_of<BF, Few<2, 4, 4>>(a, st)
-                       : launch_few_of<BF, Few<4, 4, 4>>(a, st);
+                       : launch_few_of<BF, Few<4, 4, 4>>(a, st);  // (up to 8192)
 }
 
 template <class P>
@@ -1182,10 +1196,12 @@ hipError_t launch_dz_of(const DzArgs &a, const Plan &p, hipStream_t st) {
 template <int DT>
 hipError_t launch_dz(const DzArgs &a, const Plan &p, hipStream_t st) {
   const bool kept = a.packed.codes != nullptr;
-  return a.act == FG_ACT_NONE ? launch_dz_of<DT, FG_ACT_NONE, 0>(a, p, st)
-         : a.act == FG_ACT_RELU
-             ? (kept ? launch_dz_of<DT, FG_ACT_RELU, 1> : launch_dz_of<DT, FG_ACT_RELU, 0>)(a, p, st)
-             : (kept ? launch_dz_of<DT, FG_ACT_GELU, 1> : launch_dz_of<DT, FG_ACT_GELU, 0>)(a, p, st);
+  if (a.act == FG_ACT_NONE) return launch_dz_of<DT, FG_ACT_NONE, 0>(a, p, st);
+  if (a.act == FG_ACT_RELU)
+    return kept ? launch_dz_of<DT, FG_ACT_RELU, 1>(a, p, st)
+                : launch_dz_of<DT, FG_ACT_RELU, 0>(a, p, st);
+  return kept ? launch_dz_of<DT, FG_ACT_GELU, 1>(a, p, st)
+              : launch_dz_of<DT, FG_ACT_GELU, 0>(a, p, st);
 }
 
 hipError_t pad(const uint16_t *x, int64_t ld, int64_t n, uint16_t *to, int64_t rows,
@@ -1227,7 +1243,8 @@ hipError_t launch_linear_fwd(const fg_linear_desc &d, const void *x, const void 
   e.y_ld = ld(d.y_ld), e.r_ld = ld(d.r_ld), e.z_ld = ld(d.z_ld);
   if (packed_z) e.packed = rows::packed_at(packed_z, p.rows, p.out);
   e.out = (int32_t)p.out, e.act = d.act;
-  if (p.rows <= kFewRows && !packed_z) return bf ? launch_few<true>(a, st) : launch_few<false>(a, st);
+  if (few_rows(p.rows, p.out) && !packed_z)
+    return bf ? launch_few<true>(a, st) : launch_few<false>(a, st);
   a.Mq = (int32_t)p.out8, a.pstride = p.rows * p.out8;
   const bool split = p.s1.ns > 1;
   if (split) a.part = (float *)(base + p.p1);

@@ -223,6 +223,13 @@ def test_few_rows(dt, rows, k, m):
     assert untouched(y) and untouched(z)
 
 
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("rows", [1, 32, 33, 64])
+@pytest.mark.parametrize("k,m", [(40, 8192), (41, 8193), (1032, 8200)])
+def test_few_rows_of_many_outputs(dt, rows, k, m):
+    test_few_rows(dt, rows, k, m)
+
+
 @pytest.mark.parametrize("shape", [(40, 24, 17), (300, 520, 264)], ids=str)
 @pytest.mark.parametrize("act", ACTS)
 def test_each_output_alone(act, shape):
@@ -299,7 +306,8 @@ def test_gradients_against_differences(act):
         noise = 6 * 2.0 ** -11 * float((dy.double() * y0).norm())
         noise += 2.0 ** -9 * float((dy.double() * (zh - zl)).abs().sum())
         noise += 2.0 ** -11 * float((exact * moved).abs().sum())
-        print(f"{i}: off {abs(diff - want):.3g}, curved {curved:.3g}, noise {noise:.3g} of {want:.4g}")
+        print(f"{i}: off {abs(diff - want):.3g}, curved {curved:.3g}, noise {noise:.3g}, "
+              f"of {want:.4g}")
         assert abs(diff - want) <= curved + noise, (i, diff, want)
 
 
