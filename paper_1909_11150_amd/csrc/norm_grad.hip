@@ -196,6 +196,9 @@ struct MakePlan {
   hipError_t go() const {
     using M = Grad<TL, W, N>;
     p->wide = M::WIDE;
+    // Two a CU, one of wide rows: the fewest parts to join that keep the memory busy (both passes of
+    // 65536 x 512 fp16 with 256, 512, 1024 workgroups: 94, 89, 91 us; of 4099 x 1003 fp32 27.5,
+    // 28.5, 33; of 8192 x 4096 bf16 with 128, 256: 99, 80).
     p->blocks = std::min<int64_t>((rows + M::TEAMS - 1) / M::TEAMS, M::WIDE <= 1024 ? 512 : 256);
     return hipSuccess;
   }
