@@ -32,6 +32,10 @@ using rows::TypeOf;
 // 128 x 128 in a ring of four, for launches of a workgroup per CU or less: with two, each
 // stage waits for its loads (dx of 4096 x 1024 -> 4096 43.1 -> 35.8 us).
 using P128D = Pipe<64, 4, 2, 2, 128, 128>;
+// For short sums, whose epilogue is most of the work: three workgroups of 128 x 128 a CU, or two
+// of 256 outputs x 128 rows with 16 waves between them, one in its epilogue while another loads.
+using S128 = Pipe<32, 3, 2, 2, 128, 128>;
+using S256 = Pipe<32, 3, 4, 2, 256, 128>;
 struct FwdTiles {
   using T256 = Pipe<64, 2, 2, 4, 256, 256>;
 };
@@ -1050,6 +1054,20 @@ void pick(const Need *p, int np, Shape *s) {
   }
 }
 
+// Forward sums of up to 512 by the tiles for them, where there is more than one round of those:
+// S256 unless S128 has fewer outputs past the end. Before and with them, with gelu, bias and
+// checkpoint; and with bias and residual, fp16: 65536 x 256 -> 1024 104 -> 91 us, 100 -> 87;
+// 44017 x 200 -> 700 70 -> 56, 90 -> 49; 100000 x 104 -> 6448 1026 -> 987, 847 -> 847; 30000 x 333
+// -> 1111 98 -> 89, 140 -> 116; 16384 x 512 -> 2048 69 -> 66, 58 -> 58. One round of 8192 x 256 ->
+// 2048 29 -> 29, 24.5 -> 23; sums of 768 (16384 -> 4096) 156 -> 160, 144 -> 153.
+enum { kS128 = kTiles, kS256 };
+Shape for_short_sums(const Shape &s, const Need &p) {
+  if (p.K > 512 || s.ns > 1 || (s.tile != 1 && s.tile != 2)) return s;
+  const bool wide = up(p.M, 256) == up(p.M, 128);
+  const int64_t n = ((p.N + 127) / 128) * (wide ? up(p.M, 256) / 256 : up(p.M, 128) / 128);
+  return n > 256 * (wide ? 2 : 3) ? Shape{wide ? kS256 : kS128, s.ns, s.kper} : s;
+}
+
 struct Plan {
   int64_t rows, in, out, in8, out8, K;   // K: columns of x and w as the products read them
   bool narrow;                           // fewer than 8: padded copies
@@ -1067,7 +1085,10 @@ Plan find_plan(const fg_linear_desc &d, bool grad) {
   p.narrow = p.in < 8;
   p.K = std::max<int64_t>(p.in, 8);
   const Need fwd = {p.out, p.rows, p.K}, bwd[2] = {{p.in, p.rows, p.out8}, {p.in, p.out, p.rows}};
-  if (!grad) pick(&fwd, 1, &p.s1);
+  if (!grad) {
+    pick(&fwd, 1, &p.s1);
+    p.s1 = for_short_sums(p.s1, fwd);
+  }
   Shape both[2] = {};  // one launch, one tile for both products
   if (grad) pick(bwd, 2, both);
   p.s2 = both[0], p.s3 = both[1];
@@ -1140,6 +1161,14 @@ hipError_t launch_fwd(FwdArgs a, int ns, hipStream_t st) {
   const TileMap tm = tile_map((a.rows + P::TN - 1) / P::TN, a.ntile, ns);
   hipLaunchKernelGGL(linear_fwd_kernel<P>, dim3(8 * tm.per), dim3(P::NT), 0, st, a, tm);
   return hipGetLastError();
+}
+
+hipError_t launch_fwd_of(const Shape &s, bool bf, const FwdArgs &a, hipStream_t st) {
+  if (s.tile == kS256)
+    return bf ? launch_fwd<Bf16<S256>>(a, s.ns, st) : launch_fwd<S256>(a, s.ns, st);
+  if (s.tile == kS128)
+    return bf ? launch_fwd<Bf16<S128>>(a, s.ns, st) : launch_fwd<S128>(a, s.ns, st);
+  return FG_LINEAR_TILE(launch_fwd, FwdTiles, s.tile, bf, a, s.ns, st);
 }
 
 template <bool BF, class F>
@@ -1248,7 +1277,7 @@ hipError_t launch_linear_fwd(const fg_linear_desc &d, const void *x, const void 
   a.Mq = (int32_t)p.out8, a.pstride = p.rows * p.out8;
   const bool split = p.s1.ns > 1;
   if (split) a.part = (float *)(base + p.p1);
-  FG_TRY(FG_LINEAR_TILE(launch_fwd, FwdTiles, p.s1.tile, bf, a, p.s1.ns, st));
+  FG_TRY(launch_fwd_of(p.s1, bf, a, st));
   if (!split) return hipSuccess;
   const JoinFwd j = {a.part, a.pstride, p.rows, p.s1.ns, a.Mq, (int32_t)up(p.out, 32), e};
   const dim3 grid((uint32_t)((p.rows * (j.wide / 8) + 255) / 256)), block(256);

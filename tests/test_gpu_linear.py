@@ -205,6 +205,15 @@ def test_matches_the_formulas(dt, act, shape):
 
 
 @pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("shape", [(16641, 72, 1000), (70000, 8, 200), (11140, 41, 1111),
+                                   (33000, 512, 384), (98400, 1, 129)], ids=str)
+def test_short_sums_of_many_tiles(dt, act, shape):
+    """More than a round of the tiles for short sums: 256 outputs by 128 rows, or 128 by 128."""
+    test_matches_the_formulas(dt, act, shape)
+
+
+@pytest.mark.parametrize("dt", TYPES)
 @pytest.mark.parametrize("rows", [1, 2, 15, 16, 17, 32, 33, 48, 64, 65])
 @pytest.mark.parametrize("k,m", [(1, 1), (7, 20), (8, 16), (31, 5), (32, 33), (33, 100),
                                  (300, 17), (2048, 1000), (5001, 40)])
