@@ -6,7 +6,7 @@
 //
 // Bound by the matrix pipes where all three sizes are long (forward, fp32 sums included, 462 us
 // of 16384 x 2048 -> 8192 bf16, 1.19 PFLOP/s; with bias, gelu and checkpoint 546), by memory
-// where the sum is short (65536 x 256 -> 1024: 58 us, 93 with them) or the rows are few.
+// where the sum is short (65536 x 256 -> 1024: 67 us, 94 with them) or the rows are few.
 //
 // Products run on the MFMA tiles that dma_pipe.h feeds by LDS DMA. The forward tile holds
 // outputs x rows, so 32 consecutive outputs of a row lie in two lanes' registers: bias,
@@ -32,8 +32,9 @@ using rows::TypeOf;
 // 128 x 128 in a ring of four, for launches of a workgroup per CU or less: with two, each
 // stage waits for its loads (dx of 4096 x 1024 -> 4096 43.1 -> 35.8 us).
 using P128D = Pipe<64, 4, 2, 2, 128, 128>;
-// For short sums, whose epilogue is most of the work: three workgroups of 128 x 128 a CU, or two
-// of 256 outputs x 128 rows with 16 waves between them, one in its epilogue while another loads.
+// For short sums, where the beginning and end are most of the work: three workgroups of 128 x
+// 128 a CU, or two of 256 outputs x 128 rows with 16 waves between them, one in its epilogue
+// while another loads.
 using S128 = Pipe<32, 3, 2, 2, 128, 128>;
 using S256 = Pipe<32, 3, 4, 2, 256, 128>;
 struct FwdTiles {
@@ -990,19 +991,37 @@ __global__ __launch_bounds__(256) void linear_pad_kernel(const uint16_t *x, int6
 // Tile and number of parts for up to two products of a launch: the least of the times
 // estimated for rounds of the workgroups that the chip holds. A round of m workgroups whose
 // sums are k long takes f + e x + k (g + h x), x = m / (256 occ): its beginning and end, and
-// each stage, both longer where the chip is full. Fitted to 420 timings (22 shapes of 100 ..
-// 65536 rows and 64 .. 8000 columns, each pass by every tile in 1 .. 64 parts): within 11% of
-// them (rms), and the choice within 1.5% of the best on average, 21% at worst.
+// each stage, both longer where the chip is full. A join takes a start and its bytes' time.
+// Forward: fitted to 420 timings (22 shapes of 100 .. 65536 rows and 64 .. 8000 columns, by
+// every tile in 1 .. 64 parts), the choice within 1.5% of the best on average. Gradients, each
+// alone and both: to 7800 (94 shapes of 200 .. 100000 rows and 16 .. 8000 columns), the choice
+// within 4% (weighted by the time's root; with forward's constants and tiles 9%). On 86 other
+// shapes the calls for both gain 4% by it, those for dx 8%, for dw 4%, a tile for one alone
+// included.
+enum { kT64, kT128, kT256, kT128D, kS256, kTiles, kS128 = kTiles };
+constexpr int kSideM[] = {64, 128, 256, 128, 256}, kSideN[] = {64, 128, 256, 128, 128};
 struct Cost {
   int occ;
   double f, e, g, h;
 };
-constexpr int kTiles = 4;
-constexpr int kSide[kTiles] = {64, 128, 256, 128};
-constexpr Cost kCost[kTiles] = {{3, 0.0, 2.2, .0029, .0043},
-                                {2, 0.6, 3.5, .0068, .0053},
-                                {1, 7.6, 0.0, .0151, .0020},
-                                {1, 2.2, 1.6, .0060, .0012}};
+struct Costs {
+  int tiles;
+  Cost c[kTiles];
+  double join, rate;   // us; bytes a us
+};
+constexpr Costs kFwd = {4,
+                        {{3, 0.0, 2.2, .0029, .0043},
+                         {2, 0.6, 3.5, .0068, .0053},
+                         {1, 7.6, 0.0, .0151, .0020},
+                         {1, 2.2, 1.6, .0060, .0012}},
+                        3.75, 6.2e6};
+constexpr Costs kBwd = {5,
+                        {{3, 3.1, 0.0, .0030, .0068},
+                         {2, 1.5, 3.7, .0078, .0038},
+                         {1, 6.8, 1.9, .0117, .0052},
+                         {1, 5.6, 0.0, .0059, .0022},
+                         {2, 2.7, 3.3, .0119, .0070}},
+                        2.5, 3.2e6};
 struct Need {
   int64_t M, N, K;
 };
@@ -1020,32 +1039,35 @@ struct Parts {
   double n, k, join;   // workgroups; length of a part; time to join
   int ns, kper;
 };
+int64_t tiles_of(const Need &p, int t) {
+  return up(p.M, kSideM[t]) / kSideM[t] * (up(p.N, kSideN[t]) / kSideN[t]);
+}
 // The numbers of parts worth a look.
-int parts_of(const Need &p, int t, Parts (&out)[10]) {
-  const int64_t side = kSide[t];
-  const int64_t tiles = ((p.M + side - 1) / side) * ((p.N + side - 1) / side);
+int parts_of(const Need &p, const Costs &cost, int t, Parts (&out)[10]) {
+  const int64_t tiles = tiles_of(p, t);
   int n = 0;
   for (int ns = 1; ns <= 512; ns *= 2) {
     const int64_t kper = std::max<int64_t>(64, ((p.K + ns - 1) / ns + 63) / 64 * 64);
     const int64_t parts = std::max<int64_t>(1, (p.K + kper - 1) / kper);
     if (ns > 1 && (kper < 128 || tiles * parts > 4096)) break;
     out[n++] = {(double)(tiles * parts), (double)kper,
-                parts > 1 ? (double)parts * p.M * p.N * 8 / 6.2e6 : 0.0, (int)parts, (int)kper};
+                parts > 1 ? (double)parts * p.M * p.N * 8 / cost.rate : 0.0, (int)parts,
+                (int)kper};
   }
   return n;
 }
-void pick(const Need *p, int np, Shape *s) {
+void pick(const Costs &cost, const Need *p, int np, Shape *s) {
   double best = 1e300;
-  for (int t = 0; t < kTiles; ++t) {
+  for (int t = 0; t < cost.tiles; ++t) {
     Parts a[10], b[10];
-    const int na = parts_of(p[0], t, a), nb = np > 1 ? parts_of(p[1], t, b) : 1;
+    const int na = parts_of(p[0], cost, t, a), nb = np > 1 ? parts_of(p[1], cost, t, b) : 1;
     if (np == 1) b[0] = {0, 0, 0, 0, 0};
     for (int i = 0; i < na; ++i)
       for (int j = 0; j < nb; ++j) {
         const double n = a[i].n + b[j].n;
-        double us = rounds(kCost[t], n, (a[i].n * a[i].k + b[j].n * b[j].k) / n,
+        double us = rounds(cost.c[t], n, (a[i].n * a[i].k + b[j].n * b[j].k) / n,
                            std::max(a[i].k, b[j].k)) + a[i].join + b[j].join;
-        if (a[i].join + b[j].join > 0) us += 3.75;
+        if (a[i].join + b[j].join > 0) us += cost.join;
         if (us >= best) continue;
         best = us;
         s[0] = {t, a[i].ns, a[i].kper};
@@ -1054,15 +1076,25 @@ void pick(const Need *p, int np, Shape *s) {
   }
 }
 
+// The tile for one product whose parts are settled.
+int tile_for(const Costs &cost, const Need &p, const Shape &s) {
+  int best = s.tile;
+  double least = 1e300;
+  for (int t = 0; t < cost.tiles; ++t) {
+    const double us = rounds(cost.c[t], (double)(tiles_of(p, t) * s.ns), s.kper, s.kper);
+    if (us < least) least = us, best = t;
+  }
+  return best;
+}
+
 // Forward sums of up to 512 by the tiles for them, where there is more than one round of those:
 // S256 unless S128 has fewer outputs past the end. Before and with them, with gelu, bias and
 // checkpoint; and with bias and residual, fp16: 65536 x 256 -> 1024 104 -> 91 us, 100 -> 87;
 // 44017 x 200 -> 700 70 -> 56, 90 -> 49; 100000 x 104 -> 6448 1026 -> 987, 847 -> 847; 30000 x 333
 // -> 1111 98 -> 89, 140 -> 116; 16384 x 512 -> 2048 69 -> 66, 58 -> 58. One round of 8192 x 256 ->
 // 2048 29 -> 29, 24.5 -> 23; sums of 768 (16384 -> 4096) 156 -> 160, 144 -> 153.
-enum { kS128 = kTiles, kS256 };
 Shape for_short_sums(const Shape &s, const Need &p) {
-  if (p.K > 512 || s.ns > 1 || (s.tile != 1 && s.tile != 2)) return s;
+  if (p.K > 512 || s.ns > 1 || (s.tile != kT128 && s.tile != kT256)) return s;
   const bool wide = up(p.M, 256) == up(p.M, 128);
   const int64_t n = ((p.N + 127) / 128) * (wide ? up(p.M, 256) / 256 : up(p.M, 128) / 128);
   return n > 256 * (wide ? 2 : 3) ? Shape{wide ? kS256 : kS128, s.ns, s.kper} : s;
@@ -1071,27 +1103,33 @@ Shape for_short_sums(const Shape &s, const Need &p) {
 struct Plan {
   int64_t rows, in, out, in8, out8, K;   // K: columns of x and w as the products read them
   bool narrow;                           // fewer than 8: padded copies
-  Shape s1, s2, s3;
+  Shape s1, s2, s3;                      // forward, dx, dw
+  int tile;                              // of the gradients
   int tlog;
   int64_t cblocks, rblocks, per;         // of the kernel that forms dz
   // workspace, bytes
   size_t xpad, wpad, p1, xu, dz, db, pdx, pdw, total;
 };
 
-Plan find_plan(const fg_linear_desc &d, bool grad) {
+// What a call wants: the forward pass, or of the products of the gradients these.
+enum { kForward = 0, kDx = 1, kDw = 2, kBoth = 3 };
+Plan find_plan(const fg_linear_desc &d, int want) {
   Plan p{};
   p.rows = d.rows, p.in = d.in, p.out = d.out;
   p.in8 = up(p.in, 8), p.out8 = up(p.out, 8);
   p.narrow = p.in < 8;
   p.K = std::max<int64_t>(p.in, 8);
   const Need fwd = {p.out, p.rows, p.K}, bwd[2] = {{p.in, p.rows, p.out8}, {p.in, p.out, p.rows}};
-  if (!grad) {
-    pick(&fwd, 1, &p.s1);
+  if (want == kForward) {
+    pick(kFwd, &fwd, 1, &p.s1);
     p.s1 = for_short_sums(p.s1, fwd);
+  } else {
+    // one launch, one tile for both products; each alone in the same parts, for the same bits
+    Shape s[2] = {};
+    pick(kBwd, bwd, 2, s);
+    p.s2 = s[0], p.s3 = s[1];
+    p.tile = want == kBoth ? s[0].tile : tile_for(kBwd, bwd[want - 1], s[want - 1]);
   }
-  Shape both[2] = {};  // one launch, one tile for both products
-  if (grad) pick(bwd, 2, both);
-  p.s2 = both[0], p.s3 = both[1];
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t was = at;
@@ -1099,7 +1137,7 @@ Plan find_plan(const fg_linear_desc &d, bool grad) {
     return was;
   };
   p.wpad = take(p.narrow ? (size_t)p.out * 16 : 0);
-  if (!grad) {
+  if (want == kForward) {
     p.xpad = take(p.narrow ? (size_t)p.rows * 16 : 0);
     p.p1 = take(p.s1.ns > 1 ? (size_t)p.s1.ns * p.rows * p.out8 * 4 : 0);
     p.total = at;
@@ -1116,32 +1154,39 @@ Plan find_plan(const fg_linear_desc &d, bool grad) {
   p.xu = take((size_t)p.rows * p.in8 * 2);
   p.dz = take(d.act != FG_ACT_NONE || p.out % 8 ? (size_t)p.rows * p.out8 * 2 : 0);
   p.db = take((size_t)p.rblocks * p.out8 * 4);
-  p.pdx = take(p.s2.ns > 1 ? (size_t)p.s2.ns * p.rows * p.in8 * 4 : 0);
-  p.pdw = take(p.s3.ns > 1 ? (size_t)p.s3.ns * p.out * p.in8 * 4 : 0);
+  p.pdx = take(want & kDx && p.s2.ns > 1 ? (size_t)p.s2.ns * p.rows * p.in8 * 4 : 0);
+  p.pdw = take(want & kDw && p.s3.ns > 1 ? (size_t)p.s3.ns * p.out * p.in8 * 4 : 0);
   p.total = at;
   return p;
 }
 
-// A function of the descriptor alone, remembered for a few of them by each host thread: a call
-// asks for it twice, and a look at every tile takes longer than a launch.
-Plan make_plan(const fg_linear_desc &d, bool grad) {
-  struct Entry {
-    fg_linear_desc d;
-    int grad;  // 0: empty
-    Plan p;
-  };
+// Functions of the descriptor alone, remembered for a few of them by each host thread: a call
+// asks for its plan twice, and a look at every tile takes longer than a launch.
+struct Plans {
+  fg_linear_desc d;
+  int grad;      // 0: empty; 1: forward; 2: gradients
+  Plan p[3];     // forward alone; dx, dw, both
+  size_t bytes;  // workspace of any
+};
+const Plans &plans_of(const fg_linear_desc &d, bool grad) {
   constexpr int kPlans = 32;
-  static thread_local Entry kept[kPlans] = {};
+  static thread_local Plans kept[kPlans] = {};
   static thread_local unsigned next = 0;
   const int g = grad ? 2 : 1;
-  for (const Entry &e : kept)
-    if (e.grad == g && !memcmp(&e.d, &d, sizeof(d))) return e.p;
-  Entry &e = kept[next++ % kPlans];
-  e.p = find_plan(d, grad);
+  for (const Plans &e : kept)
+    if (e.grad == g && !memcmp(&e.d, &d, sizeof(d))) return e;
+  Plans &e = kept[next++ % kPlans];
+  e.bytes = 0;
+  for (int k = 0; k < (grad ? 3 : 1); ++k) {
+    e.p[k] = find_plan(d, grad ? kDx + k : kForward);
+    e.bytes = std::max(e.bytes, e.p[k].total);
+  }
   e.d = d;
   e.grad = g;
-  return e.p;
+  return e;
 }
+Plan fwd_plan(const fg_linear_desc &d) { return plans_of(d, false).p[0]; }
+Plan bwd_plan(const fg_linear_desc &d, int want) { return plans_of(d, true).p[want - 1]; }
 
 #define FG_TRY(x)                      \
   do {                                 \
@@ -1149,11 +1194,11 @@ Plan make_plan(const fg_linear_desc &d, bool grad) {
     if (e_ != hipSuccess) return e_;   \
   } while (0)
 
-#define FG_LINEAR_TILE(FN, TS, tile, bf, ...)                                        \
-  ((tile) == 3   ? ((bf) ? FN<Bf16<P128D>>(__VA_ARGS__) : FN<P128D>(__VA_ARGS__))     \
-   : (tile) == 2 ? ((bf) ? FN<Bf16<TS::T256>>(__VA_ARGS__) : FN<TS::T256>(__VA_ARGS__)) \
-   : (tile) == 1 ? ((bf) ? FN<Bf16<P128>>(__VA_ARGS__) : FN<P128>(__VA_ARGS__))       \
-                 : ((bf) ? FN<Bf16<P64>>(__VA_ARGS__) : FN<P64>(__VA_ARGS__)))
+#define FG_LINEAR_TILE(FN, TS, tile, bf, ...)                                              \
+  ((tile) == kT128D  ? ((bf) ? FN<Bf16<P128D>>(__VA_ARGS__) : FN<P128D>(__VA_ARGS__))       \
+   : (tile) == kT256 ? ((bf) ? FN<Bf16<TS::T256>>(__VA_ARGS__) : FN<TS::T256>(__VA_ARGS__)) \
+   : (tile) == kT128 ? ((bf) ? FN<Bf16<P128>>(__VA_ARGS__) : FN<P128>(__VA_ARGS__))         \
+                     : ((bf) ? FN<Bf16<P64>>(__VA_ARGS__) : FN<P64>(__VA_ARGS__)))
 
 template <class P>
 hipError_t launch_fwd(FwdArgs a, int ns, hipStream_t st) {
@@ -1213,6 +1258,14 @@ hipError_t launch_products(ProdArgs dx, int nsx, ProdArgs dw, int nsw, const Sum
   return hipGetLastError();
 }
 
+hipError_t launch_products_of(int tile, bool bf, const ProdArgs &dx, int nsx, const ProdArgs &dw,
+                              int nsw, const SumArgs &sum, hipStream_t st) {
+  if (tile == kS256)
+    return bf ? launch_products<Bf16<S256>>(dx, nsx, dw, nsw, sum, st)
+              : launch_products<S256>(dx, nsx, dw, nsw, sum, st);
+  return FG_LINEAR_TILE(launch_products, BwdTiles, tile, bf, dx, nsx, dw, nsw, sum, st);
+}
+
 template <int DT, int ACT, int KEPT>
 hipError_t launch_dz_of(const DzArgs &a, const Plan &p, hipStream_t st) {
   const dim3 grid((uint32_t)p.cblocks, (uint32_t)p.rblocks), block(256);
@@ -1244,15 +1297,15 @@ hipError_t pad(const uint16_t *x, int64_t ld, int64_t n, uint16_t *to, int64_t r
 
 // (a training step's workspace serves its forward pass too)
 size_t linear_ws_bytes(const fg_linear_desc &d, bool grad) {
-  const size_t fwd = linear::make_plan(d, false).total;
-  return grad ? std::max(fwd, linear::make_plan(d, true).total) : fwd;
+  const size_t fwd = linear::plans_of(d, false).bytes;
+  return grad ? std::max(fwd, linear::plans_of(d, true).bytes) : fwd;
 }
 
 hipError_t launch_linear_fwd(const fg_linear_desc &d, const void *x, const void *w,
                              const void *bias, const void *residual, void *y, void *z,
                              void *packed_z, void *ws, hipStream_t st) {
   using namespace linear;
-  const Plan p = make_plan(d, false);
+  const Plan p = fwd_plan(d);
   uint8_t *base = static_cast<uint8_t *>(ws);
   const bool bf = d.dtype == FG_BF16;
   FwdArgs a{};
@@ -1293,7 +1346,7 @@ hipError_t launch_linear_bwd(const fg_linear_desc &d, const void *dy, const void
                              const void *packed_z, void *dx, void *dw, void *dbias,
                              int32_t *flag, void *ws, hipStream_t st) {
   using namespace linear;
-  const Plan p = make_plan(d, true);
+  const Plan p = bwd_plan(d, (dx && !dw) ? kDx : (dw && !dx) ? kDw : kBoth);
   uint8_t *base = static_cast<uint8_t *>(ws);
   const bool bf = d.dtype == FG_BF16;
   const auto ld = [&](int64_t v, int64_t width) { return v ? v : width; };
@@ -1369,7 +1422,7 @@ hipError_t launch_linear_bwd(const fg_linear_desc &d, const void *dy, const void
           shared_log(nsw)};
   }
   if (!nsx && !nsw) return hipSuccess;
-  FG_TRY(FG_LINEAR_TILE(launch_products, BwdTiles, p.s2.tile, bf, a, nsx, b, nsw, sum, st));
+  FG_TRY(launch_products_of(p.tile, bf, a, nsx, b, nsw, sum, st));
   const auto blocks = [&](int64_t n, const JoinArgs &j) {
     const int wide = 256 >> j.slog;
     return (n * (p.in8 / 8) + wide - 1) / wide;
