@@ -260,6 +260,24 @@ def test_each_output_alone(act, shape):
     assert torch.equal(dx, ex) and torch.equal(dw, ew) and torch.equal(db, eb)
 
 
+# sums of each length by every tile of the gradients, in one part and in several
+TILES = [(4000, 1000, 17), (2000, 2048, 2056), (5001, 4100, 17), (2000, 2048, 3001),
+         (33001, 1030, 129), (8200, 100, 3001), (2000, 3000, 256), (12345, 1030, 384)]
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("act", ["none", "gelu"])
+@pytest.mark.parametrize("shape", TILES, ids=str)
+def test_tiles_of_the_gradients(dt, act, shape):
+    test_matches_the_formulas(dt, act, shape)
+
+
+@pytest.mark.parametrize("act", ["none", "relu"])
+@pytest.mark.parametrize("shape", TILES, ids=str)
+def test_each_output_alone_by_its_own_tile(act, shape):
+    test_each_output_alone(act, shape)
+
+
 @pytest.mark.parametrize("shape", [(1, 512, 77), (50, 100, 77), (700, 2000, 300),
                                    (3000, 512, 1000)], ids=str)
 def test_in_place_of_the_residual(shape):
