@@ -12,6 +12,7 @@ template <int TL_, int W_, int N_, int NT_ = 64 * W_ < 256 ? 256 : 64 * W_>
 struct Team {
   static constexpr int TL = TL_, W = W_, N = N_, NT = NT_;
   static constexpr int TEAM = TL * W, TEAMS = NT / TEAM, WIDE = 8 * TEAM * N;
+  static constexpr int MORE_THAN = TL == 8 ? 0 : WIDE / 2;  // columns of its rows
   static __device__ __forceinline__ int col(int t, int n) { return 8 * (t + TEAM * n); }
 };
 
@@ -60,8 +61,8 @@ constexpr int kFwdBlocks = 1024;
 
 // f.go<type, TL, W, N>() for the team that takes a row. Backward, where 16 sums a chunk stay in
 // registers, wide rows take more waves with a chunk to a lane each (16384 x 1024 fp16 27.5 us,
-// 31.1 with two); forward, two chunks and half the exchanges (8192 x 4096 bf16 27.4 us, 39 with
-// one).
+// 31.1 with two; both passes of 3000 x 5000 fp16 from the checkpoint 58, 65 with two); forward,
+// two chunks and half the exchanges (8192 x 4096 bf16 27.4 us, 39 with one).
 enum Pass { kForward, kGrad };
 template <int DT, Pass P, class F>
 hipError_t for_cols(int cols, const F &f) {
@@ -73,7 +74,7 @@ hipError_t for_cols(int cols, const F &f) {
          : cols <= 1024 ? f.template go<DT, 64, W, N>()
          : cols <= 2048 ? f.template go<DT, 64, 2 * W, N>()
          : cols <= 4096 ? f.template go<DT, 64, 4 * W, N>()
-         : cols <= 8192 ? f.template go<DT, 64, 8, 2>()
+         : cols <= 8192 ? f.template go<DT, 64, 8 * W, N>()
                         : f.template go<DT, 64, 16, 2>();
 }
 template <Pass P, class F>

@@ -31,8 +31,8 @@ struct Loads {
   float2 stat;
 };
 
-// Bound by memory: 65536 x 512 fp16 from the checkpoint 37.0 us (4.6 TB/s), 8192 x 4096 bf16
-// with another gradient to add 45.5 (5.9 TB/s, part of it from the Infinity Cache), then 5 us
+// Bound by memory: 65536 x 512 fp16 from the checkpoint 36.1 us (4.7 TB/s), 8192 x 4096 bf16
+// with another gradient to add 44.5 (6.0 TB/s, part of it from the Infinity Cache), then 5 us
 // for the join of the workgroups' sums. Eight waves a workgroup: half as many parts to join as
 // with four. Bounds: with a chunk to a lane, the registers of two workgroups on a CU (4 waves a
 // SIMD), which all types need so that one's loads cover the other's exchanges.
@@ -44,8 +44,13 @@ __global__ __launch_bounds__((Grad<TL, W, N>::NT),
   constexpr int FOLD = M::TEAMS / 2;  // teams whose sums wait in LDS at a time
   constexpr int LDS = FOLD * M::TEAM * N * 16;
   constexpr int EX = 4 * (M::NT / 64);  // the sums' exchange, two of them in turn
+  // 16 waves with two chunks a lane each have no registers for the next row's loads, nor for the
+  // weights in fp32: with both, 250 of them spilled (both passes of 2048 x 16384 bf16 398 us,
+  // 112 without).
+  constexpr bool kAhead = W < 16 || N == 1;
   __shared__ __attribute__((aligned(16))) float lds[LDS > EX ? LDS : EX];
   const int t = threadIdx.x % M::TEAM, team = threadIdx.x / M::TEAM, cols = a.cols;
+  __builtin_assume(cols > M::MORE_THAN);
   const T *dy = static_cast<const T *>(a.dy), *x = static_cast<const T *>(a.x),
           *w = static_cast<const T *>(a.weight), *add = static_cast<const T *>(a.add);
   T *dx = static_cast<T *>(a.dx);
@@ -74,13 +79,21 @@ __global__ __launch_bounds__((Grad<TL, W, N>::NT),
   };
   const int64_t step = (int64_t)gridDim.x * M::TEAMS;
   int64_t r0 = (int64_t)blockIdx.x * M::TEAMS;
-  load(r0 + team);
+  if (kAhead) load(r0 + team);
   int turn = 0;
   for (; r0 < a.rows; r0 += step, turn ^= 1) {
     const int64_t r = r0 + team;
     const bool on = r < a.rows, ragged = r0 + M::TEAMS > a.rows;  // (the latter for all alike)
+    if (!kAhead) {
+      load(r);
+      // the weights stay as they are in memory, not taken out of the loop in fp32
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (u32x4 &q : rw[n].w) asm volatile("" : "+v"(q));
+    }
     const Loads<T, N, PACKED> now = next;
-    if (r0 + step < a.rows) load(r + step);
+    if (kAhead && r0 + step < a.rows) load(r + step);
     float g[N][8], xh[N][8], s[2] = {0.f, 0.f};
 #pragma unroll
     for (int n = 0; n < N; ++n) {
@@ -196,8 +209,8 @@ struct MakePlan {
   hipError_t go() const {
     using M = Grad<TL, W, N>;
     p->wide = M::WIDE;
-    // Two a CU, one of wide rows: the fewest parts to join that keep the memory busy (both passes of
-    // 65536 x 512 fp16 with 256, 512, 1024 workgroups: 94, 89, 91 us; of 4099 x 1003 fp32 27.5,
+    // Two a CU, one of wide rows: the fewest parts to join that keep the memory busy (both passes
+    // of 65536 x 512 fp16 with 256, 512, 1024 workgroups: 94, 89, 91 us; of 4099 x 1003 fp32 27.5,
     // 28.5, 33; of 8192 x 4096 bf16 with 128, 256: 99, 80).
     p->blocks = std::min<int64_t>((rows + M::TEAMS - 1) / M::TEAMS, M::WIDE <= 1024 ? 512 : 256);
     return hipSuccess;

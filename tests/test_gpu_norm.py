@@ -121,6 +121,13 @@ def test_matches_the_formulas(dt, shape):
         assert torch.equal(whole, was)
 
 
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("shape", [(600, 5001, 5003, 1), (515, 8192, 8192, 0),
+                                   (700, 12001, 12001, 0), (300, 16384, 16384, 0)], ids=str)
+def test_several_wide_rows_to_a_workgroup(dt, shape):
+    test_matches_the_formulas(dt, shape)
+
+
 @pytest.mark.parametrize("cols", [40, 1000, 4096])
 def test_parts_left_out(cols):
     """No weight, bias or sums; each output alone; results in place of dy and of add."""
