@@ -6,24 +6,10 @@
 // 256 fp16 of rows of 1024: packed in 11.2 us, unpacked in 12.2 (50.9 MB each way, 4.5 and 4.2
 // TB/s; called one after the other without a profiler 20.5 us for both, 5.0 TB/s); 8191 x 1023
 // bf16, whose rows begin at odd words, 7.0 and 6.6 us (3.6 and 3.9 TB/s).
-#include "rows.h"
+#include "act8.h"
 
 namespace fg {
 namespace act8 {
-
-using namespace rows;
-
-constexpr int kThreads = 256;
-
-struct Args {
-  const void *x;
-  void *y;
-  int64_t ld;
-  Packed p;
-  uint32_t n;         // chunks of 8 columns
-  int32_t cols;
-  dma::FastDiv div;   // by a row's chunks
-};
 
 template <int DT>
 __global__ __launch_bounds__(kThreads) void act8_pack_kernel(Args a) {
@@ -39,21 +25,12 @@ __global__ __launch_bounds__(kThreads) void act8_pack_kernel(Args a) {
 
 template <int DT>
 __global__ __launch_bounds__(kThreads) void act8_unpack_kernel(Args a) {
-  using T = typename TypeOf<DT>::T;
-  const uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= a.n) return;
-  const uint32_t row = a.div.div((uint32_t)i);
-  const int c = 8 * (int)((uint32_t)i - row * (uint32_t)(a.p.wide / 8));
-  if (c >= a.cols) return;
-  float v[8];
-  decode8(*reinterpret_cast<const u32x2 *>(a.p.codes + (int64_t)row * a.p.wide + c),
-          a.p.exps[(int64_t)row * (a.p.wide / 32) + c / 32], v);
-  store8(static_cast<T *>(a.y) + row * a.ld, c, a.cols, v);
+  unpack_block<DT>(a, blockIdx.x);
 }
 
 template <int DT>
 hipError_t launch(const Args &a, bool pack, hipStream_t st) {
-  const dim3 grid((uint32_t)((a.n + (uint64_t)kThreads - 1) / kThreads)), block(kThreads);
+  const dim3 grid(blocks_of(a)), block(kThreads);
   if (pack)
     hipLaunchKernelGGL(act8_pack_kernel<DT>, grid, block, 0, st, a);
   else
@@ -70,13 +47,7 @@ size_t act8_size(int64_t rows, int64_t cols) {
 
 hipError_t launch_act8(const fg_act8_desc &d, const void *x, void *y, void *packed,
                        hipStream_t st) {
-  act8::Args a{};
-  a.x = x, a.y = y;
-  a.ld = d.x_ld ? d.x_ld : d.cols;
-  a.p = rows::packed_at(packed, d.rows, d.cols);
-  a.n = (uint32_t)(d.rows * (a.p.wide / 8));
-  a.cols = (int32_t)d.cols;
-  a.div = dma::make_fastdiv((uint32_t)(a.p.wide / 8));
+  const act8::Args a = act8::args_of(d, x, y, packed);
   const bool pack = x != nullptr;
   return d.dtype == FG_F16    ? act8::launch<FG_F16>(a, pack, st)
          : d.dtype == FG_BF16 ? act8::launch<FG_BF16>(a, pack, st)

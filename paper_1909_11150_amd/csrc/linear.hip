@@ -19,7 +19,7 @@
 
 #include <algorithm>
 
-#include "rows.h"
+#include "act8.h"
 #include "tiles.h"
 
 namespace fg {
@@ -586,6 +586,7 @@ struct DzArgs {
   float *part;           // [row blocks][Mp] or null
   int64_t rows, dy_ld, z_ld, per;   // rows of a workgroup
   int32_t out, Mp, act, tlog;       // 2^tlog lanes side by side
+  uint32_t cblocks, blocks;         // workgroups side by side; all
 };
 
 // dz = dy act'(z), rounded to the type that the products take, in rows of a multiple of 8
@@ -632,15 +633,21 @@ struct DzLoads {
   }
 };
 
+// The workgroups behind these unpack x's checkpoint, if any: no launch of its own.
 template <int DT, int ACT, int KEPT, bool EVEN>
-__global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a) {
+__global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a, act8::Args x) {
   using T = typename TypeOf<DT>::T;
   using Loads = DzLoads<T, ACT, KEPT, EVEN>;
   __shared__ float sums[256][9];
+  if (blockIdx.x >= a.blocks) {
+    act8::unpack_block<DT>(x, blockIdx.x - a.blocks);
+    return;
+  }
+  const int by = (int)(blockIdx.x / a.cblocks), bx = (int)(blockIdx.x - by * a.cblocks);
   const int tl = 1 << a.tlog, t = threadIdx.x & (tl - 1), team = threadIdx.x >> a.tlog;
   const int teams = 256 >> a.tlog;
-  const int c = 8 * ((int)blockIdx.x * tl + t);
-  const int64_t r0 = (int64_t)blockIdx.y * a.per + team, r1 = min(a.rows, r0 - team + a.per);
+  const int c = 8 * (bx * tl + t);
+  const int64_t r0 = (int64_t)by * a.per + team, r1 = min(a.rows, r0 - team + a.per);
   T *dz = reinterpret_cast<T *>(a.dz);
   float s[8] = {};
   if (c < a.Mp) {
@@ -683,11 +690,11 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a) {
   for (int i = 0; i < 8; ++i) sums[threadIdx.x][i] = s[i];
   __syncthreads();
   for (int k = threadIdx.x; k < 8 * tl; k += 256) {
-    const int col = 8 * (int)blockIdx.x * tl + k;
+    const int col = 8 * bx * tl + k;
     if (col >= a.Mp) break;
     float v = 0.f;
     for (int j = 0; j < teams; ++j) v += sums[(j << a.tlog) + k / 8][k % 8];
-    a.part[(int64_t)blockIdx.y * a.Mp + col] = v;
+    a.part[(int64_t)by * a.Mp + col] = v;
   }
 }
 
@@ -1267,23 +1274,23 @@ hipError_t launch_products_of(int tile, bool bf, const ProdArgs &dx, int nsx, co
 }
 
 template <int DT, int ACT, int KEPT>
-hipError_t launch_dz_of(const DzArgs &a, const Plan &p, hipStream_t st) {
-  const dim3 grid((uint32_t)p.cblocks, (uint32_t)p.rblocks), block(256);
-  if (p.out % 8 == 0)
-    hipLaunchKernelGGL((linear_dz_kernel<DT, ACT, KEPT, true>), grid, block, 0, st, a);
+hipError_t launch_dz_of(const DzArgs &a, const act8::Args &x, hipStream_t st) {
+  const dim3 grid(a.blocks + act8::blocks_of(x)), block(256);
+  if (a.out % 8 == 0)
+    hipLaunchKernelGGL((linear_dz_kernel<DT, ACT, KEPT, true>), grid, block, 0, st, a, x);
   else
-    hipLaunchKernelGGL((linear_dz_kernel<DT, ACT, KEPT, false>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((linear_dz_kernel<DT, ACT, KEPT, false>), grid, block, 0, st, a, x);
   return hipGetLastError();
 }
 template <int DT>
-hipError_t launch_dz(const DzArgs &a, const Plan &p, hipStream_t st) {
+hipError_t launch_dz(const DzArgs &a, const act8::Args &x, hipStream_t st) {
   const bool kept = a.packed.codes != nullptr;
-  if (a.act == FG_ACT_NONE) return launch_dz_of<DT, FG_ACT_NONE, 0>(a, p, st);
+  if (a.act == FG_ACT_NONE) return launch_dz_of<DT, FG_ACT_NONE, 0>(a, x, st);
   if (a.act == FG_ACT_RELU)
-    return kept ? launch_dz_of<DT, FG_ACT_RELU, 1>(a, p, st)
-                : launch_dz_of<DT, FG_ACT_RELU, 0>(a, p, st);
-  return kept ? launch_dz_of<DT, FG_ACT_GELU, 1>(a, p, st)
-              : launch_dz_of<DT, FG_ACT_GELU, 0>(a, p, st);
+    return kept ? launch_dz_of<DT, FG_ACT_RELU, 1>(a, x, st)
+                : launch_dz_of<DT, FG_ACT_RELU, 0>(a, x, st);
+  return kept ? launch_dz_of<DT, FG_ACT_GELU, 1>(a, x, st)
+              : launch_dz_of<DT, FG_ACT_GELU, 0>(a, x, st);
 }
 
 hipError_t pad(const uint16_t *x, int64_t ld, int64_t n, uint16_t *to, int64_t rows,
@@ -1361,8 +1368,15 @@ hipError_t launch_linear_bwd(const fg_linear_desc &d, const void *dy, const void
   z1.part = dbias ? (float *)(base + p.db) : nullptr;
   z1.rows = p.rows, z1.per = p.per;
   z1.out = (int32_t)p.out, z1.Mp = (int32_t)p.out8, z1.act = d.act, z1.tlog = p.tlog;
-  if ((formed || dbias) && p.rows) {
-    FG_TRY((bf ? launch_dz<FG_BF16> : launch_dz<FG_F16>)(z1, p, st));
+  z1.cblocks = (uint32_t)p.cblocks, z1.blocks = (uint32_t)(p.cblocks * p.rblocks);
+  const bool unpacked = dw && packed_x && p.rows, first = (formed || dbias) && p.rows;
+  const fg_act8_desc u = {p.rows, p.in, p.in8, d.dtype};
+  if (first) {
+    act8::Args au{};
+    if (unpacked) au = act8::args_of(u, nullptr, base + p.xu, const_cast<void *>(packed_x));
+    FG_TRY((bf ? launch_dz<FG_BF16> : launch_dz<FG_F16>)(z1, au, st));
+  } else if (unpacked) {
+    FG_TRY(launch_act8(u, nullptr, base + p.xu, const_cast<void *>(packed_x), st));
   }
   SumArgs sum{};
   if (dbias)
@@ -1402,9 +1416,7 @@ hipError_t launch_linear_bwd(const fg_linear_desc &d, const void *dy, const void
   }
   if (dw) {
     b.a = (const uint16_t *)x, b.a_ld = ld(d.x_ld, p.in);
-    if (packed_x && p.rows) {
-      const fg_act8_desc u = {p.rows, p.in, p.in8, d.dtype};
-      FG_TRY(launch_act8(u, nullptr, base + p.xu, const_cast<void *>(packed_x), st));
+    if (unpacked) {
       b.a = (const uint16_t *)(base + p.xu), b.a_ld = p.in8;
     }
     if (p.narrow && p.rows) {
