@@ -634,7 +634,8 @@ typedef struct {
 } fg_norm_desc;
 
 /* y = (x - mean) * rstd * weight + bias, rstd = 1 / sqrt(mean((x - mean)^2) + eps), in fp32,
- * rounded once. weight and bias (cols elements) may be null (1 and 0). stats (fp32 mean and
+ * rounded once; the mean is corrected by that of x - mean, so that rows far from zero lose
+ * nothing to the rounding of its sum (stats hold it in fp32). weight and bias (cols elements) may be null (1 and 0). stats (fp32 mean and
  * rstd per row, 8-byte aligned) and packed (the 8-bit checkpoint of x) may be null. y may be x
  * itself at the same stride. */
 fg_status layer_norm_fwd(const fg_norm_desc *d, const void *x, const void *weight,

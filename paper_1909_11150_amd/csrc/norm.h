@@ -37,13 +37,6 @@ __device__ __forceinline__ void team_sums(float (&v)[R], float *red) {
       for (int k = 0; k < R; ++k) v[k] += red[(wave / M::W * M::W + i) * R + k];
   }
 }
-template <class M>
-__device__ __forceinline__ float team_sum(float v, float *red, int place) {
-  float s[1] = {v};
-  team_sums<M, 1>(s, red + place * (M::NT / 64));
-  return s[0];
-}
-
 struct FwdArgs {
   const void *x, *weight, *bias;
   void *y;
