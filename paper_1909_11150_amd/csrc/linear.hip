@@ -67,10 +67,11 @@ __device__ __forceinline__ float gelu(float z) {
   return fmaf(-__builtin_amdgcn_fmed3f(fabsf(z), 0.f, 64.f), phi_below(z),
               __builtin_amdgcn_fmed3f(z, 0.f, INFINITY));
 }
-// Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi)
+// Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi). For negative z Phi is phi_below itself: as 1 less its
+// complement, what is left of it at z = -5 would be off by 3e-3 (0.5 + copysign(0.5 - p, z) is).
 __device__ __forceinline__ float gelu_slope(float z) {
   const float bell = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
-  const float phi = 0.5f + copysignf(0.5f - phi_below(z), z);
+  const float p = phi_below(z), phi = z < 0.f ? p : 1.f - p;
   return fmaf(__builtin_amdgcn_fmed3f(z, -64.f, 64.f) * 0.39894228f, bell, phi);
 }
 __device__ __forceinline__ float apply(float z, int act) {
