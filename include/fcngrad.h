@@ -677,7 +677,9 @@ typedef struct {
 /* Device workspace in bytes that linear_fwd needs, or (grad != 0) linear_bwd and linear_fwd
  * one after the other; 0 for an invalid or unsupported descriptor, and where none is needed.
  * For gradients it holds dz and x's values from its checkpoint in 16 bits, and fp32 parts of
- * split sums. Calls that may overlap in time need workspaces of their own. */
+ * split sums. linear_fwd without packed_z of up to 64 rows (32 where out > 8192) needs none (in
+ * < 8: 16 bytes a row of x and of w, each rounded up to 256), whatever is said here. Calls that
+ * may overlap in time need workspaces of their own. */
 size_t fg_linear_workspace_bytes(const fg_linear_desc *d, int grad);
 
 /* y = residual + act(z), z = x w^T + bias: products and sums in fp32, one rounding. x: rows x

@@ -1243,7 +1243,7 @@ fg_status linear_fwd(const fg_linear_desc *d, const void *x, const void *w, cons
   if (d->act == FG_ACT_NONE && (z || packed_z)) return FG_EINVAL;
   if (!d->rows) return FG_OK;
   if (!x || !w || !y || ((uintptr_t)packed_z & 15)) return FG_EINVAL;
-  const size_t need = linear_ws_bytes(*d, false);
+  const size_t need = linear_fwd_ws_bytes(*d, packed_z != nullptr);
   if (need && (!ws || ws_bytes < need || ((uintptr_t)ws & 15))) return FG_EWORKSPACE;
   const int64_t n = d->rows, k = d->in, m = d->out;
   const Region t[] = {region(x, n, d->x_ld, k, 2, false), region(w, m, d->w_ld, k, 2, false),

@@ -205,6 +205,7 @@ hipError_t launch_layer_norm_bwd(const fg_norm_desc &d, const void *dy, const vo
                                  int32_t *flag, void *ws, hipStream_t st);
 
 size_t linear_ws_bytes(const fg_linear_desc &d, bool grad);
+size_t linear_fwd_ws_bytes(const fg_linear_desc &d, bool packed_z);
 hipError_t launch_linear_fwd(const fg_linear_desc &d, const void *x, const void *w,
                              const void *bias, const void *residual, void *y, void *z,
                              void *packed_z, void *ws, hipStream_t st);

@@ -1120,14 +1120,32 @@ struct Plan {
   size_t xpad, wpad, p1, xu, dz, db, pdx, pdw, total;
 };
 
-// What a call wants: the forward pass, or of the products of the gradients these.
-enum { kForward = 0, kDx = 1, kDw = 2, kBoth = 3 };
-Plan find_plan(const fg_linear_desc &d, int want) {
+// Its sizes, and the padded copies: all that the kernel of few rows needs.
+struct Layout {
+  size_t at = 0;
+  size_t take(size_t bytes) {
+    const size_t was = at;
+    at += (bytes + 255) / 256 * 256;
+    return was;
+  }
+};
+Plan sizes_of(const fg_linear_desc &d, bool grad) {
   Plan p{};
   p.rows = d.rows, p.in = d.in, p.out = d.out;
   p.in8 = up(p.in, 8), p.out8 = up(p.out, 8);
   p.narrow = p.in < 8;
   p.K = std::max<int64_t>(p.in, 8);
+  Layout l;
+  p.wpad = l.take(p.narrow ? (size_t)p.out * 16 : 0);
+  if (!grad) p.xpad = l.take(p.narrow ? (size_t)p.rows * 16 : 0);
+  p.total = l.at;
+  return p;
+}
+
+// What a call wants: the forward pass, or of the products of the gradients these.
+enum { kForward = 0, kDx = 1, kDw = 2, kBoth = 3 };
+Plan find_plan(const fg_linear_desc &d, int want) {
+  Plan p = sizes_of(d, want != kForward);
   const Need fwd = {p.out, p.rows, p.K}, bwd[2] = {{p.in, p.rows, p.out8}, {p.in, p.out, p.rows}};
   if (want == kForward) {
     pick(kFwd, &fwd, 1, &p.s1);
@@ -1139,17 +1157,10 @@ Plan find_plan(const fg_linear_desc &d, int want) {
     p.s2 = s[0], p.s3 = s[1];
     p.tile = want == kBoth ? s[0].tile : tile_for(kBwd, bwd[want - 1], s[want - 1]);
   }
-  size_t at = 0;
-  auto take = [&](size_t bytes) {
-    const size_t was = at;
-    at += (bytes + 255) / 256 * 256;
-    return was;
-  };
-  p.wpad = take(p.narrow ? (size_t)p.out * 16 : 0);
+  Layout l{p.total};
   if (want == kForward) {
-    p.xpad = take(p.narrow ? (size_t)p.rows * 16 : 0);
-    p.p1 = take(p.s1.ns > 1 ? (size_t)p.s1.ns * p.rows * p.out8 * 4 : 0);
-    p.total = at;
+    p.p1 = l.take(p.s1.ns > 1 ? (size_t)p.s1.ns * p.rows * p.out8 * 4 : 0);
+    p.total = l.at;
     return p;
   }
   p.tlog = 0;
@@ -1160,12 +1171,12 @@ Plan find_plan(const fg_linear_desc &d, int want) {
       1, std::min<int64_t>((p.rows + 4 * teams - 1) / (4 * teams), 2048 / p.cblocks));
   p.per = up((std::max<int64_t>(p.rows, 1) + p.rblocks - 1) / p.rblocks, 4 * teams);
   p.rblocks = std::max<int64_t>(1, (p.rows + p.per - 1) / p.per);
-  p.xu = take((size_t)p.rows * p.in8 * 2);
-  p.dz = take(d.act != FG_ACT_NONE || p.out % 8 ? (size_t)p.rows * p.out8 * 2 : 0);
-  p.db = take((size_t)p.rblocks * p.out8 * 4);
-  p.pdx = take(want & kDx && p.s2.ns > 1 ? (size_t)p.s2.ns * p.rows * p.in8 * 4 : 0);
-  p.pdw = take(want & kDw && p.s3.ns > 1 ? (size_t)p.s3.ns * p.out * p.in8 * 4 : 0);
-  p.total = at;
+  p.xu = l.take((size_t)p.rows * p.in8 * 2);
+  p.dz = l.take(d.act != FG_ACT_NONE || p.out % 8 ? (size_t)p.rows * p.out8 * 2 : 0);
+  p.db = l.take((size_t)p.rblocks * p.out8 * 4);
+  p.pdx = l.take(want & kDx && p.s2.ns > 1 ? (size_t)p.s2.ns * p.rows * p.in8 * 4 : 0);
+  p.pdw = l.take(want & kDw && p.s3.ns > 1 ? (size_t)p.s3.ns * p.out * p.in8 * 4 : 0);
+  p.total = l.at;
   return p;
 }
 
@@ -1304,9 +1315,14 @@ hipError_t pad(const uint16_t *x, int64_t ld, int64_t n, uint16_t *to, int64_t r
 
 }  // namespace linear
 
+// Without a checkpoint of z to write, few rows have a kernel that splits no sums over workgroups.
+size_t linear_fwd_ws_bytes(const fg_linear_desc &d, bool packed_z) {
+  return linear::few_rows(d.rows, d.out) && !packed_z ? linear::sizes_of(d, false).total
+                                                      : linear::plans_of(d, false).bytes;
+}
 // (a training step's workspace serves its forward pass too)
 size_t linear_ws_bytes(const fg_linear_desc &d, bool grad) {
-  const size_t fwd = linear::plans_of(d, false).bytes;
+  const size_t fwd = linear_fwd_ws_bytes(d, d.act != FG_ACT_NONE);
   return grad ? std::max(fwd, linear::plans_of(d, true).bytes) : fwd;
 }
 
@@ -1314,7 +1330,8 @@ hipError_t launch_linear_fwd(const fg_linear_desc &d, const void *x, const void 
                              const void *bias, const void *residual, void *y, void *z,
                              void *packed_z, void *ws, hipStream_t st) {
   using namespace linear;
-  const Plan p = fwd_plan(d);
+  const bool few = few_rows(d.rows, d.out) && !packed_z;
+  const Plan p = few ? sizes_of(d, false) : fwd_plan(d);
   uint8_t *base = static_cast<uint8_t *>(ws);
   const bool bf = d.dtype == FG_BF16;
   FwdArgs a{};
@@ -1334,7 +1351,7 @@ hipError_t launch_linear_fwd(const fg_linear_desc &d, const void *x, const void 
   e.y_ld = ld(d.y_ld), e.r_ld = ld(d.r_ld), e.z_ld = ld(d.z_ld);
   if (packed_z) e.packed = rows::packed_at(packed_z, p.rows, p.out);
   e.out = (int32_t)p.out, e.act = d.act;
-  if (few_rows(p.rows, p.out) && !packed_z)
+  if (few)
     return bf ? launch_few<true>(a, st) : launch_few<false>(a, st);
   a.Mq = (int32_t)p.out8, a.pstride = p.rows * p.out8;
   const bool split = p.s1.ns > 1;
