@@ -40,8 +40,8 @@
  *     the address of the scratch array on each GPU (under a mutex); and per
  *     host thread the one-shot profiling events of fg_profile_next_launch and
  *     the plans of up to 64 data-convolution and 64 kernel-gradient shapes and
- *     of 32 linear layers' calls (functions of the descriptor and the pass
- *     alone; some 40 KiB, freed with the thread).
+ *     of 32 linear layers (functions of the descriptor and the pass alone;
+ *     some 56 KiB, freed with the thread).
  *   - GPU work is enqueued on `stream` (0 = the null stream) and the call
  *     returns without synchronising; results are valid once the caller has
  *     synchronised the stream. Device faults surface at that synchronisation.

@@ -1142,27 +1142,26 @@ Plan sizes_of(const fg_linear_desc &d, bool grad) {
   return p;
 }
 
-// What a call wants: the forward pass, or of the products of the gradients these.
-enum { kForward = 0, kDx = 1, kDw = 2, kBoth = 3 };
-Plan find_plan(const fg_linear_desc &d, int want) {
-  Plan p = sizes_of(d, want != kForward);
-  const Need fwd = {p.out, p.rows, p.K}, bwd[2] = {{p.in, p.rows, p.out8}, {p.in, p.out, p.rows}};
-  if (want == kForward) {
-    pick(kFwd, &fwd, 1, &p.s1);
-    p.s1 = for_short_sums(p.s1, fwd);
-  } else {
-    // one launch, one tile for both products; each alone in the same parts, for the same bits
-    Shape s[2] = {};
-    pick(kBwd, bwd, 2, s);
-    p.s2 = s[0], p.s3 = s[1];
-    p.tile = want == kBoth ? s[0].tile : tile_for(kBwd, bwd[want - 1], s[want - 1]);
-  }
+Plan forward_plan(const fg_linear_desc &d) {
+  Plan p = sizes_of(d, false);
+  const Need fwd = {p.out, p.rows, p.K};
+  pick(kFwd, &fwd, 1, &p.s1);
+  p.s1 = for_short_sums(p.s1, fwd);
   Layout l{p.total};
-  if (want == kForward) {
-    p.p1 = l.take(p.s1.ns > 1 ? (size_t)p.s1.ns * p.rows * p.out8 * 4 : 0);
-    p.total = l.at;
-    return p;
-  }
+  p.p1 = l.take(p.s1.ns > 1 ? (size_t)p.s1.ns * p.rows * p.out8 * 4 : 0);
+  p.total = l.at;
+  return p;
+}
+
+// Of the gradients' products a call wants these.
+enum { kDx = 1, kDw = 2, kBoth = 3 };
+// Both are one launch, with one tile; each alone in the same parts, for the same bits.
+void gradient_plans(const fg_linear_desc &d, Plan (&out)[3]) {
+  Plan p = sizes_of(d, true);
+  const Need need[2] = {{p.in, p.rows, p.out8}, {p.in, p.out, p.rows}};
+  Shape s[2] = {};
+  pick(kBwd, need, 2, s);
+  p.s2 = s[0], p.s3 = s[1];
   p.tlog = 0;
   while (p.tlog < 6 && (8 << p.tlog) < p.out8) ++p.tlog;
   p.cblocks = (p.out8 + (8 << p.tlog) - 1) / (8 << p.tlog);
@@ -1171,42 +1170,54 @@ Plan find_plan(const fg_linear_desc &d, int want) {
       1, std::min<int64_t>((p.rows + 4 * teams - 1) / (4 * teams), 2048 / p.cblocks));
   p.per = up((std::max<int64_t>(p.rows, 1) + p.rblocks - 1) / p.rblocks, 4 * teams);
   p.rblocks = std::max<int64_t>(1, (p.rows + p.per - 1) / p.per);
+  Layout l{p.total};
   p.xu = l.take((size_t)p.rows * p.in8 * 2);
   p.dz = l.take(d.act != FG_ACT_NONE || p.out % 8 ? (size_t)p.rows * p.out8 * 2 : 0);
   p.db = l.take((size_t)p.rblocks * p.out8 * 4);
-  p.pdx = l.take(want & kDx && p.s2.ns > 1 ? (size_t)p.s2.ns * p.rows * p.in8 * 4 : 0);
-  p.pdw = l.take(want & kDw && p.s3.ns > 1 ? (size_t)p.s3.ns * p.out * p.in8 * 4 : 0);
-  p.total = l.at;
-  return p;
+  for (int want = kDx; want <= kBoth; ++want) {
+    Plan &q = out[want - 1] = p;
+    Layout own = l;
+    q.tile = want == kBoth ? s[0].tile : tile_for(kBwd, need[want - 1], s[want - 1]);
+    q.pdx = own.take(want & kDx && p.s2.ns > 1 ? (size_t)p.s2.ns * p.rows * p.in8 * 4 : 0);
+    q.pdw = own.take(want & kDw && p.s3.ns > 1 ? (size_t)p.s3.ns * p.out * p.in8 * 4 : 0);
+    q.total = own.at;
+  }
 }
 
 // Functions of the descriptor alone, remembered for a few of them by each host thread: a call
-// asks for its plan twice, and a look at every tile takes longer than a launch.
+// asks for its plan twice, and a look at every tile takes longer than a launch. One place holds
+// both passes of a layer, each found when it is first asked for.
 struct Plans {
   fg_linear_desc d;
-  int grad;      // 0: empty; 1: forward; 2: gradients
-  Plan p[3];     // forward alone; dx, dw, both
-  size_t bytes;  // workspace of any
+  bool used, fwd, grad;
+  Plan f, g[3];       // forward; dx, dw, both
+  size_t grad_bytes;  // workspace of any of the latter
 };
-const Plans &plans_of(const fg_linear_desc &d, bool grad) {
+Plans &plans_of(const fg_linear_desc &d) {
   constexpr int kPlans = 32;
   static thread_local Plans kept[kPlans] = {};
   static thread_local unsigned next = 0;
-  const int g = grad ? 2 : 1;
-  for (const Plans &e : kept)
-    if (e.grad == g && !memcmp(&e.d, &d, sizeof(d))) return e;
+  for (Plans &e : kept)
+    if (e.used && !memcmp(&e.d, &d, sizeof(d))) return e;
   Plans &e = kept[next++ % kPlans];
-  e.bytes = 0;
-  for (int k = 0; k < (grad ? 3 : 1); ++k) {
-    e.p[k] = find_plan(d, grad ? kDx + k : kForward);
-    e.bytes = std::max(e.bytes, e.p[k].total);
-  }
   e.d = d;
-  e.grad = g;
+  e.used = true, e.fwd = e.grad = false;
   return e;
 }
-Plan fwd_plan(const fg_linear_desc &d) { return plans_of(d, false).p[0]; }
-Plan bwd_plan(const fg_linear_desc &d, int want) { return plans_of(d, true).p[want - 1]; }
+const Plan &fwd_plan(const fg_linear_desc &d) {
+  Plans &e = plans_of(d);
+  if (!e.fwd) e.f = forward_plan(d), e.fwd = true;
+  return e.f;
+}
+const Plans &grad_plans(const fg_linear_desc &d) {
+  Plans &e = plans_of(d);
+  if (!e.grad) {
+    gradient_plans(d, e.g);
+    e.grad_bytes = std::max({e.g[0].total, e.g[1].total, e.g[2].total});
+    e.grad = true;
+  }
+  return e;
+}
 
 #define FG_TRY(x)                      \
   do {                                 \
@@ -1318,12 +1329,12 @@ hipError_t pad(const uint16_t *x, int64_t ld, int64_t n, uint16_t *to, int64_t r
 // Without a checkpoint of z to write, few rows have a kernel that splits no sums over workgroups.
 size_t linear_fwd_ws_bytes(const fg_linear_desc &d, bool packed_z) {
   return linear::few_rows(d.rows, d.out) && !packed_z ? linear::sizes_of(d, false).total
-                                                      : linear::plans_of(d, false).bytes;
+                                                      : linear::fwd_plan(d).total;
 }
 // (a training step's workspace serves its forward pass too)
 size_t linear_ws_bytes(const fg_linear_desc &d, bool grad) {
   const size_t fwd = linear_fwd_ws_bytes(d, d.act != FG_ACT_NONE);
-  return grad ? std::max(fwd, linear::plans_of(d, true).bytes) : fwd;
+  return grad ? std::max(fwd, linear::grad_plans(d).grad_bytes) : fwd;
 }
 
 hipError_t launch_linear_fwd(const fg_linear_desc &d, const void *x, const void *w,
@@ -1372,7 +1383,7 @@ hipError_t launch_linear_bwd(const fg_linear_desc &d, const void *dy, const void
                              const void *packed_z, void *dx, void *dw, void *dbias,
                              int32_t *flag, void *ws, hipStream_t st) {
   using namespace linear;
-  const Plan p = bwd_plan(d, (dx && !dw) ? kDx : (dw && !dx) ? kDw : kBoth);
+  const Plan p = grad_plans(d).g[((dx && !dw) ? kDx : (dw && !dx) ? kDw : kBoth) - 1];
   uint8_t *base = static_cast<uint8_t *>(ws);
   const bool bf = d.dtype == FG_BF16;
   const auto ld = [&](int64_t v, int64_t width) { return v ? v : width; };
