@@ -58,6 +58,18 @@ __device__ __forceinline__ f32x16 mfma32_bf16(const u32x4 &a, const u32x4 &b, co
                                                  __builtin_bit_cast(bf8, b), c, 0, 0, 0);
 }
 
+// 4, 8 and 16 bytes at any element's address: global memory is accessed in one instruction
+// whatever the alignment (the compiler's default for this target), only slower across lines.
+struct __attribute__((packed, aligned(2))) Any4 {
+  uint32_t v;
+};
+struct __attribute__((packed, aligned(2))) Any8 {
+  u32x2 v;
+};
+struct __attribute__((packed, aligned(2))) Any16 {
+  u32x4 v;
+};
+
 // Select the low (sel=0) or high (sel=1) 16-bit half of each of two words
 // and pack them as (lo_word_part, hi_word_part).
 __device__ __forceinline__ uint32_t pack_lo(uint32_t a, uint32_t b) {

@@ -247,9 +247,6 @@ __device__ __forceinline__ void pack_block(const f32x16 (&acc)[P::FM][P::FN], co
 }
 
 // 4 elements of a vector of n from c on, zeros past its end.
-struct __attribute__((packed, aligned(2))) Any8 {
-  u32x2 v;
-};
 __device__ __forceinline__ void load4(const uint16_t *p, int c, int n, bool bf, float (&v)[4]) {
   if (c + 4 <= n) {
     const u32x2 q = reinterpret_cast<const Any8 *>(p + c)->v;

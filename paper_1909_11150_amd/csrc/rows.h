@@ -23,12 +23,6 @@ struct TypeOf<FG_F32> {
   using T = float;
 };
 
-// 16 bytes at any element's address: global memory is accessed in one instruction whatever
-// the alignment, only slower across lines.
-struct __attribute__((packed, aligned(2))) Any16 {
-  u32x4 v;
-};
-
 // 8 elements as they are in memory.
 template <class T>
 struct Raw {
@@ -126,12 +120,6 @@ __device__ __forceinline__ void store8(T *row, int c, int cols, const float (&v)
   const int n = cols - c;
   if (n <= 0) return;
   typedef uint16_t bits;
-  struct __attribute__((packed, aligned(2))) Any8 {
-    u32x2 v;
-  };
-  struct __attribute__((packed, aligned(2))) Any4 {
-    uint32_t v;
-  };
   if constexpr (sizeof(T) == 2) {
     u32x2 w = {r.w[0][0], r.w[0][1]};
     if (n & 4) {

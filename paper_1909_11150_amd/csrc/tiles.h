@@ -13,12 +13,6 @@ using namespace dma;
 using P128 = Pipe<64, 2, 2, 2, 128, 128>;  // 4 waves of 64 x 64
 using P64 = Pipe<64, 3, 2, 2, 64, 64>;     // 4 waves of 32 x 32
 
-// 16 bytes at any address: global memory is accessed in one instruction whatever the
-// alignment (the compiler's default for this target), only slower across lines.
-struct __attribute__((packed, aligned(2))) Any16 {
-  u32x4 v;
-};
-
 // Rows are taken in chunks of 8 elements. A width that is no multiple of 8 has a last
 // chunk that begins before its place, at width - 8, so that nothing outside the row is
 // read or written; what it repeats is left out of sums over the width (logits), and
@@ -142,7 +136,6 @@ inline TileMap tile_map(int64_t n0, int64_t n1, int64_t n2) {
           kOutputMajor};
 }
 
-constexpr int kTileOf[3] = {64, 128, 256};
 struct Shape {
   int tile, ns, kper;  // tile: index; parts of the sum, length of one
 };

@@ -1432,6 +1432,7 @@ constexpr int64_t kInPlace = (int64_t)1 << 32;
 // against two: 8192 x 4096 x 131072 21.1 and 22.2 ms, 5000 x 512 x 131072 2.73 and 3.05.)
 constexpr int64_t kPieceBytes = (int64_t)1 << 30;
 
+constexpr int kTileOf[3] = {64, 128, 256};
 // Tile and number of parts for a product of M x N sums of length K: the least of the
 // times estimated for rounds of the workgroups that the chip holds. A round costs a
 // fixed time (first loads, store) and one per unit of K, by the tile and the
