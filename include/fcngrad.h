@@ -686,7 +686,7 @@ size_t fg_linear_workspace_bytes(const fg_linear_desc *d, int grad);
  * in, w: out x in, bias: out (null: 0), residual: rows x out (null: 0). For the backward pass of
  * an activation, z (rows x out, rounded) and packed_z (its 8-bit checkpoint) may be kept;
  * either may be null, and both must be without one. y may be the residual itself at the same
- * stride. Phi(-|z|) is within 1.2e-5 of itself up to |z| = 6, and of 1e-9 beyond.
+ * stride. Phi(-|z|) is within 6.2e-6 + 2^-23 z^2 of itself up to |z| = 6, and of 1e-9 beyond.
  * FG_EUNSUPPORTED also for FG_F32, rows of 2^28, in or out above 2^17, strides of 2^20, rows *
  * in or rows * out of 2^34 or more. */
 fg_status linear_fwd(const fg_linear_desc *d, const void *x, const void *w, const void *bias,
@@ -699,7 +699,9 @@ fg_status linear_fwd(const fg_linear_desc *d, const void *x, const void *w, cons
  * read for dx; x, given itself or as its checkpoint packed_x, for dw; z, or its checkpoint
  * packed_z, where there is an activation (of ReLU any tensor that is positive where z is, e.g. y
  * without residual). What is not read may be null; x and packed_x, z and packed_z are not given
- * both. relu'(0) = 0; a NaN in z reaches dz. found_nonfinite (device int32, may be null) is set
+ * both. relu'(0) = 0, also for a positive z whose code in packed_z is 0, being less than half a
+ * step (1.1% of the positive ones of normally distributed z): z itself, or y, keeps those
+ * gradients. gelu'(z) takes Phi(z) as above, for z < 0 itself. A NaN in z reaches dz. found_nonfinite (device int32, may be null) is set
  * to 1 if an element of dw or dbias is infinite or NaN, never cleared. Limits as linear_fwd. */
 fg_status linear_bwd(const fg_linear_desc *d, const void *dy, const void *x,
                      const void *packed_x, const void *w, const void *z, const void *packed_z,

@@ -753,7 +753,8 @@ def linear_fwd(desc, x, w, y, bias=None, residual=None, z=None, packed_z=None, w
                stream=None):
     """y = residual + act(x w^T + bias) (see include/fcngrad.h). z, packed_z: what an
     activation's backward pass needs of z = x w^T + bias, in desc's type or in 8 bits. ws:
-    uint8 tensor of linear_workspace_bytes(desc, False)."""
+    uint8 tensor of linear_workspace_bytes(desc, False); without packed_z and of up to 64 rows
+    (32 where fan_out > 8192) none where fan_in >= 8."""
     n, k, m, dt, cur = desc.rows, desc.fan_in, desc.fan_out, desc.dtype, _current()
     wp, wb = _scratch(ws, cur)
     st = lib().linear_fwd(
@@ -769,8 +770,9 @@ def linear_fwd(desc, x, w, y, bias=None, residual=None, z=None, packed_z=None, w
 def linear_bwd(desc, dy, x=None, packed_x=None, w=None, z=None, packed_z=None, dx=None, dw=None,
                dbias=None, found_nonfinite=None, ws=None, stream=None):
     """Gradients of linear_fwd from dy: dx (reads w), dw (reads x or its checkpoint packed_x),
-    dbias; z or its checkpoint packed_z with an activation. ws: uint8 tensor of
-    linear_workspace_bytes(desc, True)."""
+    dbias; z or its checkpoint packed_z with an activation (ReLU has no slope where a code is 0:
+    z, or y of linear_fwd without residual, keeps the smallest positive ones). ws: uint8 tensor
+    of linear_workspace_bytes(desc, True)."""
     n, k, m, dt, cur = desc.rows, desc.fan_in, desc.fan_out, desc.dtype, _current()
     wp, wb = _scratch(ws, cur)
     st = lib().linear_bwd(

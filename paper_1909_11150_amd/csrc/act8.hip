@@ -3,7 +3,7 @@
 // Bound by memory: an fp16 element is read in 2 bytes and written in 33/32, and back. A lane
 // takes 8 columns, so that its access is 16 bytes of a 16-bit type, and 4 lanes beside each
 // other a group: its largest magnitude goes around in two moves between lanes, no LDS. 65536 x
-// 256 fp16 of rows of 1024: packed in 11.2 us, unpacked in 12.2 (50.9 MB each way, 4.5 and 4.2
+// 256 fp16 of rows of 1024: packed in 11.0 us, unpacked in 10.3 (50.9 MB each way, 4.6 and 4.9
 // TB/s; called one after the other without a profiler 20.5 us for both, 5.0 TB/s); 8191 x 1023
 // bf16, whose rows begin at odd words, 7.0 and 6.6 us (3.6 and 3.9 TB/s).
 #include "act8.h"

@@ -4,9 +4,10 @@
 //   z = x w^T + b,  y = residual + act(z)
 //   dz = dy act'(z),  dx = dz w,  dw = dz^T x,  db = sum of dz over the rows
 //
-// Bound by the matrix pipes where all three sizes are long (forward, fp32 sums included, 462 us
-// of 16384 x 2048 -> 8192 bf16, 1.19 PFLOP/s; with bias, gelu and checkpoint 546), by memory
-// where the sum is short (65536 x 256 -> 1024: 67 us, 94 with them) or the rows are few.
+// Bound by the matrix pipes where all three sizes are long (the forward pass by itself 464 us of
+// 16384 x 2048 -> 8192 bf16, 1.18 PFLOP/s; with bias, gelu and checkpoint 540, and 577 to 593 in a
+// step, whose products leave the clock lower), by memory where the sum is short (65536 x 256 ->
+// 1024: 59 us, 98 with them) or the rows are few.
 //
 // Products run on the MFMA tiles that dma_pipe.h feeds by LDS DMA. The forward tile holds
 // outputs x rows, so 32 consecutive outputs of a row lie in two lanes' registers: bias,
@@ -103,7 +104,8 @@ struct FwdArgs {
 };
 
 // Keeps the compiler from working on more of the accumulators at once than it has registers
-// for: without it the largest tiles spill 465 of them (65536 x 256 -> 1024 in 149 us, not 60).
+// for: without it the 256 x 128 tile spills 8 of them (at the same times: 65536 x 256 -> 1024 59
+// us either way).
 __device__ __forceinline__ void apart() { __builtin_amdgcn_sched_barrier(0); }
 
 // A block's activation, into registers of its own: changed in place under a branch, the whole
@@ -587,8 +589,10 @@ struct DzArgs {
   uint32_t cblocks, blocks;         // workgroups side by side; all
 };
 
-// dz = dy act'(z), rounded to the type that the products take, in rows of a multiple of 8
-// with zeros behind them; its columns' fp32 sums per workgroup, before the rounding. Bound by
+// dz = dy act'(z), rounded to the type that the products take (the matrix pipes' operands have 16
+// bits; it is all by which dx and dw differ from products of dz in fp32: off the exact values by
+// 2.9e-4 in norm, 2.1e-4 without, of 65536 x 256 -> 1024 fp16, and 2.3e-3, 1.7e-3 without, of 16384
+// x 2048 -> 8192 bf16), in rows of a multiple of 8 with zeros behind them; its columns' fp32 sums per workgroup, before the rounding. Bound by
 // memory: the next kRows rows are on their way while these are worked on. KEPT: z in 16 bits
 // or (1) its checkpoint; EVEN: 8 divides the columns, no masks.
 // 16384 x 8192 bf16 from z's checkpoint, gelu: 161 us, 4.2 TB/s (175, 4.4, with the checkpoint of

@@ -47,15 +47,16 @@ struct FwdArgs {
   float inv, eps;    // 1 / cols
 };
 
-// Workgroups of the forward pass: some more than the chip holds at once, so that each takes
-// several rows with the next one's loads on their way (16384 x 1024 fp16: 16.6 us with 2048,
-// 17.1 with 1280, 15.4 with 1024; one row to a team without the loop 17.4 and more).
+// Workgroups of the forward pass: 4 waves a SIMD where they are of 4 waves, which the chip holds
+// at once, each taking several rows with the next one's loads on their way. With 512, 1024, 1280,
+// 2048 of them: 16384 x 1024 fp16 14.5, 13.8, 14.5, 13.9 us; 65536 x 512 fp16 with the checkpoint
+// 45, 35.8, 34.0, 34.2; 2000 x 12001 fp32 39, 45, 47, 52.
 constexpr int kFwdBlocks = 1024;
 
 // f.go<type, TL, W, N>() for the team that takes a row. Backward, where 16 sums a chunk stay in
 // registers, wide rows take more waves with a chunk to a lane each (16384 x 1024 fp16 27.5 us,
 // 31.1 with two; both passes of 3000 x 5000 fp16 from the checkpoint 58, 65 with two); forward,
-// two chunks and half the exchanges (8192 x 4096 bf16 27.4 us, 39 with one).
+// two chunks and half the exchanges (8192 x 4096 bf16 25.0 us, 29.6 with one).
 enum Pass { kForward, kGrad };
 template <int DT, Pass P, class F>
 hipError_t for_cols(int cols, const F &f) {
